@@ -2,8 +2,9 @@
  * dapple_kernels.h -- kernel-level entry points of the stage library.
  *
  * The forward and backward tasks of a stage (dapple_stage.h) are sequences of the
- * kernels below.  They are exported so that each can be checked against the CPU
- * oracle on its own and timed on its own; they add no functionality.  All
+ * kernels in the first part.  They are exported so that each can be checked against the CPU
+ * oracle on its own and timed on its own; they add no functionality.  The second part
+ * holds operators of layers and training steps that a stage does not build itself.  All
  * pointers are DEVICE pointers owned by the caller, `stream` is a hipStream_t
  * (NULL = default stream), work is enqueued and not waited for, the return value
  * is 0 or a negative STAGE_E_* code (see dapple_stage.h).
@@ -119,6 +120,28 @@ int dapple_colsum(int dtype, const void* X, int rows, int cols, int ld, float* p
  * overlap on that GPU (different streams, no ordering between them) race; calls on one stream are safe. */
 #define DAPPLE_COLSUM_STATIC_MAX_FLOATS (1 << 20)
 int dapple_colsum_static(int dtype, const void* X, int rows, int cols, int ld, float* out, void* stream);
+
+/* ------------------------------------------------------------------ operators of layers and training steps
+ * Checked on the host before anything is enqueued: a refused call returns STAGE_E_NULL or STAGE_E_CONFIG and
+ * stage_last_error() says why.  Nothing is allocated and nothing waited for; results are the same bits from call to call;
+ * every call can be captured into a HIP graph (after one eager call of the same kind).  `workspace` is device memory of
+ * the size that the operator's *_workspace function returns (host only; a negative code for a call that would be refused),
+ * 16-byte aligned, whose contents do not matter before or after: calls that may overlap need one each. */
+
+/* The global norm of n gradient tensors, all of one dtype: grads and sizes are HOST arrays of n device pointers (aligned to
+ * their elements) and element counts (0 is allowed, its pointer is not looked at).
+ *   norm_dev[0] = |grad_scale| * sqrt(sum of all squares)      (squares and sums in 64 bits)
+ *   norm_dev[1] = min(1, max_norm / norm_dev[0]), 0 if the norm is not finite
+ * grad_scale: what the gradients are multiplied with later (1 / samples for accumulated sums).  max_norm > 0, may be
+ * infinite.  The gradients of all stages of a model may be given in one call.  workspace: 8-byte aligned is enough. */
+int64_t dapple_grad_norm_workspace(const int64_t* sizes, int n);
+int dapple_grad_norm(int dtype, const void* const* grads, const int64_t* sizes, int n, float grad_scale, float max_norm,
+                     float* norm_dev, void* workspace, void* stream);
+/* outs[i] = grads[i] * norm_dev[1], zeros if norm_dev[0] is not finite (grad_scale is not applied).  outs: HOST array of n
+ * device pointers, NULL = in place; outs[i] is grads[i] or overlaps none of the tensors, and no tensor is listed twice.
+ * stage_apply_adam_clipped (dapple_stage.h) takes norm_dev itself and needs no clipped copy. */
+int dapple_grad_clip(int dtype, const void* const* grads, void* const* outs, const int64_t* sizes, int n,
+                     const float* norm_dev, void* stream);
 
 #ifdef __cplusplus
 }

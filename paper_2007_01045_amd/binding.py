@@ -72,6 +72,7 @@ SYMBOLS = {
     "stage_grads": (_i, [_vp, C.POINTER(_vp), C.POINTER(C.c_uint64)]),
     "stage_zero_grads": (_i, [_vp]),
     "stage_apply_adam": (_i, [_vp, _vp, _vp, _vp, _vp, _i, _f, _f, _f, _f, _f, _i]),
+    "stage_apply_adam_clipped": (_i, [_vp, _vp, _vp, _vp, _vp, _i, _f, _f, _f, _f, _f, _i, _vp]),
     "stage_stats": (_i, [_vp, C.POINTER(stage_stats_t)]),
     "stage_reset_stats": (_i, [_vp]),
     "stage_profile_enable": (_i, [_vp, _i]),
@@ -101,6 +102,9 @@ SYMBOLS = {
     "dapple_layernorm_bwd": (_i, [_i, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i, _i, _vp]),
     "dapple_colsum": (_i, [_i, _vp, _i, _i, _i, _vp, _vp, _vp]),
     "dapple_colsum_static": (_i, [_i, _vp, _i, _i, _i, _vp, _vp]),
+    "dapple_grad_norm_workspace": (C.c_int64, [C.POINTER(C.c_int64), _i]),
+    "dapple_grad_norm": (_i, [_i, _pp, C.POINTER(C.c_int64), _i, _f, _f, _vp, _vp, _vp]),
+    "dapple_grad_clip": (_i, [_i, _pp, _pp, C.POINTER(C.c_int64), _i, _vp, _vp]),
 }
 
 _lib = None
@@ -313,6 +317,12 @@ def stage_apply_adam(h, weights_ptr, master_ptr, m_ptr, v_ptr, step, lr, beta1=0
                                    grad_scale, int(zero_grads)))
 
 
+def stage_apply_adam_clipped(h, weights_ptr, master_ptr, m_ptr, v_ptr, step, lr, norm_ptr, beta1=0.9, beta2=0.999,
+                             eps=1e-8, grad_scale=1.0, zero_grads=False):
+    _check(load().stage_apply_adam_clipped(h, weights_ptr, master_ptr, m_ptr, v_ptr, step, lr, beta1, beta2, eps,
+                                           grad_scale, int(zero_grads), norm_ptr))
+
+
 def stage_stats(h) -> stage_stats_t:
     out = stage_stats_t()
     _check(load().stage_stats(h, C.byref(out)))
@@ -425,6 +435,30 @@ def dapple_colsum_static(dtype, X, rows, cols, ld, out, stream_ptr=None):
         raise StageError(rc, last_error())
 
 
+# ---- operators of layers and training steps (second part of dapple_kernels.h) ----
+def _i64_array(sizes):
+    return (C.c_int64 * len(sizes))(*sizes)
+
+
+def dapple_grad_norm_workspace(sizes) -> int:
+    """Bytes of device memory that dapple_grad_norm needs for tensors of so many elements each."""
+    return _check(load().dapple_grad_norm_workspace(_i64_array(sizes), len(sizes)))
+
+
+def dapple_grad_norm(dtype, grad_ptrs, sizes, max_norm, norm_ptr, workspace_ptr, grad_scale=1.0, stream_ptr=None):
+    """norm_ptr (device float [2]): the global norm of the tensors and the factor that clips it to max_norm."""
+    n = len(sizes)
+    _check(load().dapple_grad_norm(dtype, _ptr_array(grad_ptrs, n), _i64_array(sizes), n, grad_scale, max_norm, norm_ptr,
+                                   workspace_ptr, stream_ptr))
+
+
+def dapple_grad_clip(dtype, grad_ptrs, out_ptrs, sizes, norm_ptr, stream_ptr=None):
+    """out = grad times the factor that dapple_grad_norm left; out_ptrs None: in place."""
+    n = len(sizes)
+    _check(load().dapple_grad_clip(dtype, _ptr_array(grad_ptrs, n), _ptr_array(out_ptrs, n), _i64_array(sizes), n, norm_ptr,
+                                   stream_ptr))
+
+
 # ---- convenience: device memory through torch ------------------------------
 class StageRunner:
     """Owns the device buffers of one stage (weights, arena, per-micro-batch inputs
@@ -464,6 +498,24 @@ class StageRunner:
         self.step += 1
         stage_apply_adam(self.h, self.weights.data_ptr(), self.master.data_ptr(), self.m.data_ptr(),
                          self.v.data_ptr(), self.step, lr, beta1, beta2, eps, grad_scale, zero_grads)
+
+    def apply_adam_clipped(self, lr, max_norm, beta1=0.9, beta2=0.999, eps=1e-8, grad_scale=1.0, zero_grads=False, norm=None):
+        """The update with the gradients clipped to max_norm by this stage's own norm, or by `norm` (device float [2] of
+        dapple_grad_norm over the accumulators of all stages).  Returns that tensor."""
+        torch = self.torch
+        sp = self.stream.cuda_stream
+        if norm is None:
+            sizes = [self.sizes.n_params]
+            if not hasattr(self, "norm"):
+                self.norm = torch.empty(2, dtype=torch.float32, device=self.device)
+                self.norm_ws = torch.empty(dapple_grad_norm_workspace(sizes), dtype=torch.uint8, device=self.device)
+            norm = self.norm
+            dapple_grad_norm(DTYPE_F32, [self.grads.data_ptr()], sizes, max_norm, norm.data_ptr(), self.norm_ws.data_ptr(),
+                             grad_scale, sp)
+        self.step += 1
+        stage_apply_adam_clipped(self.h, self.weights.data_ptr(), self.master.data_ptr(), self.m.data_ptr(), self.v.data_ptr(),
+                                 self.step, lr, norm.data_ptr(), beta1, beta2, eps, grad_scale, zero_grads)
+        return norm
 
     def to_dev(self, a, dtype=None):
         t = self.torch.as_tensor(a)

@@ -250,9 +250,17 @@ hipError_t launch_mul(Dtype dt, const void* a, const void* b, void* c, long n, h
 // ---------------------------------------------------------------- weight update
 // One Adam step over n parameters: g = grad_scale * G; m, v, w32 updated in fp32 (c1, c2: the
 // reciprocal bias corrections 1/(1-beta1^step), 1/(1-beta2^step)); w = w32 in the stage's dtype;
-// G is zeroed when zero_grads is set.  All fp32 pointers 16-byte aligned.
+// G is zeroed when zero_grads is set.  All fp32 pointers 16-byte aligned.  clip (may be NULL): the norm and the factor
+// of launch_grad_norm, on the device; the gradient is scaled by the factor too, and nothing is updated where the norm is
+// not finite.
 hipError_t launch_adam(Dtype dt, float* G, float* w32, float* m, float* v, void* w, size_t n, float lr, float beta1,
-                       float beta2, float eps, float c1, float c2, float grad_scale, int zero_grads, hipStream_t st);
+                       float beta2, float eps, float c1, float c2, float grad_scale, int zero_grads, const float* clip, hipStream_t st);
+// norm[0] = |grad_scale| sqrt(sum of squares of n tensors), norm[1] = min(1, max_norm / norm[0]) (0 if that is not finite);
+// partial: grad_norm_blocks() doubles.  out[i] = g[i] norm[1] (zeros if norm[0] is not finite); out[i] may be g[i].
+int64_t grad_norm_blocks(const int64_t* sizes, int n);
+hipError_t launch_grad_norm(Dtype dt, const void* const* g, const int64_t* sizes, int n, float grad_scale, float max_norm, float* norm,
+                            double* partial, hipStream_t st);
+hipError_t launch_grad_clip(Dtype dt, const void* const* g, void* const* out, const int64_t* sizes, int n, const float* norm, hipStream_t st);
 
 // ---------------------------------------------------------------- host-side plumbing shared by the C-ABI files
 // records the message stage_last_error() returns and hands the code back

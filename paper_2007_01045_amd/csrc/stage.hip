@@ -1357,8 +1357,8 @@ int stage_zero_grads(stage_handle h) {
   return h->run(KC_COPY, 0, [&](hipStream_t q) { return launch_zero(h->grads, h->L.grad_bytes, q); });
 }
 
-int stage_apply_adam(stage_handle h, void* weights_dev, float* master_dev, float* m_dev, float* v_dev, int step, float lr,
-                     float beta1, float beta2, float eps, float grad_scale, int zero_grads) {
+static int apply_adam(stage_handle h, void* weights_dev, float* master_dev, float* m_dev, float* v_dev, int step, float lr,
+                      float beta1, float beta2, float eps, float grad_scale, int zero_grads, const float* clip_dev) {
   if (!h) return fail(STAGE_E_NULL, "handle is NULL");
   if (step < 1) return fail(STAGE_E_CONFIG, "step counts from 1 (got %d)", step);
   if (!(beta1 >= 0.f && beta1 < 1.f) || !(beta2 >= 0.f && beta2 < 1.f) || !(eps > 0.f))
@@ -1371,8 +1371,19 @@ int stage_apply_adam(stage_handle h, void* weights_dev, float* master_dev, float
   const double c1 = 1.0 / (1.0 - std::pow((double)beta1, step)), c2 = 1.0 / (1.0 - std::pow((double)beta2, step));
   return h->run(KC_COPY, 0, [&](hipStream_t q) {
     return launch_adam(h->dt, h->grads, master_dev, m_dev, v_dev, weights_dev, h->L.n_params, lr, beta1, beta2, eps,
-                       (float)c1, (float)c2, grad_scale, zero_grads, q);
+                       (float)c1, (float)c2, grad_scale, zero_grads, clip_dev, q);
   });
+}
+
+int stage_apply_adam(stage_handle h, void* weights_dev, float* master_dev, float* m_dev, float* v_dev, int step, float lr,
+                     float beta1, float beta2, float eps, float grad_scale, int zero_grads) {
+  return apply_adam(h, weights_dev, master_dev, m_dev, v_dev, step, lr, beta1, beta2, eps, grad_scale, zero_grads, nullptr);
+}
+
+int stage_apply_adam_clipped(stage_handle h, void* weights_dev, float* master_dev, float* m_dev, float* v_dev, int step, float lr,
+                             float beta1, float beta2, float eps, float grad_scale, int zero_grads, const float* norm_dev) {
+  if (h && !h->dry && !norm_dev) return fail(STAGE_E_NULL, "norm_dev must not be NULL");
+  return apply_adam(h, weights_dev, master_dev, m_dev, v_dev, step, lr, beta1, beta2, eps, grad_scale, zero_grads, norm_dev);
 }
 
 int stage_stats(stage_handle h, stage_stats_t* out) {

@@ -1,0 +1,216 @@
+"""The global gradient norm, clipping, and the Adam update that takes the factor on the device, against float64.
+
+Tolerances: the sums are taken in 64 bits, so the norm and the factor are off by their last rounding to fp32 (2^-24) and
+by what |grad_scale| adds (none in 64 bits): 2^-23 leaves a factor of two.  A clipped fp32 value has the factor's rounding
+and the product's, 2^-24 each; a bf16 one 2^-8 more for its own."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import stage_oracle as O
+from paper_2007_01045_amd import binding as B
+from paper_2007_01045_amd import inputs as I
+from tests.stage_util import c_config
+
+pytestmark = pytest.mark.gpu
+TD = {B.DTYPE_F32: torch.float32, B.DTYPE_BF16: torch.bfloat16}
+DTYPES = [B.DTYPE_F32, B.DTYPE_BF16]
+
+
+def tensors(dtype, sizes, scale=1.0, pad=0, seed=5):
+    """Views one behind the other (at any alignment of their elements), `pad` elements in front of the first."""
+    flat = torch.from_numpy((scale * I.normal(seed, "grads", pad + sum(sizes))).astype(np.float32)).cuda().to(TD[dtype])
+    out, at = [], pad
+    for n in sizes:
+        out.append(flat[at:at + n])
+        at += n
+    return flat, out
+
+
+def ptrs(ts):
+    return [t.data_ptr() for t in ts]
+
+
+def norm_of(dtype, ts, max_norm, grad_scale=1.0, stream=None):
+    sizes = [t.numel() for t in ts]
+    norm = torch.full((2,), float("nan"), device="cuda")
+    ws = torch.full((B.dapple_grad_norm_workspace(sizes),), 0xff, dtype=torch.uint8, device="cuda")   # (NaN everywhere)
+    B.dapple_grad_norm(dtype, ptrs(ts), sizes, max_norm, norm.data_ptr(), ws.data_ptr(), grad_scale, stream)
+    return norm
+
+
+def check_norm(norm, ts, max_norm, grad_scale=1.0):
+    want = abs(grad_scale) * math.sqrt(sum(float(np.square(t.float().cpu().numpy().astype(np.float64)).sum()) for t in ts))
+    got = norm.cpu().numpy().astype(np.float64)
+    factor = min(1.0, max_norm / want) if want else 1.0
+    assert abs(got[0] - want) <= 2.0 ** -23 * want, (got, want)
+    assert abs(got[1] - factor) <= 2.0 ** -23 * factor, (got, factor)
+    return factor
+
+
+SIZES = [[1], [7], [4096], [4097], [0, 1, 0, 2, 3, 5, 31, 4095, 16385], [100003, 8, 50001], [3] * 300, [1 << 24, 16385, 1]]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("sizes", SIZES, ids=lambda s: f"{len(s)}x{sum(s)}")
+def test_norm_and_clip(dtype, sizes):
+    for pad in (0, 1, 3):
+        flat, ts = tensors(dtype, sizes, 0.3, pad)
+        before = flat.clone()
+        norm = norm_of(dtype, ts, 0.05, -0.25)
+        factor = check_norm(norm, ts, 0.05, -0.25)
+        assert factor < 1 or sum(sizes) == 1
+        # into a copy of another alignment, with guards around and between
+        for shift in (pad, pad + 1):
+            out = torch.full((sum(sizes) + shift + 5,), 7.0, device="cuda").to(TD[dtype])
+            outs, at = [], shift
+            for n in sizes:
+                outs.append(out[at:at + n])
+                at += n
+            B.dapple_grad_clip(dtype, ptrs(ts), ptrs(outs), sizes, norm.data_ptr())
+            want = before[pad:].double() * factor
+            got = out[shift:shift + sum(sizes)].double()
+            tol = 2.0 ** -23 * 1.01 + (2.0 ** -8 if dtype == B.DTYPE_BF16 else 0.0)
+            assert bool(((got - want).abs() <= tol * want.abs() + 1e-44).all())
+            assert bool((out[:shift] == 7).all()) and bool((out[shift + sum(sizes):] == 7).all())
+        assert torch.equal(flat, before)
+        clipped = out[shift:shift + sum(sizes)].clone()
+        B.dapple_grad_clip(dtype, ptrs(ts), None, sizes, norm.data_ptr())      # in place
+        assert torch.equal(flat[pad:], clipped) and torch.equal(flat[:pad], before[:pad])
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_small_norm_is_left_alone(dtype):
+    flat, ts = tensors(dtype, [1000, 24], 1e-3)
+    for max_norm in (1.0, math.inf):
+        norm = norm_of(dtype, ts, max_norm)
+        check_norm(norm, ts, max_norm)
+        before = flat.clone()
+        B.dapple_grad_clip(dtype, ptrs(ts), None, [1000, 24], norm.data_ptr())
+        assert float(norm[1]) == 1.0 and torch.equal(flat, before)
+    flat.zero_()
+    assert norm_of(dtype, ts, 1.0).tolist() == [0.0, 1.0]
+    assert norm_of(dtype, [], 1.0).tolist() == [0.0, 1.0]
+
+
+@pytest.mark.parametrize("scale", [1e-25, 1e25])
+def test_squares_neither_vanish_nor_overflow(scale):
+    _, ts = tensors(B.DTYPE_F32, [5000, 77], scale)
+    check_norm(norm_of(B.DTYPE_F32, ts, 1.0), ts, 1.0)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+def test_a_norm_that_is_not_finite(dtype, bad):
+    flat, ts = tensors(dtype, [300, 70000])
+    ts[1][69999] = bad
+    norm = norm_of(dtype, ts, 1.0)
+    assert not math.isfinite(float(norm[0])) and float(norm[1]) == 0.0
+    out = torch.full_like(flat, 7.0)
+    B.dapple_grad_clip(dtype, ptrs(ts), ptrs([out[:300], out[300:]]), [300, 70000], norm.data_ptr())
+    assert bool((out == 0).all())
+
+
+def test_same_bits_on_another_stream_and_in_a_graph():
+    sizes = [3, 40000, 1 << 18] + [17] * 140
+    flat, ts = tensors(B.DTYPE_F32, sizes)
+    want = norm_of(B.DTYPE_F32, ts, 1.0)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        other = norm_of(B.DTYPE_F32, ts, 1.0, stream=side.cuda_stream)
+    torch.cuda.synchronize()
+    assert torch.equal(want, other)
+    out = torch.empty_like(flat)
+    outs, at = [], 0
+    for n in sizes:
+        outs.append(out[at:at + n])
+        at += n
+    norm = torch.empty(2, device="cuda")
+    ws = torch.empty(B.dapple_grad_norm_workspace(sizes), dtype=torch.uint8, device="cuda")
+
+    def run():
+        sp = torch.cuda.current_stream().cuda_stream
+        B.dapple_grad_norm(B.DTYPE_F32, ptrs(ts), sizes, 1.0, norm.data_ptr(), ws.data_ptr(), 1.0, sp)
+        B.dapple_grad_clip(B.DTYPE_F32, ptrs(ts), ptrs(outs), sizes, norm.data_ptr(), sp)
+
+    run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    for k in range(3):
+        flat.mul_(1.5)
+        run()
+        torch.cuda.synchronize()
+        eager = (norm.clone(), out.clone())
+        norm.zero_(), out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(norm, eager[0]) and torch.equal(out, eager[1]), k
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_adam_with_clipping(dtype):
+    cfg = I.StageConfig(1, 64, 4, 136, 16, 2, 2, 2, dtype)      # n_params is not a multiple of 4
+    theta = I.make_params(cfg, 11)
+    r = B.StageRunner(c_config(cfg, 2), theta)
+    try:
+        r.init_adam()
+        n = theta.size
+        th, m, v = r.master.cpu().numpy().astype(np.float64), np.zeros(n), np.zeros(n)
+        for step, size in ((1, 1e-3), (2, 10.0)):               # below and above the limit
+            G = (size * I.normal(3, f"G{step}", n)).astype(np.float32)
+            r.grads.copy_(torch.from_numpy(G))
+            norm = r.apply_adam_clipped(1e-2, 1.0, grad_scale=0.5, zero_grads=step == 2)
+            torch.cuda.synchronize()
+            full = 0.5 * np.linalg.norm(G.astype(np.float64))
+            factor = min(1.0, 1.0 / full)
+            assert abs(float(norm[0]) - full) <= 2.0 ** -23 * full and (factor < 1) == (step == 2)
+            th, m, v = O.adam_apply(th, m, v, G.astype(np.float64), step, 1e-2, 0.9, 0.999, 1e-8, 0.5 * factor)
+            got = r.master.cpu().numpy().astype(np.float64)
+            # (the bound of the unclipped update: its fp32 arithmetic is the same)
+            assert np.abs(got - th).max() <= 2e-6 * 1e-2 + 1e-6 * np.abs(th).max()
+            assert np.count_nonzero(r.grads.cpu().numpy()) == (0 if step == 2 else n)
+        # the same factor given from outside, and one that clips nothing: the unclipped update, bit for bit
+        state = [t.clone() for t in (r.master, r.m, r.v)]
+        r.grads.copy_(torch.from_numpy(G))
+        r.apply_adam(1e-2, grad_scale=0.5)
+        plain = [t.clone() for t in (r.master, r.m, r.v)]
+        for t, s in zip((r.master, r.m, r.v), state):
+            t.copy_(s)
+        r.step -= 1
+        r.apply_adam_clipped(1e-2, 1.0, grad_scale=0.5, norm=torch.tensor([3.0, 1.0], device="cuda"))
+        assert all(torch.equal(a, b) for a, b in zip(plain, (r.master, r.m, r.v)))
+        # a norm that is not finite: nothing moves, the accumulators are cleared
+        before = [t.clone() for t in (r.master, r.m, r.v, r.weights)]
+        r.grads[5] = math.inf
+        norm = r.apply_adam_clipped(1e-2, 1.0, zero_grads=True)
+        torch.cuda.synchronize()
+        assert not math.isfinite(float(norm[0]))
+        assert all(torch.equal(a, b) for a, b in zip(before, (r.master, r.m, r.v, r.weights)))
+        assert np.count_nonzero(r.grads.cpu().numpy()) == 0
+    finally:
+        r.close()
+
+
+def test_one_norm_over_the_stages_of_a_pipeline():
+    runners = [B.StageRunner(c_config(I.StageConfig(1, 64, 4, f, 16, 2, 2, 2, "f32"), 2),
+                             I.make_params(I.StageConfig(1, 64, 4, f, 16, 2, 2, 2, "f32"), 11 + f)) for f in (136, 256)]
+    try:
+        for i, r in enumerate(runners):
+            r.init_adam()
+            r.grads.copy_(torch.from_numpy(I.normal(9, f"G{i}", r.grads.numel()).astype(np.float32)))
+        norm = norm_of(B.DTYPE_F32, [r.grads for r in runners], 1.0)
+        check_norm(norm, [r.grads for r in runners], 1.0)
+        for r in runners:
+            G, th = r.grads.cpu().numpy().astype(np.float64), r.master.cpu().numpy().astype(np.float64)
+            want, _, _ = O.adam_apply(th, 0 * th, 0 * th, G, 1, 1e-2, 0.9, 0.999, 1e-3, float(norm[1]))
+            r.apply_adam_clipped(1e-2, 1.0, eps=1e-3, norm=norm)
+            torch.cuda.synchronize()
+            assert np.abs(r.master.cpu().numpy() - want).max() <= 2e-6 * 1e-2 + 1e-6 * np.abs(th).max()
+    finally:
+        for r in runners:
+            r.close()

@@ -1,0 +1,55 @@
+"""What the operators of dapple_kernels.h refuse, checked on the host: every call here returns before anything is enqueued
+(the pointers are no memory)."""
+import math
+
+import pytest
+
+from paper_2007_01045_amd import binding as B
+
+P = 0x10000        # an aligned address that nothing looks at
+
+
+def refused(code, f, *args, **kw):
+    with pytest.raises(B.StageError) as e:
+        f(*args, **kw)
+    assert e.value.code == code, (e.value, args, kw)
+    assert str(e.value).split(": ", 1)[1], "the refusal gives no reason"
+
+
+def test_grad_norm_refusals():
+    ok = dict(dtype=B.DTYPE_F32, grad_ptrs=[P, P], sizes=[3, 5], max_norm=1.0, norm_ptr=P, workspace_ptr=P, grad_scale=1.0)
+    for code, change in [(B.STAGE_E_NULL, dict(norm_ptr=None)), (B.STAGE_E_NULL, dict(workspace_ptr=None)),
+                         (B.STAGE_E_NULL, dict(grad_ptrs=None)), (B.STAGE_E_NULL, dict(grad_ptrs=[P, None])),
+                         (B.STAGE_E_CONFIG, dict(dtype=2)), (B.STAGE_E_CONFIG, dict(sizes=[3, -1])),
+                         (B.STAGE_E_CONFIG, dict(sizes=[3, 1 << 41])), (B.STAGE_E_CONFIG, dict(max_norm=0.0)),
+                         (B.STAGE_E_CONFIG, dict(max_norm=-1.0)), (B.STAGE_E_CONFIG, dict(max_norm=math.nan)),
+                         (B.STAGE_E_CONFIG, dict(grad_scale=math.inf)), (B.STAGE_E_CONFIG, dict(grad_scale=math.nan)),
+                         (B.STAGE_E_CONFIG, dict(grad_ptrs=[P, P + 2])), (B.STAGE_E_CONFIG, dict(workspace_ptr=P + 4)),
+                         (B.STAGE_E_CONFIG, dict(norm_ptr=P + 2))]:
+        refused(code, B.dapple_grad_norm, **dict(ok, **change))
+    refused(B.STAGE_E_CONFIG, B.dapple_grad_norm, **dict(ok, dtype=B.DTYPE_BF16, grad_ptrs=[P, P + 1]))
+    refused(B.STAGE_E_CONFIG, B.dapple_grad_norm_workspace, [-1])
+    assert B.dapple_grad_norm_workspace([]) > 0 and B.dapple_grad_norm_workspace([0, 0]) > 0
+    assert B.dapple_grad_norm_workspace([1, 0, 1]) == 2 * B.dapple_grad_norm_workspace([1])
+
+
+def test_grad_clip_refusals():
+    ok = dict(dtype=B.DTYPE_F32, grad_ptrs=[P, P], out_ptrs=[P, P], sizes=[3, 5], norm_ptr=P)
+    for code, change in [(B.STAGE_E_NULL, dict(norm_ptr=None)), (B.STAGE_E_NULL, dict(grad_ptrs=None)),
+                         (B.STAGE_E_NULL, dict(out_ptrs=[P, None])), (B.STAGE_E_CONFIG, dict(dtype=-1)),
+                         (B.STAGE_E_CONFIG, dict(sizes=[-3, 5])), (B.STAGE_E_CONFIG, dict(out_ptrs=[P, P + 1]))]:
+        refused(code, B.dapple_grad_clip, **dict(ok, **change))
+
+
+def test_clipped_adam_refusals():
+    cfg = B.make_config(1, 64, 4, 128, 16, 2, 2, B.DTYPE_F32, flags=B.FLAG_DRY_RUN)
+    h = B.stage_init(cfg, None, None, 0)
+    try:
+        B.stage_apply_adam_clipped(h, None, None, None, None, 1, 1e-3, None)      # (a dry run has no device memory)
+        refused(B.STAGE_E_CONFIG, B.stage_apply_adam_clipped, h, P, P, P, P, 0, 1e-3, P)
+        refused(B.STAGE_E_CONFIG, B.stage_apply_adam_clipped, h, P, P, P, P, 1, 1e-3, P, eps=0.0)
+        B.stage_fwd(h, 0, None, None)
+        refused(B.STAGE_E_BAD_ORDER, B.stage_apply_adam_clipped, h, P, P, P, P, 1, 1e-3, P)
+    finally:
+        B.stage_destroy(h)
+    refused(B.STAGE_E_NULL, B.stage_apply_adam_clipped, None, P, P, P, P, 1, 1e-3, P)
