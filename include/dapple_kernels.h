@@ -128,6 +128,51 @@ int dapple_colsum_static(int dtype, const void* X, int rows, int cols, int ld, f
  * the size that the operator's *_workspace function returns (host only; a negative code for a call that would be refused),
  * 16-byte aligned, whose contents do not matter before or after: calls that may overlap need one each. */
 
+/* RMS norm of every query and key head and the rotation by position, in one pass (forward), and its gradient.
+ * Row r of q holds A heads of d columns, head h in columns [h d, (h+1) d) of q + r*ldq; k holds Ak heads likewise (Ak = 0: no
+ * keys, its pointers are not looked at).  Per head:
+ *   n = x * gamma / sqrt(mean(x^2) + eps)         gamma_q for queries, gamma_k for keys, [d]; both NULL: n = x
+ *   the first `rot` columns turn in pairs, (a, b) -> (a c - b s, a s + b c), (c, s) = table[position][pair]:
+ *     interleaved = 0: pair i is columns i and i + rot/2;   1: columns 2i and 2i + 1
+ *   columns from rot on are n's.  rot = 0: no rotation (table is not looked at).
+ * table: fp32 [max_pos][rot/2][2], as dapple_rope_table or the caller makes it.  positions: int32 [rows], NULL = r % seq (seq 0:
+ * r); a position outside [0, max_pos) reads nothing and gives NaN in the columns that turn.
+ * Types: q, k, gammas and outputs of dtype; table, dgamma and all arithmetic fp32.  Row strides in elements, 0 = dense.  An
+ * output may be its input (yq = q with ldyq = ldq, dq = dyq, ...), else they do not overlap.  Limits: d <= 256, rot even and <= d,
+ * rows >= 1; interleaved needs d and the strides even and addresses aligned to two elements; everything aligned to 16 bytes
+ * (d, rot/2 or interleaved rot, strides, addresses) is fastest.
+ * Backward: dyq, dyk in, dq, dk out (q and k are read only with gammas), dgamma_q, dgamma_k [d] fp32: set, or with accumulate != 0
+ * added to; NULL = not wanted.  workspace only where a dgamma is wanted. */
+typedef struct {
+  const void* q;
+  const void* k;
+  const void* gamma_q;
+  const void* gamma_k;
+  const int32_t* positions;
+  const float* table;
+  void* yq;
+  void* yk;
+  const void* dyq;
+  const void* dyk;
+  void* dq;
+  void* dk;
+  float* dgamma_q;
+  float* dgamma_k;
+  void* workspace;
+  int32_t rows, A, Ak, d, rot, interleaved, seq, max_pos, accumulate;
+  int32_t ldq, ldk, ldyq, ldyk, lddyq, lddyk, lddq, lddk;
+  float eps;
+} dapple_qk_rope_desc;
+int dapple_qk_rope_fwd(int dtype, const dapple_qk_rope_desc* d, void* stream);
+int64_t dapple_qk_rope_workspace(int dtype, const dapple_qk_rope_desc* d);
+int dapple_qk_rope_bwd(int dtype, const dapple_qk_rope_desc* d, void* stream);
+/* table[p][i] = magnitude * (cos, sin)(p * f_i), i < rot/2, angles and functions in 64 bits.  With w_i = base^(-2i/rot):
+ *   factor = 1: f_i = w_i;   original = 0: f_i = w_i / factor (positions interpolated)
+ *   original > 0, the context that the model was trained on: by parts, f_i = w_i (g + (1 - g) / factor), g = 0 for pairs that turn
+ *   at most `low` times within it, 1 from `high` times on, linear in the turns between. */
+int dapple_rope_table(float* table, int max_pos, int rot, double base, double factor, int original, double low, double high,
+                      double magnitude, void* stream);
+
 /* The global norm of n gradient tensors, all of one dtype: grads and sizes are HOST arrays of n device pointers (aligned to
  * their elements) and element counts (0 is allowed, its pointer is not looked at).
  *   norm_dev[0] = |grad_scale| * sqrt(sum of all squares)      (squares and sums in 64 bits)

@@ -55,6 +55,15 @@ class dapple_gemm_desc(C.Structure):
                 ("k_valid", C.c_int32), ("epi", C.c_int32), ("tile", C.c_int32)]
 
 
+class qk_rope_desc(C.Structure):      # dapple_qk_rope_desc
+    _fields_ = [(n, C.c_void_p) for n in
+                ("q", "k", "gamma_q", "gamma_k", "positions", "table", "yq", "yk", "dyq", "dyk", "dq", "dk", "dgamma_q", "dgamma_k",
+                 "workspace")] + \
+               [(n, C.c_int32) for n in
+                ("rows", "A", "Ak", "d", "rot", "interleaved", "seq", "max_pos", "accumulate",
+                 "ldq", "ldk", "ldyq", "ldyk", "lddyq", "lddyk", "lddq", "lddk")] + [("eps", C.c_float)]
+
+
 # every symbol the two headers declare: name -> (restype, argtypes)
 _vp, _i, _f = C.c_void_p, C.c_int, C.c_float
 _pp = C.POINTER(C.c_void_p)
@@ -102,6 +111,10 @@ SYMBOLS = {
     "dapple_layernorm_bwd": (_i, [_i, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i, _i, _vp]),
     "dapple_colsum": (_i, [_i, _vp, _i, _i, _i, _vp, _vp, _vp]),
     "dapple_colsum_static": (_i, [_i, _vp, _i, _i, _i, _vp, _vp]),
+    "dapple_qk_rope_fwd": (_i, [_i, C.POINTER(qk_rope_desc), _vp]),
+    "dapple_qk_rope_workspace": (C.c_int64, [_i, C.POINTER(qk_rope_desc)]),
+    "dapple_qk_rope_bwd": (_i, [_i, C.POINTER(qk_rope_desc), _vp]),
+    "dapple_rope_table": (_i, [_vp, _i, _i, C.c_double, C.c_double, _i, C.c_double, C.c_double, C.c_double, _vp]),
     "dapple_grad_norm_workspace": (C.c_int64, [C.POINTER(C.c_int64), _i]),
     "dapple_grad_norm": (_i, [_i, _pp, C.POINTER(C.c_int64), _i, _f, _f, _vp, _vp, _vp]),
     "dapple_grad_clip": (_i, [_i, _pp, _pp, C.POINTER(C.c_int64), _i, _vp, _vp]),
@@ -436,6 +449,24 @@ def dapple_colsum_static(dtype, X, rows, cols, ld, out, stream_ptr=None):
 
 
 # ---- operators of layers and training steps (second part of dapple_kernels.h) ----
+def dapple_qk_rope_fwd(dtype, desc: qk_rope_desc, stream_ptr=None):
+    _check(load().dapple_qk_rope_fwd(dtype, C.byref(desc), stream_ptr))
+
+
+def dapple_qk_rope_workspace(dtype, desc: qk_rope_desc) -> int:
+    return _check(load().dapple_qk_rope_workspace(dtype, C.byref(desc)))
+
+
+def dapple_qk_rope_bwd(dtype, desc: qk_rope_desc, stream_ptr=None):
+    _check(load().dapple_qk_rope_bwd(dtype, C.byref(desc), stream_ptr))
+
+
+def dapple_rope_table(table_ptr, max_pos, rot, base=10000.0, factor=1.0, original=0, low=1.0, high=32.0, magnitude=1.0,
+                      stream_ptr=None):
+    """Fills the fp32 table [max_pos, rot / 2, 2] of dapple_qk_rope_fwd and _bwd on the device."""
+    _check(load().dapple_rope_table(table_ptr, max_pos, rot, base, factor, original, low, high, magnitude, stream_ptr))
+
+
 def _i64_array(sizes):
     return (C.c_int64 * len(sizes))(*sizes)
 

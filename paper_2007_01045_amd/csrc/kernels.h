@@ -220,6 +220,27 @@ hipError_t launch_reduce_jobs(const ReduceJobs& J, hipStream_t st);
 hipError_t launch_copy(void* dst, const void* src, size_t bytes, hipStream_t st);
 hipError_t launch_zero(void* dst, size_t bytes, hipStream_t st);
 
+// ---------------------------------------------------------------- head norms and rotation (qk_rope.hip)
+// rows of A query heads and Ak key heads of d columns at row strides in elements; table [max_pos][rot / 2] of (cos, sin)
+struct QkRopeArgs {
+  const void *q, *k, *gamma_q, *gamma_k;   // gammas NULL: no norm
+  const int32_t* positions;                // NULL: row % seq (seq 0: the row)
+  const float* table;
+  void *yq, *yk;
+  const void *dyq, *dyk;
+  void *dq, *dk;
+  float *dgamma_q, *dgamma_k;              // NULL: not wanted
+  int rows, A, Ak, d, rot, interleaved, seq, max_pos, accumulate;
+  int ldq, ldk, ldyq, ldyk, lddyq, lddyk, lddq, lddk;
+  float eps;
+};
+bool qk_rope_takes(Dtype dt, const QkRopeArgs& a, bool bwd);   // (neighbouring pairs at odd strides or addresses: not)
+int qk_rope_blocks(long rows);   // partial: that many blocks of 2 d floats
+hipError_t launch_qk_rope_fwd(Dtype dt, const QkRopeArgs& a, hipStream_t st);
+hipError_t launch_qk_rope_bwd(Dtype dt, const QkRopeArgs& a, float* partial, hipStream_t st);
+// freq: host, up to 128 of them
+hipError_t launch_rope_table(float* table, int max_pos, int pairs, const double* freq, double magnitude, hipStream_t st);
+
 // ---------------------------------------------------------------- embedding / head
 // e[r] = E_w[ids[r]] + E_p[r % s]
 hipError_t launch_embed_gather(Dtype dt, const int32_t* ids, const void* Ew, const void* Ep, void* e, int rows, int s,

@@ -17,6 +17,96 @@ static int rc_of(hipError_t e) {
   return e == hipSuccess ? STAGE_OK : set_error(STAGE_E_DEVICE, "a launch failed: %s", hipGetErrorString(e));
 }
 
+// ------------------------------------------------------------------ head norms and rotation
+// the launcher's arguments; workspace_only: what the size of the workspace depends on
+static int rope_args(int dtype, const dapple_qk_rope_desc* d, bool bwd, bool workspace_only, QkRopeArgs& a) {
+  if (!d) return set_error(STAGE_E_NULL, "the descriptor is NULL");
+  if (bad_dtype(dtype)) return set_error(STAGE_E_CONFIG, "dtype %d", dtype);
+  if (d->rows < 1 || d->A < 1 || d->Ak < 0 || d->d < 1 || d->d > 256)
+    return set_error(STAGE_E_CONFIG, "rows %d, heads %d and %d of %d columns (at most 256)", d->rows, d->A, d->Ak, d->d);
+  if (workspace_only) return STAGE_OK;
+  if (d->rot < 0 || d->rot % 2 || d->rot > d->d) return set_error(STAGE_E_CONFIG, "%d of %d columns to turn", d->rot, d->d);
+  if (d->seq < 0 || (d->rot && d->max_pos < 1)) return set_error(STAGE_E_CONFIG, "seq %d, max_pos %d", d->seq, d->max_pos);
+  const bool keys = d->Ak > 0, norm = d->gamma_q != nullptr;
+  if (keys && norm != (d->gamma_k != nullptr)) return set_error(STAGE_E_CONFIG, "one gamma without the other");
+  if (!norm && !d->rot) return set_error(STAGE_E_CONFIG, "neither a norm nor a rotation");
+  if (norm && !(d->eps >= 0.f)) return set_error(STAGE_E_CONFIG, "eps must not be negative");
+  if (d->rot && !d->table) return set_error(STAGE_E_NULL, "table is NULL");
+  if (((!bwd || norm) && (!d->q || (keys && !d->k))) || (!bwd && (!d->yq || (keys && !d->yk))) ||
+      (bwd && (!d->dyq || !d->dq || (keys && (!d->dyk || !d->dk)))))
+    return set_error(STAGE_E_NULL, "a tensor is NULL");
+  a.q = d->q; a.gamma_q = d->gamma_q; a.yq = d->yq; a.dyq = d->dyq; a.dq = d->dq; a.dgamma_q = norm ? d->dgamma_q : nullptr;
+  if (keys) {
+    a.k = d->k; a.gamma_k = d->gamma_k; a.yk = d->yk; a.dyk = d->dyk; a.dk = d->dk; a.dgamma_k = norm ? d->dgamma_k : nullptr;
+  }
+  a.positions = d->positions; a.table = d->table;
+  a.rows = d->rows; a.A = d->A; a.Ak = d->Ak; a.d = d->d; a.rot = d->rot; a.interleaved = d->interleaved != 0; a.seq = d->seq;
+  a.max_pos = d->max_pos; a.accumulate = d->accumulate != 0; a.eps = d->eps;
+  const struct { int given; int heads; int* to; } lds[] = {{d->ldq, d->A, &a.ldq}, {d->ldk, d->Ak, &a.ldk},
+      {d->ldyq, d->A, &a.ldyq}, {d->ldyk, d->Ak, &a.ldyk}, {d->lddyq, d->A, &a.lddyq}, {d->lddyk, d->Ak, &a.lddyk},
+      {d->lddq, d->A, &a.lddq}, {d->lddk, d->Ak, &a.lddk}};
+  for (const auto& l : lds) {
+    const long dense = (long)l.heads * d->d;
+    if (dense > 0x7fffffffL || l.given < 0 || (l.given && l.given < dense))
+      return set_error(STAGE_E_CONFIG, "a row stride of %d for %ld columns", l.given, dense);
+    *l.to = l.given ? l.given : (int)dense;
+  }
+  const size_t es = dtype == STAGE_DTYPE_BF16 ? 2 : 4;
+  const void* ps[] = {a.q, a.k, a.gamma_q, a.gamma_k, bwd ? a.dyq : a.yq, bwd ? a.dyk : a.yk, bwd ? a.dq : nullptr, bwd ? a.dk : nullptr};
+  for (const void* p : ps)
+    if (!aligned_to(p, es)) return set_error(STAGE_E_CONFIG, "a tensor is not aligned to its elements");
+  if (!aligned_to(a.table, 8) || !aligned_to(a.positions, 4) || !aligned_to(a.dgamma_q, 4) || !aligned_to(a.dgamma_k, 4))
+    return set_error(STAGE_E_CONFIG, "table, positions or dgamma not aligned");
+  if (!qk_rope_takes(type_of(dtype), a, bwd))
+    return set_error(STAGE_E_CONFIG, "interleaved pairs need an even d, even strides and addresses aligned to two elements");
+  return STAGE_OK;
+}
+
+extern "C" {
+
+int dapple_qk_rope_fwd(int dtype, const dapple_qk_rope_desc* d, void* stream) {
+  QkRopeArgs a{};
+  const int rc = rope_args(dtype, d, false, false, a);
+  return rc != STAGE_OK ? rc : rc_of(launch_qk_rope_fwd(type_of(dtype), a, (hipStream_t)stream));
+}
+
+int64_t dapple_qk_rope_workspace(int dtype, const dapple_qk_rope_desc* d) {
+  QkRopeArgs a{};
+  const int rc = rope_args(dtype, d, true, true, a);
+  return rc != STAGE_OK ? rc : (int64_t)qk_rope_blocks(d->rows) * 2 * d->d * 4;
+}
+
+int dapple_qk_rope_bwd(int dtype, const dapple_qk_rope_desc* d, void* stream) {
+  QkRopeArgs a{};
+  const int rc = rope_args(dtype, d, true, false, a);
+  if (rc != STAGE_OK) return rc;
+  if (a.dgamma_q || a.dgamma_k) {
+    if (!d->workspace) return set_error(STAGE_E_NULL, "workspace is NULL");
+    if (!aligned_to(d->workspace, 16)) return set_error(STAGE_E_CONFIG, "workspace not aligned to 16 bytes");
+  }
+  return rc_of(launch_qk_rope_bwd(type_of(dtype), a, (float*)d->workspace, (hipStream_t)stream));
+}
+
+int dapple_rope_table(float* table, int max_pos, int rot, double base, double factor, int original, double low, double high,
+                      double magnitude, void* stream) {
+  if (!table) return set_error(STAGE_E_NULL, "table is NULL");
+  if (max_pos < 1 || rot < 2 || rot % 2 || rot > 256) return set_error(STAGE_E_CONFIG, "max_pos %d, rot %d", max_pos, rot);
+  if (!(base > 0) || !std::isfinite(base) || !(factor > 0) || !std::isfinite(factor) || !std::isfinite(magnitude) || original < 0 ||
+      (original > 0 && !(low < high && std::isfinite(low) && std::isfinite(high))))
+    return set_error(STAGE_E_CONFIG, "base and factor must be positive and finite, low below high");
+  if (!aligned_to(table, 8)) return set_error(STAGE_E_CONFIG, "table not aligned to 8 bytes");
+  double f[128];
+  for (int i = 0; i < rot / 2; ++i) {
+    const double w = std::pow(base, -2.0 * i / rot);
+    double g = 0.0;
+    if (original > 0) g = std::fmin(1.0, std::fmax(0.0, (original * w / (2.0 * M_PI) - low) / (high - low)));
+    f[i] = w * (g + (1.0 - g) / factor);
+  }
+  return rc_of(launch_rope_table(table, max_pos, rot / 2, f, magnitude, (hipStream_t)stream));
+}
+
+}  // extern "C"
+
 // ------------------------------------------------------------------ gradient norm
 static int check_sizes(const int64_t* sizes, int n) {
   if (n < 0) return set_error(STAGE_E_CONFIG, "%d tensors", n);

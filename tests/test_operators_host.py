@@ -53,3 +53,36 @@ def test_clipped_adam_refusals():
     finally:
         B.stage_destroy(h)
     refused(B.STAGE_E_NULL, B.stage_apply_adam_clipped, None, P, P, P, P, 1, 1e-3, P)
+
+
+def test_qk_rope_refusals():
+    ok = dict(q=P, k=P, gamma_q=P, gamma_k=P, positions=P, table=P, yq=P, yk=P, dyq=P, dyk=P, dq=P, dk=P, dgamma_q=P, dgamma_k=P,
+              workspace=P, rows=4, A=2, Ak=1, d=64, rot=32, interleaved=0, seq=0, max_pos=16, eps=1e-6)
+    null, conf = B.STAGE_E_NULL, B.STAGE_E_CONFIG
+    both = [(null, dict(q=None)), (null, dict(k=None)), (null, dict(table=None)), (conf, dict(rows=0)), (conf, dict(A=0)), (conf, dict(Ak=-1)),
+            (conf, dict(d=0)), (conf, dict(d=257)), (conf, dict(rot=33)), (conf, dict(rot=66)), (conf, dict(rot=-2)), (conf, dict(max_pos=0)),
+            (conf, dict(seq=-1)), (conf, dict(gamma_k=None)), (conf, dict(gamma_q=None)), (conf, dict(gamma_q=None, gamma_k=None, rot=0)),
+            (conf, dict(eps=-1.0)), (conf, dict(eps=math.nan)), (conf, dict(ldq=127)), (conf, dict(ldk=-64)), (conf, dict(q=P + 1)),
+            (conf, dict(table=P + 4)), (conf, dict(positions=P + 2)), (conf, dict(interleaved=1, ldq=129)),
+            (conf, dict(interleaved=1, k=P + 2)), (conf, dict(interleaved=1, d=63, rot=32))]
+    for dt in (B.DTYPE_BF16, 2):
+        for code, change in both if dt == B.DTYPE_BF16 else [(conf, {})]:
+            for f in (B.dapple_qk_rope_fwd, B.dapple_qk_rope_bwd):
+                refused(code, f, dt, B.qk_rope_desc(**dict(ok, **change)))
+    for change in (dict(yq=None), dict(yk=None)):
+        refused(null, B.dapple_qk_rope_fwd, B.DTYPE_F32, B.qk_rope_desc(**dict(ok, **change)))
+    for change in (dict(dyq=None), dict(dyk=None), dict(dq=None), dict(dk=None), dict(workspace=None)):
+        refused(null, B.dapple_qk_rope_bwd, B.DTYPE_F32, B.qk_rope_desc(**dict(ok, **change)))
+    refused(conf, B.dapple_qk_rope_bwd, B.DTYPE_F32, B.qk_rope_desc(**dict(ok, workspace=P + 8)))
+    refused(conf, B.dapple_qk_rope_bwd, B.DTYPE_F32, B.qk_rope_desc(**dict(ok, dgamma_q=P + 2)))
+    refused(conf, B.dapple_qk_rope_workspace, B.DTYPE_F32, B.qk_rope_desc(**dict(ok, rows=0)))
+    assert B.dapple_qk_rope_workspace(B.DTYPE_F32, B.qk_rope_desc(**ok)) >= 2 * 64 * 4
+
+
+def test_rope_table_refusals():
+    refused(B.STAGE_E_NULL, B.dapple_rope_table, None, 4, 8)
+    for args, kw in [((0, 8), {}), ((4, 0), {}), ((4, 7), {}), ((4, 258), {}), ((4, 8), dict(base=0.0)), ((4, 8), dict(base=math.nan)),
+                     ((4, 8), dict(factor=0.0)), ((4, 8), dict(factor=math.inf)), ((4, 8), dict(original=-1)),
+                     ((4, 8), dict(original=16, low=2.0, high=2.0)), ((4, 8), dict(magnitude=math.nan))]:
+        refused(B.STAGE_E_CONFIG, B.dapple_rope_table, P, *args, **kw)
+    refused(B.STAGE_E_CONFIG, B.dapple_rope_table, P + 4, 4, 8)
