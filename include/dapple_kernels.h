@@ -128,6 +128,40 @@ int dapple_colsum_static(int dtype, const void* X, int rows, int cols, int ld, f
  * the size that the operator's *_workspace function returns (host only; a negative code for a call that would be refused),
  * 16-byte aligned, whose contents do not matter before or after: calls that may overlap need one each. */
 
+/* Attention with a window, first tokens that stay visible, shared key heads and sequences of their own lengths.
+ * b sequences of s rows; row r of q holds A heads of d columns (head h in columns [h d, (h+1) d) of q + r*ldq), k and v hold
+ * Ak heads, Ak divides A, query head h reads key head h / (A / Ak).  Query i sees key j of its sequence where
+ *   j < len  and  (causal = 0 or j <= i)  and  (window = 0 or |i - j| < window or j < sinks)
+ * lens: device int32 [b], clamped to [0, s]; NULL = s.  Rows at and behind len see nothing and are seen by nobody; what q, k, v
+ * and dctx hold there is not used, and their ctx, dq, dk, dv are set to 0, their lse to -infinity.  Before len, inputs are finite.
+ * fwd: ctx = softmax(scale q k^T) v of the visible keys, lse [b,A,s] fp32 = log2 of the sum of 2^(scale log2(e) q k).  ctx32 (may be
+ * NULL): an unrounded fp32 ctx in ctx's layout; given to bwd, the row sums of dctx*ctx come from it (a bf16 ctx costs dq and dk
+ * accuracy where gradients are sums of many layers').
+ * bwd: dq, dk, dv from dctx and the ctx, ctx32 (or NULL) and lse of fwd; dk and dv are summed over the heads that share them.
+ * scale > 0; 0 = 1/sqrt(d).  Row strides in elements, 0 = dense; q, k, v may be columns of one buffer, and dq, dk, dv of another;
+ * outputs overlap no input.  bf16: d and strides multiples of 8; fp32: of 4; d <= 128, strides below 2^23, s * stride below 2^30 - 4096;
+ * all tensors 16-byte aligned.  Probabilities and dS are rounded once to bf16 in bf16 calls, for their products. */
+typedef struct {
+  const void* q;
+  const void* k;
+  const void* v;
+  void* ctx;
+  float* ctx32;
+  float* lse;
+  const int32_t* lens;
+  const void* dctx;
+  void* dq;
+  void* dk;
+  void* dv;
+  void* workspace; /* bwd */
+  int32_t b, s, A, Ak, d, window, sinks, causal;
+  int32_t ldq, ldk, ldv, ldc, lddc, lddq, lddk, lddv; /* ldc: of ctx and ctx32 */
+  float scale;
+} dapple_attention_window_desc;
+int dapple_attention_window_fwd(int dtype, const dapple_attention_window_desc* d, void* stream);
+int64_t dapple_attention_window_workspace(int dtype, const dapple_attention_window_desc* d);
+int dapple_attention_window_bwd(int dtype, const dapple_attention_window_desc* d, void* stream);
+
 /* RMS norm of every query and key head and the rotation by position, in one pass (forward), and its gradient.
  * Row r of q holds A heads of d columns, head h in columns [h d, (h+1) d) of q + r*ldq; k holds Ak heads likewise (Ak = 0: no
  * keys, its pointers are not looked at).  Per head:

@@ -64,6 +64,14 @@ class qk_rope_desc(C.Structure):      # dapple_qk_rope_desc
                  "ldq", "ldk", "ldyq", "ldyk", "lddyq", "lddyk", "lddq", "lddk")] + [("eps", C.c_float)]
 
 
+class attention_window_desc(C.Structure):      # dapple_attention_window_desc
+    _fields_ = [(n, C.c_void_p) for n in
+                ("q", "k", "v", "ctx", "ctx32", "lse", "lens", "dctx", "dq", "dk", "dv", "workspace")] + \
+               [(n, C.c_int32) for n in
+                ("b", "s", "A", "Ak", "d", "window", "sinks", "causal",
+                 "ldq", "ldk", "ldv", "ldc", "lddc", "lddq", "lddk", "lddv")] + [("scale", C.c_float)]
+
+
 # every symbol the two headers declare: name -> (restype, argtypes)
 _vp, _i, _f = C.c_void_p, C.c_int, C.c_float
 _pp = C.POINTER(C.c_void_p)
@@ -111,6 +119,9 @@ SYMBOLS = {
     "dapple_layernorm_bwd": (_i, [_i, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i, _i, _vp]),
     "dapple_colsum": (_i, [_i, _vp, _i, _i, _i, _vp, _vp, _vp]),
     "dapple_colsum_static": (_i, [_i, _vp, _i, _i, _i, _vp, _vp]),
+    "dapple_attention_window_fwd": (_i, [_i, C.POINTER(attention_window_desc), _vp]),
+    "dapple_attention_window_workspace": (C.c_int64, [_i, C.POINTER(attention_window_desc)]),
+    "dapple_attention_window_bwd": (_i, [_i, C.POINTER(attention_window_desc), _vp]),
     "dapple_qk_rope_fwd": (_i, [_i, C.POINTER(qk_rope_desc), _vp]),
     "dapple_qk_rope_workspace": (C.c_int64, [_i, C.POINTER(qk_rope_desc)]),
     "dapple_qk_rope_bwd": (_i, [_i, C.POINTER(qk_rope_desc), _vp]),
@@ -449,6 +460,18 @@ def dapple_colsum_static(dtype, X, rows, cols, ld, out, stream_ptr=None):
 
 
 # ---- operators of layers and training steps (second part of dapple_kernels.h) ----
+def dapple_attention_window_fwd(dtype, desc: attention_window_desc, stream_ptr=None):
+    _check(load().dapple_attention_window_fwd(dtype, C.byref(desc), stream_ptr))
+
+
+def dapple_attention_window_workspace(dtype, desc: attention_window_desc) -> int:
+    return _check(load().dapple_attention_window_workspace(dtype, C.byref(desc)))
+
+
+def dapple_attention_window_bwd(dtype, desc: attention_window_desc, stream_ptr=None):
+    _check(load().dapple_attention_window_bwd(dtype, C.byref(desc), stream_ptr))
+
+
 def dapple_qk_rope_fwd(dtype, desc: qk_rope_desc, stream_ptr=None):
     _check(load().dapple_qk_rope_fwd(dtype, C.byref(desc), stream_ptr))
 

@@ -13,62 +13,9 @@
 // useful work); the library's exp2f, which keeps denormal probabilities, is 3% of that.
 #include <type_traits>
 
-#include "device_common.h"
-#include "kernels.h"
+#include "attention_tile.h"
 
 namespace dapple {
-
-static constexpr float LOG2E = 1.4426950408889634f;
-
-#define MFMA4(a, b, c) __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0)
-
-// D: the head block's width (16, 32, 64 or 128; narrower heads are padded with zeros); blocks of 32 rows
-constexpr int BR = 32;
-template <int D>
-struct F32Block {
-  // row stride D + 8 floats: the four lane groups of a 4-byte read lie 4 rows = 32 banks (mod 64) apart
-  static constexpr int LD = D + 8, CPR = D / 4, N = BR * CPR / 256 > 0 ? BR * CPR / 256 : 1;
-  f32x4 c[N];
-  __device__ __forceinline__ void load(const float* g, int ldg, int tid, int rows, int d) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int p = tid + 256 * i, r = p / CPR, k = p % CPR * 4;
-      c[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-      if (p < BR * CPR && r < rows && k < d) c[i] = *(const f32x4*)(g + (long)r * ldg + k);
-    }
-  }
-  __device__ __forceinline__ void store(float* S, int tid) const {
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int p = tid + 256 * i;
-      if (p < BR * CPR) *(f32x4*)(S + p / CPR * LD + p % CPR * 4) = c[i];
-    }
-  }
-};
-// row r0 + (lane & 15), k = 16 kk + 4 (lane >> 4) + 0..3
-template <int D>
-__device__ __forceinline__ f32x4 frow(const float* S, int r0, int kk, int lane) {
-  return *(const f32x4*)(S + (r0 + (lane & 15)) * (D + 8) + 16 * kk + 4 * (lane >> 4));
-}
-// column c0 + (lane & 15) of row r0 + 4 (lane >> 4) + e
-template <int D>
-__device__ __forceinline__ float fcol(const float* S, int c0, int r0, int e, int lane) {
-  return S[(r0 + 4 * (lane >> 4) + e) * (D + 8) + c0 + (lane & 15)];
-}
-// the row a lane owns in registers, k = 16 kk + 4 (lane >> 4) + 0..3
-template <int D>
-__device__ __forceinline__ void own_row(const float* row, bool ok, int d, int lane, f32x4 (&f)[D / 16]) {
-#pragma unroll
-  for (int kk = 0; kk < D / 16; ++kk) {
-    const int k = 16 * kk + 4 * (lane >> 4);
-    f[kk] = f32x4{0.f, 0.f, 0.f, 0.f};
-    if (ok && k < d) f[kk] = *(const f32x4*)(row + k);
-  }
-}
-__device__ __forceinline__ float over_groups_sum(float v) {   // the four lanes of one owned row, pairs first
-  v += __shfl_xor(v, 16, 64);
-  return v + __shfl_xor(v, 32, 64);
-}
 
 template <int D>
 __global__ __launch_bounds__(256) void attn_fwd_f32(AttnArgs a, float scale2) {

@@ -1,0 +1,969 @@
+// Attention of the visible pairs only, forward and backward:
+//   query i sees key j of its sequence where  j < len  and  (not causal or j <= i)  and  (W = 0 or |i - j| < W or j < S)
+//   -- a window of W positions, and the first S keys for every query.  A query heads share Ak key heads, A / Ak
+//   neighbouring ones each.  ctx = softmax(scale q k^T) v over the visible keys, lse = log2 of the sum of 2^(scale2 q k)
+//   (-infinity and ctx = 0 for rows at and behind len: they see nothing),  delta = rowsum(dctx o ctx),
+//   dv = P^T dctx,  dS = P o (dP - delta),  dq = scale dS k,  dk = scale dS^T q, dk and dv summed over the sharing heads.
+//
+// The orientation is that of attention.hip: a wave owns 32 query rows (forward, dq) or 32 key rows (dk, dv), 64-row blocks of the
+// other side stream through a ring in LDS, the accumulator's lane index is the row the wave owns.  What is visible to a row
+// is one run of the other side's rows, and for queries the sinks besides: [lo, hi) and [0, S).  So a workgroup walks the
+// blocks that hold sinks and then the blocks of its rows' runs, skips in each wave what none of its 32 rows sees, and compares
+// element by element only in blocks that some row sees in part.  Bound by the chain MFMA -> exponentials -> MFMA like the kernels
+// without a window; the work is that of the visible blocks.
+//
+// dk and dv of a key: the query blocks that see it, for each of the sharing heads, one walk.  Where the walks are longer than
+// others (keys among the sinks: every query sees them) or too few to fill the chip, a walk is cut into parts of CS blocks; each
+// part leaves fp32 sums in the workspace, and a second kernel adds them in ascending order: no atomics, the same bits every time.
+//
+// Rows at and behind len may hold anything: their q, k, v and dctx are never used (they read as zeros, past the buffer's records),
+// and their outputs are zeros.
+#include <algorithm>
+#include <type_traits>
+
+#include "attention_tile.h"
+
+namespace dapple {
+
+// Workgroups go round robin to the eight XCDs, each with an L2 of its own: XCD x takes the x-th eighth of the range, so that
+// tiles of one head, and heads that share keys, find each other's rows there.
+__device__ __forceinline__ unsigned spread(unsigned id, unsigned n) {
+  const unsigned per = n / 8;
+  return id < per * 8 ? (id & 7) * per + (id >> 3) : id;
+}
+
+__device__ __forceinline__ int len_of(const AttnWinArgs& a, int bi) {
+  return a.lens ? min(max(a.lens[bi], 0), a.s) : a.s;
+}
+
+// keys that query i sees: [lo, hi) and [0, min(S, hi))
+__device__ __forceinline__ int key_lo(const AttnWinArgs& a, int i) { return a.W ? max(0, i - a.W + 1) : 0; }
+__device__ __forceinline__ int key_hi(const AttnWinArgs& a, int i, int len) {
+  return min(len, a.causal ? i + 1 : a.W ? max(i + a.W, a.S) : len);   // (W < s and S <= s, below 2^27)
+}
+// queries that see key j: [lo, hi)
+__device__ __forceinline__ int query_lo(const AttnWinArgs& a, int j) { return a.causal ? j : a.W && j >= a.S ? max(0, j - a.W + 1) : 0; }
+__device__ __forceinline__ int query_hi(const AttnWinArgs& a, int j, int len) { return a.W && j >= a.S ? min(len, j + a.W) : len; }
+
+// The blocks of BLK keys that the queries q0 .. q1 of a workgroup see: `first` ones of the sinks, then from lo on, n in all
+struct KeyWalk {
+  int first, lo, n;
+  __device__ __forceinline__ KeyWalk(const AttnWinArgs& a, int q0, int q1, int len, int blk) {
+    lo = key_lo(a, q0) / blk;
+    first = a.W ? min((a.S + blk - 1) / blk, lo) : 0;
+    n = q0 < len ? first + (key_hi(a, q1, len) + blk - 1) / blk - lo : 0;
+  }
+  __device__ __forceinline__ int block(int t) const { return t < first ? t : lo + t - first; }
+};
+// What the queries qa .. qb (valid rows) see of keys k0 .. k1: nothing, all, or part
+enum Seen { NONE, PART, ALL };
+__device__ __forceinline__ Seen seen_keys(const AttnWinArgs& a, int qa, int qb, int k0, int k1, int len) {
+  if (k0 >= key_hi(a, qb, len) || (k1 < key_lo(a, qa) && k0 >= a.S)) return NONE;
+  return k1 < key_hi(a, qa, len) && (k0 >= key_lo(a, qb) || k1 < a.S) ? ALL : PART;
+}
+__device__ __forceinline__ bool sees(const AttnWinArgs& a, int j, int lo, int hi) { return j < hi && (j >= lo || j < a.S); }
+
+// A workgroup of the dk, dv launch: KT keys of a key head, and a part of their walk over the sharing heads' query blocks
+struct KeyTask {
+  int bi, kv, k0, len, qlo, nq, n0, n1, slot;   // blocks of the walk [n0, n1): head n / nq, block qlo + n % nq; slot < 0: no parts
+  bool run;
+  __device__ __forceinline__ void span(const AttnWinArgs& a, int kt, int blk) {
+    const int k1 = min(k0 + kt, len) - 1;
+    qlo = nq = 0;
+    if (k0 >= len) return;
+    const bool sink = a.W && k0 < a.S;   // the walk of the tile's first key has the lower end of all, its last key's the upper,
+                                         // but a sink's is everything
+    qlo = (sink && !a.causal ? 0 : query_lo(a, k0)) / blk;
+    nq = ((sink ? len : query_hi(a, k1, len)) + blk - 1) / blk - qlo;
+  }
+  __device__ __forceinline__ KeyTask(const AttnWinArgs& a, unsigned t, int kt, int blk) {
+    const WinPlan& p = a.plan;
+    const int sinks = p.sink_tiles * p.sink_parts, per = sinks + (p.key_tiles - p.sink_tiles) * p.parts;
+    const int head = t / per, r = t % per;
+    bi = head / a.Ak;
+    kv = head % a.Ak;
+    const bool sink = r < sinks;
+    const int parts = sink ? p.sink_parts : p.parts, u = sink ? r : r - sinks;
+    const int tile = u / parts + (sink ? 0 : p.sink_tiles), part = u % parts;
+    k0 = tile * kt;
+    len = len_of(a, bi);
+    span(a, kt, blk);
+    const int all = nq * (a.A / a.Ak);
+    n0 = parts > 1 ? min(all, part * p.steps) : 0;
+    n1 = parts > 1 ? min(all, n0 + p.steps) : all;
+    slot = parts > 1 ? head * p.slots + (sink || p.sink_parts == 1 ? 0 : sinks) + u : -1;
+    run = parts == 1 || n0 < n1;
+  }
+};
+
+// ------------------------------------------------------------------ bf16
+template <int D, int NW, bool STATS>
+using WinRing = Ring<D, NW, D == 128 ? 2 : 3, STATS>;
+
+// o: accumulators of 32 rows (lane & 31) x D columns; D = 128 in two halves, which the ring's LDS has room for
+template <int D>
+__device__ __forceinline__ void store_rows(unsigned char* sm, int wave, const f32x16* o, float f, bf16* C, float* C32, long ld, int rows, int d, int lane) {
+  constexpr int NDB = D / 32 < 2 ? D / 32 : 2;
+  float* const S = (float*)(sm + wave * OutTile<NDB>::BYTES);
+#pragma unroll
+  for (int c = 0; c < D / 32; c += NDB)
+    OutTile<NDB>::store(S, o + c, f, C + 32 * c, C32 ? C32 + 32 * c : nullptr, ld, rows, d - 32 * c, lane);
+}
+
+// NW: waves per workgroup (4, or 2 where the grid is small), each with 32 query rows
+template <int D, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void attn_win_fwd(AttnWinArgs a, float scale2) {
+  constexpr int NKK = D / 16, NDB = D / 32;
+  typedef WinRing<D, NW, false> R;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char asm_[];
+  const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int q_tiles = (a.s + 32 * NW - 1) / (32 * NW);
+  const unsigned id = spread(blockIdx.x, gridDim.x);
+  const int head = id / q_tiles, tile = q_tiles - 1 - id % q_tiles;   // (causal: the longest walks first)
+  const int bi = head / a.A, hh = head % a.A, kv = hh / (a.A / a.Ak);
+  const int len = len_of(a, bi), d = a.d;
+  const long r0 = (long)bi * a.s;
+  const bf16 *Q = (const bf16*)a.q + r0 * a.ldq + hh * d, *K = (const bf16*)a.k + r0 * a.ldk + kv * d, *V = (const bf16*)a.v + r0 * a.ldv + kv * d;
+  const int q0 = tile * 32 * NW, row0 = q0 + wave * 32, qrow = row0 + (lane & 31);
+  const bool qok = qrow < len;
+  const KeyWalk walk(a, q0, min(q0 + 32 * NW, len) - 1, len, 64);
+  const int lo = key_lo(a, qrow), hi = qok ? key_hi(a, qrow, len) : 0;
+  const int qb = min(row0 + 32, len) - 1;
+  bf16x8 qf[NKK];
+#pragma unroll
+  for (int kk = 0; kk < NKK; ++kk) qf[kk] = frag_global<true>(Q, qrow, qok, a.ldq, kk, lane, d);
+  R ring;
+  ring.init(wave < NW / 2 ? K : V, wave < NW / 2 ? a.ldk : a.ldv, len, d, wave, lane, [](int) { return (const float*)nullptr; });
+  __builtin_amdgcn_s_waitcnt(0x0F70);   // the query fragments are here: the counts below are the ring's alone
+  int asked = 0;
+  auto ask = [&](int stage) __attribute__((always_inline)) {
+    if (asked == walk.first) ring.seek(walk.lo, len, 0, 0);
+    if (asked >= walk.n) ring.stop();   // past the last block: reads nothing
+    ring.request(stage, lane);
+    ++asked;
+  };
+#pragma unroll
+  for (int t = 0; t < R::NS - 1; ++t) ask(t);
+
+  float m = -3e38f, l = 0.f;   // (finite: a row that has seen nothing yet keeps m - m = 0)
+  f32x16 o[NDB];  // rows d = 32 dblk + 8 blk + 4 h + e, column = the lane's query
+#pragma unroll
+  for (int db = 0; db < NDB; ++db) o[db] = zero16();
+
+  int stage = 0;
+  for (int t = 0; t < walk.n; ++t) {
+    R::wait();
+    ask(stage == 0 ? R::NS - 1 : stage - 1);
+    const bf16 *Ks = (const bf16*)(asm_ + stage * R::STAGE), *Vs = (const bf16*)((const unsigned char*)Ks + R::Y_OFF);
+    stage = stage + 1 == R::NS ? 0 : stage + 1;
+    const int k0 = walk.block(t) * 64;
+    if (row0 >= len) continue;
+    Seen see = seen_keys(a, row0, qb, k0, k0 + 63, len);
+    if (see == NONE) continue;
+    if (row0 + 31 >= len) see = PART;
+    float p[2][16];
+    float mx = -INFINITY;
+    // (all LDS reads of a phase before its first MFMA: see attn_fwd_mfma)
+    bf16x8 kf[2][NKK], vf[4][NDB];
+    constexpr bool WHOLE = D <= 64;
+    if (WHOLE) {
+#pragma unroll
+      for (int kb2 = 0; kb2 < 2; ++kb2)
+#pragma unroll
+        for (int kk = 0; kk < NKK; ++kk) kf[kb2][kk] = frag_rows<D>(Ks, kb2 * 32, kk, lane);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int kb2 = 0; kb2 < 2; ++kb2) {
+      if (!WHOLE) {
+#pragma unroll
+        for (int kk = 0; kk < NKK; ++kk) kf[kb2][kk] = frag_rows<D>(Ks, kb2 * 32, kk, lane);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      f32x16 sa = zero16();  // rows: key 32 kb2 + 8 blk + 4 h + e, column: query
+#pragma unroll
+      for (int kk = 0; kk < NKK; ++kk) sa = MFMA(kf[kb2][kk], qf[kk], sa);
+#pragma unroll
+      for (int v = 0; v < 16; ++v) p[kb2][v] = sa[v];
+    }
+    if (see == PART) {
+#pragma unroll
+      for (int kb2 = 0; kb2 < 2; ++kb2)
+#pragma unroll
+        for (int v = 0; v < 16; ++v)
+          if (!sees(a, k0 + kb2 * 32 + 8 * (v >> 2) + 4 * h + (v & 3), lo, hi)) p[kb2][v] = -INFINITY;
+    }
+#pragma unroll
+    for (int kb2 = 0; kb2 < 2; ++kb2)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) mx = fmaxf(mx, p[kb2][v]);
+    if (WHOLE) {
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+        for (int db = 0; db < NDB; ++db) vf[ks][db] = frag_cols<D>(Vs, db * 32, ks * 16, lane);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    const float mn = fmaxf(m, halves_max(mx) * scale2);
+    const float alpha = __builtin_amdgcn_exp2f(m - mn);
+    float rs = 0.f;
+#pragma unroll
+    for (int kb2 = 0; kb2 < 2; ++kb2)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        // (the bare v_exp_f32: a probability below 2^-126 may be zero, it is rounded to bf16)
+        p[kb2][v] = __builtin_amdgcn_exp2f(fmaf(p[kb2][v], scale2, -mn));
+        rs += p[kb2][v];
+      }
+    l = l * alpha + halves_sum(rs);
+    m = mn;
+    if (__builtin_amdgcn_ballot_w64(alpha != 1.f)) {
+#pragma unroll
+      for (int db = 0; db < NDB; ++db)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) o[db][v] *= alpha;
+    }
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) {
+      const bf16x8 pf = acc_to_operand(p[ks >> 1], ks & 1);
+      if (!WHOLE) {
+#pragma unroll
+        for (int db = 0; db < NDB; ++db) vf[ks][db] = frag_cols<D>(Vs, db * 32, ks * 16, lane);
+      }
+#pragma unroll
+      for (int db = 0; db < NDB; ++db) o[db] = MFMA(vf[ks][db], pf, o[db]);
+    }
+  }
+  __builtin_amdgcn_s_waitcnt(0x0F70);   // the ring's last requests (they read nothing) before the wave may end
+  __syncthreads();                      // every wave is done with the ring
+  const float inv = l > 0.f ? 1.0f / l : 0.f;
+  if (!qok) {   // (not 0 times what an infinite v may have made of them)
+#pragma unroll
+    for (int db = 0; db < NDB; ++db) o[db] = zero16();
+  }
+  const long o0 = (r0 + row0) * a.ldc + hh * d;
+  store_rows<D>(asm_, wave, o, inv, (bf16*)a.ctx + o0, a.ctx32 ? a.ctx32 + o0 : nullptr, a.ldc, a.s - row0, d, lane);
+  if (qrow < a.s && h == 0) a.lse[((long)bi * a.A + hh) * a.s + qrow] = l > 0.f ? m + log2f(l) : -INFINITY;
+}
+
+// dk, dv of 32 keys a wave; query blocks of 64 stream through LDS with their lse and delta
+template <int D, int NW, typename R>
+__device__ __forceinline__ void win_dkdv(const AttnWinArgs& a, unsigned task, float scale2, float scale, unsigned char* sm) {
+  constexpr int NKK = D / 16, NDB = D / 32;
+  const KeyTask w(a, task, 32 * NW, 64);
+  if (!w.run) return;
+  const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int len = w.len, d = a.d, h0 = w.kv * (a.A / a.Ak);
+  const long r0 = (long)w.bi * a.s;
+  const bf16 *Q = (const bf16*)a.q + r0 * a.ldq + h0 * d, *G = (const bf16*)a.dctx + r0 * a.lddc + h0 * d;
+  const bf16 *K = (const bf16*)a.k + r0 * a.ldk + w.kv * d, *V = (const bf16*)a.v + r0 * a.ldv + w.kv * d;
+  const float *lse = a.lse + ((long)w.bi * a.A + h0) * a.s, *delta = a.delta + ((long)w.bi * a.A + h0) * a.s;
+  const int row0 = w.k0 + wave * 32, krow = row0 + (lane & 31);
+  const bool kok = krow < len;
+  const int lo = query_lo(a, krow), hi = kok ? query_hi(a, krow, len) : 0;
+  // of the wave's keys: the least and the greatest end of what sees them
+  const int kb = min(row0 + 32, len) - 1;
+  const bool sink = a.W && row0 < a.S;
+  const int lo_min = sink && !a.causal ? 0 : query_lo(a, row0), lo_max = query_lo(a, kb);
+  const int hi_max = sink ? len : query_hi(a, kb, len), hi_min = query_hi(a, sink ? min(kb, a.S) : row0, len);
+
+  bf16x8 kf[NKK], vf[NKK];
+#pragma unroll
+  for (int kk = 0; kk < NKK; ++kk) {
+    kf[kk] = frag_global<true>(K, krow, kok, a.ldk, kk, lane, d);
+    vf[kk] = frag_global<true>(V, krow, kok, a.ldv, kk, lane, d);
+  }
+  f32x16 dv[NDB], dk[NDB];  // rows d, column = the lane's key
+#pragma unroll
+  for (int db = 0; db < NDB; ++db) dv[db] = dk[db] = zero16();
+  R ring;
+  const bool first = wave < NW / 2;
+  // (a query beyond the last: zero rows, lse and delta 0, and not visible)
+  ring.init(first ? Q : G, first ? a.ldq : a.lddc, len, d, wave, lane, [&](int r) { return r == 0 ? lse : (r == 1 ? delta : nullptr); });
+  __builtin_amdgcn_s_waitcnt(0x0F70);   // the key and value fragments are here: the counts below are the ring's alone
+  int asked = w.n0, ahead = w.nq ? w.n0 / w.nq : 0, aq = w.nq ? w.n0 % w.nq : 0;   // the next block to request: head, block
+  bool jump = true;
+  auto ask = [&](int stage) __attribute__((always_inline)) {
+    if (jump) ring.seek(w.qlo + aq, len, ahead * d * 2, (long)ahead * a.s * 4);
+    if (asked >= w.n1) ring.stop();
+    ring.request(stage, lane);
+    ++asked;
+    jump = ++aq == w.nq;
+    if (jump) {
+      aq = 0;
+      ++ahead;
+    }
+  };
+#pragma unroll
+  for (int t = 0; t < R::NS - 1; ++t) ask(t);
+
+  int stage = 0, qblk = w.nq ? w.n0 % w.nq : 0;
+  for (int n = w.n0; n < w.n1; ++n) {
+    R::wait();
+    ask(stage == 0 ? R::NS - 1 : stage - 1);
+    const bf16 *Qs = (const bf16*)(sm + stage * R::STAGE), *Gs = (const bf16*)((const unsigned char*)Qs + R::Y_OFF);
+    const float *Ls = (const float*)((const unsigned char*)Qs + R::S_OFF), *Ds = Ls + 64;
+    stage = stage + 1 == R::NS ? 0 : stage + 1;
+    const int i0 = (w.qlo + qblk) * 64;
+    qblk = qblk + 1 == w.nq ? 0 : qblk + 1;
+    if (row0 >= len) continue;
+#pragma unroll
+    for (int qb2 = 0; qb2 < 2; ++qb2) {
+      const int j0 = i0 + qb2 * 32;
+      if (j0 >= hi_max || j0 + 31 < lo_min) continue;
+      const bool all = row0 + 31 < len && j0 >= lo_max && j0 + 31 < hi_min;
+      bf16x8 qf[NKK], gf[NKK], gc[2][NDB], qc[2][NDB];
+      f32x4 L4[4], D4[4];
+#pragma unroll
+      for (int kk = 0; kk < NKK; ++kk) {
+        qf[kk] = frag_rows<D>(Qs, qb2 * 32, kk, lane);
+        gf[kk] = frag_rows<D>(Gs, qb2 * 32, kk, lane);
+      }
+#pragma unroll
+      for (int blk = 0; blk < 4; ++blk) {
+        L4[blk] = *(const f32x4*)(Ls + qb2 * 32 + 8 * blk + 4 * h);
+        D4[blk] = *(const f32x4*)(Ds + qb2 * 32 + 8 * blk + 4 * h);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      f32x16 sa = zero16(), dp = zero16();  // rows: query 32 qb2 + 8 blk + 4 h + e, column: key
+#pragma unroll
+      for (int kk = 0; kk < NKK; ++kk) {
+        sa = MFMA(qf[kk], kf[kk], sa);
+        dp = MFMA(gf[kk], vf[kk], dp);
+      }
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+        for (int db = 0; db < NDB; ++db) {
+          gc[ks][db] = frag_cols<D>(Gs, db * 32, qb2 * 32 + ks * 16, lane);
+          qc[ks][db] = frag_cols<D>(Qs, db * 32, qb2 * 32 + ks * 16, lane);
+        }
+      __builtin_amdgcn_sched_barrier(0);
+      float p[16], ds[16];
+#pragma unroll
+      for (int blk = 0; blk < 4; ++blk)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          p[4 * blk + e] = __builtin_amdgcn_exp2f(fmaf(sa[4 * blk + e], scale2, -L4[blk][e]));
+          ds[4 * blk + e] = (dp[4 * blk + e] - D4[blk][e]) * p[4 * blk + e];
+        }
+      if (!all) {
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          const int i = j0 + 8 * (v >> 2) + 4 * h + (v & 3);
+          if (!(i >= lo && i < hi)) p[v] = ds[v] = 0.f;
+        }
+      }
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks) {
+        const bf16x8 pf = acc_to_operand(p, ks), dsf = acc_to_operand(ds, ks);
+#pragma unroll
+        for (int db = 0; db < NDB; ++db) {
+          dv[db] = MFMA(gc[ks][db], pf, dv[db]);
+          dk[db] = MFMA(qc[ks][db], dsf, dk[db]);
+        }
+      }
+    }
+  }
+  __builtin_amdgcn_s_waitcnt(0x0F70);
+  if (w.slot >= 0) {   // sums of a part, in the accumulators' own order
+    float* const P = a.partial + (long)w.slot * 2 * 32 * NW * D;
+#pragma unroll
+    for (int db = 0; db < NDB; ++db)
+#pragma unroll
+      for (int blk = 0; blk < 4; ++blk) {
+        const int u = (((wave * NDB + db) * 4 + blk) * 64 + lane) * 4;
+        *(f32x4*)(P + u) = f32x4{dk[db][4 * blk], dk[db][4 * blk + 1], dk[db][4 * blk + 2], dk[db][4 * blk + 3]};
+        *(f32x4*)(P + 32 * NW * D + u) = f32x4{dv[db][4 * blk], dv[db][4 * blk + 1], dv[db][4 * blk + 2], dv[db][4 * blk + 3]};
+      }
+    return;
+  }
+  __syncthreads();
+  store_rows<D>(sm, wave, dk, scale, (bf16*)a.dk + (r0 + row0) * a.lddk + w.kv * d, nullptr, a.lddk, a.s - row0, d, lane);
+  store_rows<D>(sm, wave, dv, 1.f, (bf16*)a.dv + (r0 + row0) * a.lddv + w.kv * d, nullptr, a.lddv, a.s - row0, d, lane);
+}
+
+// dq of 32 queries a wave; key blocks of 64 stream through LDS
+template <int D, int NW, typename R>
+__device__ __forceinline__ void win_dq(const AttnWinArgs& a, unsigned id, float scale2, float scale, unsigned char* sm) {
+  constexpr int NKK = D / 16, NDB = D / 32;
+  const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int q_tiles = (a.s + 32 * NW - 1) / (32 * NW);
+  const int head = id / q_tiles, tile = q_tiles - 1 - id % q_tiles;
+  const int bi = head / a.A, hh = head % a.A, kv = hh / (a.A / a.Ak);
+  const int len = len_of(a, bi), d = a.d;
+  const long r0 = (long)bi * a.s;
+  const bf16 *Q = (const bf16*)a.q + r0 * a.ldq + hh * d, *G = (const bf16*)a.dctx + r0 * a.lddc + hh * d;
+  const bf16 *K = (const bf16*)a.k + r0 * a.ldk + kv * d, *V = (const bf16*)a.v + r0 * a.ldv + kv * d;
+  const int q0 = tile * 32 * NW, row0 = q0 + wave * 32, qrow = row0 + (lane & 31);
+  const bool qok = qrow < len;
+  const KeyWalk walk(a, q0, min(q0 + 32 * NW, len) - 1, len, 64);
+  const int lo = key_lo(a, qrow), hi = qok ? key_hi(a, qrow, len) : 0;
+  const int qb = min(row0 + 32, len) - 1;
+  const long st = ((long)bi * a.A + hh) * a.s + qrow;
+  const float Lq = qok ? a.lse[st] : 0.f, Dq = qok ? a.delta[st] : 0.f;
+  bf16x8 qf[NKK], gf[NKK];
+#pragma unroll
+  for (int kk = 0; kk < NKK; ++kk) {
+    qf[kk] = frag_global<true>(Q, qrow, qok, a.ldq, kk, lane, d);
+    gf[kk] = frag_global<true>(G, qrow, qok, a.lddc, kk, lane, d);
+  }
+  f32x16 dq[NDB];  // rows d, column = the lane's query
+#pragma unroll
+  for (int db = 0; db < NDB; ++db) dq[db] = zero16();
+  R ring;
+  ring.init(wave < NW / 2 ? K : V, wave < NW / 2 ? a.ldk : a.ldv, len, d, wave, lane, [](int) { return (const float*)nullptr; });   // (the statistics' loads read nothing)
+  __builtin_amdgcn_s_waitcnt(0x0F70);
+  int asked = 0;
+  auto ask = [&](int stage) __attribute__((always_inline)) {
+    if (asked == walk.first) ring.seek(walk.lo, len, 0, 0);
+    if (asked >= walk.n) ring.stop();
+    ring.request(stage, lane);
+    ++asked;
+  };
+#pragma unroll
+  for (int t = 0; t < R::NS - 1; ++t) ask(t);
+
+  int stage = 0;
+  for (int t = 0; t < walk.n; ++t) {
+    R::wait();
+    ask(stage == 0 ? R::NS - 1 : stage - 1);
+    const bf16 *Ks = (const bf16*)(sm + stage * R::STAGE), *Vs = (const bf16*)((const unsigned char*)Ks + R::Y_OFF);
+    stage = stage + 1 == R::NS ? 0 : stage + 1;
+    const int k0 = walk.block(t) * 64;
+    if (row0 >= len) continue;
+#pragma unroll
+    for (int kb2 = 0; kb2 < 2; ++kb2) {
+      const int j0 = k0 + kb2 * 32;
+      Seen see = seen_keys(a, row0, qb, j0, j0 + 31, len);
+      if (see == NONE) continue;
+      if (row0 + 31 >= len) see = PART;
+      bf16x8 kr[NKK], vr[NKK], kc[2][NDB];
+#pragma unroll
+      for (int kk = 0; kk < NKK; ++kk) {
+        kr[kk] = frag_rows<D>(Ks, kb2 * 32, kk, lane);
+        vr[kk] = frag_rows<D>(Vs, kb2 * 32, kk, lane);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      f32x16 sa = zero16(), dp = zero16();  // rows: key 32 kb2 + 8 blk + 4 h + e, column: query
+#pragma unroll
+      for (int kk = 0; kk < NKK; ++kk) {
+        sa = MFMA(kr[kk], qf[kk], sa);
+        dp = MFMA(vr[kk], gf[kk], dp);
+      }
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+        for (int db = 0; db < NDB; ++db) kc[ks][db] = frag_cols<D>(Ks, db * 32, kb2 * 32 + ks * 16, lane);
+      __builtin_amdgcn_sched_barrier(0);
+      float ds[16];
+#pragma unroll
+      for (int v = 0; v < 16; ++v) ds[v] = __builtin_amdgcn_exp2f(fmaf(sa[v], scale2, -Lq)) * (dp[v] - Dq);
+      if (see == PART) {
+#pragma unroll
+        for (int v = 0; v < 16; ++v)
+          if (!sees(a, j0 + 8 * (v >> 2) + 4 * h + (v & 3), lo, hi)) ds[v] = 0.f;
+      }
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks) {
+        const bf16x8 dsf = acc_to_operand(ds, ks);
+#pragma unroll
+        for (int db = 0; db < NDB; ++db) dq[db] = MFMA(kc[ks][db], dsf, dq[db]);
+      }
+    }
+  }
+  __builtin_amdgcn_s_waitcnt(0x0F70);
+  __syncthreads();
+  if (!qok) {
+#pragma unroll
+    for (int db = 0; db < NDB; ++db) dq[db] = zero16();
+  }
+  store_rows<D>(sm, wave, dq, scale, (bf16*)a.dq + (r0 + row0) * a.lddq + hh * d, nullptr, a.lddq, a.s - row0, d, lane);
+}
+
+// Both kinds of workgroups in one launch, dk and dv first: they share a compute unit and fill each other's waits (as in attention.hip)
+template <int D, int NW>
+__global__ __launch_bounds__(64 * NW, D <= 64 ? 2 : 1) void attn_win_bwd(AttnWinArgs a, float scale2, float scale) {
+  extern __shared__ __attribute__((aligned(1024))) unsigned char asm_[];
+  typedef WinRing<D, NW, true> R;
+  const unsigned nk = a.plan.key_tasks;
+  if (blockIdx.x < nk) win_dkdv<D, NW, R>(a, spread(blockIdx.x, nk), scale2, scale, asm_);
+  else win_dq<D, NW, R>(a, spread(blockIdx.x - nk, gridDim.x - nk), scale2, scale, asm_);
+}
+
+// ------------------------------------------------------------------ fp32 (see attention_f32.hip)
+template <int D>
+__global__ __launch_bounds__(256) void attn_win_fwd_f32(AttnWinArgs a, float scale2) {
+  constexpr int NK = D / 16;
+  __shared__ __attribute__((aligned(16))) float Ks[BR * (D + 8)];
+  __shared__ __attribute__((aligned(16))) float Vs[BR * (D + 8)];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g4 = lane >> 4;
+  const int q_tiles = (a.s + 63) / 64;
+  const unsigned id = spread(blockIdx.x, gridDim.x);
+  const int head = id / q_tiles, tile = q_tiles - 1 - id % q_tiles;
+  const int bi = head / a.A, hh = head % a.A, kv = hh / (a.A / a.Ak), len = len_of(a, bi), d = a.d;
+  const long r0 = (long)bi * a.s;
+  const float *Q = (const float*)a.q + r0 * a.ldq + hh * d, *K = (const float*)a.k + r0 * a.ldk + kv * d, *V = (const float*)a.v + r0 * a.ldv + kv * d;
+  const int q0 = tile * 64, row0 = q0 + wave * 16, qrow = row0 + (lane & 15), qb = min(row0 + 16, len) - 1;
+  const bool qok = qrow < len;
+  const KeyWalk walk(a, q0, min(q0 + 64, len) - 1, len, BR);
+  const int lo = key_lo(a, qrow), hi = qok ? key_hi(a, qrow, len) : 0;
+  f32x4 qf[NK];
+  own_row<D>(Q + (long)qrow * a.ldq, qok, d, lane, qf);
+  F32Block<D> kb, vb;
+  auto load = [&](int t) {
+    const int k0 = walk.block(t) * BR;
+    kb.load(K + (long)k0 * a.ldk, a.ldk, tid, len - k0, d);
+    vb.load(V + (long)k0 * a.ldv, a.ldv, tid, len - k0, d);
+  };
+  if (walk.n > 0) load(0);
+  float m = -3e38f, l = 0.f;
+  f32x4 o[NK];   // rows d = 16 i + 4 g4 + e, column = the lane's query
+#pragma unroll
+  for (int i = 0; i < NK; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int n = 0; n < walk.n; ++n) {
+    __syncthreads();
+    kb.store(Ks, tid);
+    vb.store(Vs, tid);
+    __syncthreads();
+    if (n + 1 < walk.n) load(n + 1);
+    const int k0 = walk.block(n) * BR;
+    if (row0 >= len || seen_keys(a, row0, qb, k0, k0 + BR - 1, len) == NONE) continue;
+    f32x4 p[2];
+    float mx = -INFINITY;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {   // rows: key k0 + 16 t + 4 g4 + e, column: query
+      f32x4 s{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int kk = 0; kk < NK; ++kk) {
+        const f32x4 kf = frow<D>(Ks, 16 * t, kk, lane);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s = MFMA4(kf[e], qf[kk][e], s);
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        p[t][e] = sees(a, k0 + 16 * t + 4 * g4 + e, lo, hi) ? s[e] * scale2 : -INFINITY;
+        mx = fmaxf(mx, p[t][e]);
+      }
+    }
+    mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+    const float mn = fmaxf(m, mx), alpha = exp2f(m - mn);
+    float rs = 0.f;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        p[t][e] = exp2f(p[t][e] - mn);
+        rs += p[t][e];
+      }
+    l = l * alpha + over_groups_sum(rs);
+    m = mn;
+    if (__builtin_amdgcn_ballot_w64(alpha != 1.f)) {
+#pragma unroll
+      for (int i = 0; i < NK; ++i) o[i] *= alpha;
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int i = 0; i < NK; ++i) o[i] = MFMA4(fcol<D>(Vs, 16 * i, 16 * t, e, lane), p[t][e], o[i]);
+  }
+  if (qrow < a.s) {
+    const float inv = l > 0.f ? 1.0f / l : 0.f;
+    const long at = (r0 + qrow) * a.ldc + hh * d;
+#pragma unroll
+    for (int i = 0; i < NK; ++i) {
+      const int col = 16 * i + 4 * g4;
+      if (col < d) {
+        const f32x4 v = qok ? o[i] * inv : f32x4{0.f, 0.f, 0.f, 0.f};
+        *(f32x4*)((float*)a.ctx + at + col) = v;
+        if (a.ctx32) *(f32x4*)(a.ctx32 + at + col) = v;
+      }
+    }
+    if (g4 == 0) a.lse[((long)bi * a.A + hh) * a.s + qrow] = l > 0.f ? m + log2f(l) : -INFINITY;
+  }
+}
+
+template <int D>
+__device__ __forceinline__ void win_dq_f32(const AttnWinArgs& a, unsigned id, float scale2, float scale, float* Ks, float* Vs) {
+  constexpr int NK = D / 16;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g4 = lane >> 4;
+  const int q_tiles = (a.s + 63) / 64, head = id / q_tiles, tile = q_tiles - 1 - id % q_tiles;
+  const int bi = head / a.A, hh = head % a.A, kv = hh / (a.A / a.Ak), len = len_of(a, bi), d = a.d;
+  const long r0 = (long)bi * a.s;
+  const float *K = (const float*)a.k + r0 * a.ldk + kv * d, *V = (const float*)a.v + r0 * a.ldv + kv * d;
+  const int q0 = tile * 64, row0 = q0 + wave * 16, qrow = row0 + (lane & 15), qb = min(row0 + 16, len) - 1;
+  const bool qok = qrow < len;
+  const KeyWalk walk(a, q0, min(q0 + 64, len) - 1, len, BR);
+  const int lo = key_lo(a, qrow), hi = qok ? key_hi(a, qrow, len) : 0;
+  f32x4 qf[NK], gf[NK];
+  own_row<D>((const float*)a.q + (r0 + qrow) * a.ldq + hh * d, qok, d, lane, qf);
+  own_row<D>((const float*)a.dctx + (r0 + qrow) * a.lddc + hh * d, qok, d, lane, gf);
+  const long st = ((long)bi * a.A + hh) * a.s + qrow;
+  const float Lq = qok ? a.lse[st] : 0.f, Dq = qok ? a.delta[st] : 0.f;
+  f32x4 dq[NK];
+#pragma unroll
+  for (int i = 0; i < NK; ++i) dq[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  F32Block<D> kb, vb;
+  auto load = [&](int t) {
+    const int k0 = walk.block(t) * BR;
+    kb.load(K + (long)k0 * a.ldk, a.ldk, tid, len - k0, d);
+    vb.load(V + (long)k0 * a.ldv, a.ldv, tid, len - k0, d);
+  };
+  if (walk.n > 0) load(0);
+  for (int n = 0; n < walk.n; ++n) {
+    __syncthreads();
+    kb.store(Ks, tid);
+    vb.store(Vs, tid);
+    __syncthreads();
+    if (n + 1 < walk.n) load(n + 1);
+    const int k0 = walk.block(n) * BR;
+    if (row0 >= len) continue;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      if (seen_keys(a, row0, qb, k0 + 16 * t, k0 + 16 * t + 15, len) == NONE) continue;
+      f32x4 s{0.f, 0.f, 0.f, 0.f}, dp{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int kk = 0; kk < NK; ++kk) {
+        const f32x4 kf = frow<D>(Ks, 16 * t, kk, lane), vf = frow<D>(Vs, 16 * t, kk, lane);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          s = MFMA4(kf[e], qf[kk][e], s);
+          dp = MFMA4(vf[e], gf[kk][e], dp);
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        float ds = exp2f(s[e] * scale2 - Lq) * (dp[e] - Dq);
+        if (!sees(a, k0 + 16 * t + 4 * g4 + e, lo, hi)) ds = 0.f;
+#pragma unroll
+        for (int i = 0; i < NK; ++i) dq[i] = MFMA4(fcol<D>(Ks, 16 * i, 16 * t, e, lane), ds, dq[i]);
+      }
+    }
+  }
+  if (qrow < a.s) {
+#pragma unroll
+    for (int i = 0; i < NK; ++i) {
+      const int col = 16 * i + 4 * g4;
+      if (col < d) *(f32x4*)((float*)a.dq + (r0 + qrow) * a.lddq + hh * d + col) = qok ? dq[i] * scale : f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+  }
+}
+
+template <int D>
+__device__ __forceinline__ void win_dkdv_f32(const AttnWinArgs& a, unsigned task, float scale2, float scale, float* Qs, float* Gs, float* Ls, float* Ds) {
+  constexpr int NK = D / 16;
+  const KeyTask w(a, task, 64, BR);
+  if (!w.run) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g4 = lane >> 4;
+  const int len = w.len, d = a.d, h0 = w.kv * (a.A / a.Ak);
+  const long r0 = (long)w.bi * a.s;
+  const float *Q = (const float*)a.q + r0 * a.ldq + h0 * d, *G = (const float*)a.dctx + r0 * a.lddc + h0 * d;
+  const float *lse = a.lse + ((long)w.bi * a.A + h0) * a.s, *delta = a.delta + ((long)w.bi * a.A + h0) * a.s;
+  const int row0 = w.k0 + wave * 16, krow = row0 + (lane & 15);
+  const bool kok = krow < len;
+  const int lo = query_lo(a, krow), hi = kok ? query_hi(a, krow, len) : 0;
+  const int kb = min(row0 + 16, len) - 1;
+  const bool sink = a.W && row0 < a.S;
+  const int lo_min = sink && !a.causal ? 0 : query_lo(a, row0), hi_max = sink ? len : query_hi(a, kb, len);
+  f32x4 kf[NK], vf[NK], dk[NK], dv[NK];
+  own_row<D>((const float*)a.k + (r0 + krow) * a.ldk + w.kv * d, kok, d, lane, kf);
+  own_row<D>((const float*)a.v + (r0 + krow) * a.ldv + w.kv * d, kok, d, lane, vf);
+#pragma unroll
+  for (int i = 0; i < NK; ++i) dk[i] = dv[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  F32Block<D> qb, gb;
+  float L = 0.f, De = 0.f;
+  int hd = w.nq ? w.n0 / w.nq : 0, blk = w.nq ? w.n0 % w.nq : 0;   // the next block to load: head, block
+  auto load = [&]() {
+    const int i0 = (w.qlo + blk) * BR;
+    qb.load(Q + (long)i0 * a.ldq + hd * d, a.ldq, tid, len - i0, d);
+    gb.load(G + (long)i0 * a.lddc + hd * d, a.lddc, tid, len - i0, d);
+    const bool in = tid < BR && i0 + tid < len;
+    L = in ? lse[(long)hd * a.s + i0 + tid] : 0.f;
+    De = in ? delta[(long)hd * a.s + i0 + tid] : 0.f;
+    if (++blk == w.nq) {
+      blk = 0;
+      ++hd;
+    }
+  };
+  if (w.n0 < w.n1) load();
+  int cur = w.nq ? w.n0 % w.nq : 0;
+  for (int n = w.n0; n < w.n1; ++n) {
+    __syncthreads();
+    qb.store(Qs, tid);
+    gb.store(Gs, tid);
+    if (tid < BR) {
+      Ls[tid] = L;
+      Ds[tid] = De;
+    }
+    __syncthreads();
+    if (n + 1 < w.n1) load();
+    const int i0 = (w.qlo + cur) * BR;
+    cur = cur + 1 == w.nq ? 0 : cur + 1;
+    if (row0 >= len) continue;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {   // rows: query i0 + 16 t + 4 g4 + e, column: key
+      if (i0 + 16 * t >= hi_max || i0 + 16 * t + 15 < lo_min) continue;
+      f32x4 s{0.f, 0.f, 0.f, 0.f}, dp{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int kk = 0; kk < NK; ++kk) {
+        const f32x4 qf = frow<D>(Qs, 16 * t, kk, lane), gf = frow<D>(Gs, 16 * t, kk, lane);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          s = MFMA4(qf[e], kf[kk][e], s);
+          dp = MFMA4(gf[e], vf[kk][e], dp);
+        }
+      }
+      const f32x4 L4 = *(const f32x4*)(Ls + 16 * t + 4 * g4), D4 = *(const f32x4*)(Ds + 16 * t + 4 * g4);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int i = i0 + 16 * t + 4 * g4 + e;
+        const bool ok = i >= lo && i < hi;
+        const float p = ok ? exp2f(s[e] * scale2 - L4[e]) : 0.f, ds = ok ? p * (dp[e] - D4[e]) : 0.f;
+#pragma unroll
+        for (int c = 0; c < NK; ++c) {
+          dv[c] = MFMA4(fcol<D>(Gs, 16 * c, 16 * t, e, lane), p, dv[c]);
+          dk[c] = MFMA4(fcol<D>(Qs, 16 * c, 16 * t, e, lane), ds, dk[c]);
+        }
+      }
+    }
+  }
+  if (w.slot >= 0) {
+    float* const P = a.partial + (long)w.slot * 2 * 64 * D;
+#pragma unroll
+    for (int i = 0; i < NK; ++i) {
+      *(f32x4*)(P + ((wave * NK + i) * 64 + lane) * 4) = dk[i];
+      *(f32x4*)(P + 64 * D + ((wave * NK + i) * 64 + lane) * 4) = dv[i];
+    }
+    return;
+  }
+  if (krow < a.s) {
+#pragma unroll
+    for (int i = 0; i < NK; ++i) {
+      const int col = 16 * i + 4 * g4;
+      if (col < d) {
+        *(f32x4*)((float*)a.dk + (r0 + krow) * a.lddk + w.kv * d + col) = dk[i] * scale;
+        *(f32x4*)((float*)a.dv + (r0 + krow) * a.lddv + w.kv * d + col) = dv[i];
+      }
+    }
+  }
+}
+
+template <int D>
+__global__ __launch_bounds__(256) void attn_win_bwd_f32(AttnWinArgs a, float scale2, float scale) {
+  __shared__ __attribute__((aligned(16))) float X[BR * (D + 8)];
+  __shared__ __attribute__((aligned(16))) float Y[BR * (D + 8)];
+  __shared__ __attribute__((aligned(16))) float Ls[BR];
+  __shared__ __attribute__((aligned(16))) float Ds[BR];
+  const unsigned nk = a.plan.key_tasks;
+  if (blockIdx.x < nk) win_dkdv_f32<D>(a, spread(blockIdx.x, nk), scale2, scale, X, Y, Ls, Ds);
+  else win_dq_f32<D>(a, spread(blockIdx.x - nk, gridDim.x - nk), scale2, scale, X, Y);
+}
+
+// ------------------------------------------------------------------ both types
+// delta [b, A, s]: 16 lanes per head, V columns each, four heads of a row per wave
+template <typename T>
+__global__ __launch_bounds__(256) void attn_win_delta(AttnWinArgs a) {
+  constexpr int V = 16 / sizeof(T);
+  const int lane = threadIdx.x & 63;
+  const long row = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (row >= (long)a.b * a.s) return;
+  const int bi = (int)(row / a.s), qi = (int)(row % a.s);
+  if (qi >= len_of(a, bi)) return;   // (nothing reads it)
+  const T *G = (const T*)a.dctx + row * a.lddc, *O = (const T*)a.ctx + row * a.ldc;
+  const float* O32 = a.ctx32 ? a.ctx32 + row * a.ldc : nullptr;
+  for (int h = lane >> 4; h - (lane >> 4) < a.A; h += 4) {
+    float t = 0.f;
+    if (h < a.A)
+      for (int c = (lane & 15) * V; c < a.d; c += 16 * V) {
+        const int at = h * a.d + c;
+        typedef T TV __attribute__((ext_vector_type(V)));
+        const TV g = *(const TV*)(G + at);
+        if (O32) {
+          typedef float FV __attribute__((ext_vector_type(V)));
+          const FV o = *(const FV*)(O32 + at);
+#pragma unroll
+          for (int e = 0; e < V; ++e) t = fmaf(to_f32((T)g[e]), o[e], t);
+        } else {
+          const TV o = *(const TV*)(O + at);
+#pragma unroll
+          for (int e = 0; e < V; ++e) t = fmaf(to_f32((T)g[e]), to_f32((T)o[e]), t);
+        }
+      }
+#pragma unroll
+    for (int x = 1; x < 16; x <<= 1) t += __shfl_xor(t, x, 64);
+    if (h < a.A && (lane & 15) == 0) a.delta[((long)bi * a.A + h) * a.s + qi] = t;
+  }
+}
+
+// dk (z = 0), dv of the tiles whose walk has parts: the parts' sums in ascending order.  RW: rows (keys) of a wave; an
+// accumulator block is RW rows x 64 * 4 / RW columns.
+template <typename T, int D, int KT, int RW, int BLK>
+__global__ __launch_bounds__(256) void attn_win_join(AttnWinArgs a, float scale) {
+  constexpr int UNITS = KT * D / 4 / 256;   // workgroups per tile, four elements to a lane
+  const WinPlan& p = a.plan;
+  const int head = blockIdx.y, nt = (p.sink_parts > 1 ? p.sink_tiles : 0);
+  int tile = blockIdx.x / UNITS;
+  if (nt == 0) tile += p.sink_tiles;   // (then the other tiles have parts)
+  const bool sink = tile < p.sink_tiles;
+  const int sinks = p.sink_tiles * p.sink_parts;
+  // the tile's first task (KeyTask counts the same)
+  KeyTask w(a, head * (sinks + (p.key_tiles - p.sink_tiles) * p.parts) + (sink ? tile * p.sink_parts : sinks + (tile - p.sink_tiles) * p.parts), KT, BLK);
+  const int all = w.nq * (a.A / a.Ak), used = (all + p.steps - 1) / p.steps;
+  const int u = (blockIdx.x % UNITS) * 256 + threadIdx.x, lane = u & 63, blk = u >> 6;
+  constexpr int CB = 256 / RW;              // columns of an accumulator register block
+  const int row = blk / (D / CB) * RW + (lane & (RW - 1)), col = blk % (D / CB) * CB + 4 * (lane / RW);
+  const float* src = a.partial + ((long)w.slot * 2 + blockIdx.z) * KT * D + (long)u * 4;
+  f32x4 t{0.f, 0.f, 0.f, 0.f};
+  int i = 0;
+  for (; i + 3 < used; i += 4) {
+    f32x4 x[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) x[q] = *(const f32x4*)(src + (long)(i + q) * 2 * KT * D);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) t += x[q];
+  }
+  for (; i < used; ++i) t += *(const f32x4*)(src + (long)i * 2 * KT * D);
+  if (w.k0 + row >= a.s || col >= a.d) return;
+  if (blockIdx.z == 0) t *= scale;
+  T* const out = (T*)(blockIdx.z ? a.dv : a.dk) + ((long)w.bi * a.s + w.k0 + row) * (blockIdx.z ? a.lddv : a.lddk) + w.kv * a.d + col;
+  if constexpr (sizeof(T) == 2) {
+    bf16x4 o;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = (bf16)t[e];
+    *(bf16x4*)out = o;
+  } else {
+    *(f32x4*)out = t;
+  }
+}
+
+// ------------------------------------------------------------------ launchers
+static bool al16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+
+bool attn_win_takes(Dtype dt, const AttnWinArgs& a) {
+  const int v = dt == DT_BF16 ? 8 : 4;
+  if (a.d % v || a.d > 128) return false;
+  for (int ld : {a.ldq, a.ldk, a.ldv, a.ldc, a.lddc, a.lddq, a.lddk, a.lddv})
+    // (a sequence's bytes are counted in 32 bits, and so are those of a block of 64 rows)
+    if (ld % v || ld >= (1 << 23) || (long)a.s * ld >= (1L << 30) - 4096) return false;
+  for (const void* p : {a.q, a.k, a.v, (const void*)a.ctx, (const void*)a.ctx32, a.dctx, (const void*)a.dq, (const void*)a.dk, (const void*)a.dv})
+    if (!al16(p)) return false;
+  return true;
+}
+
+// Workgroups of four waves, or of two where four would leave a quarter of the 256 units without one (bf16; as in attention.hip)
+static int fwd_waves(const AttnWinArgs& a) { return (long)((a.s + 127) / 128) * a.b * a.A < 192 ? 2 : 4; }
+static int bwd_waves(const AttnWinArgs& a) { return (long)((a.s + 127) / 128) * a.b * (a.A + a.Ak) < 192 ? 2 : 4; }
+
+// How the walks of dk and dv are cut.  Parts of CS blocks: as long as the walk of a tile without sinks where those tiles fill
+// the chip (two to a unit), else as long as two workgroups to a unit leave, eight blocks at least.
+static void make_plan(Dtype dt, AttnWinArgs& a) {
+  const int kt = dt == DT_BF16 ? 32 * bwd_waves(a) : 64, blk = dt == DT_BF16 ? 64 : BR;
+  WinPlan& p = a.plan;
+  const long G = a.A / a.Ak, nb = (a.s + blk - 1) / blk, heads = (long)a.b * a.Ak;
+  p.key_tiles = (a.s + kt - 1) / kt;
+  p.sink_tiles = a.W ? (int)std::min<long>(p.key_tiles, ((long)a.S + kt - 1) / kt) : 0;
+  const long rest = p.key_tiles - p.sink_tiles;
+  // the most blocks that a walk without sinks has, per head
+  const long reach = !a.W ? nb : std::min(nb, ((a.causal ? 1L : 2L) * (a.W - 1) + kt + blk - 2) / blk + 1);
+  const long total = heads * G * (rest * reach + p.sink_tiles * nb), fair = (total + 511) / 512;
+  long steps = heads * rest >= 512 ? G * reach : std::min(G * (rest ? reach : nb), std::max(8L, fair));
+  p.parts = (int)((G * reach + steps - 1) / steps);
+  p.sink_parts = (int)((G * nb + steps - 1) / steps);
+  if (!p.sink_tiles) p.sink_parts = 1;
+  if (!rest) p.parts = 1;
+  p.steps = (int)steps;
+  p.slots = (p.sink_parts > 1 ? p.sink_tiles * p.sink_parts : 0) + (p.parts > 1 ? (int)rest * p.parts : 0);
+  p.key_tasks = (unsigned)(heads * (p.sink_tiles * p.sink_parts + rest * p.parts));
+}
+
+template <typename F>
+static auto pick_width(Dtype dt, int d, F&& f) {
+  if (dt != DT_BF16 && d <= 16) return f(std::integral_constant<int, 16>{});
+  if (d <= 32) return f(std::integral_constant<int, 32>{});
+  if (d <= 64) return f(std::integral_constant<int, 64>{});
+  return f(std::integral_constant<int, 128>{});
+}
+
+static size_t delta_bytes(const AttnWinArgs& a) { return ((size_t)a.b * a.A * a.s * 4 + 255) / 256 * 256; }
+
+int64_t attn_win_workspace(Dtype dt, AttnWinArgs a) {
+  make_plan(dt, a);
+  const int kt = dt == DT_BF16 ? 32 * bwd_waves(a) : 64;
+  const int width = pick_width(dt, a.d, [](auto D) { return (int)decltype(D)::value; });
+  return (int64_t)delta_bytes(a) + (int64_t)a.b * a.Ak * a.plan.slots * 2 * kt * width * 4;
+}
+
+template <typename K>
+static hipError_t allow_lds(K kern, int bytes) {
+  return hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+}
+
+hipError_t launch_attn_win_fwd(Dtype dt, const AttnWinArgs& a, hipStream_t st) {
+  const float scale2 = LOG2E * a.scale;
+  return pick_width(dt, a.d, [&](auto D) {
+    constexpr int d = decltype(D)::value;
+    if (dt != DT_BF16) {
+      hipLaunchKernelGGL(attn_win_fwd_f32<d>, dim3((unsigned)((long)((a.s + 63) / 64) * a.b * a.A)), dim3(256), 0, st, a, scale2);
+      return hipGetLastError();
+    }
+    if constexpr (d >= 32) {
+      auto go = [&](auto NW) {
+        constexpr int nw = decltype(NW)::value, lds = WinRing<d, nw, false>::BYTES;
+        static const hipError_t rc = allow_lds(attn_win_fwd<d, nw>, lds);
+        if (rc != hipSuccess) return rc;
+        hipLaunchKernelGGL((attn_win_fwd<d, nw>), dim3((unsigned)((long)((a.s + 32 * nw - 1) / (32 * nw)) * a.b * a.A)), dim3(64 * nw), lds, st, a, scale2);
+        return hipGetLastError();
+      };
+      return fwd_waves(a) == 4 ? go(std::integral_constant<int, 4>{}) : go(std::integral_constant<int, 2>{});
+    }
+    return hipErrorInvalidValue;
+  });
+}
+
+hipError_t launch_attn_win_bwd(Dtype dt, AttnWinArgs a, void* workspace, hipStream_t st) {
+  make_plan(dt, a);
+  a.delta = (float*)workspace;
+  a.partial = (float*)((char*)workspace + delta_bytes(a));
+  const float scale = a.scale, scale2 = LOG2E * scale;
+  const dim3 rows((unsigned)(((long)a.b * a.s + 3) / 4));
+  if (dt == DT_BF16) hipLaunchKernelGGL(attn_win_delta<bf16>, rows, dim3(256), 0, st, a);
+  else hipLaunchKernelGGL(attn_win_delta<float>, rows, dim3(256), 0, st, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const int joined = a.plan.slots ? (a.plan.sink_parts > 1 ? a.plan.sink_tiles : 0) + (a.plan.parts > 1 ? a.plan.key_tiles - a.plan.sink_tiles : 0) : 0;
+  return pick_width(dt, a.d, [&](auto D) {
+    constexpr int d = decltype(D)::value;
+    auto join = [&](auto kern, int kt) {
+      if (!joined) return hipSuccess;
+      hipLaunchKernelGGL(kern, dim3(joined * (kt * d / 1024), a.b * a.Ak, 2), dim3(256), 0, st, a, scale);
+      return hipGetLastError();
+    };
+    if (dt != DT_BF16) {
+      const long grid = a.plan.key_tasks + (long)((a.s + 63) / 64) * a.b * a.A;
+      hipLaunchKernelGGL(attn_win_bwd_f32<d>, dim3((unsigned)grid), dim3(256), 0, st, a, scale2, scale);
+      e = hipGetLastError();
+      return e != hipSuccess ? e : join(attn_win_join<float, d, 64, 16, BR>, 64);
+    }
+    if constexpr (d >= 32) {
+      auto go = [&](auto NW) {
+        constexpr int nw = decltype(NW)::value, lds = WinRing<d, nw, true>::BYTES;
+        static const hipError_t rc = allow_lds(attn_win_bwd<d, nw>, lds);
+        if (rc != hipSuccess) return rc;
+        const long grid = a.plan.key_tasks + (long)((a.s + 32 * nw - 1) / (32 * nw)) * a.b * a.A;
+        hipLaunchKernelGGL((attn_win_bwd<d, nw>), dim3((unsigned)grid), dim3(64 * nw), lds, st, a, scale2, scale);
+        e = hipGetLastError();
+        return e != hipSuccess ? e : join(attn_win_join<bf16, d, 32 * nw, 32, 64>, 32 * nw);
+      };
+      return bwd_waves(a) == 4 ? go(std::integral_constant<int, 4>{}) : go(std::integral_constant<int, 2>{});
+    }
+    return hipErrorInvalidValue;
+  });
+}
+
+}  // namespace dapple

@@ -190,6 +190,34 @@ hipError_t launch_attn_bwd_f32(const AttnArgs& a, hipStream_t st);
 // true when its backward can take delta_blocks (a head is a whole number of 32-column blocks)
 bool attn_takes_delta_blocks(Dtype dt, const AttnArgs& a);
 
+// ---------------------------------------------------------------- attention of visible pairs (attention_window.hip)
+// how the walks of dk and dv over the query blocks are cut (make_plan)
+struct WinPlan {
+  int key_tiles, sink_tiles;     // tiles of keys; those among them that hold sinks
+  int parts, sink_parts, steps;  // parts of a tile's walk, of `steps` blocks each
+  int slots;                     // of fp32 sums, per sequence and key head
+  unsigned key_tasks;
+};
+// rows b*s at row strides in elements, 0 <= W < s (0: no window), 0 <= S <= s; lse, delta [b, A, s]; ctx32 (may be NULL) in ctx's
+// layout
+struct AttnWinArgs {
+  const void *q, *k, *v;
+  void* ctx;
+  float *ctx32, *lse;
+  const int32_t* lens;           // NULL: s each
+  const void* dctx;
+  void *dq, *dk, *dv;
+  float *delta, *partial;        // (of the workspace)
+  int b, s, A, Ak, d, W, S, causal;
+  int ldq, ldk, ldv, ldc, lddc, lddq, lddk, lddv;
+  float scale;
+  WinPlan plan;
+};
+bool attn_win_takes(Dtype dt, const AttnWinArgs& a);
+int64_t attn_win_workspace(Dtype dt, AttnWinArgs a);   // bytes of the backward's
+hipError_t launch_attn_win_fwd(Dtype dt, const AttnWinArgs& a, hipStream_t st);
+hipError_t launch_attn_win_bwd(Dtype dt, AttnWinArgs a, void* workspace, hipStream_t st);
+
 // ---------------------------------------------------------------- row kernels
 // y = LN(z) over the last dim (H), stats[2*r] = mean, stats[2*r+1] = rstd.  z_f32: z is fp32
 // although the stage is bf16 (the residual stream is kept unrounded); y32 (may be NULL): an

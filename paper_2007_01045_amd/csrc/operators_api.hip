@@ -17,6 +17,66 @@ static int rc_of(hipError_t e) {
   return e == hipSuccess ? STAGE_OK : set_error(STAGE_E_DEVICE, "a launch failed: %s", hipGetErrorString(e));
 }
 
+// ------------------------------------------------------------------ attention of visible pairs
+// the launcher's arguments; sizes_only: what the size of the workspace depends on
+static int win_args(int dtype, const dapple_attention_window_desc* d, bool bwd, bool sizes_only, AttnWinArgs& a) {
+  if (!d) return set_error(STAGE_E_NULL, "the descriptor is NULL");
+  if (bad_dtype(dtype)) return set_error(STAGE_E_CONFIG, "dtype %d", dtype);
+  if (d->b < 1 || d->s < 1 || d->A < 1 || d->Ak < 1 || d->A % d->Ak || d->d < 1)
+    return set_error(STAGE_E_CONFIG, "%d sequences of %d rows, %d query heads on %d key heads of %d columns", d->b, d->s, d->A, d->Ak, d->d);
+  if (d->window < 0 || d->sinks < 0) return set_error(STAGE_E_CONFIG, "window %d, sinks %d", d->window, d->sinks);
+  if (!(d->scale >= 0.f) || !std::isfinite(d->scale)) return set_error(STAGE_E_CONFIG, "scale must be positive and finite (0: 1/sqrt(d))");
+  const int v = dtype == STAGE_DTYPE_BF16 ? 8 : 4;
+  if (d->d % v || d->d > 128) return set_error(STAGE_E_CONFIG, "heads of %d columns: multiples of %d up to 128 are taken", d->d, v);
+  if ((long)d->b * d->s > 0x7fffffffL || (long)d->b * d->A * ((d->s + 31) / 32) > 0x3fffffffL || (long)d->b * d->A > 0x7fffffffL)
+    return set_error(STAGE_E_CONFIG, "more than 2^31 rows or 2^30 workgroups");
+  a.b = d->b; a.s = d->s; a.A = d->A; a.Ak = d->Ak; a.d = d->d; a.causal = d->causal != 0;
+  a.W = d->window < d->s ? d->window : 0;   // (a window of s positions and more hides nothing)
+  a.S = d->sinks < d->s ? d->sinks : d->s;
+  a.scale = d->scale > 0.f ? d->scale : 1.0f / sqrtf((float)d->d);
+  const struct { int given; int heads; int* to; } lds[] = {{d->ldq, d->A, &a.ldq}, {d->ldk, d->Ak, &a.ldk}, {d->ldv, d->Ak, &a.ldv},
+      {d->ldc, d->A, &a.ldc}, {d->lddc, d->A, &a.lddc}, {d->lddq, d->A, &a.lddq}, {d->lddk, d->Ak, &a.lddk}, {d->lddv, d->Ak, &a.lddv}};
+  for (const auto& l : lds) {
+    const long dense = (long)l.heads * d->d;
+    if (dense >= 1 << 23 || l.given < 0 || (l.given && l.given < dense))
+      return set_error(STAGE_E_CONFIG, "a row stride of %d for %ld columns", l.given, dense);
+    *l.to = l.given ? l.given : (int)dense;
+  }
+  if (sizes_only) return STAGE_OK;
+  if (!d->q || !d->k || !d->v || !d->ctx || !d->lse) return set_error(STAGE_E_NULL, "q, k, v, ctx and lse must not be NULL");
+  if (bwd && (!d->dctx || !d->dq || !d->dk || !d->dv || !d->workspace))
+    return set_error(STAGE_E_NULL, "dctx, dq, dk, dv and workspace must not be NULL");
+  a.q = d->q; a.k = d->k; a.v = d->v; a.ctx = d->ctx; a.ctx32 = d->ctx32; a.lse = d->lse; a.lens = d->lens;
+  if (bwd) { a.dctx = d->dctx; a.dq = d->dq; a.dk = d->dk; a.dv = d->dv; }
+  if (!aligned_to(a.lse, 4) || !aligned_to(a.lens, 4) || (bwd && !aligned_to(d->workspace, 16)))
+    return set_error(STAGE_E_CONFIG, "lse, lens or workspace not aligned");
+  if (!attn_win_takes(type_of(dtype), a))
+    return set_error(STAGE_E_CONFIG, "tensors must be 16-byte aligned, row strides multiples of %d below 2^23, a sequence below 2^30 elements", v);
+  return STAGE_OK;
+}
+
+extern "C" {
+
+int dapple_attention_window_fwd(int dtype, const dapple_attention_window_desc* d, void* stream) {
+  AttnWinArgs a{};
+  const int rc = win_args(dtype, d, false, false, a);
+  return rc != STAGE_OK ? rc : rc_of(launch_attn_win_fwd(type_of(dtype), a, (hipStream_t)stream));
+}
+
+int64_t dapple_attention_window_workspace(int dtype, const dapple_attention_window_desc* d) {
+  AttnWinArgs a{};
+  const int rc = win_args(dtype, d, true, true, a);
+  return rc != STAGE_OK ? rc : attn_win_workspace(type_of(dtype), a);
+}
+
+int dapple_attention_window_bwd(int dtype, const dapple_attention_window_desc* d, void* stream) {
+  AttnWinArgs a{};
+  const int rc = win_args(dtype, d, true, false, a);
+  return rc != STAGE_OK ? rc : rc_of(launch_attn_win_bwd(type_of(dtype), a, d->workspace, (hipStream_t)stream));
+}
+
+}  // extern "C"
+
 // ------------------------------------------------------------------ head norms and rotation
 // the launcher's arguments; workspace_only: what the size of the workspace depends on
 static int rope_args(int dtype, const dapple_qk_rope_desc* d, bool bwd, bool workspace_only, QkRopeArgs& a) {

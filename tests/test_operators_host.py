@@ -86,3 +86,26 @@ def test_rope_table_refusals():
                      ((4, 8), dict(original=16, low=2.0, high=2.0)), ((4, 8), dict(magnitude=math.nan))]:
         refused(B.STAGE_E_CONFIG, B.dapple_rope_table, P, *args, **kw)
     refused(B.STAGE_E_CONFIG, B.dapple_rope_table, P + 4, 4, 8)
+
+
+def test_attention_window_refusals():
+    ok = dict(q=P, k=P, v=P, ctx=P, lse=P, dctx=P, dq=P, dk=P, dv=P, workspace=P, b=1, s=100, A=4, Ak=2, d=64, window=10, sinks=2, causal=1)
+    null, conf = B.STAGE_E_NULL, B.STAGE_E_CONFIG
+    both = [(null, dict(q=None)), (null, dict(k=None)), (null, dict(v=None)), (null, dict(ctx=None)), (null, dict(lse=None)), (conf, dict(b=0)),
+            (conf, dict(s=0)), (conf, dict(A=0)), (conf, dict(Ak=0)), (conf, dict(Ak=3)), (conf, dict(d=0)), (conf, dict(d=60)), (conf, dict(d=136)),
+            (conf, dict(window=-1)), (conf, dict(sinks=-1)), (conf, dict(scale=-1.0)), (conf, dict(scale=math.inf)), (conf, dict(scale=math.nan)),
+            (conf, dict(ldq=255)), (conf, dict(ldq=260)), (conf, dict(ldk=-8)), (conf, dict(ldv=1 << 23)), (conf, dict(s=1 << 22, ldq=264)),
+            (conf, dict(q=P + 8)), (conf, dict(ctx32=P + 4)), (conf, dict(lse=P + 2)), (conf, dict(lens=P + 1)),
+            (conf, dict(b=1 << 20, s=1 << 12)), (conf, dict(b=1 << 16, A=1 << 15, Ak=1 << 15, s=1))]
+    for code, change in both:
+        for f in (B.dapple_attention_window_fwd, B.dapple_attention_window_bwd):
+            refused(code, f, B.DTYPE_BF16, B.attention_window_desc(**dict(ok, **change)))
+    for change in (dict(dctx=None), dict(dq=None), dict(dk=None), dict(dv=None), dict(workspace=None)):
+        refused(null, B.dapple_attention_window_bwd, B.DTYPE_F32, B.attention_window_desc(**dict(ok, **change)))
+    for change in (dict(dctx=P + 8), dict(dv=P + 4), dict(lddq=258), dict(workspace=P + 8)):
+        refused(conf, B.dapple_attention_window_bwd, B.DTYPE_F32, B.attention_window_desc(**dict(ok, **change)))
+    refused(conf, B.dapple_attention_window_fwd, 2, B.attention_window_desc(**ok))
+    refused(conf, B.dapple_attention_window_fwd, B.DTYPE_F32, B.attention_window_desc(**dict(ok, d=66)))
+    refused(conf, B.dapple_attention_window_workspace, B.DTYPE_BF16, B.attention_window_desc(**dict(ok, d=4)))
+    for dt in (B.DTYPE_F32, B.DTYPE_BF16):
+        assert B.dapple_attention_window_workspace(dt, B.attention_window_desc(**ok)) >= 4 * 4 * 100
