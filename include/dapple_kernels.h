@@ -207,6 +207,40 @@ int dapple_qk_rope_bwd(int dtype, const dapple_qk_rope_desc* d, void* stream);
 int dapple_rope_table(float* table, int max_pos, int rot, double base, double factor, int original, double low, double high,
                       double magnitude, void* stream);
 
+/* The gated feed-forward block:  g = x Wg + bg,  u = x Wu + bu,  h = act(g) * u,  y = h Wo + bo, and its gradients.
+ * x [T, H], y [T, H] at row strides ldx, ldy; w_in [H, 2F]: the columns of Wg, then those of Wu; b_in [2F] likewise; w_out [F, H],
+ * b_out [H]; biases may be NULL.  h [T, F] and gu [T, 2F] (g and u, before the activation) are dense: h is always written (the second
+ * product reads it), gu only if given; both are what the backward needs.  act: SiLU g / (1 + e^-g) or GELU (erf).
+ * bwd: from x, the weights, gu, h and dy: dgu [T, 2F] (dense, always written), dx (NULL = not wanted), and the weights' gradients
+ * dw_in, dw_out (both or neither) with db_in, db_out (NULL = not wanted).  accumulate = 0: these four are of dtype and set;
+ * accumulate != 0: fp32, and added to, as a stage sums its micro-batches.
+ * Outputs overlap no input.  bf16: H, F and strides multiples of 8; fp32: of 4; all 16-byte aligned; T * 2F, T * stride and H * 2F
+ * below 2^30 - 4096.  bf16 calls round g, u, h, dg and du once each (products are summed in fp32). */
+enum { DAPPLE_ACT_SILU = 0, DAPPLE_ACT_GELU = 1 };
+typedef struct {
+  const void* x;
+  const void* w_in;
+  const void* b_in;
+  const void* w_out;
+  const void* b_out;
+  void* gu;
+  void* h;
+  void* y;
+  const void* dy;
+  void* dgu;
+  void* dx;
+  void* dw_in;
+  void* db_in;
+  void* dw_out;
+  void* db_out;
+  void* workspace; /* bwd */
+  int32_t T, H, F, act, accumulate;
+  int32_t ldx, ldy, lddy, lddx; /* in elements, 0 = H */
+} dapple_gated_ffn_desc;
+int dapple_gated_ffn_fwd(int dtype, const dapple_gated_ffn_desc* d, void* stream);
+int64_t dapple_gated_ffn_workspace(int dtype, const dapple_gated_ffn_desc* d);
+int dapple_gated_ffn_bwd(int dtype, const dapple_gated_ffn_desc* d, void* stream);
+
 /* The global norm of n gradient tensors, all of one dtype: grads and sizes are HOST arrays of n device pointers (aligned to
  * their elements) and element counts (0 is allowed, its pointer is not looked at).
  *   norm_dev[0] = |grad_scale| * sqrt(sum of all squares)      (squares and sums in 64 bits)

@@ -24,6 +24,7 @@ FLAG_RECOMPUTE = 2
 FLAG_ONE_STREAM = 4
 EPI_BIAS, EPI_ADD, EPI_MUL, EPI_GELU, EPI_ACC32, EPI_BSUM = 1, 2, 4, 8, 16, 128
 EPI_OUT32, EPI_AUX32, EPI_ROWDOT = 32, 64, 256
+ACT_SILU, ACT_GELU = 0, 1
 
 
 class stage_config(C.Structure):
@@ -70,6 +71,13 @@ class attention_window_desc(C.Structure):      # dapple_attention_window_desc
                [(n, C.c_int32) for n in
                 ("b", "s", "A", "Ak", "d", "window", "sinks", "causal",
                  "ldq", "ldk", "ldv", "ldc", "lddc", "lddq", "lddk", "lddv")] + [("scale", C.c_float)]
+
+
+class gated_ffn_desc(C.Structure):      # dapple_gated_ffn_desc
+    _fields_ = [(n, C.c_void_p) for n in
+                ("x", "w_in", "b_in", "w_out", "b_out", "gu", "h", "y", "dy", "dgu", "dx", "dw_in", "db_in", "dw_out", "db_out",
+                 "workspace")] + \
+               [(n, C.c_int32) for n in ("T", "H", "F", "act", "accumulate", "ldx", "ldy", "lddy", "lddx")]
 
 
 # every symbol the two headers declare: name -> (restype, argtypes)
@@ -126,6 +134,9 @@ SYMBOLS = {
     "dapple_qk_rope_workspace": (C.c_int64, [_i, C.POINTER(qk_rope_desc)]),
     "dapple_qk_rope_bwd": (_i, [_i, C.POINTER(qk_rope_desc), _vp]),
     "dapple_rope_table": (_i, [_vp, _i, _i, C.c_double, C.c_double, _i, C.c_double, C.c_double, C.c_double, _vp]),
+    "dapple_gated_ffn_fwd": (_i, [_i, C.POINTER(gated_ffn_desc), _vp]),
+    "dapple_gated_ffn_workspace": (C.c_int64, [_i, C.POINTER(gated_ffn_desc)]),
+    "dapple_gated_ffn_bwd": (_i, [_i, C.POINTER(gated_ffn_desc), _vp]),
     "dapple_grad_norm_workspace": (C.c_int64, [C.POINTER(C.c_int64), _i]),
     "dapple_grad_norm": (_i, [_i, _pp, C.POINTER(C.c_int64), _i, _f, _f, _vp, _vp, _vp]),
     "dapple_grad_clip": (_i, [_i, _pp, _pp, C.POINTER(C.c_int64), _i, _vp, _vp]),
@@ -488,6 +499,18 @@ def dapple_rope_table(table_ptr, max_pos, rot, base=10000.0, factor=1.0, origina
                       stream_ptr=None):
     """Fills the fp32 table [max_pos, rot / 2, 2] of dapple_qk_rope_fwd and _bwd on the device."""
     _check(load().dapple_rope_table(table_ptr, max_pos, rot, base, factor, original, low, high, magnitude, stream_ptr))
+
+
+def dapple_gated_ffn_fwd(dtype, desc: gated_ffn_desc, stream_ptr=None):
+    _check(load().dapple_gated_ffn_fwd(dtype, C.byref(desc), stream_ptr))
+
+
+def dapple_gated_ffn_workspace(dtype, desc: gated_ffn_desc) -> int:
+    return _check(load().dapple_gated_ffn_workspace(dtype, C.byref(desc)))
+
+
+def dapple_gated_ffn_bwd(dtype, desc: gated_ffn_desc, stream_ptr=None):
+    _check(load().dapple_gated_ffn_bwd(dtype, C.byref(desc), stream_ptr))
 
 
 def _i64_array(sizes):

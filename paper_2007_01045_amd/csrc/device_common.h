@@ -49,6 +49,18 @@ __device__ __forceinline__ float gelu_grad_f(float u) {
   return gp;
 }
 
+// The activation of a gated feed-forward block and its derivative: SiLU, g sigma(g) with sigma = 1 / (1 + 2^(-g log2 e)) -- 1 / (1 +
+// infinity) where 2^... overflows --, or GELU.
+__device__ __forceinline__ void gate_act(bool silu, float g, float& a, float& da) {
+  if (silu) {
+    const float f = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(g * -1.4426950408889634f));
+    a = g * f;
+    da = f * fmaf(g, 1.0f - f, 1.0f);
+  } else {
+    gelu_both(g, a, da);
+  }
+}
+
 // LDS transpose read (gfx950): the 16 lanes of a group each point at 4
 // consecutive 16-bit elements; lanes 4e..4e+3 together supply "row e" (16
 // elements), and lane i of the group receives element i of rows 0..3.

@@ -94,6 +94,18 @@ struct OperandTile {
       if (MASKED) vfull[j] = voff[j];
     }
   }
+  // k-strided, columns in pairs of 32-wide blocks: block 2i of the tile is columns r0 + 32 i .. of the operand, block 2i + 1 the
+  // same columns F further on (a gated projection: gate and value of a column in one wave's accumulators)
+  __device__ __forceinline__ void init_pairs(int ld, int r0, int F, int wave, int lane) {
+    static_assert(KS, "a k-strided operand");
+    over = 0;
+#pragma unroll
+    for (int j = 0; j < NI; ++j) {
+      const int pos = (wave * NI + j) * 64 + lane;
+      const int krow = pos / (R / 8), c = (pos % (R / 8)) ^ kswz(krow), blk = c >> 2;
+      voff[j] = (krow * ld + r0 + (blk >> 1) * 32 + (c & 3) * 8 + (blk & 1) * F) * 2 + BIAS - (j % GROUP) * 1024;
+    }
+  }
   // the next k-tile to be requested is (or is not) the short one at the end of a segment
   __device__ __forceinline__ void set_short(bool is_short) {
     if constexpr (MASKED) {
@@ -317,12 +329,114 @@ struct GemmTile {
   static constexpr int MIN_WAVES = !SEG && NW == 8 && TWO ? 4 : (SEG || (NW == 4 && TWO) ? 2 : 1);
 };
 
+// The epilogue of a gated block's products (GATE, see gemm_mfma_tile): as there, 32 rows at a time through the wave's staging
+// tile, so that a lane has four neighbouring columns, of the gate and of the value.
+template <typename CFG, int GATE, bool BIG, typename ACC>
+__device__ __forceinline__ void gate_epilogue(const GemmArgs& g, const ACC& acc, float* stg, int row0, int col0, bool interior, int lane) {
+  constexpr int MI = CFG::MI, NI = CFG::NI;
+  constexpr int C4 = CFG::WN / (GATE == 1 ? 8 : 4), RS = 64 / C4, NIT = 32 / RS;   // a row's pieces of four columns; rows per instruction
+  static_assert(GATE == 2 || NI % 2 == 0, "gate and value of a column belong to one wave");
+  constexpr int HB = NIT < 4 ? NIT : 4;
+  const int r = lane / C4, c = lane % C4 * 4, col = col0 + c, F = g.N;
+  const bool silu = (g.epi & EPI_SILU) != 0;
+  f32x4 bg{0.f, 0.f, 0.f, 0.f}, bu = bg;
+  if (GATE == 1 && (g.epi & EPI_BIAS) && col < F) {
+    const bf16x4 x = *(const bf16x4*)((const bf16*)g.bias + col), y = *(const bf16x4*)((const bf16*)g.bias + F + col);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      bg[e] = (float)x[e];
+      bu[e] = (float)y[e];
+    }
+  }
+  // what the gradient reads, a unit of HB pieces ahead
+  bf16x4 pg[2][HB], pu[2][HB];
+  auto request = [&](auto K) __attribute__((always_inline)) {
+    constexpr int k = decltype(K)::value, i = k / (NIT / HB), hb = k % (NIT / HB) * HB;
+    if constexpr (GATE == 2) {
+#pragma unroll
+      for (int u = 0; u < HB; ++u) {
+        const int row = row0 + 32 * i + (hb + u) * RS + r;
+        const bf16* p = (const bf16*)g.aux + (long)row * g.ldaux + col;
+        const bool in = interior || (row < g.M && col < F);
+        pg[k & 1][u] = in ? *(const bf16x4*)p : bf16x4{};
+        pu[k & 1][u] = in ? *(const bf16x4*)(p + F) : bf16x4{};
+      }
+    }
+  };
+  request(std::integral_constant<int, 0>{});
+  static_for<MI>([&](auto I) __attribute__((always_inline)) {
+    constexpr int i = decltype(I)::value;
+#pragma unroll
+    for (int j = 0; j < NI; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        *(f32x4*)(stg + (lane & 31) * CFG::EPI_LD + j * 32 + 8 * q + 4 * (lane >> 5)) =
+            f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+    __builtin_amdgcn_wave_barrier();   // (private to the wave, whose LDS accesses execute in order)
+    static_for<NIT / HB>([&](auto Hc) __attribute__((always_inline)) {
+      constexpr int hb = decltype(Hc)::value * HB, k = i * (NIT / HB) + decltype(Hc)::value;
+      if constexpr (k + 1 < MI * (NIT / HB)) request(std::integral_constant<int, k + 1>{});   // ahead of this unit's stores
+      f32x4 a[HB], b[HB];
+#pragma unroll
+      for (int u = 0; u < HB; ++u) {
+        const float* p = stg + ((hb + u) * RS + r) * CFG::EPI_LD;
+        if constexpr (GATE == 1) {
+          a[u] = *(const f32x4*)(p + c / 32 * 64 + c % 32);
+          b[u] = *(const f32x4*)(p + c / 32 * 64 + 32 + c % 32);
+        } else {
+          a[u] = *(const f32x4*)(p + c);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < HB; ++u) {
+        const int row = row0 + 32 * i + (hb + u) * RS + r;
+        bf16x4 x, y, h;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          float act, dact;
+          if constexpr (GATE == 1) {
+            const float gate = a[u][e] + bg[e], value = b[u][e] + bu[e];
+            gate_act(silu, gate, act, dact);
+            x[e] = (bf16)gate;
+            y[e] = (bf16)value;
+            h[e] = (bf16)(act * value);
+          } else {
+            gate_act(silu, (float)pg[k & 1][u][e], act, dact);
+            x[e] = (bf16)(a[u][e] * (float)pu[k & 1][u][e] * dact);
+            y[e] = (bf16)(a[u][e] * act);
+          }
+        }
+        if (!interior && (row >= g.M || col >= F)) continue;
+        constexpr Store S = BIG ? Store::Through : Store::Plain;
+        if constexpr (GATE == 1) {
+          store_c<S>((bf16*)g.C + (long)row * g.ldc + col, h);
+          if (g.C2) {
+            bf16* q = (bf16*)g.C2 + (long)row * g.ldaux + col;
+            store_c<BIG ? Store::Far : S>(q, x);
+            store_c<BIG ? Store::Far : S>(q + F, y);
+          }
+        } else {
+          bf16* q = (bf16*)g.C + (long)row * g.ldc + col;
+          store_c<S>(q, x);
+          store_c<S>(q + F, y);
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    __builtin_amdgcn_wave_barrier();
+  });
+}
+
 // CS: the variant that can also sum B over k (EPI_BSUM); KT: the variant for K segments that are no multiple of 64
 // when an operand is k-contiguous (see OperandTile); SEG: an accumulating product over several K segments, each one's
 // sum added to C on its own, in order (EPI_SEGACC): a second set of accumulators holds C and takes the sums of the
 // segments as they are complete, so C is read and written once whatever their number; PACK: the k-tiles of several
-// segments follow each other without a gap (see packs)
-template <int BM, int BN, int WGM, int WGN, int NS, bool AKS, bool BKS, int BK, bool CS, bool KT = false, bool SEG = false, bool PACK = false>
+// segments follow each other without a gap (see packs); GATE: the products of a gated feed-forward block (gemm_gate.hip):
+// 1: the projections, BN / 2 columns of gate and of value side by side (g.N = F, B and bias 2F wide, n_valid = 2F); C = act * value,
+//    C2 (may be NULL) the two before the activation, at strides ldaux, F apart;
+// 2: the gradient before the activation: aux the two (F apart, ldaux), C their gradients (F apart, ldc)
+template <int BM, int BN, int WGM, int WGN, int NS, bool AKS, bool BKS, int BK, bool CS, bool KT = false, bool SEG = false, bool PACK = false,
+          int GATE = 0>
 __device__ __forceinline__ void gemm_mfma_tile(const GemmArgs& g, int tiles_m, int tiles_n, const int bid, const int z) {
   typedef GemmTile<BM, BN, WGM, WGN, NS, AKS, BKS, BK, KT, SEG> CFG;
   typedef typename CFG::TA TA;
@@ -336,12 +450,13 @@ __device__ __forceinline__ void gemm_mfma_tile(const GemmArgs& g, int tiles_m, i
 
   int tm, tn;
   tile_of(bid, tiles_m, tiles_n, BM, BN, tm, tn);
-  const int m0 = tm * BM, n0 = tn * BN;
+  constexpr int BNC = GATE == 1 ? BN / 2 : BN;   // columns of C
+  const int m0 = tm * BM, n0 = tn * BNC;
   // (the small tiles: every argument the prologue and the first requests need in one go of scalar loads, not a round trip
   // per branch that uses some.  Not the 128x64 tile in eight waves, 80 registers a lane, 102 with it: 1400 x 1024 x 4096 21.2
   // us, 22.4 with it, gradient 20.3 and 21.7, with cold weights 31.9 and 32.4)
   constexpr bool EARLY = CFG::NW <= 4 && MI * (CFG::WN / 8) <= 8;
-  if constexpr (EARLY)
+  if constexpr (EARLY && !GATE)
     asm volatile("" ::"s"(g.A), "s"(g.B), "s"(g.C), "s"(g.bias), "s"(g.aux), "s"(g.M), "s"(g.N), "s"(g.K), "s"(g.lda), "s"(g.ldb),
                  "s"(g.ldc), "s"(g.ldaux), "s"(g.kseg_len), "s"(g.segA), "s"(g.segB), "s"(g.ln_stats), "s"(g.ln_gamma),
                  "s"(g.ln_beta), "s"(g.k_valid), "s"(g.m_valid), "s"(g.n_valid), "s"(g.epi));
@@ -362,7 +477,8 @@ __device__ __forceinline__ void gemm_mfma_tile(const GemmArgs& g, int tiles_m, i
   TB tb;
   const int last_chunks = (g.kseg_len - (seg_tiles - 1) * BK) / 8;   // 16-byte chunks of a segment's last k-tile
   ta.init(g.lda, m0, wave, lane, last_chunks);
-  tb.init(g.ldb, n0, wave, lane, last_chunks);
+  if constexpr (GATE == 1) tb.init_pairs(g.ldb, n0, g.N, wave, lane);
+  else tb.init(g.ldb, n0, wave, lane, last_chunks);
   ta.set_short(seg_tiles == 1);
   tb.set_short(seg_tiles == 1);
   FragAddr<BM, AKS, MI, BK> fa;
@@ -470,7 +586,7 @@ __device__ __forceinline__ void gemm_mfma_tile(const GemmArgs& g, int tiles_m, i
   constexpr bool PRE = !CS && !SEG && MI * NIT <= 16;   // (the column-sum variant serves accumulating products only)
   const int epi = g.epi;
   const int lane_col = n0 + wn0 + lane % C4 * 4;   // the lane's four columns
-  const bool interior = m0 + BM <= g.M && n0 + BN <= g.N;
+  const bool interior = m0 + BM <= g.M && n0 + BNC <= g.N;
   // What a product's epilogue reads, as a constant: flags tested per request have the loads wait for each other where
   // the branches meet (gate of 8192 x 4096 x 1024: 108 us, 89 with the whole operand requested in one go).
   //   AUXH: a bf16 second operand, all of it ahead; AUXF: an fp32 one; AUXL: one whose LayerNorm is added (EPI_AUXLN);
@@ -583,7 +699,7 @@ __device__ __forceinline__ void gemm_mfma_tile(const GemmArgs& g, int tiles_m, i
     const int col = n0 + wn0 + 32 * j + (lane & 31);
     bsum0[j] = do_cs && lane < 32 && col < g.N ? bsum_ptr[col] : 0.f;
   }
-  if constexpr (EARLY) {
+  if constexpr (EARLY && !GATE) {
     with_mode([&](auto MODE) __attribute__((always_inline)) {
       if (interior) request_first(MODE, std::true_type{});
       else request_first(MODE, std::false_type{});
@@ -788,6 +904,13 @@ __device__ __forceinline__ void gemm_mfma_tile(const GemmArgs& g, int tiles_m, i
     }
   }
   __builtin_amdgcn_s_waitcnt(0x0F70);  // the tail requests (they read nothing) must be done before LDS is reused
+  if constexpr (GATE != 0) {
+    __builtin_amdgcn_s_waitcnt(0xC07F);
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    gate_epilogue<CFG, GATE, BM == 256>(g, acc, (float*)smem + wave * 32 * CFG::EPI_LD, m0 + wm0, n0 + (GATE == 1 ? wn0 / 2 : wn0), interior, lane);
+    return;
+  }
   // epilogue: per wave, 32 output rows at a time through an fp32 LDS staging tile that
   // turns "a lane owns 4 columns of one row" into row-contiguous stores.
   // acc[i][j][v]: row = wm0 + 32 i + (lane & 31), col = wn0 + 32 j + 8 (v>>2) + 4 (lane>>5) + (v&3)

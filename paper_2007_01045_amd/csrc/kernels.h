@@ -34,7 +34,8 @@ enum GemmEpi {
   EPI_SEGACC = 512,
   // with EPI_ADD | EPI_AUX32: what is added is the LayerNorm of aux, (aux[m,n] - mean[m]) rstd[m] gamma[n] + beta[n] --
   // the residual input of a bf16 stage, unrounded, from the sums it was normalised from.  Batch 1.
-  EPI_AUXLN = 1024
+  EPI_AUXLN = 1024,
+  EPI_SILU = 2048   // a gated block's activation is SiLU, else GELU (launch_gate_fwd, launch_gate_bwd)
 };
 
 struct GemmArgs {
@@ -143,6 +144,25 @@ bool gemm_f32_takes(const GemmArgs& g);
 hipError_t launch_gemm_f32(const GemmArgs& g, hipStream_t st);
 // true when the MFMA kernel takes this problem (else the plain ALU kernel does)
 bool gemm_uses_mfma(Dtype dt, const GemmArgs& g);
+
+// ---------------------------------------------------------------- gated feed-forward block (gated_ffn.hip)
+// x [T, H] at row stride ldx, likewise the others; w_in [H, 2F] (gate columns, then value columns), w_out [F, H]; dense gu and
+// dgu [T, 2F], h [T, F].  NULL: b_in, b_out (no bias), gu in the forward (not kept), dx, the weights' gradients (not wanted).
+struct GatedFfnArgs {
+  const void *x, *w_in, *b_in, *w_out, *b_out;
+  void *gu, *h, *y;
+  const void* dy;
+  void *dgu, *dx, *dw_in, *db_in, *dw_out, *db_out;
+  int T, H, F, ldx, ldy, lddy, lddx;
+  bool silu, accumulate;   // accumulate: the weights' gradients are fp32 and added to, else set in the call's type
+};
+bool gated_ffn_takes(Dtype dt, const GatedFfnArgs& a, bool bwd);
+int64_t gated_ffn_workspace(Dtype dt, const GatedFfnArgs& a);
+hipError_t launch_gated_ffn_fwd(Dtype dt, const GatedFfnArgs& a, hipStream_t st);
+hipError_t launch_gated_ffn_bwd(Dtype dt, const GatedFfnArgs& a, void* workspace, hipStream_t st);
+// its two products with an activation in the epilogue, bf16 (gemm_gate.hip; arguments: GATE of gemm_mfma_tile)
+hipError_t launch_gate_fwd(const GemmArgs& g, hipStream_t st);
+hipError_t launch_gate_bwd(const GemmArgs& g, hipStream_t st);
 
 // ---------------------------------------------------------------- attention
 // q,k,v,ctx,dq,dk,dv,dctx: [b*s, H] row-major, head h in columns [h*d, (h+1)*d).

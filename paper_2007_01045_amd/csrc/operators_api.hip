@@ -167,6 +167,60 @@ int dapple_rope_table(float* table, int max_pos, int rot, double base, double fa
 
 }  // extern "C"
 
+// ------------------------------------------------------------------ gated feed-forward block
+static int ffn_args(int dtype, const dapple_gated_ffn_desc* d, bool bwd, bool sizes_only, GatedFfnArgs& a) {
+  if (!d) return set_error(STAGE_E_NULL, "the descriptor is NULL");
+  if (bad_dtype(dtype)) return set_error(STAGE_E_CONFIG, "dtype %d", dtype);
+  const int v = dtype == STAGE_DTYPE_BF16 ? 8 : 4;
+  const long most = (1L << 30) - 4096;
+  if (d->T < 1 || d->H < 1 || d->F < 1 || d->H % v || d->F % v)
+    return set_error(STAGE_E_CONFIG, "%d rows, %d and %d columns: the columns must be multiples of %d", d->T, d->H, d->F, v);
+  if (2L * d->T * d->F >= most || 2L * d->H * d->F >= most) return set_error(STAGE_E_CONFIG, "T * 2F or H * 2F of 2^30 - 4096 and more");
+  if (d->act != DAPPLE_ACT_SILU && d->act != DAPPLE_ACT_GELU) return set_error(STAGE_E_CONFIG, "activation %d", d->act);
+  a.T = d->T; a.H = d->H; a.F = d->F; a.silu = d->act == DAPPLE_ACT_SILU; a.accumulate = d->accumulate != 0;
+  const struct { int given; int* to; } lds[] = {{d->ldx, &a.ldx}, {d->ldy, &a.ldy}, {d->lddy, &a.lddy}, {d->lddx, &a.lddx}};
+  for (const auto& l : lds) {
+    *l.to = l.given ? l.given : d->H;
+    if (*l.to < d->H || *l.to % v || (long)d->T * *l.to >= most) return set_error(STAGE_E_CONFIG, "a row stride of %d", l.given);
+  }
+  if (sizes_only) return STAGE_OK;
+  if (!d->x || !d->w_in || !d->w_out || !d->h) return set_error(STAGE_E_NULL, "x, w_in, w_out and h must not be NULL");
+  if (!bwd && !d->y) return set_error(STAGE_E_NULL, "y must not be NULL");
+  if (bwd && (!d->dy || !d->gu || !d->dgu || !d->workspace)) return set_error(STAGE_E_NULL, "dy, gu, dgu and workspace must not be NULL");
+  if (bwd && (!d->dw_in != !d->dw_out || (!d->dw_in && (d->db_in || d->db_out))))
+    return set_error(STAGE_E_CONFIG, "dw_in and dw_out are wanted both or not at all, biases' gradients with them");
+  a.x = d->x; a.w_in = d->w_in; a.b_in = d->b_in; a.w_out = d->w_out; a.b_out = d->b_out; a.gu = d->gu; a.h = d->h; a.y = d->y;
+  if (bwd) {
+    a.dy = d->dy; a.dgu = d->dgu; a.dx = d->dx; a.dw_in = d->dw_in; a.db_in = d->db_in; a.dw_out = d->dw_out; a.db_out = d->db_out;
+    if (!aligned_to(d->workspace, 16) || !aligned_to(a.db_in, 16) || !aligned_to(a.db_out, 16))
+      return set_error(STAGE_E_CONFIG, "workspace, db_in or db_out not aligned to 16 bytes");
+  }
+  if (!gated_ffn_takes(type_of(dtype), a, bwd)) return set_error(STAGE_E_CONFIG, "a tensor is not aligned to 16 bytes");
+  return STAGE_OK;
+}
+
+extern "C" {
+
+int dapple_gated_ffn_fwd(int dtype, const dapple_gated_ffn_desc* d, void* stream) {
+  GatedFfnArgs a{};
+  const int rc = ffn_args(dtype, d, false, false, a);
+  return rc != STAGE_OK ? rc : rc_of(launch_gated_ffn_fwd(type_of(dtype), a, (hipStream_t)stream));
+}
+
+int64_t dapple_gated_ffn_workspace(int dtype, const dapple_gated_ffn_desc* d) {
+  GatedFfnArgs a{};
+  const int rc = ffn_args(dtype, d, true, true, a);
+  return rc != STAGE_OK ? rc : gated_ffn_workspace(type_of(dtype), a);
+}
+
+int dapple_gated_ffn_bwd(int dtype, const dapple_gated_ffn_desc* d, void* stream) {
+  GatedFfnArgs a{};
+  const int rc = ffn_args(dtype, d, true, false, a);
+  return rc != STAGE_OK ? rc : rc_of(launch_gated_ffn_bwd(type_of(dtype), a, d->workspace, (hipStream_t)stream));
+}
+
+}  // extern "C"
+
 // ------------------------------------------------------------------ gradient norm
 static int check_sizes(const int64_t* sizes, int n) {
   if (n < 0) return set_error(STAGE_E_CONFIG, "%d tensors", n);

@@ -109,3 +109,28 @@ def test_attention_window_refusals():
     refused(conf, B.dapple_attention_window_workspace, B.DTYPE_BF16, B.attention_window_desc(**dict(ok, d=4)))
     for dt in (B.DTYPE_F32, B.DTYPE_BF16):
         assert B.dapple_attention_window_workspace(dt, B.attention_window_desc(**ok)) >= 4 * 4 * 100
+
+
+def test_gated_ffn_refusals():
+    ok = dict(x=P, w_in=P, b_in=P, w_out=P, b_out=P, gu=P, h=P, y=P, dy=P, dgu=P, dx=P, dw_in=P, db_in=P, dw_out=P, db_out=P, workspace=P,
+              T=10, H=64, F=128)
+    null, conf = B.STAGE_E_NULL, B.STAGE_E_CONFIG
+    both = [(null, dict(x=None)), (null, dict(w_in=None)), (null, dict(w_out=None)), (null, dict(h=None)), (conf, dict(T=0)), (conf, dict(H=0)),
+            (conf, dict(F=0)), (conf, dict(H=68)), (conf, dict(F=132)), (conf, dict(act=2)), (conf, dict(ldx=56)), (conf, dict(ldy=68)),
+            (conf, dict(lddx=-64)), (conf, dict(T=1 << 22)), (conf, dict(H=1 << 16, F=1 << 14)), (conf, dict(T=1 << 20, ldx=1 << 10)),
+            (conf, dict(w_out=P + 8)), (conf, dict(h=P + 8)), (conf, dict(gu=P + 4))]
+    for code, change in both:
+        for f in (B.dapple_gated_ffn_fwd, B.dapple_gated_ffn_bwd):
+            refused(code, f, B.DTYPE_BF16, B.gated_ffn_desc(**dict(ok, **change)))
+    refused(null, B.dapple_gated_ffn_fwd, B.DTYPE_F32, B.gated_ffn_desc(**dict(ok, y=None)))
+    refused(conf, B.dapple_gated_ffn_fwd, B.DTYPE_F32, B.gated_ffn_desc(**dict(ok, H=66)))
+    refused(conf, B.dapple_gated_ffn_fwd, B.DTYPE_F32, B.gated_ffn_desc(**dict(ok, x=P + 8)))
+    refused(conf, B.dapple_gated_ffn_fwd, 3, B.gated_ffn_desc(**ok))
+    for change in (dict(dy=None), dict(gu=None), dict(dgu=None), dict(workspace=None)):
+        refused(null, B.dapple_gated_ffn_bwd, B.DTYPE_F32, B.gated_ffn_desc(**dict(ok, **change)))
+    for change in (dict(dw_in=None), dict(dw_out=None), dict(dw_in=None, dw_out=None), dict(workspace=P + 4), dict(db_in=P + 4), dict(dy=P + 4),
+                   dict(dgu=P + 8), dict(dw_in=P + 8), dict(dx=P + 8)):
+        refused(conf, B.dapple_gated_ffn_bwd, B.DTYPE_F32, B.gated_ffn_desc(**dict(ok, **change)))
+    refused(conf, B.dapple_gated_ffn_workspace, B.DTYPE_BF16, B.gated_ffn_desc(**dict(ok, F=12)))
+    for dt in (B.DTYPE_F32, B.DTYPE_BF16):
+        assert B.dapple_gated_ffn_workspace(dt, B.gated_ffn_desc(**ok)) > 0
