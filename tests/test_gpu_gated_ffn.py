@@ -120,7 +120,8 @@ class Case:
 
 
 SHAPES = [(1, 8, 8), (5, 64, 128), (16, 128, 256), (33, 72, 40), (130, 64, 200), (300, 256, 512), (1000, 96, 1000), (1030, 128, 1544),
-          (2049, 128, 264), (8200, 64, 1544), (8200, 72, 1544), (700, 1096, 96)]
+          (2049, 128, 264), (8200, 64, 1544), (8200, 72, 1544), (700, 1096, 96),
+          (32, 1032, 520), (31, 264, 2056), (17, 2048, 40)]
 
 
 @pytest.mark.parametrize("dtype", [F32, BF])
