@@ -32,12 +32,12 @@ __device__ __forceinline__ int aswz(int r) {
 // registers, one block ahead, every block waited for memory: a block's arithmetic is about 0.6 us, a request takes
 // longer.)  1 KiB per wave instruction in lane order, so the swizzle is applied to WHICH chunk a lane fetches; rows
 // past the end lie beyond the buffer's record count and read as zero, columns past d get an offset out of range.
-// A wave owns PER consecutive instructions of one of the two matrices.
+// A wave owns PER consecutive instructions of one of the two matrices.  ROWS: of a block.
 typedef int i32x4 __attribute__((ext_vector_type(4)));
-template <int D, int NW, int NS_, bool STATS>
+template <int D, int NW, int NS_, bool STATS, int ROWS = 64>
 struct Ring {
-  static constexpr int NS = NS_, IPM = D / 8, PER = 2 * IPM / NW;          // instructions per matrix and block; per wave
-  static constexpr int Y_OFF = 64 * D * 2, S_OFF = 2 * Y_OFF;              // X, Y, then rows of 64 fp32 (STATS)
+  static constexpr int NS = NS_, IPM = D * ROWS / 512, PER = 2 * IPM / NW; // instructions per matrix and block; per wave
+  static constexpr int Y_OFF = ROWS * D * 2, S_OFF = 2 * Y_OFF;            // X, Y, then rows of 64 fp32 (STATS)
   static constexpr int SROWS = NW > 4 ? NW : 4, STAGE = S_OFF + (STATS ? SROWS * 256 : 0), BYTES = NS * STAGE;
   static constexpr int SPW = STATS ? SROWS / NW : 0;   // rows of the statistics per wave
   static constexpr int BIAS = 3072, LOADS = PER + SPW;
@@ -57,7 +57,7 @@ struct Ring {
       voff[j] = c * 8 < d ? (r * ld + c * 8) * 2 + BIAS - (j % 4) * 1024 : (int)0x80000000;
     }
     set(rs, (uint64_t)g - BIAS);
-    step = 64 * ld * 2;
+    step = ROWS * ld * 2;
     left = left0 = ((s - 1) * ld + d) * 2;
     base0 = (uint64_t)g - BIAS;
     m0w = __builtin_amdgcn_readfirstlane(wave * PER * 1024);
@@ -113,8 +113,8 @@ struct Ring {
           :
           : "s"(ms), "v"(off), "s"(st[i])
           : "memory", "m0");
-      set(st[i], (((uint64_t)(uint32_t)st[i][1] << 32) | (uint32_t)st[i][0]) + 256);
-      sleft[i] -= 256;
+      set(st[i], (((uint64_t)(uint32_t)st[i][1] << 32) | (uint32_t)st[i][0]) + 4 * ROWS);
+      sleft[i] -= 4 * ROWS;
     }
     set(rs, (((uint64_t)(uint32_t)rs[1] << 32) | (uint32_t)rs[0]) + (uint64_t)step);
     left -= step;
@@ -135,8 +135,8 @@ struct Ring {
     left = left0 - block * step;
 #pragma unroll
     for (int i = 0; i < SPW; ++i) {
-      set(st[i], stat0[i] + (uint64_t)(stat_bytes + block * 256L));
-      sleft[i] = stat0[i] ? s * 4 - block * 256 : 0;
+      set(st[i], stat0[i] + (uint64_t)(stat_bytes + block * (4L * ROWS)));
+      sleft[i] = stat0[i] ? s * 4 - block * (4 * ROWS) : 0;
     }
   }
   // what is requested from here on reads nothing

@@ -55,13 +55,32 @@ struct KeyWalk {
   }
   __device__ __forceinline__ int block(int t) const { return t < first ? t : lo + t - first; }
 };
-// What the queries qa .. qb (valid rows) see of keys k0 .. k1: nothing, all, or part
-enum Seen { NONE, PART, ALL };
-__device__ __forceinline__ Seen seen_keys(const AttnWinArgs& a, int qa, int qb, int k0, int k1, int len) {
-  if (k0 >= key_hi(a, qb, len) || (k1 < key_lo(a, qa) && k0 >= a.S)) return NONE;
-  return k1 < key_hi(a, qa, len) && (k0 >= key_lo(a, qb) || k1 < a.S) ? ALL : PART;
+// whether a wave's rows, whose runs begin at lo_min and end at hi_max, see any of keys k0 .. k1
+__device__ __forceinline__ bool any_seen(const AttnWinArgs& a, int k0, int k1, int lo_min, int hi_max) {
+  return k0 < hi_max && (k1 >= lo_min || k0 < a.S);
 }
 __device__ __forceinline__ bool sees(const AttnWinArgs& a, int j, int lo, int hi) { return j < hi && (j >= lo || j < a.S); }
+
+// x[v] = hidden where a lane's row does not see element v of a 32-row accumulator block that begins at row r0 of the other side:
+// rows r0 + 8 (v >> 2) + 4 h + (v & 3), the row's run [lo, hi), and [0, S) besides.  In an instruction or two per bound: the bounds
+// are taken relative to the lane's first row, and one that lies outside the block for all rows of the wave is not compared
+// (below: some row's run begins inside; above: some row's ends inside).
+template <bool SINKS>
+__device__ __forceinline__ void hide(float (&x)[16], float hidden, int r0, int h, int lo, int hi, int S, bool below, bool above) {
+  const int l = lo - r0 - 4 * h, u = hi - r0 - 4 * h, s = S - r0 - 4 * h;
+  if (above) {
+#pragma unroll
+    for (int v = 0; v < 16; ++v) x[v] = 8 * (v >> 2) + (v & 3) < u ? x[v] : hidden;
+  }
+  if (!below) return;
+  if (SINKS && S > r0) {
+#pragma unroll
+    for (int v = 0; v < 16; ++v) x[v] = 8 * (v >> 2) + (v & 3) >= l || 8 * (v >> 2) + (v & 3) < s ? x[v] : hidden;
+  } else {
+#pragma unroll
+    for (int v = 0; v < 16; ++v) x[v] = 8 * (v >> 2) + (v & 3) >= l ? x[v] : hidden;
+  }
+}
 
 // A workgroup of the dk, dv launch: KT keys of a key head, and a part of their walk over the sharing heads' query blocks
 struct KeyTask {
@@ -112,7 +131,7 @@ __device__ __forceinline__ void store_rows(unsigned char* sm, int wave, const f3
 
 // NW: waves per workgroup (4, or 2 where the grid is small), each with 32 query rows
 template <int D, int NW>
-__global__ __launch_bounds__(64 * NW, 2) void attn_win_fwd(AttnWinArgs a, float scale2) {
+__global__ __launch_bounds__(64 * NW, D <= 64 ? 3 : 2) void attn_win_fwd(AttnWinArgs a, float scale2) {
   constexpr int NKK = D / 16, NDB = D / 32;
   typedef WinRing<D, NW, false> R;
   extern __shared__ __attribute__((aligned(1024))) unsigned char asm_[];
@@ -129,13 +148,13 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_win_fwd(AttnWinArgs a, float 
   const bool qok = qrow < len;
   const KeyWalk walk(a, q0, min(q0 + 32 * NW, len) - 1, len, 64);
   const int lo = key_lo(a, qrow), hi = qok ? key_hi(a, qrow, len) : 0;
-  const int qb = min(row0 + 32, len) - 1;
+  const int qb = min(row0 + 32, len) - 1;   // the wave's last row; the ends of its rows' runs
+  const int lo_min = key_lo(a, row0), lo_max = key_lo(a, qb), hi_min = row0 + 31 < len ? key_hi(a, row0, len) : 0, hi_max = key_hi(a, qb, len);
   bf16x8 qf[NKK];
 #pragma unroll
   for (int kk = 0; kk < NKK; ++kk) qf[kk] = frag_global<true>(Q, qrow, qok, a.ldq, kk, lane, d);
   R ring;
   ring.init(wave < NW / 2 ? K : V, wave < NW / 2 ? a.ldk : a.ldv, len, d, wave, lane, [](int) { return (const float*)nullptr; });
-  __builtin_amdgcn_s_waitcnt(0x0F70);   // the query fragments are here: the counts below are the ring's alone
   int asked = 0;
   auto ask = [&](int stage) __attribute__((always_inline)) {
     if (asked == walk.first) ring.seek(walk.lo, len, 0, 0);
@@ -145,6 +164,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_win_fwd(AttnWinArgs a, float 
   };
 #pragma unroll
   for (int t = 0; t < R::NS - 1; ++t) ask(t);
+  __builtin_amdgcn_s_waitcnt(0x0F70);   // (once, with the ring's first blocks: below, the counts are the ring's alone)
 
   float m = -3e38f, l = 0.f;   // (finite: a row that has seen nothing yet keeps m - m = 0)
   f32x16 o[NDB];  // rows d = 32 dblk + 8 blk + 4 h + e, column = the lane's query
@@ -159,9 +179,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_win_fwd(AttnWinArgs a, float 
     stage = stage + 1 == R::NS ? 0 : stage + 1;
     const int k0 = walk.block(t) * 64;
     if (row0 >= len) continue;
-    Seen see = seen_keys(a, row0, qb, k0, k0 + 63, len);
-    if (see == NONE) continue;
-    if (row0 + 31 >= len) see = PART;
+    if (!any_seen(a, k0, k0 + 63, lo_min, hi_max)) continue;
     float p[2][16];
     float mx = -INFINITY;
     // (all LDS reads of a phase before its first MFMA: see attn_fwd_mfma)
@@ -187,13 +205,8 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_win_fwd(AttnWinArgs a, float 
 #pragma unroll
       for (int v = 0; v < 16; ++v) p[kb2][v] = sa[v];
     }
-    if (see == PART) {
 #pragma unroll
-      for (int kb2 = 0; kb2 < 2; ++kb2)
-#pragma unroll
-        for (int v = 0; v < 16; ++v)
-          if (!sees(a, k0 + kb2 * 32 + 8 * (v >> 2) + 4 * h + (v & 3), lo, hi)) p[kb2][v] = -INFINITY;
-    }
+    for (int kb2 = 0; kb2 < 2; ++kb2) hide<true>(p[kb2], -INFINITY, k0 + kb2 * 32, h, lo, hi, a.S, lo_max > k0 + kb2 * 32, hi_min < k0 + kb2 * 32 + 32);
 #pragma unroll
     for (int kb2 = 0; kb2 < 2; ++kb2)
 #pragma unroll
@@ -247,6 +260,20 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_win_fwd(AttnWinArgs a, float 
   if (qrow < a.s && h == 0) a.lse[((long)bi * a.A + hh) * a.s + qrow] = l > 0.f ? m + log2f(l) : -INFINITY;
 }
 
+// the sums of a part of a walk, in the accumulators' own order
+template <int D, int NW>
+__device__ __forceinline__ void store_part(const AttnWinArgs& a, int slot, int wave, const f32x16* dk, const f32x16* dv, int lane) {
+  float* const P = a.partial + (long)slot * 2 * 32 * NW * D;
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int blk = 0; blk < 4; ++blk) {
+      const int u = (((wave * (D / 32) + db) * 4 + blk) * 64 + lane) * 4;
+      *(f32x4*)(P + u) = f32x4{dk[db][4 * blk], dk[db][4 * blk + 1], dk[db][4 * blk + 2], dk[db][4 * blk + 3]};
+      *(f32x4*)(P + 32 * NW * D + u) = f32x4{dv[db][4 * blk], dv[db][4 * blk + 1], dv[db][4 * blk + 2], dv[db][4 * blk + 3]};
+    }
+}
+
 // dk, dv of 32 keys a wave; query blocks of 64 stream through LDS with their lse and delta
 template <int D, int NW, typename R>
 __device__ __forceinline__ void win_dkdv(const AttnWinArgs& a, unsigned task, float scale2, float scale, unsigned char* sm) {
@@ -267,7 +294,8 @@ __device__ __forceinline__ void win_dkdv(const AttnWinArgs& a, unsigned task, fl
   const int kb = min(row0 + 32, len) - 1;
   const bool sink = a.W && row0 < a.S;
   const int lo_min = sink && !a.causal ? 0 : query_lo(a, row0), lo_max = query_lo(a, kb);
-  const int hi_max = sink ? len : query_hi(a, kb, len), hi_min = query_hi(a, sink ? min(kb, a.S) : row0, len);
+  const int hi_max = sink ? len : query_hi(a, kb, len);
+  const int hi_min = row0 + 31 < len ? query_hi(a, sink ? min(kb, a.S) : row0, len) : 0;
 
   bf16x8 kf[NKK], vf[NKK];
 #pragma unroll
@@ -282,7 +310,6 @@ __device__ __forceinline__ void win_dkdv(const AttnWinArgs& a, unsigned task, fl
   const bool first = wave < NW / 2;
   // (a query beyond the last: zero rows, lse and delta 0, and not visible)
   ring.init(first ? Q : G, first ? a.ldq : a.lddc, len, d, wave, lane, [&](int r) { return r == 0 ? lse : (r == 1 ? delta : nullptr); });
-  __builtin_amdgcn_s_waitcnt(0x0F70);   // the key and value fragments are here: the counts below are the ring's alone
   int asked = w.n0, ahead = w.nq ? w.n0 / w.nq : 0, aq = w.nq ? w.n0 % w.nq : 0;   // the next block to request: head, block
   bool jump = true;
   auto ask = [&](int stage) __attribute__((always_inline)) {
@@ -298,6 +325,7 @@ __device__ __forceinline__ void win_dkdv(const AttnWinArgs& a, unsigned task, fl
   };
 #pragma unroll
   for (int t = 0; t < R::NS - 1; ++t) ask(t);
+  __builtin_amdgcn_s_waitcnt(0x0F70);   // (as in attn_win_fwd)
 
   int stage = 0, qblk = w.nq ? w.n0 % w.nq : 0;
   for (int n = w.n0; n < w.n1; ++n) {
@@ -313,9 +341,10 @@ __device__ __forceinline__ void win_dkdv(const AttnWinArgs& a, unsigned task, fl
     for (int qb2 = 0; qb2 < 2; ++qb2) {
       const int j0 = i0 + qb2 * 32;
       if (j0 >= hi_max || j0 + 31 < lo_min) continue;
-      const bool all = row0 + 31 < len && j0 >= lo_max && j0 + 31 < hi_min;
+      // (all LDS reads of a phase before its first MFMA, see attn_fwd_mfma)
       bf16x8 qf[NKK], gf[NKK], gc[2][NDB], qc[2][NDB];
       f32x4 L4[4], D4[4];
+      f32x16 sa = zero16(), dp = zero16();  // rows: query 32 qb2 + 8 blk + 4 h + e, column: key
 #pragma unroll
       for (int kk = 0; kk < NKK; ++kk) {
         qf[kk] = frag_rows<D>(Qs, qb2 * 32, kk, lane);
@@ -327,7 +356,6 @@ __device__ __forceinline__ void win_dkdv(const AttnWinArgs& a, unsigned task, fl
         D4[blk] = *(const f32x4*)(Ds + qb2 * 32 + 8 * blk + 4 * h);
       }
       __builtin_amdgcn_sched_barrier(0);
-      f32x16 sa = zero16(), dp = zero16();  // rows: query 32 qb2 + 8 blk + 4 h + e, column: key
 #pragma unroll
       for (int kk = 0; kk < NKK; ++kk) {
         sa = MFMA(qf[kk], kf[kk], sa);
@@ -349,13 +377,8 @@ __device__ __forceinline__ void win_dkdv(const AttnWinArgs& a, unsigned task, fl
           p[4 * blk + e] = __builtin_amdgcn_exp2f(fmaf(sa[4 * blk + e], scale2, -L4[blk][e]));
           ds[4 * blk + e] = (dp[4 * blk + e] - D4[blk][e]) * p[4 * blk + e];
         }
-      if (!all) {
-#pragma unroll
-        for (int v = 0; v < 16; ++v) {
-          const int i = j0 + 8 * (v >> 2) + 4 * h + (v & 3);
-          if (!(i >= lo && i < hi)) p[v] = ds[v] = 0.f;
-        }
-      }
+      hide<false>(p, 0.f, j0, h, lo, hi, 0, lo_max > j0, hi_min < j0 + 32);
+      hide<false>(ds, 0.f, j0, h, lo, hi, 0, lo_max > j0, hi_min < j0 + 32);
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks) {
         const bf16x8 pf = acc_to_operand(p, ks), dsf = acc_to_operand(ds, ks);
@@ -368,16 +391,8 @@ __device__ __forceinline__ void win_dkdv(const AttnWinArgs& a, unsigned task, fl
     }
   }
   __builtin_amdgcn_s_waitcnt(0x0F70);
-  if (w.slot >= 0) {   // sums of a part, in the accumulators' own order
-    float* const P = a.partial + (long)w.slot * 2 * 32 * NW * D;
-#pragma unroll
-    for (int db = 0; db < NDB; ++db)
-#pragma unroll
-      for (int blk = 0; blk < 4; ++blk) {
-        const int u = (((wave * NDB + db) * 4 + blk) * 64 + lane) * 4;
-        *(f32x4*)(P + u) = f32x4{dk[db][4 * blk], dk[db][4 * blk + 1], dk[db][4 * blk + 2], dk[db][4 * blk + 3]};
-        *(f32x4*)(P + 32 * NW * D + u) = f32x4{dv[db][4 * blk], dv[db][4 * blk + 1], dv[db][4 * blk + 2], dv[db][4 * blk + 3]};
-      }
+  if (w.slot >= 0) {
+    store_part<D, NW>(a, w.slot, wave, dk, dv, lane);
     return;
   }
   __syncthreads();
@@ -402,7 +417,8 @@ __device__ __forceinline__ void win_dq(const AttnWinArgs& a, unsigned id, float 
   const bool qok = qrow < len;
   const KeyWalk walk(a, q0, min(q0 + 32 * NW, len) - 1, len, 64);
   const int lo = key_lo(a, qrow), hi = qok ? key_hi(a, qrow, len) : 0;
-  const int qb = min(row0 + 32, len) - 1;
+  const int qb = min(row0 + 32, len) - 1;   // the wave's last row; the ends of its rows' runs
+  const int lo_min = key_lo(a, row0), lo_max = key_lo(a, qb), hi_min = row0 + 31 < len ? key_hi(a, row0, len) : 0, hi_max = key_hi(a, qb, len);
   const long st = ((long)bi * a.A + hh) * a.s + qrow;
   const float Lq = qok ? a.lse[st] : 0.f, Dq = qok ? a.delta[st] : 0.f;
   bf16x8 qf[NKK], gf[NKK];
@@ -416,7 +432,6 @@ __device__ __forceinline__ void win_dq(const AttnWinArgs& a, unsigned id, float 
   for (int db = 0; db < NDB; ++db) dq[db] = zero16();
   R ring;
   ring.init(wave < NW / 2 ? K : V, wave < NW / 2 ? a.ldk : a.ldv, len, d, wave, lane, [](int) { return (const float*)nullptr; });   // (the statistics' loads read nothing)
-  __builtin_amdgcn_s_waitcnt(0x0F70);
   int asked = 0;
   auto ask = [&](int stage) __attribute__((always_inline)) {
     if (asked == walk.first) ring.seek(walk.lo, len, 0, 0);
@@ -426,6 +441,7 @@ __device__ __forceinline__ void win_dq(const AttnWinArgs& a, unsigned id, float 
   };
 #pragma unroll
   for (int t = 0; t < R::NS - 1; ++t) ask(t);
+  __builtin_amdgcn_s_waitcnt(0x0F70);   // (as in attn_win_fwd)
 
   int stage = 0;
   for (int t = 0; t < walk.n; ++t) {
@@ -438,40 +454,44 @@ __device__ __forceinline__ void win_dq(const AttnWinArgs& a, unsigned id, float 
 #pragma unroll
     for (int kb2 = 0; kb2 < 2; ++kb2) {
       const int j0 = k0 + kb2 * 32;
-      Seen see = seen_keys(a, row0, qb, j0, j0 + 31, len);
-      if (see == NONE) continue;
-      if (row0 + 31 >= len) see = PART;
-      bf16x8 kr[NKK], vr[NKK], kc[2][NDB];
-#pragma unroll
-      for (int kk = 0; kk < NKK; ++kk) {
-        kr[kk] = frag_rows<D>(Ks, kb2 * 32, kk, lane);
-        vr[kk] = frag_rows<D>(Vs, kb2 * 32, kk, lane);
-      }
-      __builtin_amdgcn_sched_barrier(0);
+      if (!any_seen(a, j0, j0 + 31, lo_min, hi_max)) continue;
+      // (all LDS reads of a phase before its first MFMA, see attn_fwd_mfma; D = 128 in halves, for registers)
+      constexpr int KB = D == 128 ? NKK / 2 : NKK, KS = D == 128 ? 1 : 2;
+      bf16x8 kr[KB], vr[KB], kc[KS][NDB];
       f32x16 sa = zero16(), dp = zero16();  // rows: key 32 kb2 + 8 blk + 4 h + e, column: query
 #pragma unroll
-      for (int kk = 0; kk < NKK; ++kk) {
-        sa = MFMA(kr[kk], qf[kk], sa);
-        dp = MFMA(vr[kk], gf[kk], dp);
+      for (int k8 = 0; k8 < NKK; k8 += KB) {
+#pragma unroll
+        for (int kk = 0; kk < KB; ++kk) {
+          kr[kk] = frag_rows<D>(Ks, kb2 * 32, k8 + kk, lane);
+          vr[kk] = frag_rows<D>(Vs, kb2 * 32, k8 + kk, lane);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int kk = 0; kk < KB; ++kk) {
+          sa = MFMA(kr[kk], qf[k8 + kk], sa);
+          dp = MFMA(vr[kk], gf[k8 + kk], dp);
+        }
+        if (D == 128) __builtin_amdgcn_sched_barrier(0);
       }
 #pragma unroll
-      for (int ks = 0; ks < 2; ++ks)
+      for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
         for (int db = 0; db < NDB; ++db) kc[ks][db] = frag_cols<D>(Ks, db * 32, kb2 * 32 + ks * 16, lane);
       __builtin_amdgcn_sched_barrier(0);
       float ds[16];
 #pragma unroll
       for (int v = 0; v < 16; ++v) ds[v] = __builtin_amdgcn_exp2f(fmaf(sa[v], scale2, -Lq)) * (dp[v] - Dq);
-      if (see == PART) {
-#pragma unroll
-        for (int v = 0; v < 16; ++v)
-          if (!sees(a, j0 + 8 * (v >> 2) + 4 * h + (v & 3), lo, hi)) ds[v] = 0.f;
-      }
+      hide<true>(ds, 0.f, j0, h, lo, hi, a.S, lo_max > j0, hi_min < j0 + 32);
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks) {
         const bf16x8 dsf = acc_to_operand(ds, ks);
+        if (ks >= KS) {
 #pragma unroll
-        for (int db = 0; db < NDB; ++db) dq[db] = MFMA(kc[ks][db], dsf, dq[db]);
+          for (int db = 0; db < NDB; ++db) kc[0][db] = frag_cols<D>(Ks, db * 32, kb2 * 32 + ks * 16, lane);
+        }
+#pragma unroll
+        for (int db = 0; db < NDB; ++db) dq[db] = MFMA(kc[ks < KS ? ks : 0][db], dsf, dq[db]);
       }
     }
   }
@@ -484,14 +504,270 @@ __device__ __forceinline__ void win_dq(const AttnWinArgs& a, unsigned id, float 
   store_rows<D>(sm, wave, dq, scale, (bf16*)a.dq + (r0 + row0) * a.lddq + hh * d, nullptr, a.lddq, a.s - row0, d, lane);
 }
 
-// Both kinds of workgroups in one launch, dk and dv first: they share a compute unit and fill each other's waits (as in attention.hip)
+// Both kinds of workgroups in one launch, dk and dv first: they share a compute unit and fill each other's waits (as in attention.hip).
+// D <= 64
 template <int D, int NW>
-__global__ __launch_bounds__(64 * NW, D <= 64 ? 2 : 1) void attn_win_bwd(AttnWinArgs a, float scale2, float scale) {
+__global__ __launch_bounds__(64 * NW, 2) void attn_win_bwd(AttnWinArgs a, float scale2, float scale) {
   extern __shared__ __attribute__((aligned(1024))) unsigned char asm_[];
   typedef WinRing<D, NW, true> R;
   const unsigned nk = a.plan.key_tasks;
   if (blockIdx.x < nk) win_dkdv<D, NW, R>(a, spread(blockIdx.x, nk), scale2, scale, asm_);
   else win_dq<D, NW, R>(a, spread(blockIdx.x - nk, gridDim.x - nk), scale2, scale, asm_);
+}
+
+// dk and dv of 128 keys at D = 128.  A wave that does all four products holds 128 registers of sums, 64 of keys and values and 32 of
+// the products before the exponentials, and is alone on its SIMD: its chain of MFMA -> exponentials -> MFMA waits for itself.  So the
+// chain is cut in two: waves 0-3 own 32 keys each, make S and dP of 32 queries (a step) and leave P and dS in LDS, as the operands
+// they are; waves 4-7, a step behind, hold the sums of the same keys and add dctx^T P and Q^T dS to them.  One of each on a SIMD.  Waves
+// 0-3 make the next step's S and dP between the exponentials of the current one.  Either kind reads its next fragments behind the
+// MFMAs that used the last ones.
+// Waves 0-3 do step i between barriers i and i + 1, waves 4-7 between i + 1 and i + 2.  Blocks of 32 queries lie in a ring of seven:
+// block i + 2 has landed at barrier i, behind which its first fragments are read, and there block i + 5 is requested, into the place of
+// block i - 2, whose last fragments were read before.
+// 8192 rows, 16 heads on 4, window 1024: with waves that do all four products, one to a SIMD, dk, dv and dq took 432 us with the joining of
+// parts, 343 so.  A step takes 2100 clocks, 1024 of them MFMAs on each SIMD; LDS is asked for 208 KB in it (1660 clocks at 128 bytes).
+// A lane's LDS addresses of fragments (frag_rows, frag_cols) in a block of 64 x 128: all that depends on the lane, kept in a few
+// registers; the block's place is added once a step, rows and the matrix are an instruction's immediate offset.
+struct RowsAt {
+  unsigned a[8];
+  __device__ __forceinline__ explicit RowsAt(int lane) {
+    const int r = lane & 31;
+#pragma unroll
+    for (int kk = 0; kk < 8; ++kk) a[kk] = r * 256 + (((kk * 2 + (lane >> 5)) ^ aswz<128>(r)) << 4);
+  }
+  // AT: rows' and the matrix's bytes
+  template <int AT>
+  __device__ __forceinline__ bf16x8 get(const unsigned char* sm, unsigned block, int kk) const {
+    return *(const bf16x8*)(sm + (a[kk] + block) + AT);
+  }
+};
+struct ColsAt {
+  unsigned a[4][2];
+  __device__ __forceinline__ explicit ColsAt(int lane) {
+    const int i16 = lane & 15, r = 4 * (lane >> 5) + (i16 >> 2), c = 16 * ((lane >> 4) & 1) + 4 * (i16 & 3);
+#pragma unroll
+    for (int db = 0; db < 4; ++db)
+#pragma unroll
+      for (int k = 0; k < 2; ++k) a[db][k] = (r + 8 * k) * 256 + ((((db * 32 + c) >> 3) ^ aswz<128>(r + 8 * k)) << 4) + (c & 7) * 2;
+  }
+  template <int AT>
+  __device__ __forceinline__ bf16x8 get(const unsigned char* sm, unsigned block, int db) const {
+    return join8(lds_read_tr16((const bf16*)(sm + (a[db][0] + block) + AT)), lds_read_tr16((const bf16*)(sm + (a[db][1] + block) + AT)));
+  }
+};
+constexpr int PAIR_X = 4 * 4 * 1024;   // P and dS of a step: per wave two operands each of 16 bytes a lane
+typedef Ring<128, 8, 7, true, 32> PairRing;
+typedef Ring<128, 8, 4, true> PairDqRing;
+constexpr int PAIR_BYTES = PairRing::BYTES + 2 * PAIR_X;
+static_assert(PAIR_BYTES <= 160 * 1024 && PairDqRing::BYTES <= PAIR_BYTES && 8 * OutTile<2>::BYTES <= PairRing::BYTES,
+              "LDS of a compute unit; the output's staging lies where the ring was");
+
+__device__ __forceinline__ void win_dkdv_pair(const AttnWinArgs& a, unsigned task, float scale2, float scale, unsigned char* sm) {
+  constexpr int D = 128, NKK = 8, NDB = 4;
+  typedef PairRing R;
+  const KeyTask w(a, task, 128, 32);
+  if (!w.run) return;
+  const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), own = wave & 3;   // which 32 of the keys
+  const int len = w.len, d = a.d, h0 = w.kv * (a.A / a.Ak);
+  const long r0 = (long)w.bi * a.s;
+  const bf16 *Q = (const bf16*)a.q + r0 * a.ldq + h0 * d, *G = (const bf16*)a.dctx + r0 * a.lddc + h0 * d;
+  const float *lse = a.lse + ((long)w.bi * a.A + h0) * a.s, *delta = a.delta + ((long)w.bi * a.A + h0) * a.s;
+  const int row0 = w.k0 + own * 32, krow = row0 + (lane & 31);
+  const bool kok = krow < len;
+  const int kb = min(row0 + 32, len) - 1;   // (as in win_dkdv)
+  const bool sink = a.W && row0 < a.S;
+  const int lo_min = sink && !a.causal ? 0 : query_lo(a, row0), lo_max = query_lo(a, kb);
+  const int hi_max = row0 < len ? (sink ? len : query_hi(a, kb, len)) : 0;
+  const int hi_min = row0 + 31 < len ? query_hi(a, sink ? min(kb, a.S) : row0, len) : 0;
+  unsigned char* const X = sm + R::BYTES + own * 4096 + lane * 16;
+
+  R ring;
+  const bool first = wave < 4;
+  ring.init(first ? Q : G, first ? a.ldq : a.lddc, len, d, wave, lane, [&](int r) { return r == 0 ? lse : (r == 1 ? delta : nullptr); });
+  int asked = w.n0, ahead = w.nq ? w.n0 / w.nq : 0, aq = w.nq ? w.n0 % w.nq : 0, slot = 0;   // the next block to request: head, block
+  bool jump = true;
+  auto ask = [&]() __attribute__((always_inline)) {
+    if (jump) ring.seek(w.qlo + aq, len, ahead * d * 2, (long)ahead * a.s * 4);
+    if (asked >= w.n1) ring.stop();
+    ring.request(slot, lane);
+    slot = slot == R::NS - 1 ? 0 : slot + 1;
+    ++asked;
+    jump = ++aq == w.nq;
+    if (jump) {
+      aq = 0;
+      ++ahead;
+    }
+  };
+  auto barrier = []() __attribute__((always_inline)) { R::wait<-3 * R::LOADS>(); };   // all but the two newest blocks have landed
+  int stage = 0;
+  if (first) {
+    int qblk = w.nq ? w.n0 % w.nq : 0;
+    const bf16 *K = (const bf16*)a.k + r0 * a.ldk + w.kv * d, *V = (const bf16*)a.v + r0 * a.ldv + w.kv * d;
+    const int lo = query_lo(a, krow), hi = kok ? query_hi(a, krow, len) : 0;
+    bf16x8 kf[NKK], vf[NKK], qf[4], gf[4];   // (qf, gf: four k-steps' fragments, read four ahead of their use)
+#pragma unroll
+    for (int kk = 0; kk < NKK; ++kk) {
+      kf[kk] = frag_global<true>(K, krow, kok, a.ldk, kk, lane, d);
+      vf[kk] = frag_global<true>(V, krow, kok, a.ldv, kk, lane, d);
+    }
+    for (int t = 0; t < R::NS - 2; ++t) ask();
+    __builtin_amdgcn_s_waitcnt(0x0F70);   // (as in attn_win_fwd)
+    barrier();
+    __builtin_amdgcn_s_setprio(2);   // (their products first: the exponentials then run beside the other wave's)
+    const RowsAt fr(lane);
+    // k-step kk of the fragments' block at `at` (kk < 8), or kk - 8 of the one at `next`
+    auto fetch = [&](int kk, unsigned at, unsigned next) __attribute__((always_inline)) {
+      qf[kk & 3] = fr.get<0>(sm, kk < 8 ? at : next, kk & 7);
+      gf[kk & 3] = fr.get<R::Y_OFF>(sm, kk < 8 ? at : next, kk & 7);
+    };
+    auto slot_after = [](int t) { return t == R::NS - 1 ? 0 : t + 1; };
+    // sa, dp: S and dP of the current step (rows: query 8 blk + 4 h + e of its block, column: key); sn, dn: of the next one, made
+    // meanwhile: two MFMAs and two elements' exponentials by turns
+    enum { HIDDEN, WHOLE, PART };
+    auto step = [&](auto MODE, const f32x16& sa, const f32x16& dp, f32x16& sn, f32x16& dn, unsigned cur, unsigned at, unsigned next, unsigned char* x,
+                    int j0) __attribute__((always_inline)) {
+      constexpr int mode = decltype(MODE)::value;
+      const float *Ls = (const float*)(sm + cur + R::S_OFF) + 4 * h, *Ds = Ls + 64;
+      const int l = lo - j0 - 4 * h, u = hi - j0 - 4 * h;
+      f32x4 L4[4], D4[4];
+      if constexpr (mode != HIDDEN) {
+#pragma unroll
+        for (int blk = 0; blk < 4; ++blk) {
+          L4[blk] = *(const f32x4*)(Ls + 8 * blk);
+          D4[blk] = *(const f32x4*)(Ds + 8 * blk);
+        }
+      }
+      sn = dn = zero16();
+      float p[16], ds[16];
+#pragma unroll
+      for (int kk = 0; kk < NKK; ++kk) {
+        sn = MFMA(qf[kk & 3], kf[kk], sn);
+        dn = MFMA(gf[kk & 3], vf[kk], dn);
+        fetch(kk + 4, at, next);
+        if constexpr (mode != HIDDEN) {
+#pragma unroll
+          for (int v = 2 * kk; v < 2 * kk + 2; ++v) {
+            p[v] = __builtin_amdgcn_exp2f(fmaf(sa[v], scale2, -L4[v >> 2][v & 3]));
+            ds[v] = (dp[v] - D4[v >> 2][v & 3]) * p[v];
+            if constexpr (mode == PART) {
+              const bool in = 8 * (v >> 2) + (v & 3) >= l && 8 * (v >> 2) + (v & 3) < u;
+              p[v] = in ? p[v] : 0.f;
+              ds[v] = in ? ds[v] : 0.f;
+            }
+          }
+        }
+        if (kk % 4 == 3) {
+          const int ks = kk / 4;
+          if constexpr (mode == HIDDEN) {   // (zeros: a branch round the other waves' products would move their sums between registers)
+            *(f32x4*)(x + ks * 1024) = *(f32x4*)(x + (2 + ks) * 1024) = f32x4{0.f, 0.f, 0.f, 0.f};
+          } else {
+            *(bf16x8*)(x + ks * 1024) = acc_to_operand(p, ks);
+            *(bf16x8*)(x + (2 + ks) * 1024) = acc_to_operand(ds, ks);
+          }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    };
+    typedef std::integral_constant<int, HIDDEN> Hidden;
+    typedef std::integral_constant<int, WHOLE> Whole;
+    typedef std::integral_constant<int, PART> Part;
+    f32x16 s0, d0, s1, d1;
+    int cur = 0, at = 1;   // places of the current step's block and the next one's
+    {
+#pragma unroll
+      for (int kk = 0; kk < 4; ++kk) fetch(kk, 0, 0);
+      s0 = d0 = zero16();
+#pragma unroll
+      for (int kk = 0; kk < NKK; ++kk) {
+        s0 = MFMA(qf[kk & 3], kf[kk], s0);
+        d0 = MFMA(gf[kk & 3], vf[kk], d0);
+        fetch(kk + 4, 0, R::STAGE);
+      }
+    }
+    int n = w.n0;
+    auto one = [&](const f32x16& sa, const f32x16& dp, f32x16& sn, f32x16& dn) __attribute__((always_inline)) {
+      const int after = slot_after(at), j0 = (w.qlo + qblk) * 32;
+      qblk = qblk + 1 == w.nq ? 0 : qblk + 1;
+      unsigned char* const x = X + (n & 1) * PAIR_X;
+      barrier();
+      ask();
+      const unsigned c = cur * R::STAGE, f = at * R::STAGE, g = after * R::STAGE;
+      if (j0 >= hi_max || j0 + 31 < lo_min) step(Hidden{}, sa, dp, sn, dn, c, f, g, x, j0);   // none of the wave's keys is seen
+      else if (lo_max > j0 || hi_min < j0 + 32) step(Part{}, sa, dp, sn, dn, c, f, g, x, j0);
+      else step(Whole{}, sa, dp, sn, dn, c, f, g, x, j0);
+      cur = at;
+      at = after;
+      return ++n < w.n1;
+    };
+    if (n < w.n1)
+      while (one(s0, d0, s1, d1) && one(s1, d1, s0, d0)) {}
+    barrier();                            // (the last step of waves 4-7)
+    __builtin_amdgcn_s_waitcnt(0x0F70);   // the last requests (they read nothing) before the wave may end
+    __syncthreads();
+    return;
+  }
+  f32x16 dv[NDB], dk[NDB];  // rows d, column = the lane's key
+#pragma unroll
+  for (int db = 0; db < NDB; ++db) dv[db] = dk[db] = zero16();
+  for (int t = 0; t < R::NS - 2; ++t) ask();
+  barrier();
+  const ColsAt fc(lane);
+  bf16x8 gc[NDB], qc[NDB];   // (of 16 queries, read that many MFMAs ahead of their use)
+#pragma unroll
+  for (int db = 0; db < NDB; ++db) {
+    gc[db] = fc.get<R::Y_OFF>(sm, 0, db);
+    qc[db] = fc.get<0>(sm, 0, db);
+  }
+  barrier();   // 0
+  ask();
+  for (int n = w.n0; n < w.n1; ++n) {
+    const unsigned at = stage * R::STAGE;
+    stage = stage == R::NS - 1 ? 0 : stage + 1;
+    const unsigned next = stage * R::STAGE;
+    const unsigned char* const x = X + (n & 1) * PAIR_X;
+    barrier();   // n + 1
+    ask();
+    bf16x8 pf[2], dsf[2];
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+      pf[ks] = *(const bf16x8*)(x + ks * 1024);
+      dsf[ks] = *(const bf16x8*)(x + (2 + ks) * 1024);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+      for (int db = 0; db < NDB; ++db) {
+        dv[db] = MFMA(gc[db], pf[ks], dv[db]);
+        dk[db] = MFMA(qc[db], dsf[ks], dk[db]);
+        // the step's second 16 queries, the next step's first
+        gc[db] = ks ? fc.get<R::Y_OFF>(sm, next, db) : fc.get<R::Y_OFF + 16 * 256>(sm, at, db);
+        qc[db] = ks ? fc.get<0>(sm, next, db) : fc.get<16 * 256>(sm, at, db);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+  }
+  __builtin_amdgcn_s_waitcnt(0x0F70);
+  __syncthreads();
+  if (w.slot >= 0) {
+    store_part<D, 4>(a, w.slot, own, dk, dv, lane);
+    return;
+  }
+  store_rows<D>(sm, own, dk, scale, (bf16*)a.dk + (r0 + row0) * a.lddk + w.kv * d, nullptr, a.lddk, a.s - row0, d, lane);
+  store_rows<D>(sm, own, dv, 1.f, (bf16*)a.dv + (r0 + row0) * a.lddv + w.kv * d, nullptr, a.lddv, a.s - row0, d, lane);
+}
+
+// D = 128: dk and dv, and behind them the workgroups of dq, 256 queries each (none, where those are few: attn_win_dq)
+__global__ __launch_bounds__(512, 2) void attn_win_bwd_pair(AttnWinArgs a, float scale2, float scale) {
+  extern __shared__ __attribute__((aligned(1024))) unsigned char asm_[];
+  const unsigned nk = a.plan.key_tasks;
+  if (blockIdx.x < nk) win_dkdv_pair(a, spread(blockIdx.x, nk), scale2, scale, asm_);
+  else win_dq<128, 8, PairDqRing>(a, spread(blockIdx.x - nk, gridDim.x - nk), scale2, scale, asm_);
+}
+template <int NW>
+__global__ __launch_bounds__(64 * NW, 2) void attn_win_dq(AttnWinArgs a, float scale2, float scale) {
+  extern __shared__ __attribute__((aligned(1024))) unsigned char asm_[];
+  win_dq<128, NW, WinRing<128, NW, true>>(a, spread(blockIdx.x, gridDim.x), scale2, scale, asm_);
 }
 
 // ------------------------------------------------------------------ fp32 (see attention_f32.hip)
@@ -508,6 +784,7 @@ __global__ __launch_bounds__(256) void attn_win_fwd_f32(AttnWinArgs a, float sca
   const long r0 = (long)bi * a.s;
   const float *Q = (const float*)a.q + r0 * a.ldq + hh * d, *K = (const float*)a.k + r0 * a.ldk + kv * d, *V = (const float*)a.v + r0 * a.ldv + kv * d;
   const int q0 = tile * 64, row0 = q0 + wave * 16, qrow = row0 + (lane & 15), qb = min(row0 + 16, len) - 1;
+  const int lo_min = key_lo(a, row0), hi_max = key_hi(a, qb, len);
   const bool qok = qrow < len;
   const KeyWalk walk(a, q0, min(q0 + 64, len) - 1, len, BR);
   const int lo = key_lo(a, qrow), hi = qok ? key_hi(a, qrow, len) : 0;
@@ -531,7 +808,7 @@ __global__ __launch_bounds__(256) void attn_win_fwd_f32(AttnWinArgs a, float sca
     __syncthreads();
     if (n + 1 < walk.n) load(n + 1);
     const int k0 = walk.block(n) * BR;
-    if (row0 >= len || seen_keys(a, row0, qb, k0, k0 + BR - 1, len) == NONE) continue;
+    if (row0 >= len || !any_seen(a, k0, k0 + BR - 1, lo_min, hi_max)) continue;
     f32x4 p[2];
     float mx = -INFINITY;
 #pragma unroll
@@ -598,6 +875,7 @@ __device__ __forceinline__ void win_dq_f32(const AttnWinArgs& a, unsigned id, fl
   const long r0 = (long)bi * a.s;
   const float *K = (const float*)a.k + r0 * a.ldk + kv * d, *V = (const float*)a.v + r0 * a.ldv + kv * d;
   const int q0 = tile * 64, row0 = q0 + wave * 16, qrow = row0 + (lane & 15), qb = min(row0 + 16, len) - 1;
+  const int lo_min = key_lo(a, row0), hi_max = key_hi(a, qb, len);
   const bool qok = qrow < len;
   const KeyWalk walk(a, q0, min(q0 + 64, len) - 1, len, BR);
   const int lo = key_lo(a, qrow), hi = qok ? key_hi(a, qrow, len) : 0;
@@ -626,7 +904,7 @@ __device__ __forceinline__ void win_dq_f32(const AttnWinArgs& a, unsigned id, fl
     if (row0 >= len) continue;
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      if (seen_keys(a, row0, qb, k0 + 16 * t, k0 + 16 * t + 15, len) == NONE) continue;
+      if (!any_seen(a, k0 + 16 * t, k0 + 16 * t + 15, lo_min, hi_max)) continue;
       f32x4 s{0.f, 0.f, 0.f, 0.f}, dp{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int kk = 0; kk < NK; ++kk) {
@@ -859,11 +1137,16 @@ bool attn_win_takes(Dtype dt, const AttnWinArgs& a) {
 // Workgroups of four waves, or of two where four would leave a quarter of the 256 units without one (bf16; as in attention.hip)
 static int fwd_waves(const AttnWinArgs& a) { return (long)((a.s + 127) / 128) * a.b * a.A < 192 ? 2 : 4; }
 static int bwd_waves(const AttnWinArgs& a) { return (long)((a.s + 127) / 128) * a.b * (a.A + a.Ak) < 192 ? 2 : 4; }
+// keys of a workgroup of the backward
+static int key_tile(Dtype dt, const AttnWinArgs& a) { return dt != DT_BF16 ? 64 : a.d > 64 ? 128 : 32 * bwd_waves(a); }
+
+// queries of a block of their walks
+static int walk_block(Dtype dt, const AttnWinArgs& a) { return dt != DT_BF16 ? BR : a.d > 64 ? 32 : 64; }
 
 // How the walks of dk and dv are cut.  Parts of CS blocks: as long as the walk of a tile without sinks where those tiles fill
-// the chip (two to a unit), else as long as two workgroups to a unit leave, eight blocks at least.
+// the chip, else as long as two workgroups to a unit leave, eight blocks at least.
 static void make_plan(Dtype dt, AttnWinArgs& a) {
-  const int kt = dt == DT_BF16 ? 32 * bwd_waves(a) : 64, blk = dt == DT_BF16 ? 64 : BR;
+  const int kt = key_tile(dt, a), blk = walk_block(dt, a);
   WinPlan& p = a.plan;
   const long G = a.A / a.Ak, nb = (a.s + blk - 1) / blk, heads = (long)a.b * a.Ak;
   p.key_tiles = (a.s + kt - 1) / kt;
@@ -872,7 +1155,8 @@ static void make_plan(Dtype dt, AttnWinArgs& a) {
   // the most blocks that a walk without sinks has, per head
   const long reach = !a.W ? nb : std::min(nb, ((a.causal ? 1L : 2L) * (a.W - 1) + kt + blk - 2) / blk + 1);
   const long total = heads * G * (rest * reach + p.sink_tiles * nb), fair = (total + 511) / 512;
-  long steps = heads * rest >= 512 ? G * reach : std::min(G * (rest ? reach : nb), std::max(8L, fair));
+  const long fill = dt == DT_BF16 && a.d > 64 ? 192 : 512;   // tiles that fill the chip: a unit holds one workgroup, or two
+  long steps = heads * rest >= fill ? G * reach : std::min(G * (rest ? reach : nb), std::max(8L, fair));
   p.parts = (int)((G * reach + steps - 1) / steps);
   p.sink_parts = (int)((G * nb + steps - 1) / steps);
   if (!p.sink_tiles) p.sink_parts = 1;
@@ -894,7 +1178,7 @@ static size_t delta_bytes(const AttnWinArgs& a) { return ((size_t)a.b * a.A * a.
 
 int64_t attn_win_workspace(Dtype dt, AttnWinArgs a) {
   make_plan(dt, a);
-  const int kt = dt == DT_BF16 ? 32 * bwd_waves(a) : 64;
+  const int kt = key_tile(dt, a);
   const int width = pick_width(dt, a.d, [](auto D) { return (int)decltype(D)::value; });
   return (int64_t)delta_bytes(a) + (int64_t)a.b * a.Ak * a.plan.slots * 2 * kt * width * 4;
 }
@@ -950,7 +1234,24 @@ hipError_t launch_attn_win_bwd(Dtype dt, AttnWinArgs a, void* workspace, hipStre
       e = hipGetLastError();
       return e != hipSuccess ? e : join(attn_win_join<float, d, 64, 16, BR>, 64);
     }
-    if constexpr (d >= 32) {
+    if constexpr (d == 128) {
+      static const hipError_t rc = allow_lds(attn_win_bwd_pair, PAIR_BYTES);
+      if (rc != hipSuccess) return rc;
+      const long q_tiles = (long)((a.s + 255) / 256) * a.b * a.A;
+      const bool both = q_tiles >= 256;   // (a unit holds one of these workgroups)
+      hipLaunchKernelGGL(attn_win_bwd_pair, dim3((unsigned)(a.plan.key_tasks + (both ? q_tiles : 0))), dim3(512), PAIR_BYTES, st, a, scale2, scale);
+      e = hipGetLastError();
+      if (e == hipSuccess) e = join(attn_win_join<bf16, d, 128, 32, 32>, 128);
+      if (e != hipSuccess || both) return e;
+      auto dq = [&](auto NW) {
+        constexpr int nw = decltype(NW)::value, lds = WinRing<d, nw, true>::BYTES;
+        static const hipError_t rc = allow_lds(attn_win_dq<nw>, lds);
+        if (rc != hipSuccess) return rc;
+        hipLaunchKernelGGL(attn_win_dq<nw>, dim3((unsigned)((long)((a.s + 32 * nw - 1) / (32 * nw)) * a.b * a.A)), dim3(64 * nw), lds, st, a, scale2, scale);
+        return hipGetLastError();
+      };
+      return fwd_waves(a) == 4 ? dq(std::integral_constant<int, 4>{}) : dq(std::integral_constant<int, 2>{});
+    } else if constexpr (d >= 32) {
       auto go = [&](auto NW) {
         constexpr int nw = decltype(NW)::value, lds = WinRing<d, nw, true>::BYTES;
         static const hipError_t rc = allow_lds(attn_win_bwd<d, nw>, lds);

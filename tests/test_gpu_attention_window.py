@@ -121,6 +121,7 @@ CASES = [  # dtype, b, s, A, Ak, d, W, S, causal, lens
     (H, 4, 333, 3, 3, 8, 40, 2, False, [333, 64, 65, 2]), (H, 1, 300, 2, 2, 96, 64, 0, True, None), (H, 1, 260, 5, 5, 40, 300, 7, False, None),
     (H, 16, 517, 8, 8, 64, 50, 4, True, None), (H, 2, 1030, 16, 4, 128, 256, 16, True, None), (H, 9, 140, 16, 16, 128, 1, 3, False, None),
     (H, 2, 385, 4, 4, 32, 64, 200, True, [385, 192]), (H, 1, 2100, 4, 2, 64, 0, 0, True, None), (H, 1, 2100, 2, 1, 64, 300, 1, False, [2099]),
+    (H, 4, 530, 32, 8, 128, 150, 20, True, [530, 1, 300, 511]), (H, 2, 1100, 28, 28, 104, 0, 0, True, None), (H, 3, 700, 32, 4, 72, 64, 0, False, None),
     (F, 1, 1, 1, 1, 16, 0, 0, True, None), (F, 2, 33, 2, 1, 4, 5, 1, True, None), (F, 1, 64, 2, 2, 64, 0, 0, False, None),
     (F, 3, 130, 6, 2, 64, 33, 5, False, [130, 1, 77]), (F, 2, 200, 4, 1, 80, 64, 64, True, [0, 200]), (F, 2, 517, 4, 2, 20, 100, 3, True, None),
     (F, 1, 700, 8, 1, 128, 129, 130, True, [650]), (F, 18, 260, 4, 4, 32, 50, 4, True, None), (F, 2, 333, 3, 3, 36, 40, 100, False, [333, 64]),
