@@ -283,15 +283,16 @@ struct OutTile {
 
 // D: the head block's width (16, 32, 64 or 128; narrower heads are padded with zeros); blocks of 32 rows
 constexpr int BR = 32;
-template <int D>
+// T: threads that move a block
+template <int D, int T = 256>
 struct F32Block {
   // row stride D + 8 floats: the four lane groups of a 4-byte read lie 4 rows = 32 banks (mod 64) apart
-  static constexpr int LD = D + 8, CPR = D / 4, N = BR * CPR / 256 > 0 ? BR * CPR / 256 : 1;
+  static constexpr int LD = D + 8, CPR = D / 4, N = BR * CPR / T > 0 ? BR * CPR / T : 1;
   f32x4 c[N];
   __device__ __forceinline__ void load(const float* g, int ldg, int tid, int rows, int d) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int p = tid + 256 * i, r = p / CPR, k = p % CPR * 4;
+      const int p = tid + T * i, r = p / CPR, k = p % CPR * 4;
       c[i] = f32x4{0.f, 0.f, 0.f, 0.f};
       if (p < BR * CPR && r < rows && k < d) c[i] = *(const f32x4*)(g + (long)r * ldg + k);
     }
@@ -299,7 +300,7 @@ struct F32Block {
   __device__ __forceinline__ void store(float* S, int tid) const {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int p = tid + 256 * i;
+      const int p = tid + T * i;
       if (p < BR * CPR) *(f32x4*)(S + p / CPR * LD + p % CPR * 4) = c[i];
     }
   }

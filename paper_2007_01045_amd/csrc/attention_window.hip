@@ -771,61 +771,88 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_win_dq(AttnWinArgs a, float s
 }
 
 // ------------------------------------------------------------------ fp32 (see attention_f32.hip)
-template <int D>
-__global__ __launch_bounds__(256) void attn_win_fwd_f32(AttnWinArgs a, float scale2) {
+// RG: waves of a group, NG: groups.  A wave is a chain of MFMAs, exponentials and MFMAs, and the tiles of a micro-batch seldom give a SIMD
+// more than one; so two groups share a tile, take the blocks of its walk by turns, and add what they have at the end.  Us forward
+// and backward with one group of four waves, two of four, two of two: 2 x 777 rows, 12 heads of 64 on 6, window 200 111, 110, 101;
+// 2 x 2048 rows, 16 heads, no window 940, 879, 914.
+template <int D, int RG, int NG>
+struct F32Lds {
+  static constexpr int BLK = BR * (D + 8), STAT = 2 * BR;          // floats: a block; the statistics of one
+  static constexpr int FLOATS = NG * (2 * BLK + STAT);
+  // the second group's sums (n floats of a lane; n at most 2 D / 4)
+  static_assert(NG == 1 || 64 * RG * (D / 2) <= FLOATS, "the sums lie where the blocks were");
+};
+template <int D, int RG, int NG>
+__global__ __launch_bounds__(64 * RG * NG) void attn_win_fwd_f32(AttnWinArgs a, float scale2) {
   constexpr int NK = D / 16;
-  __shared__ __attribute__((aligned(16))) float Ks[BR * (D + 8)];
-  __shared__ __attribute__((aligned(16))) float Vs[BR * (D + 8)];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g4 = lane >> 4;
-  const int q_tiles = (a.s + 63) / 64;
+  extern __shared__ __attribute__((aligned(16))) float fsm[];
+  const int tid = threadIdx.x & (64 * RG - 1), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g4 = lane >> 4;
+  const int group = __builtin_amdgcn_readfirstlane(threadIdx.x / (64 * RG));
+  float *const Ks = fsm + group * 2 * F32Lds<D, RG, NG>::BLK, *const Vs = Ks + F32Lds<D, RG, NG>::BLK;
+  const int q_tiles = (a.s + 16 * RG - 1) / (16 * RG);
   const unsigned id = spread(blockIdx.x, gridDim.x);
   const int head = id / q_tiles, tile = q_tiles - 1 - id % q_tiles;
   const int bi = head / a.A, hh = head % a.A, kv = hh / (a.A / a.Ak), len = len_of(a, bi), d = a.d;
   const long r0 = (long)bi * a.s;
   const float *Q = (const float*)a.q + r0 * a.ldq + hh * d, *K = (const float*)a.k + r0 * a.ldk + kv * d, *V = (const float*)a.v + r0 * a.ldv + kv * d;
-  const int q0 = tile * 64, row0 = q0 + wave * 16, qrow = row0 + (lane & 15), qb = min(row0 + 16, len) - 1;
+  const int q0 = tile * 16 * RG, row0 = q0 + wave * 16, qrow = row0 + (lane & 15), qb = min(row0 + 16, len) - 1;
   const int lo_min = key_lo(a, row0), hi_max = key_hi(a, qb, len);
   const bool qok = qrow < len;
-  const KeyWalk walk(a, q0, min(q0 + 64, len) - 1, len, BR);
+  const KeyWalk walk(a, q0, min(q0 + 16 * RG, len) - 1, len, BR);
   const int lo = key_lo(a, qrow), hi = qok ? key_hi(a, qrow, len) : 0;
   f32x4 qf[NK];
   own_row<D>(Q + (long)qrow * a.ldq, qok, d, lane, qf);
-  F32Block<D> kb, vb;
+  F32Block<D, 64 * RG> kb, vb;
   auto load = [&](int t) {
     const int k0 = walk.block(t) * BR;
     kb.load(K + (long)k0 * a.ldk, a.ldk, tid, len - k0, d);
     vb.load(V + (long)k0 * a.ldv, a.ldv, tid, len - k0, d);
   };
-  if (walk.n > 0) load(0);
+  __builtin_amdgcn_s_waitcnt(0x0F70);   // (the wave's own rows: waited for in the loop, the next block would be too)
+  if (group < walk.n) load(group);
   float m = -3e38f, l = 0.f;
   f32x4 o[NK];   // rows d = 16 i + 4 g4 + e, column = the lane's query
 #pragma unroll
   for (int i = 0; i < NK; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-  for (int n = 0; n < walk.n; ++n) {
+  for (int n = group; n - group < walk.n; n += NG) {   // (both groups pass the same barriers)
     __syncthreads();
     kb.store(Ks, tid);
     vb.store(Vs, tid);
     __syncthreads();
-    if (n + 1 < walk.n) load(n + 1);
+    if (n + NG < walk.n) load(n + NG);
+    if (n >= walk.n) continue;
     const int k0 = walk.block(n) * BR;
     if (row0 >= len || !any_seen(a, k0, k0 + BR - 1, lo_min, hi_max)) continue;
-    f32x4 p[2];
-    float mx = -INFINITY;
+    // All LDS reads of a phase before its first MFMA, the values' before the exponentials: read where they are used, each one was waited
+    // for, 120 clocks to two MFMAs of 32 (36.9 -> 34.9 us for 2 x 777 rows, 12 heads of 64, window 200).
+    f32x4 p[2], kf[2][NK];
+    float mx = -INFINITY, vf[2][4][NK];
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {   // rows: key k0 + 16 t + 4 g4 + e, column: query
-      f32x4 s{0.f, 0.f, 0.f, 0.f};
+    for (int t = 0; t < 2; ++t)
 #pragma unroll
-      for (int kk = 0; kk < NK; ++kk) {
-        const f32x4 kf = frow<D>(Ks, 16 * t, kk, lane);
+      for (int kk = 0; kk < NK; ++kk) kf[t][kk] = frow<D>(Ks, 16 * t, kk, lane);
+    __builtin_amdgcn_sched_barrier(0);
+    p[0] = p[1] = f32x4{0.f, 0.f, 0.f, 0.f};   // rows: key k0 + 16 t + 4 g4 + e, column: query
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s = MFMA4(kf[e], qf[kk][e], s);
-      }
+    for (int kk = 0; kk < NK; ++kk)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) p[t] = MFMA4(kf[t][kk][e], qf[kk][e], p[t]);
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int i = 0; i < NK; ++i) vf[t][e][i] = fcol<D>(Vs, 16 * i, 16 * t, e, lane);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        p[t][e] = sees(a, k0 + 16 * t + 4 * g4 + e, lo, hi) ? s[e] * scale2 : -INFINITY;
+        p[t][e] = sees(a, k0 + 16 * t + 4 * g4 + e, lo, hi) ? p[t][e] * scale2 : -INFINITY;
         mx = fmaxf(mx, p[t][e]);
       }
-    }
     mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
     mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
     const float mn = fmaxf(m, mx), alpha = exp2f(m - mn);
@@ -848,7 +875,23 @@ __global__ __launch_bounds__(256) void attn_win_fwd_f32(AttnWinArgs a, float sca
 #pragma unroll
       for (int e = 0; e < 4; ++e)
 #pragma unroll
-        for (int i = 0; i < NK; ++i) o[i] = MFMA4(fcol<D>(Vs, 16 * i, 16 * t, e, lane), p[t][e], o[i]);
+        for (int i = 0; i < NK; ++i) o[i] = MFMA4(vf[t][e][i], p[t][e], o[i]);
+  }
+  if constexpr (NG == 2) {   // the second group's maximum, sum and o, of the same rows
+    __syncthreads();
+    if (group == 1) {
+      fsm[tid] = m;
+      fsm[64 * RG + tid] = l;
+#pragma unroll
+      for (int i = 0; i < NK; ++i) *(f32x4*)(fsm + 128 * RG + (i * 64 * RG + tid) * 4) = o[i];
+    }
+    __syncthreads();
+    if (group == 1) return;
+    const float m1 = fsm[tid], l1 = fsm[64 * RG + tid], mn = fmaxf(m, m1), f0 = exp2f(m - mn), f1 = exp2f(m1 - mn);
+    l = l * f0 + l1 * f1;
+    m = mn;
+#pragma unroll
+    for (int i = 0; i < NK; ++i) o[i] = o[i] * f0 + *(const f32x4*)(fsm + 128 * RG + (i * 64 * RG + tid) * 4) * f1;
   }
   if (qrow < a.s) {
     const float inv = l > 0.f ? 1.0f / l : 0.f;
@@ -866,18 +909,37 @@ __global__ __launch_bounds__(256) void attn_win_fwd_f32(AttnWinArgs a, float sca
   }
 }
 
-template <int D>
-__device__ __forceinline__ void win_dq_f32(const AttnWinArgs& a, unsigned id, float scale2, float scale, float* Ks, float* Vs) {
+// the second group's sums are added to the first's (which alone goes on: true)
+template <int RG, int NG, int N>
+__device__ __forceinline__ bool join_groups(f32x4 (&x)[N], float* fsm, int group, int tid) {
+  if constexpr (NG == 2) {
+    __syncthreads();
+    if (group == 1) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) *(f32x4*)(fsm + (i * 64 * RG + tid) * 4) = x[i];
+    }
+    __syncthreads();
+    if (group == 1) return false;
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] += *(const f32x4*)(fsm + (i * 64 * RG + tid) * 4);
+  }
+  return true;
+}
+
+template <int D, int RG, int NG>
+__device__ __forceinline__ void win_dq_f32(const AttnWinArgs& a, unsigned id, float scale2, float scale, float* fsm) {
   constexpr int NK = D / 16;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g4 = lane >> 4;
-  const int q_tiles = (a.s + 63) / 64, head = id / q_tiles, tile = q_tiles - 1 - id % q_tiles;
+  const int tid = threadIdx.x & (64 * RG - 1), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g4 = lane >> 4;
+  const int group = __builtin_amdgcn_readfirstlane(threadIdx.x / (64 * RG));
+  float *const Ks = fsm + group * 2 * F32Lds<D, RG, NG>::BLK, *const Vs = Ks + F32Lds<D, RG, NG>::BLK;
+  const int q_tiles = (a.s + 16 * RG - 1) / (16 * RG), head = id / q_tiles, tile = q_tiles - 1 - id % q_tiles;
   const int bi = head / a.A, hh = head % a.A, kv = hh / (a.A / a.Ak), len = len_of(a, bi), d = a.d;
   const long r0 = (long)bi * a.s;
   const float *K = (const float*)a.k + r0 * a.ldk + kv * d, *V = (const float*)a.v + r0 * a.ldv + kv * d;
-  const int q0 = tile * 64, row0 = q0 + wave * 16, qrow = row0 + (lane & 15), qb = min(row0 + 16, len) - 1;
+  const int q0 = tile * 16 * RG, row0 = q0 + wave * 16, qrow = row0 + (lane & 15), qb = min(row0 + 16, len) - 1;
   const int lo_min = key_lo(a, row0), hi_max = key_hi(a, qb, len);
   const bool qok = qrow < len;
-  const KeyWalk walk(a, q0, min(q0 + 64, len) - 1, len, BR);
+  const KeyWalk walk(a, q0, min(q0 + 16 * RG, len) - 1, len, BR);
   const int lo = key_lo(a, qrow), hi = qok ? key_hi(a, qrow, len) : 0;
   f32x4 qf[NK], gf[NK];
   own_row<D>((const float*)a.q + (r0 + qrow) * a.ldq + hh * d, qok, d, lane, qf);
@@ -887,43 +949,58 @@ __device__ __forceinline__ void win_dq_f32(const AttnWinArgs& a, unsigned id, fl
   f32x4 dq[NK];
 #pragma unroll
   for (int i = 0; i < NK; ++i) dq[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-  F32Block<D> kb, vb;
+  F32Block<D, 64 * RG> kb, vb;
   auto load = [&](int t) {
     const int k0 = walk.block(t) * BR;
     kb.load(K + (long)k0 * a.ldk, a.ldk, tid, len - k0, d);
     vb.load(V + (long)k0 * a.ldv, a.ldv, tid, len - k0, d);
   };
-  if (walk.n > 0) load(0);
-  for (int n = 0; n < walk.n; ++n) {
+  __builtin_amdgcn_s_waitcnt(0x0F70);   // (as in attn_win_fwd_f32)
+  if (group < walk.n) load(group);
+  for (int n = group; n - group < walk.n; n += NG) {   // (both groups pass the same barriers)
     __syncthreads();
     kb.store(Ks, tid);
     vb.store(Vs, tid);
     __syncthreads();
-    if (n + 1 < walk.n) load(n + 1);
+    if (n + NG < walk.n) load(n + NG);
+    if (n >= walk.n) continue;
     const int k0 = walk.block(n) * BR;
     if (row0 >= len) continue;
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       if (!any_seen(a, k0 + 16 * t, k0 + 16 * t + 15, lo_min, hi_max)) continue;
-      f32x4 s{0.f, 0.f, 0.f, 0.f}, dp{0.f, 0.f, 0.f, 0.f};
+      f32x4 s{0.f, 0.f, 0.f, 0.f}, dp{0.f, 0.f, 0.f, 0.f}, kf[NK], vf[NK];   // (reads first: see attn_win_fwd_f32)
+      float kc[4][NK], ds[4];
 #pragma unroll
       for (int kk = 0; kk < NK; ++kk) {
-        const f32x4 kf = frow<D>(Ks, 16 * t, kk, lane), vf = frow<D>(Vs, 16 * t, kk, lane);
+        kf[kk] = frow<D>(Ks, 16 * t, kk, lane);
+        vf[kk] = frow<D>(Vs, 16 * t, kk, lane);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int kk = 0; kk < NK; ++kk)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          s = MFMA4(kf[e], qf[kk][e], s);
-          dp = MFMA4(vf[e], gf[kk][e], dp);
+          s = MFMA4(kf[kk][e], qf[kk][e], s);
+          dp = MFMA4(vf[kk][e], gf[kk][e], dp);
         }
-      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int i = 0; i < NK; ++i) kc[e][i] = fcol<D>(Ks, 16 * i, 16 * t, e, lane);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        float ds = exp2f(s[e] * scale2 - Lq) * (dp[e] - Dq);
-        if (!sees(a, k0 + 16 * t + 4 * g4 + e, lo, hi)) ds = 0.f;
-#pragma unroll
-        for (int i = 0; i < NK; ++i) dq[i] = MFMA4(fcol<D>(Ks, 16 * i, 16 * t, e, lane), ds, dq[i]);
+        ds[e] = exp2f(s[e] * scale2 - Lq) * (dp[e] - Dq);
+        if (!sees(a, k0 + 16 * t + 4 * g4 + e, lo, hi)) ds[e] = 0.f;
       }
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int i = 0; i < NK; ++i) dq[i] = MFMA4(kc[e][i], ds[e], dq[i]);
     }
   }
+  if (!join_groups<RG, NG>(dq, fsm, group, tid)) return;
   if (qrow < a.s) {
 #pragma unroll
     for (int i = 0; i < NK; ++i) {
@@ -933,12 +1010,15 @@ __device__ __forceinline__ void win_dq_f32(const AttnWinArgs& a, unsigned id, fl
   }
 }
 
-template <int D>
-__device__ __forceinline__ void win_dkdv_f32(const AttnWinArgs& a, unsigned task, float scale2, float scale, float* Qs, float* Gs, float* Ls, float* Ds) {
+template <int D, int RG, int NG>
+__device__ __forceinline__ void win_dkdv_f32(const AttnWinArgs& a, unsigned task, float scale2, float scale, float* fsm) {
   constexpr int NK = D / 16;
-  const KeyTask w(a, task, 64, BR);
+  const KeyTask w(a, task, 16 * RG, BR);
   if (!w.run) return;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g4 = lane >> 4;
+  const int tid = threadIdx.x & (64 * RG - 1), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g4 = lane >> 4;
+  const int group = __builtin_amdgcn_readfirstlane(threadIdx.x / (64 * RG));
+  float *const Qs = fsm + group * 2 * F32Lds<D, RG, NG>::BLK, *const Gs = Qs + F32Lds<D, RG, NG>::BLK;
+  float *const Ls = fsm + NG * 2 * F32Lds<D, RG, NG>::BLK + group * F32Lds<D, RG, NG>::STAT, *const Ds = Ls + BR;
   const int len = w.len, d = a.d, h0 = w.kv * (a.A / a.Ak);
   const long r0 = (long)w.bi * a.s;
   const float *Q = (const float*)a.q + r0 * a.ldq + h0 * d, *G = (const float*)a.dctx + r0 * a.lddc + h0 * d;
@@ -949,29 +1029,25 @@ __device__ __forceinline__ void win_dkdv_f32(const AttnWinArgs& a, unsigned task
   const int kb = min(row0 + 16, len) - 1;
   const bool sink = a.W && row0 < a.S;
   const int lo_min = sink && !a.causal ? 0 : query_lo(a, row0), hi_max = sink ? len : query_hi(a, kb, len);
-  f32x4 kf[NK], vf[NK], dk[NK], dv[NK];
+  f32x4 kf[NK], vf[NK], sum[2 * NK];   // sums: dk, dv
+  f32x4 *const dk = sum, *const dv = sum + NK;
   own_row<D>((const float*)a.k + (r0 + krow) * a.ldk + w.kv * d, kok, d, lane, kf);
   own_row<D>((const float*)a.v + (r0 + krow) * a.ldv + w.kv * d, kok, d, lane, vf);
 #pragma unroll
   for (int i = 0; i < NK; ++i) dk[i] = dv[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-  F32Block<D> qb, gb;
+  F32Block<D, 64 * RG> qb, gb;
   float L = 0.f, De = 0.f;
-  int hd = w.nq ? w.n0 / w.nq : 0, blk = w.nq ? w.n0 % w.nq : 0;   // the next block to load: head, block
-  auto load = [&]() {
-    const int i0 = (w.qlo + blk) * BR;
+  auto load = [&](int n) {
+    const int hd = n / w.nq, i0 = (w.qlo + n % w.nq) * BR;
     qb.load(Q + (long)i0 * a.ldq + hd * d, a.ldq, tid, len - i0, d);
     gb.load(G + (long)i0 * a.lddc + hd * d, a.lddc, tid, len - i0, d);
     const bool in = tid < BR && i0 + tid < len;
     L = in ? lse[(long)hd * a.s + i0 + tid] : 0.f;
     De = in ? delta[(long)hd * a.s + i0 + tid] : 0.f;
-    if (++blk == w.nq) {
-      blk = 0;
-      ++hd;
-    }
   };
-  if (w.n0 < w.n1) load();
-  int cur = w.nq ? w.n0 % w.nq : 0;
-  for (int n = w.n0; n < w.n1; ++n) {
+  __builtin_amdgcn_s_waitcnt(0x0F70);   // (as in attn_win_fwd_f32)
+  if (w.n0 + group < w.n1) load(w.n0 + group);
+  for (int n = w.n0 + group; n - group < w.n1; n += NG) {   // (both groups pass the same barriers)
     __syncthreads();
     qb.store(Qs, tid);
     gb.store(Gs, tid);
@@ -980,43 +1056,59 @@ __device__ __forceinline__ void win_dkdv_f32(const AttnWinArgs& a, unsigned task
       Ds[tid] = De;
     }
     __syncthreads();
-    if (n + 1 < w.n1) load();
-    const int i0 = (w.qlo + cur) * BR;
-    cur = cur + 1 == w.nq ? 0 : cur + 1;
-    if (row0 >= len) continue;
+    if (n + NG < w.n1) load(n + NG);
+    if (row0 >= len || n >= w.n1) continue;
+    const int i0 = (w.qlo + n % w.nq) * BR;
 #pragma unroll
     for (int t = 0; t < 2; ++t) {   // rows: query i0 + 16 t + 4 g4 + e, column: key
       if (i0 + 16 * t >= hi_max || i0 + 16 * t + 15 < lo_min) continue;
-      f32x4 s{0.f, 0.f, 0.f, 0.f}, dp{0.f, 0.f, 0.f, 0.f};
+      f32x4 s{0.f, 0.f, 0.f, 0.f}, dp{0.f, 0.f, 0.f, 0.f}, qf[NK], gf[NK];   // (reads first: see attn_win_fwd_f32)
+      float gc[4][NK], qc[4][NK], p[4], ds[4];
 #pragma unroll
       for (int kk = 0; kk < NK; ++kk) {
-        const f32x4 qf = frow<D>(Qs, 16 * t, kk, lane), gf = frow<D>(Gs, 16 * t, kk, lane);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          s = MFMA4(qf[e], kf[kk][e], s);
-          dp = MFMA4(gf[e], vf[kk][e], dp);
-        }
+        qf[kk] = frow<D>(Qs, 16 * t, kk, lane);
+        gf[kk] = frow<D>(Gs, 16 * t, kk, lane);
       }
       const f32x4 L4 = *(const f32x4*)(Ls + 16 * t + 4 * g4), D4 = *(const f32x4*)(Ds + 16 * t + 4 * g4);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int kk = 0; kk < NK; ++kk)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          s = MFMA4(qf[kk][e], kf[kk][e], s);
+          dp = MFMA4(gf[kk][e], vf[kk][e], dp);
+        }
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int c = 0; c < NK; ++c) {
+          gc[e][c] = fcol<D>(Gs, 16 * c, 16 * t, e, lane);
+          qc[e][c] = fcol<D>(Qs, 16 * c, 16 * t, e, lane);
+        }
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int i = i0 + 16 * t + 4 * g4 + e;
         const bool ok = i >= lo && i < hi;
-        const float p = ok ? exp2f(s[e] * scale2 - L4[e]) : 0.f, ds = ok ? p * (dp[e] - D4[e]) : 0.f;
+        p[e] = ok ? exp2f(s[e] * scale2 - L4[e]) : 0.f;
+        ds[e] = ok ? p[e] * (dp[e] - D4[e]) : 0.f;
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
 #pragma unroll
         for (int c = 0; c < NK; ++c) {
-          dv[c] = MFMA4(fcol<D>(Gs, 16 * c, 16 * t, e, lane), p, dv[c]);
-          dk[c] = MFMA4(fcol<D>(Qs, 16 * c, 16 * t, e, lane), ds, dk[c]);
+          dv[c] = MFMA4(gc[e][c], p[e], dv[c]);
+          dk[c] = MFMA4(qc[e][c], ds[e], dk[c]);
         }
-      }
     }
   }
+  if (!join_groups<RG, NG>(sum, fsm, group, tid)) return;
   if (w.slot >= 0) {
-    float* const P = a.partial + (long)w.slot * 2 * 64 * D;
+    float* const P = a.partial + (long)w.slot * 2 * 16 * RG * D;
 #pragma unroll
     for (int i = 0; i < NK; ++i) {
       *(f32x4*)(P + ((wave * NK + i) * 64 + lane) * 4) = dk[i];
-      *(f32x4*)(P + 64 * D + ((wave * NK + i) * 64 + lane) * 4) = dv[i];
+      *(f32x4*)(P + 16 * RG * D + ((wave * NK + i) * 64 + lane) * 4) = dv[i];
     }
     return;
   }
@@ -1032,15 +1124,12 @@ __device__ __forceinline__ void win_dkdv_f32(const AttnWinArgs& a, unsigned task
   }
 }
 
-template <int D>
-__global__ __launch_bounds__(256) void attn_win_bwd_f32(AttnWinArgs a, float scale2, float scale) {
-  __shared__ __attribute__((aligned(16))) float X[BR * (D + 8)];
-  __shared__ __attribute__((aligned(16))) float Y[BR * (D + 8)];
-  __shared__ __attribute__((aligned(16))) float Ls[BR];
-  __shared__ __attribute__((aligned(16))) float Ds[BR];
+template <int D, int RG, int NG>
+__global__ __launch_bounds__(64 * RG * NG) void attn_win_bwd_f32(AttnWinArgs a, float scale2, float scale) {
+  extern __shared__ __attribute__((aligned(16))) float fsm[];
   const unsigned nk = a.plan.key_tasks;
-  if (blockIdx.x < nk) win_dkdv_f32<D>(a, spread(blockIdx.x, nk), scale2, scale, X, Y, Ls, Ds);
-  else win_dq_f32<D>(a, spread(blockIdx.x - nk, gridDim.x - nk), scale2, scale, X, Y);
+  if (blockIdx.x < nk) win_dkdv_f32<D, RG, NG>(a, spread(blockIdx.x, nk), scale2, scale, fsm);
+  else win_dq_f32<D, RG, NG>(a, spread(blockIdx.x - nk, gridDim.x - nk), scale2, scale, fsm);
 }
 
 // ------------------------------------------------------------------ both types
@@ -1079,11 +1168,12 @@ __global__ __launch_bounds__(256) void attn_win_delta(AttnWinArgs a) {
   }
 }
 
+constexpr int join_threads(int elements) { return elements / 4 < 256 ? elements / 4 : 256; }
 // dk (z = 0), dv of the tiles whose walk has parts: the parts' sums in ascending order.  RW: rows (keys) of a wave; an
 // accumulator block is RW rows x 64 * 4 / RW columns.
 template <typename T, int D, int KT, int RW, int BLK>
 __global__ __launch_bounds__(256) void attn_win_join(AttnWinArgs a, float scale) {
-  constexpr int UNITS = KT * D / 4 / 256;   // workgroups per tile, four elements to a lane
+  constexpr int JT = join_threads(KT * D), UNITS = KT * D / 4 / JT;   // workgroups per tile, four elements to a lane
   const WinPlan& p = a.plan;
   const int head = blockIdx.y, nt = (p.sink_parts > 1 ? p.sink_tiles : 0);
   int tile = blockIdx.x / UNITS;
@@ -1093,7 +1183,7 @@ __global__ __launch_bounds__(256) void attn_win_join(AttnWinArgs a, float scale)
   // the tile's first task (KeyTask counts the same)
   KeyTask w(a, head * (sinks + (p.key_tiles - p.sink_tiles) * p.parts) + (sink ? tile * p.sink_parts : sinks + (tile - p.sink_tiles) * p.parts), KT, BLK);
   const int all = w.nq * (a.A / a.Ak), used = (all + p.steps - 1) / p.steps;
-  const int u = (blockIdx.x % UNITS) * 256 + threadIdx.x, lane = u & 63, blk = u >> 6;
+  const int u = (blockIdx.x % UNITS) * JT + threadIdx.x, lane = u & 63, blk = u >> 6;
   constexpr int CB = 256 / RW;              // columns of an accumulator register block
   const int row = blk / (D / CB) * RW + (lane & (RW - 1)), col = blk % (D / CB) * CB + 4 * (lane / RW);
   const float* src = a.partial + ((long)w.slot * 2 + blockIdx.z) * KT * D + (long)u * 4;
@@ -1138,7 +1228,11 @@ bool attn_win_takes(Dtype dt, const AttnWinArgs& a) {
 static int fwd_waves(const AttnWinArgs& a) { return (long)((a.s + 127) / 128) * a.b * a.A < 192 ? 2 : 4; }
 static int bwd_waves(const AttnWinArgs& a) { return (long)((a.s + 127) / 128) * a.b * (a.A + a.Ak) < 192 ? 2 : 4; }
 // keys of a workgroup of the backward
-static int key_tile(Dtype dt, const AttnWinArgs& a) { return dt != DT_BF16 ? 64 : a.d > 64 ? 128 : 32 * bwd_waves(a); }
+// fp32: waves of a group (16 rows each).  Four where their tiles make two workgroups for each unit, else two: us forward and
+// backward with four / two waves: 4 x 512 rows, 16 heads of 64 211 / 227; 2 x 2048, window none 879 / 914; 2 x 777, 12 heads, window
+// 200 110 / 101; 300 rows, 8 heads of 32 31 / 24
+static int f32_rows(const AttnWinArgs& a) { return (long)((a.s + 63) / 64) * a.b * a.A < 512 ? 2 : 4; }
+static int key_tile(Dtype dt, const AttnWinArgs& a) { return dt != DT_BF16 ? 16 * f32_rows(a) : a.d > 64 ? 128 : 32 * bwd_waves(a); }
 
 // queries of a block of their walks
 static int walk_block(Dtype dt, const AttnWinArgs& a) { return dt != DT_BF16 ? BR : a.d > 64 ? 32 : 64; }
@@ -1183,6 +1277,8 @@ int64_t attn_win_workspace(Dtype dt, AttnWinArgs a) {
   return (int64_t)delta_bytes(a) + (int64_t)a.b * a.Ak * a.plan.slots * 2 * kt * width * 4;
 }
 
+
+
 template <typename K>
 static hipError_t allow_lds(K kern, int bytes) {
   return hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
@@ -1193,8 +1289,14 @@ hipError_t launch_attn_win_fwd(Dtype dt, const AttnWinArgs& a, hipStream_t st) {
   return pick_width(dt, a.d, [&](auto D) {
     constexpr int d = decltype(D)::value;
     if (dt != DT_BF16) {
-      hipLaunchKernelGGL(attn_win_fwd_f32<d>, dim3((unsigned)((long)((a.s + 63) / 64) * a.b * a.A)), dim3(256), 0, st, a, scale2);
-      return hipGetLastError();
+      auto go = [&](auto RG) {
+        constexpr int rg = decltype(RG)::value, lds = F32Lds<d, rg, 2>::FLOATS * 4;
+        static const hipError_t rc = allow_lds(attn_win_fwd_f32<d, rg, 2>, lds);
+        if (rc != hipSuccess) return rc;
+        hipLaunchKernelGGL((attn_win_fwd_f32<d, rg, 2>), dim3((unsigned)((long)((a.s + 16 * rg - 1) / (16 * rg)) * a.b * a.A)), dim3(128 * rg), lds, st, a, scale2);
+        return hipGetLastError();
+      };
+      return f32_rows(a) == 4 ? go(std::integral_constant<int, 4>{}) : go(std::integral_constant<int, 2>{});
     }
     if constexpr (d >= 32) {
       auto go = [&](auto NW) {
@@ -1225,14 +1327,21 @@ hipError_t launch_attn_win_bwd(Dtype dt, AttnWinArgs a, void* workspace, hipStre
     constexpr int d = decltype(D)::value;
     auto join = [&](auto kern, int kt) {
       if (!joined) return hipSuccess;
-      hipLaunchKernelGGL(kern, dim3(joined * (kt * d / 1024), a.b * a.Ak, 2), dim3(256), 0, st, a, scale);
+      const int threads = join_threads(kt * d);
+      hipLaunchKernelGGL(kern, dim3(joined * (kt * d / 4 / threads), a.b * a.Ak, 2), dim3(threads), 0, st, a, scale);
       return hipGetLastError();
     };
     if (dt != DT_BF16) {
-      const long grid = a.plan.key_tasks + (long)((a.s + 63) / 64) * a.b * a.A;
-      hipLaunchKernelGGL(attn_win_bwd_f32<d>, dim3((unsigned)grid), dim3(256), 0, st, a, scale2, scale);
-      e = hipGetLastError();
-      return e != hipSuccess ? e : join(attn_win_join<float, d, 64, 16, BR>, 64);
+      auto go = [&](auto RG) {
+        constexpr int rg = decltype(RG)::value, lds = F32Lds<d, rg, 2>::FLOATS * 4;
+        static const hipError_t rc = allow_lds(attn_win_bwd_f32<d, rg, 2>, lds);
+        if (rc != hipSuccess) return rc;
+        const long grid = a.plan.key_tasks + (long)((a.s + 16 * rg - 1) / (16 * rg)) * a.b * a.A;
+        hipLaunchKernelGGL((attn_win_bwd_f32<d, rg, 2>), dim3((unsigned)grid), dim3(128 * rg), lds, st, a, scale2, scale);
+        e = hipGetLastError();
+        return e != hipSuccess ? e : join(attn_win_join<float, d, 16 * rg, 16, BR>, 16 * rg);
+      };
+      return f32_rows(a) == 4 ? go(std::integral_constant<int, 4>{}) : go(std::integral_constant<int, 2>{});
     }
     if constexpr (d == 128) {
       static const hipError_t rc = allow_lds(attn_win_bwd_pair, PAIR_BYTES);
