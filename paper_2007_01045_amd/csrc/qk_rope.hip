@@ -8,7 +8,7 @@
 // read once per wave for all heads of the row, and comes out of the L2s.
 //
 // A lane owns a UNIT of a head: two chunks of V consecutive columns, chosen so that both columns of every pair are the lane's
-// (i and i + rot/2, or neighbours), and the rotation needs no exchange.  G lanes (a power of two) hold a head, 64 / G heads are
+// (the chunks rot/2 apart, or neighbours in one chunk), and the rotation needs no exchange.  G lanes (a power of two) hold a head, 64 / G heads are
 // done at a time; the only exchange is the sum of squares within G lanes.  A wave takes all heads of a row, so that its part
 // of the table and of gamma stays in registers.
 #include <type_traits>
@@ -56,50 +56,69 @@ __device__ __forceinline__ void store_chunk(T* p, const float (&o)[V]) {
   }
 }
 
-// HALF: pairs (i, i + rot/2); else neighbours.  A lane's units, NU of them: where their chunks begin (-1: none) and
-// whether they turn.
+// HALF: pairs (i, i + rot/2); else neighbours.  A lane's units, NU of them: where their chunks begin (-1: none) and whether they
+// turn.  Chunks that need not be together are half of the columns apart, so that a load of a head's lanes is one piece.
 template <int V, bool HALF, int NU>
 struct Units {
   int off[NU][2];
   bool turn[NU][2];
-  int pair[NU];   // table pair of the first of the V pairs
+  int pair[NU][2];   // table pair of a chunk's first (HALF: the first's, of the V pairs of both)
   __device__ __forceinline__ void init(int d, int rot, int lane_in_head, int G) {
 #pragma unroll
     for (int i = 0; i < NU; ++i) {
-      const int u = lane_in_head + i * G, half = HALF ? rot / (2 * V) : 0;
-      int a, b;
-      if (HALF && u < half) {
-        a = u * V;
-        b = rot / 2 + u * V;
+      const int u = lane_in_head + i * G, turning = HALF ? rot / (2 * V) : 0;
+      if (HALF && u < turning) {
+        off[i][0] = u * V;
+        off[i][1] = rot / 2 + u * V;
         turn[i][0] = turn[i][1] = true;
-        pair[i] = u * V;
+        pair[i][0] = pair[i][1] = u * V;
       } else {
-        a = (HALF ? rot : 0) + 2 * (u - half) * V;
-        b = a + V;
-        turn[i][0] = !HALF && a < rot;
-        turn[i][1] = !HALF && b < rot;
-        pair[i] = a / 2;
+        const int r0 = HALF ? rot : 0, chunks = (d - r0) / V, apart = (chunks + 1) / 2, w = u - turning;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const int n = w + k * apart, o = r0 + n * V;
+          off[i][k] = w < apart && n < chunks ? o : -1;
+          turn[i][k] = !HALF && off[i][k] >= 0 && o < rot;
+          pair[i][k] = o / 2;
+        }
       }
-      off[i][0] = a < d ? a : -1;
-      off[i][1] = b < d ? b : -1;
     }
   }
 };
 
-// c, s of the V pairs of each unit; a position outside the table makes them NaN (nothing is read there)
+// c, s of the V pairs of each unit; a position outside the table makes them NaN (nothing is read there).  A chunk's pairs lie side
+// by side in the table's row: two pairs to a load.
 template <int V, bool HALF, int NU>
 __device__ __forceinline__ void load_table(const QkRopeArgs& a, const Units<V, HALF, NU>& un, int pos, float (&c)[NU][V], float (&s)[NU][V]) {
+  typedef float f4 __attribute__((ext_vector_type(4), aligned(8)));
+  constexpr int Q = HALF ? V : V / 2;   // pairs that turn or do not turn together
   const bool ok = pos >= 0 && pos < a.max_pos;
   const float2* const row = (const float2*)a.table + (long)(ok ? pos : 0) * (a.rot / 2);
+  const float none = ok ? 0.f : __builtin_nanf("");
 #pragma unroll
   for (int i = 0; i < NU; ++i)
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
-      const bool turns = HALF ? un.turn[i][0] : un.turn[i][2 * e / V];
-      float2 cs = make_float2(1.f, 0.f);
-      if (turns && un.off[i][0] >= 0) cs = row[un.pair[i] + e];
-      c[i][e] = ok || !turns ? cs.x : __builtin_nanf("");
-      s[i][e] = ok || !turns ? cs.y : __builtin_nanf("");
+    for (int q = 0; q < V; q += Q) {
+#pragma unroll
+      for (int e = q; e < q + Q; ++e) {
+        c[i][e] = 1.f;
+        s[i][e] = 0.f;
+      }
+      if (!un.turn[i][q / Q]) continue;
+      const float2* const p = row + un.pair[i][q / Q];
+#pragma unroll
+      for (int e = 0; e < Q; e += 2) {
+        if constexpr (Q >= 2) {
+          const f4 x = *(const f4*)(p + e);
+          c[i][q + e] = x[0] + none;
+          s[i][q + e] = x[1] + none;
+          c[i][q + e + 1] = x[2] + none;
+          s[i][q + e + 1] = x[3] + none;
+        } else {
+          c[i][q] = p->x + none;
+          s[i][q] = p->y + none;
+        }
+      }
     }
 }
 
@@ -200,38 +219,36 @@ __global__ __launch_bounds__(256) void qk_rope_fwd_kernel(QkRopeArgs a, int G, i
   }
 }
 
-// Rows w, w + waves, ... per wave.  A lane's sums for dgamma stay in registers over all of its rows and heads; the workgroup's
-// lanes of one unit are added in a fixed order, partial[block][q, k][d].
+// Rows w, w + waves, ... per wave, all of them for the queries, then for the keys (in one walk the two gammas' sums would stand in
+// registers side by side, and three waves of a SIMD in the place of four: 249 -> 211 us for 32768 rows, 32 + 8 heads of 128).  A lane's sums for dgamma stay in registers
+// over all of its rows and heads; the workgroup's lanes of one unit are added in a fixed order, partial[block][q, k][d].
 template <typename T, int V, bool HALF, int NU>
-__global__ __launch_bounds__(256) void qk_rope_bwd_kernel(QkRopeArgs a, int G, float* __restrict__ partial) {
+__global__ __launch_bounds__(256, V * NU <= 4 ? 1 : 4) void qk_rope_bwd_kernel(QkRopeArgs a, int G, float* __restrict__ partial) {
   __shared__ float red[256][NU * 2 * V + 1];
   const int lane = threadIdx.x & 63, per = 64 / G;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   Units<V, HALF, NU> un;
   un.init(a.d, a.rot, lane % G, G);
   const float inv_d = 1.0f / (float)a.d;
-  float g[2][NU][2][V], dg[2][NU][2][V];
-#pragma unroll
-  for (int t = 0; t < 2; ++t)
+  const bool norm = a.gamma_q != nullptr;
+#pragma unroll 1
+  for (int t = 0; t < 2; ++t) {
+    const int heads = t ? a.Ak : a.A;
+    const long ldx = t ? a.ldk : a.ldq, lddy = t ? a.lddyk : a.lddyq, lddx = t ? a.lddk : a.lddq;
+    const T *X = (const T*)(t ? a.k : a.q), *DY = (const T*)(t ? a.dyk : a.dyq), *gam = (const T*)(t ? a.gamma_k : a.gamma_q);
+    T* DX = (T*)(t ? a.dk : a.dq);
+    float g[NU][2][V], dg[NU][2][V];
 #pragma unroll
     for (int i = 0; i < NU; ++i)
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
 #pragma unroll
-        for (int e = 0; e < V; ++e) dg[t][i][k][e] = g[t][i][k][e] = 0.f;
-        const T* gam = (const T*)(t ? a.gamma_k : a.gamma_q);
-        if (gam && un.off[i][k] >= 0 && (t ? a.Ak : a.A) > 0) load_chunk<T, V>(gam + un.off[i][k], g[t][i][k]);
+        for (int e = 0; e < V; ++e) dg[i][k][e] = g[i][k][e] = 0.f;
+        if (norm && heads > 0 && un.off[i][k] >= 0) load_chunk<T, V>(gam + un.off[i][k], g[i][k]);
       }
-  for (long row = (long)blockIdx.x * 4 + wave; row < a.rows; row += (long)gridDim.x * 4) {
-    float c[NU][V], s[NU][V];
-    load_table<V, HALF, NU>(a, un, position_of(a, row), c, s);
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const int heads = t ? a.Ak : a.A;
-      if (heads == 0) continue;
-      const bool norm = a.gamma_q != nullptr;
-      const T *X = (const T*)(t ? a.k : a.q) + row * (t ? a.ldk : a.ldq), *DY = (const T*)(t ? a.dyk : a.dyq) + row * (t ? a.lddyk : a.lddyq);
-      T* DX = (T*)(t ? a.dk : a.dq) + row * (t ? a.lddk : a.lddq);
+    for (long row = (long)blockIdx.x * 4 + wave; heads > 0 && row < a.rows; row += (long)gridDim.x * 4) {
+      float c[NU][V], s[NU][V];
+      load_table<V, HALF, NU>(a, un, position_of(a, row), c, s);
       for (int h0 = 0; h0 < heads; h0 += per) {
         const int h = h0 + lane / G;
         float x[NU][2][V], y[NU][2][V];
@@ -242,8 +259,8 @@ __global__ __launch_bounds__(256) void qk_rope_bwd_kernel(QkRopeArgs a, int G, f
 #pragma unroll
             for (int e = 0; e < V; ++e) x[i][k][e] = y[i][k][e] = 0.f;
             if (h < heads && un.off[i][k] >= 0) {
-              load_chunk<T, V>(DY + h * a.d + un.off[i][k], y[i][k]);
-              if (norm) load_chunk<T, V>(X + h * a.d + un.off[i][k], x[i][k]);
+              load_chunk<T, V>(DY + row * lddy + h * a.d + un.off[i][k], y[i][k]);
+              if (norm) load_chunk<T, V>(X + row * ldx + h * a.d + un.off[i][k], x[i][k]);
             }
           }
 #pragma unroll
@@ -257,7 +274,7 @@ __global__ __launch_bounds__(256) void qk_rope_bwd_kernel(QkRopeArgs a, int G, f
 #pragma unroll
               for (int e = 0; e < V; ++e) {
                 q = fmaf(x[i][k][e], x[i][k][e], q);
-                p = fmaf(x[i][k][e], y[i][k][e] * g[t][i][k][e], p);
+                p = fmaf(x[i][k][e], y[i][k][e] * g[i][k][e], p);
               }
           const float rstd = rsqrtf(group_sum(q, G) * inv_d + a.eps);
           const float m = group_sum(p, G) * inv_d * rstd;   // mean of dn gamma x rstd
@@ -268,28 +285,25 @@ __global__ __launch_bounds__(256) void qk_rope_bwd_kernel(QkRopeArgs a, int G, f
 #pragma unroll
               for (int e = 0; e < V; ++e) {
                 const float xh = x[i][k][e] * rstd;
-                dg[t][i][k][e] = fmaf(y[i][k][e], xh, dg[t][i][k][e]);
-                y[i][k][e] = rstd * (y[i][k][e] * g[t][i][k][e] - xh * m);
+                dg[i][k][e] = fmaf(y[i][k][e], xh, dg[i][k][e]);
+                y[i][k][e] = rstd * (y[i][k][e] * g[i][k][e] - xh * m);
               }
         }
 #pragma unroll
         for (int i = 0; i < NU; ++i)
 #pragma unroll
           for (int k = 0; k < 2; ++k)
-            if (h < heads && un.off[i][k] >= 0) store_chunk<T, V>(DX + h * a.d + un.off[i][k], y[i][k]);
+            if (h < heads && un.off[i][k] >= 0) store_chunk<T, V>(DX + row * lddx + h * a.d + un.off[i][k], y[i][k]);
       }
     }
-  }
-  if (!partial) return;   // (no gammas: the whole grid)
-#pragma unroll
-  for (int t = 0; t < 2; ++t) {
+    if (!partial) continue;   // (no dgamma is wanted: the whole grid)
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < NU; ++i)
 #pragma unroll
       for (int k = 0; k < 2; ++k)
 #pragma unroll
-        for (int e = 0; e < V; ++e) red[threadIdx.x][(i * 2 + k) * V + e] = dg[t][i][k][e];
+        for (int e = 0; e < V; ++e) red[threadIdx.x][(i * 2 + k) * V + e] = dg[i][k][e];
     __syncthreads();
     // thread (u, j): value j of the lanes that hold the units u, u + G of a head
     for (int n = threadIdx.x; n < G * NU * 2 * V; n += 256) {
