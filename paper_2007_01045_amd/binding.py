@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+from array import array
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libdapple_stage.so")
@@ -513,8 +514,17 @@ def dapple_gated_ffn_bwd(dtype, desc: gated_ffn_desc, stream_ptr=None):
     _check(load().dapple_gated_ffn_bwd(dtype, C.byref(desc), stream_ptr))
 
 
+# lists of tensors: a stage of many layers has hundreds, and ctypes converts one by one in twice the time
 def _i64_array(sizes):
-    return (C.c_int64 * len(sizes))(*sizes)
+    return (C.c_int64 * len(sizes)).from_buffer(array("q", sizes)) if sizes else None
+
+
+def _tensor_array(ptrs, n):
+    if ptrs is None:
+        return None
+    if len(ptrs) != n:
+        raise ValueError(f"{len(ptrs)} tensors, {n} sizes")
+    return (C.c_void_p * n).from_buffer(array("Q", [p or 0 for p in ptrs])) if n else None
 
 
 def dapple_grad_norm_workspace(sizes) -> int:
@@ -525,14 +535,14 @@ def dapple_grad_norm_workspace(sizes) -> int:
 def dapple_grad_norm(dtype, grad_ptrs, sizes, max_norm, norm_ptr, workspace_ptr, grad_scale=1.0, stream_ptr=None):
     """norm_ptr (device float [2]): the global norm of the tensors and the factor that clips it to max_norm."""
     n = len(sizes)
-    _check(load().dapple_grad_norm(dtype, _ptr_array(grad_ptrs, n), _i64_array(sizes), n, grad_scale, max_norm, norm_ptr,
+    _check(load().dapple_grad_norm(dtype, _tensor_array(grad_ptrs, n), _i64_array(sizes), n, grad_scale, max_norm, norm_ptr,
                                    workspace_ptr, stream_ptr))
 
 
 def dapple_grad_clip(dtype, grad_ptrs, out_ptrs, sizes, norm_ptr, stream_ptr=None):
     """out = grad times the factor that dapple_grad_norm left; out_ptrs None: in place."""
     n = len(sizes)
-    _check(load().dapple_grad_clip(dtype, _ptr_array(grad_ptrs, n), _ptr_array(out_ptrs, n), _i64_array(sizes), n, norm_ptr,
+    _check(load().dapple_grad_clip(dtype, _tensor_array(grad_ptrs, n), _tensor_array(out_ptrs, n), _i64_array(sizes), n, norm_ptr,
                                    stream_ptr))
 
 

@@ -82,6 +82,14 @@ static GemmArgs bwd_dw(const GatedFfnArgs& a, bool in, float* bsum) {
   return g;
 }
 
+// The tile of a weight gradient's product (T rows deep): 256x256 or 256x128 where three quarters of the 256 units get one, else 0,
+// the choice for the encoder layers (128x128, eight waves).  With the bias' sums, T = 8192: 2048 x 16384 756 -> 468 us (256x256),
+// 8192 x 2048 273 -> 215; 1024 x 8192 139 -> 131 (256x128; 256x256 166), T = 2048, 4096 x 2048 38 -> 36 (49).
+static int dw_tile(const GemmArgs& g) {
+  auto tiles = [&](int m, int n) { return (long)((g.M + m - 1) / m) * ((g.N + n - 1) / n); };
+  return tiles(256, 256) >= 192 ? 1 : tiles(256, 128) >= 192 ? 2 : 0;
+}
+
 bool gated_ffn_takes(Dtype dt, const GatedFfnArgs& a, bool bwd) {
   auto takes = [&](const GemmArgs& g) { return dt == DT_BF16 ? gemm_uses_mfma(dt, g) : gemm_f32_takes(g); };
   float some = 0.f;
@@ -154,7 +162,9 @@ hipError_t launch_gated_ffn_bwd(Dtype dt, const GatedFfnArgs& a, void* workspace
   }
   if (e == hipSuccess && a.dx) e = launch_gemm(dt, bwd_dx(a), st);
   if (e != hipSuccess || !a.dw_in) return e;
-  if (a.accumulate) {   // both in one launch
+  GemmArgs win = bwd_dw(a, true, nullptr), wout = bwd_dw(a, false, nullptr);
+  if (dt == DT_BF16) win.tile = dw_tile(win), wout.tile = dw_tile(wout);
+  if (a.accumulate && !win.tile && !wout.tile) {   // both in one launch
     WgradGroup w{};
     w.p[0] = WgradProblem{a.x, a.dgu, (float*)a.dw_in, (float*)a.db_in, a.H, 2 * a.F, a.ldx, 2 * a.F, 2 * a.F};
     w.p[1] = WgradProblem{a.h, a.dy, (float*)a.dw_out, (float*)a.db_out, a.F, a.H, a.F, a.lddy, a.H};
@@ -162,16 +172,22 @@ hipError_t launch_gated_ffn_bwd(Dtype dt, const GatedFfnArgs& a, void* workspace
     w.K = w.kseg = a.T;
     return launch_wgrad_group(dt, w, st);
   }
-  const bool sums = a.db_in || a.db_out, ws = dt == DT_BF16;
+  const bool sums = a.db_in || a.db_out, ws = dt == DT_BF16 && !a.accumulate;
   float *bi = ws ? (float*)workspace : (float*)a.db_in, *bo = ws ? (float*)workspace + 2 * a.F : (float*)a.db_out;
   const int ni = a.db_in ? 2 * a.F : 0, no = a.db_out ? a.H : 0;
-  if (sums) {
+  if (sums && !a.accumulate) {
     hipLaunchKernelGGL(zero_f32_kernel, dim3((ni + no + 255) / 256), dim3(256), 0, st, bi, ni, bo, no);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  e = launch_gemm(dt, bwd_dw(a, true, ni ? bi : nullptr), st);
-  if (e == hipSuccess) e = launch_gemm(dt, bwd_dw(a, false, no ? bo : nullptr), st);
+  auto with_sum = [](GemmArgs& g, float* sum) {
+    g.bsum = sum;
+    if (sum) g.epi |= EPI_BSUM;
+  };
+  with_sum(win, ni ? bi : nullptr);
+  with_sum(wout, no ? bo : nullptr);
+  e = launch_gemm(dt, win, st);
+  if (e == hipSuccess) e = launch_gemm(dt, wout, st);
   if (e != hipSuccess || !sums || !ws) return e;
   hipLaunchKernelGGL(round_bias_kernel, dim3((2 * a.F + a.H + 255) / 256), dim3(256), 0, st, bi, (bf16*)a.db_in, 2 * a.F, (bf16*)a.db_out, a.H);
   return hipGetLastError();

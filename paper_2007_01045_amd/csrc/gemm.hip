@@ -153,12 +153,12 @@ bool gemm_uses_mfma(Dtype dt, const GemmArgs& g) {
 static int choose_tile(const GemmArgs& g, bool tt, bool short_k) {
   auto tiles = [&](long m, long n) { return ((g.M + m - 1) / m) * ((g.N + n - 1) / n) * g.batch; };
   const long t128 = tiles(128, 128), U = g.units > 0 ? g.units : 256, most = 3 * U / 4;
-  const bool bsum = (g.epi & EPI_BSUM) != 0;   // (offered for the weight-gradient layout only)
+  const bool bsum = (g.epi & EPI_BSUM) != 0;   // (offered for the weight-gradient layout only, five stages without)
   int tile = g.tile < 0 || g.tile == 11 || g.tile > 12 ? 7 : g.tile;   // GemmArgs::tile names a configuration instead (tests, timing)
   if (tile == 5 && !tt) tile = 3;
   if (tile == 8 && g.a_kstrided) tile = tt ? 5 : 3;   // (products whose rows are activations only)
   if (tile >= 9 && g.a_kstrided) tile = 7;
-  if (bsum && (tile == 1 || tile == 2 || tile == 6)) tile = 0;
+  if (bsum && tile == 6) tile = 0;
   if (short_k) return tile == 3 || (tile != 4 && t128 >= most) ? 3 : 4;
   if (g.epi & EPI_SEGACC) tile = 0;
   if (tile) return tile;

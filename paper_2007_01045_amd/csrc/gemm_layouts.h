@@ -64,8 +64,12 @@ static hipError_t launch_tt(const GemmArgs& g, const GemmLaunch& l, LaunchMfma p
       }
     }
   switch (l.tile) {
-    case 1: return launch_mfma<256, 256, 2, 4, 4, true, true, 32, PACK>(g, l, packed);
-    case 2: return launch_mfma<256, 128, 4, 2, 3, true, true, 64, PACK>(g, l, packed);
+    case 1:
+      return bsum ? launch_mfma<256, 256, 2, 4, 4, true, true, 32, PACK, true>(g, l, packed)
+                  : launch_mfma<256, 256, 2, 4, 4, true, true, 32, PACK>(g, l, packed);
+    case 2:
+      return bsum ? launch_mfma<256, 128, 4, 2, 3, true, true, 64, PACK, true>(g, l, packed)
+                  : launch_mfma<256, 128, 4, 2, 3, true, true, 64, PACK>(g, l, packed);
     case 3:
       return bsum ? launch_mfma<128, 128, 2, 4, 2, true, true, 64, PACK, true>(g, l, packed)
                   : launch_mfma<128, 128, 2, 4, 2, true, true, 64, PACK>(g, l, packed);

@@ -143,6 +143,14 @@ def test_what_is_not_wanted(dtype, kw):
         c.check()
 
 
+@pytest.mark.parametrize("accumulate", [0, 1])
+def test_large_weight_gradients(accumulate):
+    # tiles of 256x256 and of 256x128, with rests in every direction
+    c = Case(BF, 75, 1912, 4360, accumulate=accumulate)
+    c.run()
+    c.check()
+
+
 def test_fp32_only_shapes():
     # multiples of four
     for shape in ((3, 12, 20), (77, 100, 36), (513, 260, 132)):
