@@ -3,8 +3,8 @@
 //   dh = dy Wo^T,  du = dh act(g),  dg = dh u act'(g),  dx = [dg du] [Wg Wu]^T,  dW = x^T [dg du],  dWo = h^T dy, biases: column sums
 // bf16: h leaves the product that makes g and u, dg and du the one that makes dh (gemm_gate.hip); the others are products as the
 // encoder layers have them.  Bound by the matrix cores, 6 T H F flops forward and 12 backward; few rows by reading the weights.
-// fp32: the fp32 matrix rate is a fifteenth of the bf16 one and a pass over [T, 2F] is small beside such a product, so the
-// activations are passes of their own.
+// fp32: the same shape where the products have tiles enough (gated_ffn_f32.hip); with fewer of them they go to the kernels that
+// split K over a workgroup's waves (gemm_f32.hip), and the activations are passes of their own.
 #include "device_common.h"
 #include "kernels.h"
 
@@ -105,6 +105,7 @@ static unsigned pass_blocks(long n) { return (unsigned)((n + 255) / 256 < 65536 
 
 hipError_t launch_gated_ffn_fwd(Dtype dt, const GatedFfnArgs& a, hipStream_t st) {
   hipError_t e;
+  const RingPlan ring = dt == DT_F32 ? gated_ffn_f32_plan(a) : RingPlan{};
   if (dt == DT_BF16) {
     GemmArgs g = fwd_in(a, a.h, a.F);
     g.N = a.F;
@@ -113,6 +114,8 @@ hipError_t launch_gated_ffn_fwd(Dtype dt, const GatedFfnArgs& a, hipStream_t st)
     with_bias(g, a.b_in);
     if (a.silu) g.epi |= EPI_SILU;
     e = launch_gate_fwd(g, st);
+  } else if (ring.in) {
+    e = launch_ring_f32_in(a, st);
   } else {
     const long n4 = (long)a.T * a.F / 4;
     if (a.gu) {
@@ -142,17 +145,20 @@ hipError_t launch_gated_ffn_fwd(Dtype dt, const GatedFfnArgs& a, hipStream_t st)
     }
   }
   if (e != hipSuccess) return e;
-  return launch_gemm(dt, fwd_out(a), st);
+  return ring.out ? launch_ring_f32_out(a, st) : launch_gemm(dt, fwd_out(a), st);
 }
 
 hipError_t launch_gated_ffn_bwd(Dtype dt, const GatedFfnArgs& a, void* workspace, hipStream_t st) {
   hipError_t e;
+  const RingPlan ring = dt == DT_F32 ? gated_ffn_f32_plan(a) : RingPlan{};
   if (dt == DT_BF16) {
     GemmArgs g = bwd_dh(a, a.dgu);
     g.aux = a.gu;
     g.ldaux = 2 * a.F;
     if (a.silu) g.epi |= EPI_SILU;
     e = launch_gate_bwd(g, st);
+  } else if (ring.dh) {
+    e = launch_ring_f32_dh(a, st);
   } else {
     const long n4 = (long)a.T * a.F / 4;
     e = launch_gemm(dt, bwd_dh(a, (float*)a.dgu + a.F), st);
@@ -160,8 +166,9 @@ hipError_t launch_gated_ffn_bwd(Dtype dt, const GatedFfnArgs& a, void* workspace
     hipLaunchKernelGGL(gate_pass_f32<Pass::GRAD>, dim3(pass_blocks(n4)), dim3(256), 0, st, (const float*)a.gu, (float*)a.dgu, n4, a.F / 4, a.silu);
     e = hipGetLastError();
   }
-  if (e == hipSuccess && a.dx) e = launch_gemm(dt, bwd_dx(a), st);
-  if (e != hipSuccess || !a.dw_in) return e;
+  if (e == hipSuccess && a.dx && !ring.dx) e = launch_gemm(dt, bwd_dx(a), st);
+  if (e == hipSuccess && (ring.dx || ring.dw)) e = launch_ring_f32_grads(a, ring, st);
+  if (e != hipSuccess || !a.dw_in || ring.dw) return e;
   GemmArgs win = bwd_dw(a, true, nullptr), wout = bwd_dw(a, false, nullptr);
   if (dt == DT_BF16) win.tile = dw_tile(win), wout.tile = dw_tile(wout);
   if (a.accumulate && !win.tile && !wout.tile) {   // both in one launch

@@ -163,6 +163,15 @@ hipError_t launch_gated_ffn_bwd(Dtype dt, const GatedFfnArgs& a, void* workspace
 // its two products with an activation in the epilogue, bf16 (gemm_gate.hip; arguments: GATE of gemm_mfma_tile)
 hipError_t launch_gate_fwd(const GemmArgs& g, hipStream_t st);
 hipError_t launch_gate_bwd(const GemmArgs& g, hipStream_t st);
+// the fp32 block's products with tiles enough for the kernels of gated_ffn_f32.hip: h and gu; y; dgu; dx and the weights' gradients
+struct RingPlan {
+  bool in, out, dh, dx, dw;
+};
+RingPlan gated_ffn_f32_plan(const GatedFfnArgs& a);
+hipError_t launch_ring_f32_in(const GatedFfnArgs& a, hipStream_t st);
+hipError_t launch_ring_f32_out(const GatedFfnArgs& a, hipStream_t st);
+hipError_t launch_ring_f32_dh(const GatedFfnArgs& a, hipStream_t st);
+hipError_t launch_ring_f32_grads(const GatedFfnArgs& a, const RingPlan& p, hipStream_t st);   // dx and dw as the plan has them
 
 // ---------------------------------------------------------------- attention
 // q,k,v,ctx,dq,dk,dv,dctx: [b*s, H] row-major, head h in columns [h*d, (h+1)*d).

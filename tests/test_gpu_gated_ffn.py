@@ -143,12 +143,23 @@ def test_what_is_not_wanted(dtype, kw):
         c.check()
 
 
+@pytest.mark.parametrize("dtype", [F32, BF])
 @pytest.mark.parametrize("accumulate", [0, 1])
-def test_large_weight_gradients(accumulate):
-    # tiles of 256x256 and of 256x128, with rests in every direction
-    c = Case(BF, 75, 1912, 4360, accumulate=accumulate)
+def test_large_weight_gradients(dtype, accumulate):
+    # bf16: tiles of 256x256 and of 256x128, with rests in every direction
+    c = Case(dtype, 75, 1912, 4360, accumulate=accumulate)
     c.run()
     c.check()
+
+
+@pytest.mark.parametrize("shape", [(2100, 1604, 1212), (1002, 772, 1020), (645, 1028, 1036), (700, 1036, 4), (1, 4, 5124), (2570, 36, 516)],
+                         ids=lambda s: "-".join(map(str, s)))
+def test_fp32_tiles(shape):
+    # large and small tiles, each with rests in every direction; products with a step or less of depth
+    for kw in (dict(), dict(act=B.ACT_GELU, pad=4, accumulate=1), dict(bias=False, dx=False), dict(keep=False, bias=False), dict(dw=False)):
+        c = Case(F32, *shape, **kw)
+        c.run()
+        c.check()
 
 
 def test_fp32_only_shapes():
