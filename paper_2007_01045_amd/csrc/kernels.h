@@ -236,7 +236,7 @@ struct AttnWinArgs {
   const int32_t* lens;           // NULL: s each
   const void* dctx;
   void *dq, *dk, *dv;
-  float *delta, *partial;        // (of the workspace)
+  float *delta, *partial;        // (of the workspace; delta negated)
   int b, s, A, Ak, d, W, S, causal;
   int ldq, ldk, ldv, ldc, lddc, lddq, lddk, lddv;
   float scale;
