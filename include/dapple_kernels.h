@@ -124,7 +124,8 @@ int dapple_colsum_static(int dtype, const void* X, int rows, int cols, int ld, f
 /* ------------------------------------------------------------------ operators of layers and training steps
  * Checked on the host before anything is enqueued: a refused call returns STAGE_E_NULL or STAGE_E_CONFIG and
  * stage_last_error() says why.  Nothing is allocated and nothing waited for; results are the same bits from call to call;
- * every call can be captured into a HIP graph (after one eager call of the same kind).  `workspace` is device memory of
+ * every call can be captured into a HIP graph (after one eager call of the same kind).  The calling thread's current device is the
+ * stream's.  `workspace` is device memory of
  * the size that the operator's *_workspace function returns (host only; a negative code for a call that would be refused),
  * 16-byte aligned, whose contents do not matter before or after: calls that may overlap need one each. */
 
@@ -139,8 +140,8 @@ int dapple_colsum_static(int dtype, const void* X, int rows, int cols, int ld, f
  * accuracy where gradients are sums of many layers').
  * bwd: dq, dk, dv from dctx and the ctx, ctx32 (or NULL) and lse of fwd; dk and dv are summed over the heads that share them.
  * scale > 0; 0 = 1/sqrt(d).  Row strides in elements, 0 = dense; q, k, v may be columns of one buffer, and dq, dk, dv of another;
- * outputs overlap no input.  bf16: d and strides multiples of 8; fp32: of 4; d <= 128, strides below 2^23, s * stride below 2^30 - 4096;
- * all tensors 16-byte aligned.  Probabilities and dS are rounded once to bf16 in bf16 calls, for their products. */
+ * outputs overlap no input.  bf16: d and strides multiples of 8; fp32: of 4; d <= 128, strides below 2^23, s * stride below 2^30 - 4096,
+ * b * s below 2^26, b * Ak below 2^16, b * A * ceil(s / 32) below 2^23; all tensors 16-byte aligned.  Probabilities and dS are rounded once to bf16 in bf16 calls, for their products. */
 typedef struct {
   const void* q;
   const void* k;
@@ -170,10 +171,10 @@ int dapple_attention_window_bwd(int dtype, const dapple_attention_window_desc* d
  *     interleaved = 0: pair i is columns i and i + rot/2;   1: columns 2i and 2i + 1
  *   columns from rot on are n's.  rot = 0: no rotation (table is not looked at).
  * table: fp32 [max_pos][rot/2][2], as dapple_rope_table or the caller makes it.  positions: int32 [rows], NULL = r % seq (seq 0:
- * r); a position outside [0, max_pos) reads nothing and gives NaN in the columns that turn.
+ * r); a position outside [0, max_pos) reads nothing and gives NaN in the columns that turn (backward: and in dgamma).
  * Types: q, k, gammas and outputs of dtype; table, dgamma and all arithmetic fp32.  Row strides in elements, 0 = dense.  An
  * output may be its input (yq = q with ldyq = ldq, dq = dyq, ...), else they do not overlap.  Limits: d <= 256, rot even and <= d,
- * rows >= 1; interleaved needs d and the strides even and addresses aligned to two elements; everything aligned to 16 bytes
+ * 1 <= rows < 2^26; interleaved needs d and the strides even and addresses aligned to two elements; everything aligned to 16 bytes
  * (d, rot/2 or interleaved rot, strides, addresses) is fastest.
  * Backward: dyq, dyk in, dq, dk out (q and k are read only with gammas), dgamma_q, dgamma_k [d] fp32: set, or with accumulate != 0
  * added to; NULL = not wanted.  workspace only where a dgamma is wanted. */
@@ -203,7 +204,8 @@ int dapple_qk_rope_bwd(int dtype, const dapple_qk_rope_desc* d, void* stream);
 /* table[p][i] = magnitude * (cos, sin)(p * f_i), i < rot/2, angles and functions in 64 bits.  With w_i = base^(-2i/rot):
  *   factor = 1: f_i = w_i;   original = 0: f_i = w_i / factor (positions interpolated)
  *   original > 0, the context that the model was trained on: by parts, f_i = w_i (g + (1 - g) / factor), g = 0 for pairs that turn
- *   at most `low` times within it, 1 from `high` times on, linear in the turns between. */
+ *   at most `low` times within it, 1 from `high` times on, linear in the turns between.
+ * rot even and at most 256, max_pos * rot below 2^31. */
 int dapple_rope_table(float* table, int max_pos, int rot, double base, double factor, int original, double low, double high,
                       double magnitude, void* stream);
 

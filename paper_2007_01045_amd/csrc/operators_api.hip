@@ -28,8 +28,10 @@ static int win_args(int dtype, const dapple_attention_window_desc* d, bool bwd, 
   if (!(d->scale >= 0.f) || !std::isfinite(d->scale)) return set_error(STAGE_E_CONFIG, "scale must be positive and finite (0: 1/sqrt(d))");
   const int v = dtype == STAGE_DTYPE_BF16 ? 8 : 4;
   if (d->d % v || d->d > 128) return set_error(STAGE_E_CONFIG, "heads of %d columns: multiples of %d up to 128 are taken", d->d, v);
-  if ((long)d->b * d->s > 0x7fffffffL || (long)d->b * d->A * ((d->s + 31) / 32) > 0x3fffffffL || (long)d->b * d->A > 0x7fffffffL)
-    return set_error(STAGE_E_CONFIG, "more than 2^31 rows or 2^30 workgroups");
+  // (a launch has 2^32 work-items at most: 512 to 32 rows of a head, 64 to a row)
+  if (d->s >= 1 << 27 || (long)d->b * d->s >= 1L << 26 || (long)d->b * d->A >= 1L << 23 || (long)d->b * d->A * ((d->s + 31) / 32) >= 1L << 23 ||
+      (long)d->b * d->Ak >= 1L << 16)
+    return set_error(STAGE_E_CONFIG, "2^26 rows, 2^16 key heads of all sequences or 2^23 times 32 rows of a head and more");
   a.b = d->b; a.s = d->s; a.A = d->A; a.Ak = d->Ak; a.d = d->d; a.causal = d->causal != 0;
   a.W = d->window < d->s ? d->window : 0;   // (a window of s positions and more hides nothing)
   a.S = d->sinks < d->s ? d->sinks : d->s;
@@ -84,6 +86,7 @@ static int rope_args(int dtype, const dapple_qk_rope_desc* d, bool bwd, bool wor
   if (bad_dtype(dtype)) return set_error(STAGE_E_CONFIG, "dtype %d", dtype);
   if (d->rows < 1 || d->A < 1 || d->Ak < 0 || d->d < 1 || d->d > 256)
     return set_error(STAGE_E_CONFIG, "rows %d, heads %d and %d of %d columns (at most 256)", d->rows, d->A, d->Ak, d->d);
+  if (d->rows >= 1 << 26) return set_error(STAGE_E_CONFIG, "2^26 rows and more");   // (a launch has 2^32 work-items at most)
   if (workspace_only) return STAGE_OK;
   if (d->rot < 0 || d->rot % 2 || d->rot > d->d) return set_error(STAGE_E_CONFIG, "%d of %d columns to turn", d->rot, d->d);
   if (d->seq < 0 || (d->rot && d->max_pos < 1)) return set_error(STAGE_E_CONFIG, "seq %d, max_pos %d", d->seq, d->max_pos);
@@ -150,7 +153,7 @@ int dapple_qk_rope_bwd(int dtype, const dapple_qk_rope_desc* d, void* stream) {
 int dapple_rope_table(float* table, int max_pos, int rot, double base, double factor, int original, double low, double high,
                       double magnitude, void* stream) {
   if (!table) return set_error(STAGE_E_NULL, "table is NULL");
-  if (max_pos < 1 || rot < 2 || rot % 2 || rot > 256) return set_error(STAGE_E_CONFIG, "max_pos %d, rot %d", max_pos, rot);
+  if (max_pos < 1 || rot < 2 || rot % 2 || rot > 256 || (long)max_pos * rot > 0x7fffffffL) return set_error(STAGE_E_CONFIG, "max_pos %d, rot %d", max_pos, rot);
   if (!(base > 0) || !std::isfinite(base) || !(factor > 0) || !std::isfinite(factor) || !std::isfinite(magnitude) || original < 0 ||
       (original > 0 && !(low < high && std::isfinite(low) && std::isfinite(high))))
     return set_error(STAGE_E_CONFIG, "base and factor must be positive and finite, low below high");

@@ -134,3 +134,17 @@ def test_gated_ffn_refusals():
     refused(conf, B.dapple_gated_ffn_workspace, B.DTYPE_BF16, B.gated_ffn_desc(**dict(ok, F=12)))
     for dt in (B.DTYPE_F32, B.DTYPE_BF16):
         assert B.dapple_gated_ffn_workspace(dt, B.gated_ffn_desc(**ok)) > 0
+
+
+def test_sizes_beyond_a_launch():
+    # 2^32 work-items; workspaces and tensors of these sizes are conceivable, so they are refused before anything is enqueued
+    rope = dict(q=P, k=P, gamma_q=P, gamma_k=P, table=P, yq=P, yk=P, dyq=P, dyk=P, dq=P, dk=P, workspace=P, rows=1 << 26, A=1, Ak=1, d=8, rot=8,
+                max_pos=16)
+    for f in (B.dapple_qk_rope_fwd, B.dapple_qk_rope_bwd, B.dapple_qk_rope_workspace):
+        refused(B.STAGE_E_CONFIG, f, B.DTYPE_BF16, B.qk_rope_desc(**rope))
+    refused(B.STAGE_E_CONFIG, B.dapple_rope_table, P, 1 << 24, 256)
+    attn = dict(q=P, k=P, v=P, ctx=P, lse=P, dctx=P, dq=P, dk=P, dv=P, workspace=P, d=8)
+    for sizes in (dict(b=1 << 16, s=1 << 10, A=1, Ak=1), dict(b=1 << 16, s=1, A=2, Ak=1), dict(b=1 << 8, s=1 << 15, A=32, Ak=1),
+                  dict(b=1, s=1 << 27, A=1, Ak=1), dict(b=0x7fffffff, s=0x7fffffff, A=0x7fffffff, Ak=1)):
+        for f in (B.dapple_attention_window_fwd, B.dapple_attention_window_bwd, B.dapple_attention_window_workspace):
+            refused(B.STAGE_E_CONFIG, f, B.DTYPE_BF16, B.attention_window_desc(**attn, **sizes))
