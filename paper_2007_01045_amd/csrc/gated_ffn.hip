@@ -113,7 +113,7 @@ hipError_t launch_gated_ffn_fwd(Dtype dt, const GatedFfnArgs& a, hipStream_t st)
     g.ldaux = 2 * a.F;
     with_bias(g, a.b_in);
     if (a.silu) g.epi |= EPI_SILU;
-    e = launch_gate_fwd(g, st);
+    e = gemm_rows_takes(g, true) ? launch_rows_gate_fwd(g, st) : launch_gate_fwd(g, st);
   } else if (ring.in) {
     e = launch_ring_f32_in(a, st);
   } else {
@@ -145,7 +145,8 @@ hipError_t launch_gated_ffn_fwd(Dtype dt, const GatedFfnArgs& a, hipStream_t st)
     }
   }
   if (e != hipSuccess) return e;
-  return ring.out ? launch_ring_f32_out(a, st) : launch_gemm(dt, fwd_out(a), st);
+  if (ring.out) return launch_ring_f32_out(a, st);
+  return dt == DT_BF16 && gemm_rows_takes(fwd_out(a), false) ? launch_rows(fwd_out(a), st) : launch_gemm(dt, fwd_out(a), st);
 }
 
 hipError_t launch_gated_ffn_bwd(Dtype dt, const GatedFfnArgs& a, void* workspace, hipStream_t st) {
@@ -156,7 +157,7 @@ hipError_t launch_gated_ffn_bwd(Dtype dt, const GatedFfnArgs& a, void* workspace
     g.aux = a.gu;
     g.ldaux = 2 * a.F;
     if (a.silu) g.epi |= EPI_SILU;
-    e = launch_gate_bwd(g, st);
+    e = gemm_rows_takes(g, false) ? launch_rows_gate_bwd(g, st) : launch_gate_bwd(g, st);
   } else if (ring.dh) {
     e = launch_ring_f32_dh(a, st);
   } else {
@@ -166,7 +167,7 @@ hipError_t launch_gated_ffn_bwd(Dtype dt, const GatedFfnArgs& a, void* workspace
     hipLaunchKernelGGL(gate_pass_f32<Pass::GRAD>, dim3(pass_blocks(n4)), dim3(256), 0, st, (const float*)a.gu, (float*)a.dgu, n4, a.F / 4, a.silu);
     e = hipGetLastError();
   }
-  if (e == hipSuccess && a.dx && !ring.dx) e = launch_gemm(dt, bwd_dx(a), st);
+  if (e == hipSuccess && a.dx && !ring.dx) e = dt == DT_BF16 && gemm_rows_takes(bwd_dx(a), false) ? launch_rows(bwd_dx(a), st) : launch_gemm(dt, bwd_dx(a), st);
   if (e == hipSuccess && (ring.dx || ring.dw)) e = launch_ring_f32_grads(a, ring, st);
   if (e != hipSuccess || !a.dw_in || ring.dw) return e;
   GemmArgs win = bwd_dw(a, true, nullptr), wout = bwd_dw(a, false, nullptr);

@@ -163,6 +163,11 @@ hipError_t launch_gated_ffn_bwd(Dtype dt, const GatedFfnArgs& a, void* workspace
 // its two products with an activation in the epilogue, bf16 (gemm_gate.hip; arguments: GATE of gemm_mfma_tile)
 hipError_t launch_gate_fwd(const GemmArgs& g, hipStream_t st);
 hipError_t launch_gate_bwd(const GemmArgs& g, hipStream_t st);
+// the same, and products with a bias or none, of so few rows that reading the weights is the time
+bool gemm_rows_takes(const GemmArgs& g, bool gate);
+hipError_t launch_rows_gate_fwd(const GemmArgs& g, hipStream_t st);
+hipError_t launch_rows_gate_bwd(const GemmArgs& g, hipStream_t st);
+hipError_t launch_rows(const GemmArgs& g, hipStream_t st);
 // the fp32 block's products with tiles enough for the kernels of gated_ffn_f32.hip: h and gu; y; dgu; dx and the weights' gradients
 struct RingPlan {
   bool in, out, dh, dx, dw;

@@ -143,6 +143,16 @@ def test_what_is_not_wanted(dtype, kw):
         c.check()
 
 
+@pytest.mark.parametrize("shape", [(16, 40, 2048), (13, 64, 2056), (32, 72, 4168), (29, 4104, 16), (2, 4104, 8), (17, 64, 64)],
+                         ids=lambda s: "-".join(map(str, s)))
+def test_few_rows(shape):
+    # depths of more and of less than a wave's part, columns that end inside sixteen
+    for kw in (dict(pad=8), dict(act=B.ACT_GELU, bias=False), dict(keep=False)):
+        c = Case(BF, *shape, **kw)
+        c.run()
+        c.check()
+
+
 @pytest.mark.parametrize("dtype", [F32, BF])
 @pytest.mark.parametrize("accumulate", [0, 1])
 def test_large_weight_gradients(dtype, accumulate):
