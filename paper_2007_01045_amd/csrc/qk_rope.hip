@@ -220,19 +220,22 @@ __global__ __launch_bounds__(256) void qk_rope_fwd_kernel(QkRopeArgs a, int G, i
 }
 
 // Rows w, w + waves, ... per wave, all of them for the queries, then for the keys (in one walk the two gammas' sums would stand in
-// registers side by side, and three waves of a SIMD in the place of four: 249 -> 211 us for 32768 rows, 32 + 8 heads of 128).  A lane's sums for dgamma stay in registers
+// registers side by side, and three waves of a SIMD in the place of four: 249 -> 209 us for 32768 rows, 32 + 8 heads of 128).  A lane's sums for dgamma stay in registers
 // over all of its rows and heads; the workgroup's lanes of one unit are added in a fixed order, partial[block][q, k][d].
+// Where a wave has one row, workgroups of their own take the keys (gridDim = 2 blocks): nothing but latencies would stand between
+// the two walks (3001 rows, 12 + 4 heads of 64 in fp32 14.1 -> 11.2 us).
 template <typename T, int V, bool HALF, int NU>
-__global__ __launch_bounds__(256, V * NU <= 4 ? 1 : 4) void qk_rope_bwd_kernel(QkRopeArgs a, int G, float* __restrict__ partial) {
+__global__ __launch_bounds__(256, V * NU <= 4 ? 1 : 4) void qk_rope_bwd_kernel(QkRopeArgs a, int G, int blocks, float* __restrict__ partial) {
   __shared__ float red[256][NU * 2 * V + 1];
   const int lane = threadIdx.x & 63, per = 64 / G;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   Units<V, HALF, NU> un;
   un.init(a.d, a.rot, lane % G, G);
   const float inv_d = 1.0f / (float)a.d;
-  const bool norm = a.gamma_q != nullptr;
+  const bool norm = a.gamma_q != nullptr, apart = (int)gridDim.x > blocks;
+  const int block = (int)blockIdx.x < blocks ? blockIdx.x : blockIdx.x - blocks;
 #pragma unroll 1
-  for (int t = 0; t < 2; ++t) {
+  for (int t = (int)blockIdx.x < blocks ? 0 : 1; t < 2; ++t) {
     const int heads = t ? a.Ak : a.A;
     const long ldx = t ? a.ldk : a.ldq, lddy = t ? a.lddyk : a.lddyq, lddx = t ? a.lddk : a.lddq;
     const T *X = (const T*)(t ? a.k : a.q), *DY = (const T*)(t ? a.dyk : a.dyq), *gam = (const T*)(t ? a.gamma_k : a.gamma_q);
@@ -246,7 +249,7 @@ __global__ __launch_bounds__(256, V * NU <= 4 ? 1 : 4) void qk_rope_bwd_kernel(Q
         for (int e = 0; e < V; ++e) dg[i][k][e] = g[i][k][e] = 0.f;
         if (norm && heads > 0 && un.off[i][k] >= 0) load_chunk<T, V>(gam + un.off[i][k], g[i][k]);
       }
-    for (long row = (long)blockIdx.x * 4 + wave; heads > 0 && row < a.rows; row += (long)gridDim.x * 4) {
+    for (long row = (long)block * 4 + wave; heads > 0 && row < a.rows; row += (long)blocks * 4) {
       float c[NU][V], s[NU][V];
       load_table<V, HALF, NU>(a, un, position_of(a, row), c, s);
       for (int h0 = 0; h0 < heads; h0 += per) {
@@ -296,7 +299,10 @@ __global__ __launch_bounds__(256, V * NU <= 4 ? 1 : 4) void qk_rope_bwd_kernel(Q
             if (h < heads && un.off[i][k] >= 0) store_chunk<T, V>(DX + row * lddx + h * a.d + un.off[i][k], y[i][k]);
       }
     }
-    if (!partial) continue;   // (no dgamma is wanted: the whole grid)
+    if (!partial) {   // (no dgamma is wanted: the whole grid)
+      if (apart) return;
+      continue;
+    }
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < NU; ++i)
@@ -313,33 +319,33 @@ __global__ __launch_bounds__(256, V * NU <= 4 ? 1 : 4) void qk_rope_bwd_kernel(Q
       float sum = 0.f;
       for (int r = u; r < 256; r += G) sum += red[r][j];
       const int off = i == 0 ? (k ? other.off[0][1] : other.off[0][0]) : (k ? other.off[NU - 1][1] : other.off[NU - 1][0]);
-      if (off >= 0) partial[((long)blockIdx.x * 2 + t) * a.d + off + e] = sum;
+      if (off >= 0) partial[((long)block * 2 + t) * a.d + off + e] = sum;
     }
+    if (apart) return;
   }
 }
 
-// dgamma from the workgroups' sums: 64 columns per workgroup, its waves add every 16th block in ascending order
+// dgamma from the workgroups' sums: 16 columns per workgroup, 64 slices of the blocks (every 64th, ascending), so that all of a
+// lane's requests are in flight; the slices in a fixed order: the four of a wave by twos, then the waves
 __global__ __launch_bounds__(1024) void qk_rope_dgamma_kernel(const float* __restrict__ partial, int blocks, int d, float* dgq, float* dgk,
                                                               int accumulate) {
-  __shared__ float red[16][64];
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
-  float t = 0.f;
+  __shared__ float red[16][16];
+  const int t = threadIdx.x & 15, slice = threadIdx.x >> 4, c = blockIdx.x * 16 + t;
+  float s = 0.f;
   if (c < 2 * d) {
-    int b = w;
-    for (; b + 7 * 16 < blocks; b += 8 * 16) {
-      float x[8];
+    float x[16];   // (at most 1024 blocks: see qk_rope_blocks)
 #pragma unroll
-      for (int u = 0; u < 8; ++u) x[u] = partial[(long)(b + 16 * u) * 2 * d + c];
+    for (int u = 0; u < 16; ++u) x[u] = slice + 64 * u < blocks ? partial[(long)(slice + 64 * u) * 2 * d + c] : 0.f;
 #pragma unroll
-      for (int u = 0; u < 8; ++u) t += x[u];
-    }
-    for (; b < blocks; b += 16) t += partial[(long)b * 2 * d + c];
+    for (int u = 0; u < 16; ++u) s += x[u];
   }
-  red[w][lane] = t;
+  s += __shfl_xor(s, 16, 64);
+  s += __shfl_xor(s, 32, 64);
+  if ((threadIdx.x & 63) < 16) red[threadIdx.x >> 6][t] = s;
   __syncthreads();
-  if (w == 0 && c < 2 * d) {
-    float r = red[0][lane];
-    for (int i = 1; i < 16; ++i) r += red[i][lane];
+  if (threadIdx.x < 16 && c < 2 * d) {
+    float r = red[0][t];
+    for (int i = 1; i < 16; ++i) r += red[i][t];
     float* const out = c < d ? dgq : dgk;
     if (out) out[c < d ? c : c - d] = accumulate ? out[c < d ? c : c - d] + r : r;
   }
@@ -434,12 +440,12 @@ hipError_t launch_qk_rope_bwd(Dtype dt, const QkRopeArgs& a, float* partial, hip
   const int blocks = qk_rope_blocks(a.rows);
   const bool sums = a.dgamma_q || a.dgamma_k;
   const hipError_t e = pick(dt, a, true, [&](auto t, auto V, auto HALF, auto NU, int G) {
-    hipLaunchKernelGGL((qk_rope_bwd_kernel<decltype(t), decltype(V)::value, decltype(HALF)::value, decltype(NU)::value>), dim3(blocks),
-                       dim3(256), 0, st, a, G, sums ? partial : nullptr);
+    hipLaunchKernelGGL((qk_rope_bwd_kernel<decltype(t), decltype(V)::value, decltype(HALF)::value, decltype(NU)::value>), dim3(a.Ak > 0 && a.rows <= 4 * blocks ? 2 * blocks : blocks),
+                       dim3(256), 0, st, a, G, blocks, sums ? partial : nullptr);
     return hipGetLastError();
   });
   if (e != hipSuccess || !sums) return e;
-  hipLaunchKernelGGL(qk_rope_dgamma_kernel, dim3((2 * a.d + 63) / 64), dim3(1024), 0, st, partial, blocks, a.d, a.dgamma_q, a.dgamma_k,
+  hipLaunchKernelGGL(qk_rope_dgamma_kernel, dim3((2 * a.d + 15) / 16), dim3(1024), 0, st, partial, blocks, a.d, a.dgamma_q, a.dgamma_k,
                      a.accumulate);
   return hipGetLastError();
 }
