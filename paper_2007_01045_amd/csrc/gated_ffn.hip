@@ -99,7 +99,9 @@ bool gated_ffn_takes(Dtype dt, const GatedFfnArgs& a, bool bwd) {
   return takes(bwd_dh(a, a.dgu)) && (!a.dx || takes(bwd_dx(a))) && (!a.dw_in || (takes(bwd_dw(a, true, &some)) && takes(bwd_dw(a, false, &some))));
 }
 
-int64_t gated_ffn_workspace(Dtype dt, const GatedFfnArgs& a) { return dt == DT_BF16 && !a.accumulate ? 4 * (2L * a.F + a.H) : 16; }
+int64_t gated_ffn_workspace(Dtype dt, const GatedFfnArgs& a) {
+  return dt == DT_F32 ? gated_ffn_f32_workspace(a) : a.accumulate ? 16 : 4 * (2L * a.F + a.H);
+}
 
 static unsigned pass_blocks(long n) { return (unsigned)((n + 255) / 256 < 65536 ? (n + 255) / 256 : 65536); }
 
@@ -168,7 +170,7 @@ hipError_t launch_gated_ffn_bwd(Dtype dt, const GatedFfnArgs& a, void* workspace
     e = hipGetLastError();
   }
   if (e == hipSuccess && a.dx && !ring.dx) e = dt == DT_BF16 && gemm_rows_takes(bwd_dx(a), false) ? launch_rows(bwd_dx(a), st) : launch_gemm(dt, bwd_dx(a), st);
-  if (e == hipSuccess && (ring.dx || ring.dw)) e = launch_ring_f32_grads(a, ring, st);
+  if (e == hipSuccess && (ring.dx || ring.dw)) e = launch_ring_f32_grads(a, ring, workspace, st);
   if (e != hipSuccess || !a.dw_in || ring.dw) return e;
   GemmArgs win = bwd_dw(a, true, nullptr), wout = bwd_dw(a, false, nullptr);
   if (dt == DT_BF16) win.tile = dw_tile(win), wout.tile = dw_tile(wout);

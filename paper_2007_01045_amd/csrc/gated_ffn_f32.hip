@@ -309,13 +309,57 @@ __global__ __launch_bounds__(64 * T::NW, 2) void ring_f32_kernel(RingProduct g) 
 }
 // dx = [dg du] [Wg Wu]^T, its tiles from dx0 on, and the weights' gradients, in one launch: neither waits for the other, and alone
 // each leaves units without a tile (T = 1000, H = 768, F = 2040: 97 + 75 + 55 us as launches of gemm_f32.hip, 165 together)
+// Few tiles of many rows have their depth cut into parts, whose sums go to the workspace (T = 8000, H = 256, F = 512: 96 tiles in five
+// parts 239 -> 145 us for the whole backward).
+struct GradTasks {
+  int dx0, ndx, nin, nout;   // tiles
+  int parts, chunk;          // of the weights' depth
+  float* partial;            // a part: dw_in, dw_out, db_in, db_out
+};
 template <typename T>
-__global__ __launch_bounds__(64 * T::NW, 2) void ring_f32_grads(RingProduct dx, RingProduct in, RingProduct out, int dx0, int ndx, int nin) {
+__global__ __launch_bounds__(64 * T::NW, 2) void ring_f32_grads(RingProduct dx, RingProduct in, RingProduct out, GradTasks w) {
   int b = blockIdx.x;
-  if (b >= dx0 && b < dx0 + ndx) return ring_tile<T, false, false, 0, false>(dx, b - dx0);
-  b -= b < dx0 ? 0 : ndx;
-  if (b < nin) ring_tile<T, true, true, 0, true>(in, b);
-  else ring_tile<T, true, true, 0, true>(out, b - nin);
+  if (b >= w.dx0 && b < w.dx0 + w.ndx) return ring_tile<T, false, false, 0, false>(dx, b - w.dx0);
+  b -= b < w.dx0 ? 0 : w.ndx;
+  const int per = w.nin + w.nout;
+  auto run = [&](RingProduct& g, int tile, long at, long sum_at) __attribute__((always_inline)) {
+    if (w.parts > 1) {
+      const int part = b / per, k0 = part * w.chunk;
+      float* const P = w.partial + part * ((long)in.M * in.N + (long)out.M * out.N + in.N + out.N);
+      g.A += (long)k0 * g.lda;
+      g.B += (long)k0 * g.ldb;
+      g.K = min(w.chunk, g.K - k0);
+      g.C = P + at;
+      g.ldc = g.N;
+      g.bsum = g.bsum ? P + sum_at : nullptr;
+      g.add = false;
+    }
+    ring_tile<T, true, true, 0, true>(g, tile);
+  };
+  const long nw = (long)in.M * in.N, no = (long)out.M * out.N;
+  if (b % per < w.nin) run(in, b % per, 0, nw + no);
+  else run(out, b % per - w.nin, nw, nw + no + in.N);
+}
+
+// the parts' sums, in ascending order: [0, n0) of dw_in, then dw_out, db_in, db_out (sizes multiples of four; NULL: not wanted)
+struct GradSums {
+  float* to[4];
+  long n[4];
+};
+__global__ __launch_bounds__(256) void ring_f32_join(const float* __restrict__ partial, int parts, GradSums s, bool add) {
+  const long all = s.n[0] + s.n[1] + s.n[2] + s.n[3], i = ((long)blockIdx.x * 256 + threadIdx.x) * 4;
+  if (i >= all) return;
+  float* to = nullptr;
+  long first = 0;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    if (i >= first && i < first + s.n[k] && s.to[k]) to = s.to[k] + (i - first);
+    first += s.n[k];
+  }
+  if (!to) return;
+  f32x4 t = *(const f32x4*)(partial + i);
+  for (int p = 1; p < parts; ++p) t += *(const f32x4*)(partial + p * all + i);
+  *(f32x4*)to = add ? *(const f32x4*)to + t : t;
 }
 
 
@@ -342,15 +386,33 @@ static hipError_t launch_dx(const RingProduct& g, hipStream_t st) {
   return large(g.M, g.N, 1) ? launch_one<Large, false, false, 0>(g, st) : launch_one<Small, false, false, 0>(g, st);
 }
 template <typename T>
-static hipError_t launch_grads(const RingProduct& dx, const RingProduct& in, const RingProduct& out, hipStream_t st) {
-  const long a = dx.C ? tiles(dx.M, dx.N, T::BM, T::BN) : 0, b = tiles(in.M, in.N, T::BM, T::BN), c = tiles(out.M, out.N, T::BM, T::BN);
-  return launch<ring_f32_grads<T>, T>(a + b + c, st, dx, in, out, dx.K > in.K ? 0 : (int)(b + c), (int)a, (int)b);   // (the deeper tiles first)
+static hipError_t launch_grads(const RingProduct& dx, const RingProduct& in, const RingProduct& out, GradTasks w, hipStream_t st) {
+  w.ndx = dx.C ? (int)tiles(dx.M, dx.N, T::BM, T::BN) : 0;
+  w.nin = (int)tiles(in.M, in.N, T::BM, T::BN);
+  w.nout = (int)tiles(out.M, out.N, T::BM, T::BN);
+  const long dw = (long)w.parts * (w.nin + w.nout);
+  w.dx0 = dx.K > w.chunk ? 0 : (int)dw;   // (the deeper tiles first)
+  return launch<ring_f32_grads<T>, T>(dw + w.ndx, st, dx, in, out, w);
 }
 // Fewer tiles than these have their K split over the waves of small ones (gemm_f32.hip).  (A lane's offset inside a tile has 32 bits.)
 static bool enough(long t64, int ld0, int ld1) { return t64 >= 160 && ld0 <= 1 << 21 && ld1 <= 1 << 21; }
 
+// parts of the weights' gradients' depth: 512 rows at least each, of tiles that leave the 256 units without two of them
+static int grad_parts(const GatedFfnArgs& a) {
+  const long w = tiles(a.H, 2L * a.F, 64, 64) + tiles(a.F, a.H, 64, 64), most = a.T / 512 < 16 ? a.T / 512 : 16, want = 512 / w;
+  const long n = want < most ? want : most;
+  if (n < 2) return 1;
+  const int chunk = ((int)((a.T + n - 1) / n) + 31) / 32 * 32;
+  return (a.T + chunk - 1) / chunk;
+}
+static int grad_chunk(const GatedFfnArgs& a, int parts) { return parts == 1 ? a.T : ((a.T + parts - 1) / parts + 31) / 32 * 32; }
+int64_t gated_ffn_f32_workspace(const GatedFfnArgs& a) {
+  const int parts = grad_parts(a);
+  return parts == 1 ? 16 : 4L * parts * (3L * a.H * a.F + 2 * a.F + a.H);
+}
+
 RingPlan gated_ffn_f32_plan(const GatedFfnArgs& a) {
-  const long t = tiles(a.T, a.H, 64, 64), w = tiles(a.H, 2L * a.F, 64, 64) + tiles(a.F, a.H, 64, 64);
+  const long t = tiles(a.T, a.H, 64, 64), w = grad_parts(a) * (tiles(a.H, 2L * a.F, 64, 64) + tiles(a.F, a.H, 64, 64));
   const int lw = 2 * a.F > a.H ? 2 * a.F : a.H, ly = a.ldx > a.lddy ? a.ldx : a.lddy;
   RingPlan p{};
   p.in = enough(tiles(a.T, 2L * a.F, 64, 64), a.ldx, lw);
@@ -379,7 +441,7 @@ hipError_t launch_ring_f32_dh(const GatedFfnArgs& a, hipStream_t st) {
   g.M = a.T; g.N = a.F; g.K = a.H; g.silu = a.silu;
   return large(a.T, a.F, 1) ? launch_one<Large, false, false, 2>(g, st) : launch_one<Small, false, false, 2>(g, st);
 }
-hipError_t launch_ring_f32_grads(const GatedFfnArgs& a, const RingPlan& p, hipStream_t st) {
+hipError_t launch_ring_f32_grads(const GatedFfnArgs& a, const RingPlan& p, void* workspace, hipStream_t st) {
   RingProduct dx{}, in{}, out{};
   if (p.dx) {
     dx.A = (const float*)a.dgu; dx.lda = 2 * a.F; dx.B = (const float*)a.w_in; dx.ldb = 2 * a.F; dx.C = (float*)a.dx; dx.ldc = a.lddx;
@@ -390,11 +452,24 @@ hipError_t launch_ring_f32_grads(const GatedFfnArgs& a, const RingPlan& p, hipSt
   in.bsum = (float*)a.db_in; in.M = a.H; in.N = 2 * a.F; in.K = a.T; in.add = a.accumulate;
   out.A = (const float*)a.h; out.lda = a.F; out.B = (const float*)a.dy; out.ldb = a.lddy; out.C = (float*)a.dw_out; out.ldc = a.H;
   out.bsum = (float*)a.db_out; out.M = a.F; out.N = a.H; out.K = a.T; out.add = a.accumulate;
-  // two rounds of 128-wide tiles at least, and no tile deeper than an even share
+  GradTasks w{};
+  w.parts = grad_parts(a);
+  w.chunk = grad_chunk(a, w.parts);
+  w.partial = (float*)workspace;
+  if (w.parts > 1) {
+    hipError_t e = launch_grads<Small>(dx, in, out, w, st);
+    if (e != hipSuccess) return e;
+    const GradSums s{{in.C, out.C, in.bsum, out.bsum}, {(long)in.M * in.N, (long)out.M * out.N, in.N, out.N}};
+    const long n = s.n[0] + s.n[1] + s.n[2] + s.n[3];
+    hipLaunchKernelGGL(ring_f32_join, dim3((unsigned)((n / 4 + 255) / 256)), dim3(256), 0, st, w.partial, w.parts, s, in.add);
+    return hipGetLastError();
+  }
+  // 128-wide tiles in two rounds at least, none deeper than an even share: T = 4096, H = 1024, F = 4096 1593 us, 64-wide ones 1720;
+  // T = 2048 there 923, 858
   const long tdx = p.dx ? tiles(dx.M, dx.N, 128, 128) : 0, tdw = tiles(in.M, in.N, 128, 128) + tiles(out.M, out.N, 128, 128);
   const long deepest = dx.K > a.T ? dx.K : a.T;
-  const bool wide = tdx + tdw >= 1024 && tdx * dx.K + tdw * a.T >= 512 * deepest;
-  return wide ? launch_grads<Large>(dx, in, out, st) : launch_grads<Small>(dx, in, out, st);
+  if (tdx + tdw >= 1024 && tdx * dx.K + tdw * a.T >= 512 * deepest) return launch_grads<Large>(dx, in, out, w, st);
+  return launch_grads<Small>(dx, in, out, w, st);
 }
 
 }  // namespace dapple

@@ -173,10 +173,11 @@ struct RingPlan {
   bool in, out, dh, dx, dw;
 };
 RingPlan gated_ffn_f32_plan(const GatedFfnArgs& a);
+int64_t gated_ffn_f32_workspace(const GatedFfnArgs& a);
 hipError_t launch_ring_f32_in(const GatedFfnArgs& a, hipStream_t st);
 hipError_t launch_ring_f32_out(const GatedFfnArgs& a, hipStream_t st);
 hipError_t launch_ring_f32_dh(const GatedFfnArgs& a, hipStream_t st);
-hipError_t launch_ring_f32_grads(const GatedFfnArgs& a, const RingPlan& p, hipStream_t st);   // dx and dw as the plan has them
+hipError_t launch_ring_f32_grads(const GatedFfnArgs& a, const RingPlan& p, void* workspace, hipStream_t st);   // dx and dw as the plan has them
 
 // ---------------------------------------------------------------- attention
 // q,k,v,ctx,dq,dk,dv,dctx: [b*s, H] row-major, head h in columns [h*d, (h+1)*d).
