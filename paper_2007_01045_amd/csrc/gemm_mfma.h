@@ -697,7 +697,7 @@ __device__ __forceinline__ void gemm_mfma_tile(const GemmArgs& g, int tiles_m, i
 #pragma unroll
   for (int j = 0; j < NI; ++j) {
     const int col = n0 + wn0 + 32 * j + (lane & 31);
-    bsum0[j] = do_cs && lane < 32 && col < g.N ? bsum_ptr[col] : 0.f;
+    bsum0[j] = do_cs && lane < 32 && col < g.N && !(g.epi & EPI_BSUM_BF16) ? bsum_ptr[col] : 0.f;
   }
   if constexpr (EARLY && !GATE) {
     with_mode([&](auto MODE) __attribute__((always_inline)) {
@@ -899,7 +899,10 @@ __device__ __forceinline__ void gemm_mfma_tile(const GemmArgs& g, int tiles_m, i
 #pragma unroll
       for (int j = 0; j < NI; ++j) {
         const int col = n0 + wn0 + 32 * j + (lane & 31);
-        if (lane < 32 && col < g.N) bsum_ptr[col] = bsum0[j];
+        if (lane < 32 && col < g.N) {
+          if (g.epi & EPI_BSUM_BF16) ((bf16*)bsum_ptr)[col] = (bf16)bsum0[j];
+          else bsum_ptr[col] = bsum0[j];
+        }
       }
     }
   }

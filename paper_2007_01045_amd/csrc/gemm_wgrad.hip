@@ -14,7 +14,7 @@ struct TileTable {
   int first[WgradGroup::MAX + 1];   // first workgroup of each problem
 };
 
-template <int BM, int BN, int WGM, int WGN, int NS, int BK, bool SEG>
+template <int BM, int BN, int WGM, int WGN, int NS, int BK, bool SEG, bool SET>
 __global__ __launch_bounds__(64 * WGM * WGN, SEG ? 2 : 1) void wgrad_group_kernel(WgradGroup w, TileTable t) {
   if ((int)blockIdx.x >= t.first[w.n]) {   // behind the products' tiles: the sums
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
@@ -38,15 +38,15 @@ __global__ __launch_bounds__(64 * WGM * WGN, SEG ? 2 : 1) void wgrad_group_kerne
     }
   g.m_valid = g.M; g.n_valid = g.N; g.K = g.k_valid = w.K; g.kseg_len = w.kseg;
   g.segA = (long)w.kseg * g.lda; g.segB = (long)w.kseg * g.ldb;
-  g.epi = EPI_ACC32 | (g.bsum ? EPI_BSUM : 0);
+  g.epi = SET ? (g.bsum ? EPI_BSUM | EPI_BSUM_BF16 : 0) : EPI_ACC32 | (g.bsum ? EPI_BSUM : 0);
   gemm_mfma_tile<BM, BN, WGM, WGN, NS, true, true, BK, true, false, SEG>(g, (g.M + BM - 1) / BM, (g.N + BN - 1) / BN,
                                                                           blockIdx.x - first, 0);
 }
 
-template <int BM, int BN, int WGM, int WGN, int NS, int BK, bool SEG>
+template <int BM, int BN, int WGM, int WGN, int NS, int BK, bool SEG, bool SET = false>
 static hipError_t launch(const WgradGroup& w, hipStream_t st) {
   typedef GemmTile<BM, BN, WGM, WGN, NS, true, true, BK, false, SEG> CFG;
-  auto kern = wgrad_group_kernel<BM, BN, WGM, WGN, NS, BK, SEG>;
+  auto kern = wgrad_group_kernel<BM, BN, WGM, WGN, NS, BK, SEG, SET>;
   static const hipError_t attr_rc = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize,
                                                         (int)CFG::LDS_BYTES);
   if (attr_rc != hipSuccess) return attr_rc;
@@ -57,20 +57,25 @@ static hipError_t launch(const WgradGroup& w, hipStream_t st) {
   return hipGetLastError();
 }
 
+template <int BM, int BN, int WGM, int WGN, int NS, int BK>
+static hipError_t launch_of(const WgradGroup& w, hipStream_t st) {
+  if (w.K > w.kseg) return w.set ? hipErrorInvalidValue : launch<BM, BN, WGM, WGN, NS, BK, true>(w, st);
+  return w.set ? launch<BM, BN, WGM, WGN, NS, BK, false, true>(w, st) : launch<BM, BN, WGM, WGN, NS, BK, false>(w, st);
+}
+
 hipError_t launch_wgrad_group_mfma(const WgradGroup& w, hipStream_t st) {
   long t128 = 0, t12864 = 0;
   for (int i = 0; i < w.n; ++i) {
     t128 += (long)((w.p[i].M + 127) / 128) * ((w.p[i].N + 127) / 128);
     t12864 += (long)((w.p[i].M + 127) / 128) * ((w.p[i].N + 63) / 64);
   }
-  const bool seg = w.K > w.kseg;
   const int U = w.units > 0 ? w.units : 256;
   // enough 128x128 tiles for one and a half per unit: four waves, two workgroups per unit; for three quarters of the
   // units: eight waves; else smaller tiles
-  if (2 * t128 >= 3 * U) return seg ? launch<128, 128, 2, 2, 4, 32, true>(w, st) : launch<128, 128, 2, 2, 4, 32, false>(w, st);
-  if (4 * t128 >= 3 * U) return seg ? launch<128, 128, 2, 4, 4, 32, true>(w, st) : launch<128, 128, 2, 4, 4, 32, false>(w, st);
-  if (4 * t12864 >= 3 * U) return seg ? launch<128, 64, 2, 2, 3, 64, true>(w, st) : launch<128, 64, 2, 2, 3, 64, false>(w, st);
-  return seg ? launch<64, 64, 2, 2, 4, 64, true>(w, st) : launch<64, 64, 2, 2, 4, 64, false>(w, st);
+  if (2 * t128 >= 3 * U) return launch_of<128, 128, 2, 2, 4, 32>(w, st);
+  if (4 * t128 >= 3 * U) return launch_of<128, 128, 2, 4, 4, 32>(w, st);
+  if (4 * t12864 >= 3 * U) return launch_of<128, 64, 2, 2, 3, 64>(w, st);
+  return launch_of<64, 64, 2, 2, 4, 64>(w, st);
 }
 
 }  // namespace dapple

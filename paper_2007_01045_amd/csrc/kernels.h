@@ -35,7 +35,8 @@ enum GemmEpi {
   // with EPI_ADD | EPI_AUX32: what is added is the LayerNorm of aux, (aux[m,n] - mean[m]) rstd[m] gamma[n] + beta[n] --
   // the residual input of a bf16 stage, unrounded, from the sums it was normalised from.  Batch 1.
   EPI_AUXLN = 1024,
-  EPI_SILU = 2048   // a gated block's activation is SiLU, else GELU (launch_gate_fwd, launch_gate_bwd)
+  EPI_SILU = 2048,  // a gated block's activation is SiLU, else GELU (launch_gate_fwd, launch_gate_bwd)
+  EPI_BSUM_BF16 = 4096   // with EPI_BSUM: bsum holds bf16 and is set (MFMA kernel only)
 };
 
 struct GemmArgs {
@@ -130,6 +131,7 @@ struct WgradGroup {
   // launch of their own is 3 to 8 us of waiting for memory with most of the chip idle, here they fill a tail.  nmb >= 1
   ReduceJobs jobs;
   int job_blocks() const { return jobs.n > 0 ? jobs.n * ((jobs.j[0].cols + 63) / 64) : 0; }   // (all of one width)
+  bool set;   // bf16, one segment: C and bsum hold bf16 and are set
 };
 // the same as one accumulating product
 GemmArgs wgrad_args(const WgradGroup& w, int i);
