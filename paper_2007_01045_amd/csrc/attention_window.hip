@@ -802,6 +802,17 @@ struct F32Lds {
   // the second group's sums (n floats of a lane; n at most 2 D / 4)
   static_assert(NG == 1 || 64 * RG * (D / 2) <= FLOATS, "the sums lie where the blocks were");
 };
+// max and sum over the four lanes of one owned row (16 apart), in all of them: rows of 16 lanes change places, then half waves, without
+// a trip through the LDS crossbar
+__device__ __forceinline__ float groups_max(float x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, x), __builtin_bit_cast(unsigned, x), false, false);
+  return halves_max(fmaxf(__builtin_bit_cast(float, (unsigned)r[0]), __builtin_bit_cast(float, (unsigned)r[1])));
+}
+__device__ __forceinline__ float groups_sum(float x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, x), __builtin_bit_cast(unsigned, x), false, false);
+  return halves_sum(__builtin_bit_cast(float, (unsigned)r[0]) + __builtin_bit_cast(float, (unsigned)r[1]));
+}
+
 template <int D, int RG, int NG>
 __global__ __launch_bounds__(64 * RG * NG) void attn_win_fwd_f32(AttnWinArgs a, float scale2) {
   constexpr int NK = D / 16;
@@ -875,18 +886,17 @@ __global__ __launch_bounds__(64 * RG * NG) void attn_win_fwd_f32(AttnWinArgs a, 
         p[t][e] = sees(a, k0 + 16 * t + 4 * g4 + e, lo, hi) ? p[t][e] * scale2 : -INFINITY;
         mx = fmaxf(mx, p[t][e]);
       }
-    mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-    const float mn = fmaxf(m, mx), alpha = exp2f(m - mn);
+    // (a maximum that moves seldom, as in attn_win_fwd)
+    const float top = groups_max(mx), mn = top > m + 8.f ? top : m, alpha = __builtin_amdgcn_exp2f(m - mn);
     float rs = 0.f;
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        p[t][e] = exp2f(p[t][e] - mn);
+        p[t][e] = __builtin_amdgcn_exp2f(p[t][e] - mn);   // (the bare v_exp_f32: below 2^-126 of the row's largest it may be zero)
         rs += p[t][e];
       }
-    l = l * alpha + over_groups_sum(rs);
+    l = l * alpha + groups_sum(rs);
     m = mn;
     if (__builtin_amdgcn_ballot_w64(alpha != 1.f)) {
 #pragma unroll
@@ -1015,7 +1025,7 @@ __device__ __forceinline__ void win_dq_f32(const AttnWinArgs& a, unsigned id, fl
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        ds[e] = exp2f(s[e] * scale2 - Lq) * (dp[e] + Dq);
+        ds[e] = __builtin_amdgcn_exp2f(s[e] * scale2 - Lq) * (dp[e] + Dq);
         if (!sees(a, k0 + 16 * t + 4 * g4 + e, lo, hi)) ds[e] = 0.f;
       }
 #pragma unroll
@@ -1114,7 +1124,7 @@ __device__ __forceinline__ void win_dkdv_f32(const AttnWinArgs& a, unsigned task
       for (int e = 0; e < 4; ++e) {
         const int i = i0 + 16 * t + 4 * g4 + e;
         const bool ok = i >= lo && i < hi;
-        p[e] = ok ? exp2f(s[e] * scale2 - L4[e]) : 0.f;
+        p[e] = ok ? __builtin_amdgcn_exp2f(s[e] * scale2 - L4[e]) : 0.f;
         ds[e] = ok ? p[e] * (dp[e] + D4[e]) : 0.f;
       }
 #pragma unroll
