@@ -40,7 +40,7 @@ struct Ring {
   static constexpr int Y_OFF = ROWS * D * 2, S_OFF = 2 * Y_OFF;            // X, Y, then rows of 64 fp32 (STATS)
   static constexpr int SROWS = NW > 4 ? NW : 4, STAGE = S_OFF + (STATS ? SROWS * 256 : 0), BYTES = NS * STAGE;
   static constexpr int SPW = STATS ? SROWS / NW : 0;   // rows of the statistics per wave
-  static constexpr int BIAS = 3072, LOADS = PER + SPW;
+  static constexpr int BIAS = 3 * 1024, LOADS = PER + SPW;
   static_assert(PER <= IPM && (PER == 2 || PER % 4 == 0), "a wave's share lies in one matrix");
   static_assert((NS - 2) * LOADS < 64, "vmcnt is a 6-bit counter");
   int voff[PER];

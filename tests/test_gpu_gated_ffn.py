@@ -172,6 +172,27 @@ def test_fp32_tiles(shape):
         c.check()
 
 
+@pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("accumulate", [0, 1])
+@pytest.mark.parametrize("shape", [(20, 64, 72), (700, 1096, 96), (4100, 64, 1544), (75, 1912, 4360)], ids=lambda s: "-".join(map(str, s)))
+def test_one_bias_gradient(dtype, accumulate, shape):
+    # either of the two without the other: the same bits as with both, and nothing written for the other
+    c = Case(dtype, *shape, accumulate=accumulate)
+    c.run()
+    want = [t.clone() for t in c.grads]
+    for keep in (1, 3):
+        for t in c.grads:
+            t.fill_(GUARD)
+        d = c.desc()
+        if keep == 1:
+            d.db_out = None
+        else:
+            d.db_in = None
+        B.dapple_gated_ffn_bwd(dtype, d)
+        for i, (got, w) in enumerate(zip(c.grads, want)):
+            assert torch.equal(got, torch.full_like(w, GUARD) if i == 4 - keep else w), (keep, i)
+
+
 def test_fp32_only_shapes():
     # multiples of four
     for shape in ((3, 12, 20), (77, 100, 36), (513, 260, 132)):
