@@ -1271,8 +1271,12 @@ static int key_tile(Dtype dt, const AttnWinArgs& a) { return dt != DT_BF16 ? 16 
 // queries of a block of their walks
 static int walk_block(Dtype dt, const AttnWinArgs& a) { return dt != DT_BF16 ? BR : a.d > 64 ? 32 : 64; }
 
-// How the walks of dk and dv are cut.  Parts of CS blocks: as long as the walk of a tile without sinks where those tiles fill
-// the chip, else as long as two workgroups to a unit leave, eight blocks at least.
+// How the walks of dk and dv are cut.  Parts: as long as the walk of a tile without sinks where that walk is short or the tiles are
+// many -- fewer than units, for dq's workgroups fill the others; but where the walks grow with the tile (causal, no window) the longest
+// is twice the mean -- else as long as two workgroups to a unit leave, eight blocks at least.  Us forward and backward, cut / whole, key
+// tiles: bf16 heads of 64, window 512, 248 tiles 73 / 60; no mask, 96 83 / 79; window 200, 72 39 / 43; causal, 84 90 / 119, 162 64 / 62, 172
+// 120 / 124; of 128, window 256, 120 145 / 114; causal, 88 200 / 225.  fp32, window 300, 372 104 / 87; window 200, 92 59 / 56; causal, 352 209 /
+// 162, 256 339 / 335, 152 170 / 189, 64 109 / 145.
 static void make_plan(Dtype dt, AttnWinArgs& a) {
   const int kt = key_tile(dt, a), blk = walk_block(dt, a);
   WinPlan& p = a.plan;
@@ -1283,8 +1287,8 @@ static void make_plan(Dtype dt, AttnWinArgs& a) {
   // the most blocks that a walk without sinks has, per head
   const long reach = !a.W ? nb : std::min(nb, ((a.causal ? 1L : 2L) * (a.W - 1) + kt + blk - 2) / blk + 1);
   const long total = heads * G * (rest * reach + p.sink_tiles * nb), fair = (total + 511) / 512;
-  const long fill = dt == DT_BF16 && a.d > 64 ? 192 : 512;   // tiles that fill the chip: a unit holds one workgroup, or two
-  long steps = heads * rest >= fill ? G * reach : std::min(G * (rest ? reach : nb), std::max(8L, fair));
+  const bool whole = rest && (heads * rest * (a.causal && !a.W ? 1 : 2) >= 192 || G * reach <= 10);
+  const long steps = whole ? G * reach : std::min(G * (rest ? reach : nb), std::max(8L, fair));
   p.parts = (int)((G * reach + steps - 1) / steps);
   p.sink_parts = (int)((G * nb + steps - 1) / steps);
   if (!p.sink_tiles) p.sink_parts = 1;
