@@ -1258,14 +1258,19 @@ bool attn_win_takes(Dtype dt, const AttnWinArgs& a) {
   return true;
 }
 
-// Workgroups of four waves, or of two where four would leave a quarter of the 256 units without one (bf16; as in attention.hip)
-static int fwd_waves(const AttnWinArgs& a) { return (long)((a.s + 127) / 128) * a.b * a.A < 192 ? 2 : 4; }
-static int bwd_waves(const AttnWinArgs& a) { return (long)((a.s + 127) / 128) * a.b * (a.A + a.Ak) < 192 ? 2 : 4; }
-// keys of a workgroup of the backward
+// Workgroups of four waves, or of two where four would leave a quarter of the 256 units without one (bf16; as in attention.hip), the
+// gradient's where they give few units a second one.  Us with two / four waves, workgroups of four: forward, heads of 64, 128 of them 9.2 / 9.8,
+// 168 12.4 / 11.6, 256 13.2 / 12.0, 512 32 / 26; forward and backward 128 30 / 31, 256 56 / 62 and 34 / 35, 320 67 / 57, 512 53 / 46
+static int fwd_waves(const AttnWinArgs& a) { return (long)((a.s + 127) / 128) * a.b * a.A < 160 ? 2 : 4; }
+static int bwd_waves(const AttnWinArgs& a) { return (long)((a.s + 127) / 128) * a.b * (a.A + a.Ak) < 288 ? 2 : 4; }
 // fp32: waves of a group (16 rows each).  Four where their tiles make two workgroups for each unit, else two: us forward and
 // backward with four / two waves: 4 x 512 rows, 16 heads of 64 211 / 227; 2 x 2048, window none 879 / 914; 2 x 777, 12 heads, window
 // 200 110 / 101; 300 rows, 8 heads of 32 31 / 24
 static int f32_rows(const AttnWinArgs& a) { return (long)((a.s + 63) / 64) * a.b * a.A < 512 ? 2 : 4; }
+// The forward of wide heads, whose blocks take two groups of two waves twice as long to bring: us 256 tiles of 64 rows, heads of 128, 31 / 27, 512
+// 89 / 70, 1024 167 / 124, but 80 39 / 50 (heads of 64: 256 14 / 15 and 51 / 48, 312 25 / 29, 512 37 / 33)
+static int f32_fwd_rows(const AttnWinArgs& a) { return a.d > 64 && (long)((a.s + 63) / 64) * a.b * a.A >= 192 ? 4 : f32_rows(a); }
+// keys of a workgroup of the backward
 static int key_tile(Dtype dt, const AttnWinArgs& a) { return dt != DT_BF16 ? 16 * f32_rows(a) : a.d > 64 ? 128 : 32 * bwd_waves(a); }
 
 // queries of a block of their walks
@@ -1334,7 +1339,7 @@ hipError_t launch_attn_win_fwd(Dtype dt, const AttnWinArgs& a, hipStream_t st) {
         hipLaunchKernelGGL((attn_win_fwd_f32<d, rg, 2>), dim3((unsigned)((long)((a.s + 16 * rg - 1) / (16 * rg)) * a.b * a.A)), dim3(128 * rg), lds, st, a, scale2);
         return hipGetLastError();
       };
-      return f32_rows(a) == 4 ? go(std::integral_constant<int, 4>{}) : go(std::integral_constant<int, 2>{});
+      return f32_fwd_rows(a) == 4 ? go(std::integral_constant<int, 4>{}) : go(std::integral_constant<int, 2>{});
     }
     if constexpr (d >= 32) {
       auto go = [&](auto NW) {
