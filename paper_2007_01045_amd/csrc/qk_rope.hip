@@ -279,7 +279,8 @@ __global__ __launch_bounds__(256, V * NU <= 4 ? 1 : 4) void qk_rope_bwd_kernel(Q
                 q = fmaf(x[i][k][e], x[i][k][e], q);
                 p = fmaf(x[i][k][e], y[i][k][e] * g[i][k][e], p);
               }
-          const float rstd = rsqrtf(group_sum(q, G) * inv_d + a.eps);
+          // (a head behind the last has no part in dgamma: its zeros with eps = 0 would be 0 times infinity)
+          const float ms = group_sum(q, G) * inv_d + a.eps, rstd = h < heads ? rsqrtf(ms) : 0.f;
           const float m = group_sum(p, G) * inv_d * rstd;   // mean of dn gamma x rstd
 #pragma unroll
           for (int i = 0; i < NU; ++i)

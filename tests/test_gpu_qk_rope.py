@@ -251,3 +251,36 @@ def test_table(rot, base, factor, original, magnitude):
     for k, f in ((0, np.cos), (1, np.sin)):
         want = magnitude * f(angle)
         assert (np.abs(got[..., k] - want) <= 2.0 ** -24 * np.abs(want) * 1.01 + 2.0 ** -30).all()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("shape", [(5, 12, 4, 64, 64, False), (4200, 3, 1, 64, 32, True), (7, 5, 3, 7, 6, False), (6, 9, 0, 96, 0, False)],
+                         ids=lambda s: "-".join(str(int(v)) for v in s))
+def test_without_eps(dtype, shape):
+    # heads that do not fill a wave's passes, whose absent ones must not reach dgamma; no head is zero
+    rows, A, Ak, d, rot, inter = shape
+    c = Case(dtype, rows, A, Ak, d, rot, inter)
+    for accumulate in (0, 1):
+        for t in c.dg:
+            t.fill_(3.0)
+        desc = c.desc(accumulate=accumulate)
+        desc.eps = 0.0
+        B.dapple_qk_rope_fwd(dtype, desc)
+        B.dapple_qk_rope_bwd(dtype, desc)
+        x, dy = c.heads(c.x), c.heads(c.dy)
+        cs = c.table[c.pos.long()].double()
+        cos, sin = (cs[:, None, :, i] if rot else None for i in (0, 1))
+        gam = torch.cat([c.gam[0].double().expand(A, d), c.gam[1].double().expand(Ak, d)])
+        rstd = 1 / torch.sqrt(x.square().mean(-1, keepdim=True))
+        xh, half, e = x * rstd, 2.0 ** -8 if dtype == B.DTYPE_BF16 else 0.0, 2.0 ** -19      # (as in want())
+        y, size = turn(xh * gam, cos, sin, rot, inter)
+        dn, dsize = turn(dy, cos, -sin if rot else None, rot, inter)
+        t = dn * gam
+        dx = rstd * (t - xh * (t * xh).mean(-1, keepdim=True))
+        c.check(c.y, (y, e * size + half * y.abs()))
+        c.check(c.dx, (dx, rstd * e * (dsize * gam.abs() + xh.abs() * (dsize * gam.abs() * xh.abs()).mean(-1, keepdim=True)) + half * dx.abs()))
+        for got, at, heads in zip(c.dg, (slice(0, A), slice(A, A + Ak)), (A, Ak)):
+            if heads:
+                start = 3.0 * accumulate
+                want, tol = start + (dn * xh)[:, at].sum((0, 1)), 2.0 ** -15 * (start + (dsize * xh.abs())[:, at].sum((0, 1)))
+                assert bool(((got.double() - want).abs() <= tol).all()), (accumulate, at)
