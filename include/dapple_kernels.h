@@ -139,6 +139,7 @@ int dapple_colsum_static(int dtype, const void* X, int rows, int cols, int ld, f
  * NULL): an unrounded fp32 ctx in ctx's layout; given to bwd, the row sums of dctx*ctx come from it (a bf16 ctx costs dq and dk
  * accuracy where gradients are sums of many layers').
  * bwd: dq, dk, dv from dctx and the ctx, ctx32 (or NULL) and lse of fwd; dk and dv are summed over the heads that share them.
+ * workspace: below 4 b A s bytes + 256 MiB, whatever window and sinks.
  * scale > 0; 0 = 1/sqrt(d).  Row strides in elements, 0 = dense; q, k, v may be columns of one buffer, and dq, dk, dv of another;
  * outputs overlap no input.  bf16: d and strides multiples of 8; fp32: of 4; d <= 128, strides below 2^23, s * stride below 2^30 - 4096,
  * b * s below 2^26, b * Ak below 2^16, b * A * ceil(s / 32) below 2^23; all tensors 16-byte aligned.  Probabilities and dS are rounded once to bf16 in bf16 calls, for their products. */

@@ -13,7 +13,7 @@
 // without a window; the work is that of the visible blocks.
 //
 // dk and dv of a key: the query blocks that see it, for each of the sharing heads, one walk.  Where the walks are longer than
-// others (keys among the sinks: every query sees them) or too few to fill the chip, a walk is cut into parts of CS blocks; each
+// others (keys among the sinks: every query sees them) or too few to fill the chip, a walk is cut into parts (make_plan); each
 // part leaves fp32 sums in the workspace, and a second kernel adds them in ascending order: no atomics, the same bits every time.
 //
 // Rows at and behind len may hold anything: their q, k, v and dctx are never used (they read as zeros, past the buffer's records),
@@ -114,9 +114,9 @@ struct KeyTask {
     k0 = tile * kt;
     len = len_of(a, bi);
     span(a, kt, blk);
-    const int all = nq * (a.A / a.Ak);
-    n0 = parts > 1 ? min(all, part * p.steps) : 0;
-    n1 = parts > 1 ? min(all, n0 + p.steps) : all;
+    const int all = nq * (a.A / a.Ak), steps = sink ? p.sink_steps : p.steps;
+    n0 = parts > 1 ? min(all, part * steps) : 0;
+    n1 = parts > 1 ? min(all, n0 + steps) : all;
     slot = parts > 1 ? head * p.slots + (sink || p.sink_parts == 1 ? 0 : sinks) + u : -1;
     run = parts == 1 || n0 < n1;
   }
@@ -1216,7 +1216,7 @@ __global__ __launch_bounds__(256) void attn_win_join(AttnWinArgs a, float scale)
   const int sinks = p.sink_tiles * p.sink_parts;
   // the tile's first task (KeyTask counts the same)
   KeyTask w(a, head * (sinks + (p.key_tiles - p.sink_tiles) * p.parts) + (sink ? tile * p.sink_parts : sinks + (tile - p.sink_tiles) * p.parts), KT, BLK);
-  const int all = w.nq * (a.A / a.Ak), used = (all + p.steps - 1) / p.steps;
+  const int all = w.nq * (a.A / a.Ak), steps = sink ? p.sink_steps : p.steps, used = (all + steps - 1) / steps;
   const int u = (blockIdx.x % UNITS) * JT + threadIdx.x, lane = u & 63, blk = u >> 6;
   constexpr int CB = 256 / RW;              // columns of an accumulator register block
   const int row = blk / (D / CB) * RW + (lane & (RW - 1)), col = blk % (D / CB) * CB + 4 * (lane / RW);
@@ -1281,7 +1281,12 @@ static int walk_block(Dtype dt, const AttnWinArgs& a) { return dt != DT_BF16 ? B
 // is twice the mean -- else as long as two workgroups to a unit leave, eight blocks at least.  Us forward and backward, cut / whole, key
 // tiles: bf16 heads of 64, window 512, 248 tiles 73 / 60; no mask, 96 83 / 79; window 200, 72 39 / 43; causal, 84 90 / 119, 162 64 / 62, 172
 // 120 / 124; of 128, window 256, 120 145 / 114; causal, 88 200 / 225.  fp32, window 300, 372 104 / 87; window 200, 92 59 / 56; causal, 352 209 /
-// 162, 256 339 / 335, 152 170 / 189, 64 109 / 145.
+// 162, 256 339 / 335, 152 170 / 189, 64 109 / 145.  (What lies on the other side of 192 by 3%, 162 causal tiles, is left there.)
+// Tiles of sinks, whose walks are the longest, are cut likewise, but into no more than two parts for each unit in all: there
+// fp32 sums of every part are written and read again, and with parts of the others' length their number grew with sinks times
+// rows.  Gradient, us and workspace, parts of the others' length / these: 16384 rows, 32 heads of 128 on 8, window 64, 1024 sinks 1535, 623 MB /
+// 1235, 69 MB; 32768 rows, 16 heads of 64, window 64, 1024 sinks 1063, 1076 MB / 720, 36 MB; 65536 rows, window 128, 4 sinks 663, 219 MB / 600,
+// 38 MB.  (One part for each unit 716 to 1262 in the first two; four 737, 1263.)
 static void make_plan(Dtype dt, AttnWinArgs& a) {
   const int kt = key_tile(dt, a), blk = walk_block(dt, a);
   WinPlan& p = a.plan;
@@ -1294,11 +1299,13 @@ static void make_plan(Dtype dt, AttnWinArgs& a) {
   const long total = heads * G * (rest * reach + p.sink_tiles * nb), fair = (total + 511) / 512;
   const bool whole = rest && (heads * rest * (a.causal && !a.W ? 1 : 2) >= 192 || G * reach <= 10);
   const long steps = whole ? G * reach : std::min(G * (rest ? reach : nb), std::max(8L, fair));
+  const long sink_steps = std::min(G * nb, std::max(steps, (heads * G * p.sink_tiles * nb + 511) / 512));
   p.parts = (int)((G * reach + steps - 1) / steps);
-  p.sink_parts = (int)((G * nb + steps - 1) / steps);
+  p.sink_parts = (int)((G * nb + sink_steps - 1) / sink_steps);
   if (!p.sink_tiles) p.sink_parts = 1;
   if (!rest) p.parts = 1;
   p.steps = (int)steps;
+  p.sink_steps = (int)sink_steps;
   p.slots = (p.sink_parts > 1 ? p.sink_tiles * p.sink_parts : 0) + (p.parts > 1 ? (int)rest * p.parts : 0);
   p.key_tasks = (unsigned)(heads * (p.sink_tiles * p.sink_parts + rest * p.parts));
 }

@@ -231,7 +231,8 @@ bool attn_takes_delta_blocks(Dtype dt, const AttnArgs& a);
 // how the walks of dk and dv over the query blocks are cut (make_plan)
 struct WinPlan {
   int key_tiles, sink_tiles;     // tiles of keys; those among them that hold sinks
-  int parts, sink_parts, steps;  // parts of a tile's walk, of `steps` blocks each
+  int parts, sink_parts;         // parts of a tile's walk: of one without sinks, of one that holds some
+  int steps, sink_steps;         // blocks of a part of either
   int slots;                     // of fp32 sums, per sequence and key head
   unsigned key_tasks;
 };

@@ -244,3 +244,14 @@ def test_same_bits_on_another_stream_and_in_a_graph(dtype):
         assert all(torch.equal(a, b) for a, b in zip([x[:, :c.A * c.d] if x.dim() == 2 else x for x in outs],
                                                      [x[:, :c.A * c.d] if x.dim() == 2 else x for x in eager])), k
         assert torch.equal(c.dqkv[:, :c.ld - c.pad], eager[3][:, :c.ld - c.pad]), k
+
+
+@pytest.mark.parametrize("case", [  # many tiles of sinks: their walks in parts of their own length, or whole, beside whole and cut ones
+    (H, 4, 1500, 16, 16, 64, 64, 700, True, [1500, 3, 1111, 699]), (H, 4, 1500, 16, 16, 64, 64, 1400, True, None),
+    (H, 2, 1500, 32, 8, 128, 64, 600, True, [1500, 900]), (H, 1, 1300, 4, 2, 128, 64, 600, False, None), (H, 1, 2500, 2, 2, 32, 500, 1500, True, None),
+    (F, 2, 700, 8, 4, 32, 40, 300, False, [700, 301]), (F, 3, 900, 8, 8, 64, 30, 860, True, None)],
+    ids=lambda c: "-".join("x" if v is None else str(v).replace(", ", "_") for v in c))
+def test_many_sinks(case):
+    c = Case(*case)
+    c.run()
+    c.check()

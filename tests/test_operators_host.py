@@ -148,3 +148,15 @@ def test_sizes_beyond_a_launch():
                   dict(b=1, s=1 << 27, A=1, Ak=1), dict(b=0x7fffffff, s=0x7fffffff, A=0x7fffffff, Ak=1)):
         for f in (B.dapple_attention_window_fwd, B.dapple_attention_window_bwd, B.dapple_attention_window_workspace):
             refused(B.STAGE_E_CONFIG, f, B.DTYPE_BF16, B.attention_window_desc(**attn, **sizes))
+
+
+def test_attention_workspace_is_bounded():
+    # fp32 sums of parts of walks: their number must not grow with sinks times rows
+    for dt, wide in ((B.DTYPE_BF16, 128), (B.DTYPE_F32, 128), (B.DTYPE_BF16, 64), (B.DTYPE_F32, 32)):
+        for b, s, A, Ak in ((1, 32768, 32, 8), (4, 8192, 16, 16), (1, 65536, 1, 1), (1, (1 << 24) - 64, 1, 1), (3, 5000, 48, 2), (64, 300, 16, 1)):
+            for window in (1, 64, 1000, 0):
+                for sinks in (0, 1, 17, 1000, s // 8, s // 2, s - 1, s):
+                    for causal in (0, 1):
+                        desc = B.attention_window_desc(b=b, s=s, A=A, Ak=Ak, d=wide, window=window, sinks=sinks, causal=causal)
+                        size = B.dapple_attention_window_workspace(dt, desc)
+                        assert 4 * b * A * s <= size < 4 * b * A * s + (1 << 28), (dt, wide, b, s, A, Ak, window, sinks, causal, size)
