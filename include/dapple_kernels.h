@@ -142,7 +142,8 @@ int dapple_colsum_static(int dtype, const void* X, int rows, int cols, int ld, f
  * workspace: below 4 b A s bytes + 256 MiB, whatever window and sinks.
  * scale > 0; 0 = 1/sqrt(d).  Row strides in elements, 0 = dense; q, k, v may be columns of one buffer, and dq, dk, dv of another;
  * outputs overlap no input.  bf16: d and strides multiples of 8; fp32: of 4; d <= 128, strides below 2^23, s * stride below 2^30 - 4096,
- * b * s below 2^26, b * Ak below 2^16, b * A * ceil(s / 32) below 2^23; all tensors 16-byte aligned.  Probabilities and dS are rounded once to bf16 in bf16 calls, for their products. */
+ * b * s up to 2^26 - 4, b * Ak below 2^16, b * A * ceil(s / 32) below 2^23, bwd b * (A + Ak) * ceil(s / 32) below 2^23 - 2048; all tensors
+ * 16-byte aligned.  Probabilities and dS are rounded once to bf16 in bf16 calls, for their products. */
 typedef struct {
   const void* q;
   const void* k;
@@ -175,7 +176,7 @@ int dapple_attention_window_bwd(int dtype, const dapple_attention_window_desc* d
  * r); a position outside [0, max_pos) reads nothing and gives NaN in the columns that turn (backward: and in dgamma).
  * Types: q, k, gammas and outputs of dtype; table, dgamma and all arithmetic fp32.  Row strides in elements, 0 = dense.  An
  * output may be its input (yq = q with ldyq = ldq, dq = dyq, ...), else they do not overlap.  Limits: d <= 256, rot even and <= d,
- * 1 <= rows < 2^26; interleaved needs d and the strides even and addresses aligned to two elements; everything aligned to 16 bytes
+ * 1 <= rows <= 2^26 - 4; interleaved needs d and the strides even and addresses aligned to two elements; everything aligned to 16 bytes
  * (d, rot/2 or interleaved rot, strides, addresses) is fastest.
  * Backward: dyq, dyk in, dq, dk out (q and k are read only with gammas), dgamma_q, dgamma_k [d] fp32: set, or with accumulate != 0
  * added to; NULL = not wanted.  workspace only where a dgamma is wanted. */
@@ -249,7 +250,8 @@ int dapple_gated_ffn_bwd(int dtype, const dapple_gated_ffn_desc* d, void* stream
  *   norm_dev[0] = |grad_scale| * sqrt(sum of all squares)      (squares and sums in 64 bits)
  *   norm_dev[1] = min(1, max_norm / norm_dev[0]), 0 if the norm is not finite
  * grad_scale: what the gradients are multiplied with later (1 / samples for accumulated sums).  max_norm > 0, may be
- * infinite.  The gradients of all stages of a model may be given in one call.  workspace: 8-byte aligned is enough. */
+ * infinite.  The gradients of all stages of a model may be given in one call, up to 2^38 - 2^22 elements in all.  workspace: 8-byte
+ * aligned is enough. */
 int64_t dapple_grad_norm_workspace(const int64_t* sizes, int n);
 int dapple_grad_norm(int dtype, const void* const* grads, const int64_t* sizes, int n, float grad_scale, float max_norm,
                      float* norm_dev, void* workspace, void* stream);

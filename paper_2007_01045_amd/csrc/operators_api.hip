@@ -28,10 +28,13 @@ static int win_args(int dtype, const dapple_attention_window_desc* d, bool bwd, 
   if (!(d->scale >= 0.f) || !std::isfinite(d->scale)) return set_error(STAGE_E_CONFIG, "scale must be positive and finite (0: 1/sqrt(d))");
   const int v = dtype == STAGE_DTYPE_BF16 ? 8 : 4;
   if (d->d % v || d->d > 128) return set_error(STAGE_E_CONFIG, "heads of %d columns: multiples of %d up to 128 are taken", d->d, v);
-  // (a launch has 2^32 work-items at most: 512 to 32 rows of a head, 64 to a row)
-  if (d->s >= 1 << 27 || (long)d->b * d->s >= 1L << 26 || (long)d->b * d->A >= 1L << 23 || (long)d->b * d->A * ((d->s + 31) / 32) >= 1L << 23 ||
-      (long)d->b * d->Ak >= 1L << 16)
-    return set_error(STAGE_E_CONFIG, "2^26 rows, 2^16 key heads of all sequences or 2^23 times 32 rows of a head and more");
+  // (A launch has fewer than 2^32 work-items: 512 to 32 rows of a head, 64 to a row.  The gradient's holds key heads beside query heads,
+  // and up to 2048 parts of walks: see make_plan.)
+  const long row_blocks = (long)d->b * ((d->s + 31L) / 32);
+  if (d->s >= 1 << 27 || (long)d->b * d->s > (1L << 26) - 4 || (long)d->b * d->A >= 1L << 23 || row_blocks * d->A >= 1L << 23 || (long)d->b * d->Ak >= 1L << 16)
+    return set_error(STAGE_E_CONFIG, "2^26 - 3 rows, 2^16 key heads of all sequences or 2^23 times 32 rows of a head and more");
+  if (bwd && row_blocks * ((long)d->A + d->Ak) >= (1L << 23) - 2048)
+    return set_error(STAGE_E_CONFIG, "2^23 - 2048 times 32 rows of a head, key heads included, and more");
   a.b = d->b; a.s = d->s; a.A = d->A; a.Ak = d->Ak; a.d = d->d; a.causal = d->causal != 0;
   a.W = d->window < d->s ? d->window : 0;   // (a window of s positions and more hides nothing)
   a.S = d->sinks < d->s ? d->sinks : d->s;
@@ -86,7 +89,7 @@ static int rope_args(int dtype, const dapple_qk_rope_desc* d, bool bwd, bool wor
   if (bad_dtype(dtype)) return set_error(STAGE_E_CONFIG, "dtype %d", dtype);
   if (d->rows < 1 || d->A < 1 || d->Ak < 0 || d->d < 1 || d->d > 256)
     return set_error(STAGE_E_CONFIG, "rows %d, heads %d and %d of %d columns (at most 256)", d->rows, d->A, d->Ak, d->d);
-  if (d->rows >= 1 << 26) return set_error(STAGE_E_CONFIG, "2^26 rows and more");   // (a launch has 2^32 work-items at most)
+  if (d->rows > (1 << 26) - 4) return set_error(STAGE_E_CONFIG, "2^26 - 3 rows and more");   // (a launch has fewer than 2^32 work-items)
   if (workspace_only) return STAGE_OK;
   if (d->rot < 0 || d->rot % 2 || d->rot > d->d) return set_error(STAGE_E_CONFIG, "%d of %d columns to turn", d->rot, d->d);
   if (d->seq < 0 || (d->rot && d->max_pos < 1)) return set_error(STAGE_E_CONFIG, "seq %d, max_pos %d", d->seq, d->max_pos);
@@ -231,7 +234,9 @@ static int check_sizes(const int64_t* sizes, int n) {
   int64_t total = 0;
   for (int i = 0; i < n; ++i) {
     if (sizes[i] < 0) return set_error(STAGE_E_CONFIG, "tensor %d has %lld elements", i, (long long)sizes[i]);
-    if (sizes[i] > (1LL << 40) || (total += sizes[i]) > (1LL << 40)) return set_error(STAGE_E_CONFIG, "more than 2^40 elements");
+    // (a launch of up to 128 tensors has fewer than 2^24 workgroups of 256: see grad_norm.hip)
+    constexpr int64_t most = (1LL << 38) - (1LL << 22);
+    if (sizes[i] > most || (total += sizes[i]) > most) return set_error(STAGE_E_CONFIG, "more than 2^38 - 2^22 elements");
   }
   return STAGE_OK;
 }

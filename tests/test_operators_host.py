@@ -160,3 +160,25 @@ def test_attention_workspace_is_bounded():
                         desc = B.attention_window_desc(b=b, s=s, A=A, Ak=Ak, d=wide, window=window, sinks=sinks, causal=causal)
                         size = B.dapple_attention_window_workspace(dt, desc)
                         assert 4 * b * A * s <= size < 4 * b * A * s + (1 << 28), (dt, wide, b, s, A, Ak, window, sinks, causal, size)
+
+
+def test_the_last_sizes_of_a_launch():
+    # one step further than what a launch of 2^32 - 1 work-items holds is refused, the step before is not (the workspaces say so)
+    rope = dict(A=1, Ak=1, d=8)
+    assert B.dapple_qk_rope_workspace(B.DTYPE_F32, B.qk_rope_desc(rows=(1 << 26) - 4, **rope)) > 0
+    refused(B.STAGE_E_CONFIG, B.dapple_qk_rope_workspace, B.DTYPE_F32, B.qk_rope_desc(rows=(1 << 26) - 3, **rope))
+    size = lambda dt, **kw: B.dapple_attention_window_workspace(dt, B.attention_window_desc(d=8, **kw))  # noqa: E731
+    ok = dict(q=P, k=P, v=P, ctx=P, lse=P, dctx=P, dq=P, dk=P, dv=P, workspace=P, d=8)
+    for dt in (B.DTYPE_F32, B.DTYPE_BF16):
+        assert size(dt, b=4, s=(1 << 24) - 1, A=1, Ak=1) > 0
+        for kw in (dict(b=1, s=(1 << 26) - 3, A=1, Ak=1),                  # rows
+                   dict(b=65535, s=1, A=128, Ak=1), dict(b=65535, s=32, A=127, Ak=1),   # query and key heads: 512 work-items to one's rows
+                   dict(b=1, s=1 << 22, A=63, Ak=1, d=64, ldq=4096)):
+            kw = dict(ok, **kw)
+            for f in (B.dapple_attention_window_bwd, B.dapple_attention_window_workspace):
+                refused(B.STAGE_E_CONFIG, f, dt, B.attention_window_desc(**kw))
+        assert size(dt, b=65535, s=32, A=126, Ak=1) > 0
+    most = (1 << 38) - (1 << 22)
+    for sizes in ([most], [1 << 31] * 127 + [(1 << 31) - (1 << 22)]):
+        assert B.dapple_grad_norm_workspace(sizes) > 0
+        refused(B.STAGE_E_CONFIG, B.dapple_grad_norm_workspace, sizes + [1])
