@@ -231,8 +231,9 @@ int stage_apply_adam(stage_handle h, void* weights_dev, float* master_dev, float
 
 /* The same update with the gradients clipped by their global norm: g = grad_scale * norm_dev[1] * G.  norm_dev: device
  * float [2], the norm and the factor that dapple_grad_norm (dapple_kernels.h) leaves for the accumulators of this stage,
- * or of all stages of the model; it is read when the update runs, so the host waits for nothing.  Give dapple_grad_norm
- * the same grad_scale.  Where norm_dev[0] is not finite nothing is updated: weights, master weights and moments stay as
+ * or of all stages of the model; it is read when the update runs, so the host waits for nothing: it has to be complete
+ * there in the order of the stage's stream (an event, where another stream makes it), and to stay until the update has
+ * run.  Give dapple_grad_norm the same grad_scale.  Where norm_dev[0] is not finite nothing is updated: weights, master weights and moments stay as
  * they are (the accumulators are cleared if zero_grads != 0). */
 int stage_apply_adam_clipped(stage_handle h, void* weights_dev, float* master_dev, float* m_dev, float* v_dev,
                              int step, float lr, float beta1, float beta2, float eps, float grad_scale,

@@ -572,6 +572,7 @@ class StageRunner:
         p, n = stage_grads(self.h)
         assert p == self.grads.data_ptr() and n == self.sizes.n_params
         self.T = cfg.micro_batch * cfg.seq
+        self.held = None      # a norm given to apply_adam_clipped, until its update has read it
 
     def init_adam(self):
         """fp32 master copy of the weights and zeroed moments (the optimizer state is the caller's)."""
@@ -579,6 +580,7 @@ class StageRunner:
         self.master = self.weights.to(torch.float32).clone().contiguous()
         self.m = torch.zeros_like(self.master)
         self.v = torch.zeros_like(self.master)
+        self.norm_ws = torch.empty(dapple_grad_norm_workspace([self.sizes.n_params]), dtype=torch.uint8, device=self.device)
         self.step = 0
 
     def apply_adam(self, lr, beta1=0.9, beta2=0.999, eps=1e-8, grad_scale=1.0, zero_grads=False):
@@ -588,21 +590,36 @@ class StageRunner:
 
     def apply_adam_clipped(self, lr, max_norm, beta1=0.9, beta2=0.999, eps=1e-8, grad_scale=1.0, zero_grads=False, norm=None):
         """The update with the gradients clipped to max_norm by this stage's own norm, or by `norm` (device float [2] of
-        dapple_grad_norm over the accumulators of all stages).  Returns that tensor."""
+        dapple_grad_norm over the accumulators of all stages).  Returns that tensor: a new one per call, or the given one.
+        Where the stage has a stream of its own, that stream waits for torch's current one (a given norm is complete there),
+        and the current one for the norm that is returned; a given norm may be dropped after the call."""
         torch = self.torch
-        sp = self.stream.cuda_stream
-        if norm is None:
+        cur = torch.cuda.current_stream(self.device)
+        apart = cur.cuda_stream != self.stream.cuda_stream
+        self._release_norm(cur)
+        given = norm is not None
+        if not given:
             sizes = [self.sizes.n_params]
-            if not hasattr(self, "norm"):
-                self.norm = torch.empty(2, dtype=torch.float32, device=self.device)
-                self.norm_ws = torch.empty(dapple_grad_norm_workspace(sizes), dtype=torch.uint8, device=self.device)
-            norm = self.norm
+            norm = torch.empty(2, dtype=torch.float32, device=self.device)
+        if apart:
+            self.stream.wait_stream(cur)      # (whoever had the new tensor's memory before, too)
+        if not given:
             dapple_grad_norm(DTYPE_F32, [self.grads.data_ptr()], sizes, max_norm, norm.data_ptr(), self.norm_ws.data_ptr(),
-                             grad_scale, sp)
+                             grad_scale, self.stream.cuda_stream)
         self.step += 1
         stage_apply_adam_clipped(self.h, self.weights.data_ptr(), self.master.data_ptr(), self.m.data_ptr(), self.v.data_ptr(),
                                  self.step, lr, norm.data_ptr(), beta1, beta2, eps, grad_scale, zero_grads)
+        if apart and given:      # (one norm for the stages of a pipeline: their updates do not wait for each other)
+            self.held = (norm, self.stream.record_event())
+        elif apart:
+            cur.wait_stream(self.stream)
         return norm
+
+    def _release_norm(self, cur):
+        """Drops the last given norm, whose memory is used again on `cur` behind the update that read it."""
+        if self.held is not None:
+            cur.wait_event(self.held[1])
+            self.held = None
 
     def to_dev(self, a, dtype=None):
         t = self.torch.as_tensor(a)
@@ -625,6 +642,7 @@ class StageRunner:
 
     def close(self):
         if self.h is not None:
+            self._release_norm(self.torch.cuda.current_stream(self.device))
             stage_destroy(self.h)
             self.h = None
 

@@ -214,3 +214,63 @@ def test_one_norm_over_the_stages_of_a_pipeline():
     finally:
         for r in runners:
             r.close()
+
+
+def busy(n):
+    """Work of some milliseconds on the current stream."""
+    x = torch.ones(4096, 4096, device="cuda")
+    for _ in range(n):
+        x = x @ x * 2.0 ** -12
+    return x
+
+
+@pytest.mark.parametrize("given", [False, True])
+def test_clipped_updates_on_streams_of_their_own(given):
+    """Two stages, on the current stream and as a pipeline's on streams of their own: the same bits, whichever stream is late."""
+    cfg = I.StageConfig(1, 64, 4, 128, 16, 2, 2, 2, "f32")
+    theta = [I.make_params(cfg, 11 + i) for i in range(2)]
+    G = [torch.from_numpy(I.normal(9, f"G{i}", theta[0].size).astype(np.float32)).cuda() for i in range(2)]
+    results = []
+    for piped in (False, True):
+        if piped:
+            pipe = B.PipelineRunner([c_config(cfg, 2)] * 2, theta, 2, parts=0)
+            runners = pipe.runners
+        else:
+            runners = [B.StageRunner(c_config(cfg, 2), th) for th in theta]
+        try:
+            for r in runners:
+                r.init_adam()
+            torch.cuda.synchronize()
+            norms, copies = [], []
+            for step in range(3):
+                norm = None
+                if given:      # complete on the current stream long after the calls below
+                    busy(40)
+                    norm = torch.full((2,), 0.125 * (step + 1), device="cuda")
+                for r, g in zip(runners, G):
+                    with torch.cuda.stream(r.stream):      # and the gradients on the stage's, as a backward leaves them
+                        busy(80)
+                        r.grads.copy_((1 + step) * g)
+                    out = r.apply_adam_clipped(1e-2, 1.0, norm=norm)
+                    assert given == (out is norm)
+                    if not given:
+                        norms.append(out)
+                        copies.append(out.clone())         # at once, on the current stream
+                del norm, out
+                spoil = [torch.full((2,), math.inf, device="cuda") for _ in range(16)]      # (where a given norm was, were it free)
+                del spoil
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(norms, copies))                    # (nor overwritten by later steps)
+            results.append([t.clone() for r in runners for t in (r.master, r.m, r.v)] + copies)
+        finally:
+            if piped:
+                pipe.close()
+            else:
+                for r in runners:
+                    r.close()
+    assert all(bool(t.isfinite().all()) for t in results[0])
+    assert len(results[0]) == len(results[1]) and all(torch.equal(a, b) for a, b in zip(*results))
+    if not given:
+        for t, (step, g) in zip(results[0][6:], [(step, g) for step in range(3) for g in G]):
+            want = (1 + step) * float(g.double().norm())
+            assert abs(float(t[0]) - want) <= 2.0 ** -22 * want      # (the products (1 + step) g are rounded too)
