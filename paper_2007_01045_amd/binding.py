@@ -565,6 +565,7 @@ class StageRunner:
         self.arena_ptr = (base + 255) // 256 * 256
         # stream_ptr: a raw hipStream_t (a partition stream of the pipeline); else torch's current stream
         self.stream = torch.cuda.current_stream(device) if stream_ptr is None else torch.cuda.ExternalStream(stream_ptr)
+        self._after_current()
         self.h = stage_init(cfg, self.weights.data_ptr(), self.arena_ptr, self.sizes.arena_bytes,
                             self.stream.cuda_stream)
         off = self.arena_ptr - base
@@ -582,6 +583,7 @@ class StageRunner:
         self.v = torch.zeros_like(self.master)
         self.norm_ws = torch.empty(dapple_grad_norm_workspace([self.sizes.n_params]), dtype=torch.uint8, device=self.device)
         self.step = 0
+        self._after_current()
 
     def apply_adam(self, lr, beta1=0.9, beta2=0.999, eps=1e-8, grad_scale=1.0, zero_grads=False):
         self.step += 1
@@ -594,31 +596,38 @@ class StageRunner:
         Where the stage has a stream of its own, that stream waits for torch's current one (a given norm is complete there),
         and the current one for the norm that is returned; a given norm may be dropped after the call."""
         torch = self.torch
-        cur = torch.cuda.current_stream(self.device)
-        apart = cur.cuda_stream != self.stream.cuda_stream
-        self._release_norm(cur)
+        self._release_norm()
         given = norm is not None
         if not given:
             sizes = [self.sizes.n_params]
             norm = torch.empty(2, dtype=torch.float32, device=self.device)
-        if apart:
-            self.stream.wait_stream(cur)      # (whoever had the new tensor's memory before, too)
+        cur = self._after_current()      # (behind whoever had the new tensor's memory before, too)
         if not given:
             dapple_grad_norm(DTYPE_F32, [self.grads.data_ptr()], sizes, max_norm, norm.data_ptr(), self.norm_ws.data_ptr(),
                              grad_scale, self.stream.cuda_stream)
         self.step += 1
         stage_apply_adam_clipped(self.h, self.weights.data_ptr(), self.master.data_ptr(), self.m.data_ptr(), self.v.data_ptr(),
                                  self.step, lr, norm.data_ptr(), beta1, beta2, eps, grad_scale, zero_grads)
-        if apart and given:      # (one norm for the stages of a pipeline: their updates do not wait for each other)
+        if cur is not None and given:      # (one norm for the stages of a pipeline: their updates do not wait for each other)
             self.held = (norm, self.stream.record_event())
-        elif apart:
+        elif cur is not None:
             cur.wait_stream(self.stream)
         return norm
 
-    def _release_norm(self, cur):
-        """Drops the last given norm, whose memory is used again on `cur` behind the update that read it."""
+    def _after_current(self):
+        """Where the stage has a stream of its own: lets it wait for torch's current one, and returns that."""
+        cur = self.torch.cuda.current_stream(self.device)
+        if cur.cuda_stream == self.stream.cuda_stream:
+            return None
+        self.stream.wait_stream(cur)
+        return cur
+
+    def _release_norm(self):
+        """Drops the last given norm, whose memory is used again on the current stream behind the update that read it."""
         if self.held is not None:
-            cur.wait_event(self.held[1])
+            cur = self.torch.cuda.current_stream(self.device)
+            if cur.cuda_stream != self.stream.cuda_stream:
+                cur.wait_event(self.held[1])
             self.held = None
 
     def to_dev(self, a, dtype=None):
@@ -631,18 +640,22 @@ class StageRunner:
         return self.torch.empty(self.T, self.cfg.hidden, dtype=self.tdtype, device=self.device)
 
     def run(self, M, K, order, xs, dys=None, auxs=None, explicit_ops=None):
-        """xs/dys/auxs: lists of device tensors.  Returns (ys, dxs) device tensors."""
+        """xs/dys/auxs: lists of device tensors.  Returns (ys, dxs) device tensors.  Where the stage has a stream of its own, that
+        stream and torch's current one wait for each other."""
         torch = self.torch
         head, emb = self.cfg.has_mlm_head, self.cfg.has_embedding
         ys = [torch.zeros(1, dtype=torch.float32, device=self.device) if head else self.empty_act() for _ in range(M)]
         dxs = None if emb else [self.empty_act() for _ in range(M)]
         ptr = lambda ts: None if ts is None else [t.data_ptr() for t in ts]
+        cur = self._after_current()      # (inputs, zeroed losses, whoever had the outputs' memory before)
         stage_run_schedule(self.h, M, K, order, ptr(xs), ptr(dys), ptr(ys), ptr(dxs), ptr(auxs), explicit_ops)
+        if cur is not None:
+            cur.wait_stream(self.stream)
         return ys, dxs
 
     def close(self):
         if self.h is not None:
-            self._release_norm(self.torch.cuda.current_stream(self.device))
+            self._release_norm()
             stage_destroy(self.h)
             self.h = None
 

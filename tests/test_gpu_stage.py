@@ -670,3 +670,30 @@ def test_fp32_head_sums_do_not_depend_on_the_group():
     a = _bits(run_gpu(cfg, theta, mbs, M, 2, B.ORDER_EARLY_BACKWARD))
     b = _bits(run_gpu(cfg, theta, mbs, M, 2, B.ORDER_GPIPE))
     assert all(np.array_equal(x, y) for x, y in zip(a, b))
+
+
+@pytest.mark.parametrize("kind", ["middle", "last"])
+def test_a_runner_on_a_stream_of_its_own_waits_for_the_current_one_and_is_waited_for(kind):
+    import torch
+    kw = dict(has_mlm_head=True, vocab=96) if kind == "last" else {}
+    cfg = I.StageConfig(2, 64, 4, 128, 16, 2, 3, 2, "f32", **kw)
+    theta, mbs = make_inputs(cfg, SEED, 3)
+    results = []
+    for st in (None, torch.cuda.Stream()):
+        late = torch.ones(4096, 4096, device="cuda")
+        for _ in range(80):      # (some milliseconds: what is made on the current stream below comes late)
+            late = late @ late * 2.0 ** -12
+        r = B.StageRunner(c_config(cfg, 2), theta, stream_ptr=None if st is None else st.cuda_stream)
+        try:
+            xs = [r.to_dev(mb["x"].reshape(cfg.tokens, cfg.hidden)) for mb in mbs]
+            dys = None if kw else [r.to_dev(mb["dy"].reshape(cfg.tokens, cfg.hidden)) for mb in mbs]
+            auxs = [r.to_dev(mb["targets"].reshape(cfg.tokens).astype(np.int32)) for mb in mbs] if kw else None
+            r.init_adam()
+            ys, dxs = r.run(3, 2, B.ORDER_EARLY_BACKWARD, xs, dys, auxs)
+            out = [t.clone() for t in ys + dxs + [r.grads]]      # on the current stream, at once
+            r.apply_adam(1e-3)
+            torch.cuda.synchronize()
+            results.append(out + [t.clone() for t in (r.master, r.m, r.v)])
+        finally:
+            r.close()
+    assert all(torch.equal(a, b) for a, b in zip(*results)) and float(results[0][0].abs().max()) > 0
