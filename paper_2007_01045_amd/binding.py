@@ -586,9 +586,9 @@ class StageRunner:
         self._after_current()
 
     def apply_adam(self, lr, beta1=0.9, beta2=0.999, eps=1e-8, grad_scale=1.0, zero_grads=False):
-        self.step += 1
         stage_apply_adam(self.h, self.weights.data_ptr(), self.master.data_ptr(), self.m.data_ptr(),
-                         self.v.data_ptr(), self.step, lr, beta1, beta2, eps, grad_scale, zero_grads)
+                         self.v.data_ptr(), self.step + 1, lr, beta1, beta2, eps, grad_scale, zero_grads)
+        self.step += 1
 
     def apply_adam_clipped(self, lr, max_norm, beta1=0.9, beta2=0.999, eps=1e-8, grad_scale=1.0, zero_grads=False, norm=None):
         """The update with the gradients clipped to max_norm by this stage's own norm, or by `norm` (device float [2] of
@@ -605,9 +605,9 @@ class StageRunner:
         if not given:
             dapple_grad_norm(DTYPE_F32, [self.grads.data_ptr()], sizes, max_norm, norm.data_ptr(), self.norm_ws.data_ptr(),
                              grad_scale, self.stream.cuda_stream)
-        self.step += 1
         stage_apply_adam_clipped(self.h, self.weights.data_ptr(), self.master.data_ptr(), self.m.data_ptr(), self.v.data_ptr(),
-                                 self.step, lr, norm.data_ptr(), beta1, beta2, eps, grad_scale, zero_grads)
+                                 self.step + 1, lr, norm.data_ptr(), beta1, beta2, eps, grad_scale, zero_grads)
+        self.step += 1
         if cur is not None and given:      # (one norm for the stages of a pipeline: their updates do not wait for each other)
             self.held = (norm, self.stream.record_event())
         elif cur is not None:

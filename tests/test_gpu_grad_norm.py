@@ -274,3 +274,19 @@ def test_clipped_updates_on_streams_of_their_own(given):
         for t, (step, g) in zip(results[0][6:], [(step, g) for step in range(3) for g in G]):
             want = (1 + step) * float(g.double().norm())
             assert abs(float(t[0]) - want) <= 2.0 ** -22 * want      # (the products (1 + step) g are rounded too)
+
+
+def test_a_refused_update_is_no_step():
+    cfg = I.StageConfig(1, 64, 4, 128, 16, 2, 2, 2, "f32")
+    r = B.StageRunner(c_config(cfg, 2), I.make_params(cfg, 11))
+    try:
+        r.init_adam()
+        for update in (lambda eps: r.apply_adam(1e-2, eps=eps), lambda eps: r.apply_adam_clipped(1e-2, 1.0, eps=eps)):
+            step = r.step
+            with pytest.raises(B.StageError):
+                update(0.0)
+            assert r.step == step
+            update(1e-8)
+            assert r.step == step + 1
+    finally:
+        r.close()
