@@ -204,13 +204,14 @@ bool wgrad_group_takes(Dtype dt, const WgradGroup& w) {
 }
 
 hipError_t launch_wgrad_group(Dtype dt, const WgradGroup& w, hipStream_t st) {
-  return dt == DT_BF16 ? launch_wgrad_group_mfma(w, st) : launch_wgrad_group_f32(w, st);
+  if (dt != DT_BF16) return w.set ? hipErrorInvalidValue : launch_wgrad_group_f32(w, st);
+  return launch_wgrad_group_mfma(w, st);
 }
 
 hipError_t launch_gemm(Dtype dt, const GemmArgs& g, hipStream_t st, GemmPlan* plan) {
   if (g.M <= 0 || g.N <= 0 || g.batch <= 0) return hipSuccess;
   const bool mfma = gemm_uses_mfma(dt, g);
-  if ((g.epi & EPI_ROWDOT) && !mfma) return hipErrorInvalidValue;  // only the MFMA kernel's epilogue has it
+  if ((g.epi & (EPI_ROWDOT | EPI_BSUM_BF16)) && !mfma) return hipErrorInvalidValue;  // only the MFMA kernel has them
   if (mfma) {
     const bool tt = g.a_kstrided && g.b_kstrided;   // the weight-gradient layout
     const bool short_k = g.kseg_len % 64 != 0 && !tt;

@@ -583,7 +583,8 @@ __device__ __forceinline__ void gemm_mfma_tile(const GemmArgs& g, int tiles_m, i
   static_assert(64 % C4 == 0, "a lane stores the same columns of every row");
   constexpr int HB = MI > 2 ? (NIT > 4 ? 4 : NIT) : (NIT > 8 ? 8 : NIT);   // processed HB at a time
   constexpr Store THROUGH = BM == 256 ? Store::Through : Store::Plain, FAR = BM == 256 ? Store::Far : Store::Plain;
-  constexpr bool PRE = !CS && !SEG && MI * NIT <= 16;   // (the column-sum variant serves accumulating products only)
+  // (the column-sum variant serves products that add to C, read a unit ahead, and the gated block's that set it)
+  constexpr bool PRE = !CS && !SEG && MI * NIT <= 16;
   const int epi = g.epi;
   const int lane_col = n0 + wn0 + lane % C4 * 4;   // the lane's four columns
   const bool interior = m0 + BM <= g.M && n0 + BNC <= g.N;
@@ -721,7 +722,7 @@ __device__ __forceinline__ void gemm_mfma_tile(const GemmArgs& g, int tiles_m, i
   // step J of tile S: the MFMAs of `use`; between them the reads of `fill` (the fragments of k-step J of tile S,
   // in the order the next step's MFMAs need them: a0, b0 .. b_NI-1, a1 ..) and this step's share of the requests
   // for the tile that goes to ring slot SN
-  // EPI_BSUM: bsum[n] += sum_k B(n,k) for this tile's columns, by the workgroups of the first tile row (tm == 0)
+  // EPI_BSUM: bsum[n] += sum_k B(n,k) (EPI_BSUM_BF16: = , as bf16) for this tile's columns, by the workgroups of the first tile row (tm == 0)
   // and there by the waves that hold the tile's first rows: each lane adds up the B fragments it holds anyway, two
   // products with one per instruction (exact, fp32 sums), between the MFMAs.  One register per 32 columns: sums
   // taken with MFMAs against a fragment of ones needed sixteen, which two sets of accumulators leave no room for.

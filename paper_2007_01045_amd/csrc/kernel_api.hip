@@ -59,7 +59,8 @@ static int gemm_args(int dtype, const dapple_gemm_desc* d, GemmArgs& g) {
   g.a_kstrided = d->a_kstrided; g.b_kstrided = d->b_kstrided;
   g.kseg_len = d->kseg_len ? d->kseg_len : d->K; g.segA = d->segA; g.segB = d->segB;
   g.batch = d->batch ? d->batch : 1; g.sA = d->sA; g.sB = d->sB; g.sC = d->sC; g.sBias = d->sBias;
-  g.k_valid = d->k_valid ? d->k_valid : d->K; g.epi = d->epi; g.tile = d->tile;
+  g.k_valid = d->k_valid ? d->k_valid : d->K; g.tile = d->tile;
+  g.epi = d->epi & ~(EPI_SILU | EPI_BSUM_BF16);   // (the gated block's own; a caller's bsum is fp32)
   g.m_valid = d->M; g.n_valid = d->N; g.bsum = d->bsum;
   if (g.K % g.kseg_len) return STAGE_E_CONFIG;
   g.rowdot = d->rowdot;

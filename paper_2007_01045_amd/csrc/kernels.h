@@ -24,7 +24,8 @@ enum GemmEpi {
   EPI_ACC32 = 16,  // C is fp32 and C += t (weight-gradient accumulation)
   EPI_OUT32 = 32,  // C is fp32 and C = t
   EPI_AUX32 = 64,  // aux is fp32 (residual stream of a bf16 stage)
-  EPI_BSUM = 128,  // bsum[n] += sum_k B(n,k): the bias gradient rides along with the weight gradient
+  // bsum[n] += sum_k B(n,k), fp32 (EPI_BSUM_BF16: set, bf16): the bias gradient rides along with the weight gradient
+  EPI_BSUM = 128,
   // rowdot[j*M + m] = sum over the 32 columns n of block j of C[m,n] (as stored, rounded to bf16) * aux[m,n];
   // aux is neither added nor multiplied in.  MFMA kernel only, bf16 output, batch 1.  (The attention
   // backward's delta = rowsum(dctx o ctx) per head leaves the product that makes dctx this way.)
@@ -36,7 +37,7 @@ enum GemmEpi {
   // the residual input of a bf16 stage, unrounded, from the sums it was normalised from.  Batch 1.
   EPI_AUXLN = 1024,
   EPI_SILU = 2048,  // a gated block's activation is SiLU, else GELU (launch_gate_fwd, launch_gate_bwd)
-  EPI_BSUM_BF16 = 4096   // with EPI_BSUM: bsum holds bf16 and is set (MFMA kernel only)
+  EPI_BSUM_BF16 = 4096   // with EPI_BSUM: bsum holds bf16 and is set (MFMA kernel only, any other launch is an error)
 };
 
 struct GemmArgs {
@@ -53,7 +54,7 @@ struct GemmArgs {
   long segA, segB;
   int batch;
   long sA, sB, sC, sBias;
-  float* bsum;    // EPI_BSUM: fp32 [N], of instance 0; both operands k-strided
+  float* bsum;    // EPI_BSUM: fp32 [N] (EPI_BSUM_BF16: bf16), of instance 0; both operands k-strided
   const float* ln_stats;               // EPI_AUXLN: mean and rstd of every row, gamma and beta in the product's type
   const void *ln_gamma, *ln_beta;
   float* rowdot;  // EPI_ROWDOT: fp32 [ceil(N/32)][M]

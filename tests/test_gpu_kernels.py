@@ -543,3 +543,11 @@ def test_attention_random_shapes():
         s = rng.choice([64, 128, 192, 320, 8, 24, 100])
         print(f"case {case}: dtype={dtype} b={b} s={s} A={A} d={d}", flush=True)
         attention_case(dtype, b, s, A, d)
+
+
+@pytest.mark.parametrize("dtype", [B.DTYPE_F32, B.DTYPE_BF16])
+def test_flags_that_the_header_does_not_name_change_nothing(dtype):
+    # (2048 and 4096 are the library's own: a caller's bsum stays fp32 and added to)
+    for flags in (2048, 4096, 2048 | 4096):
+        gemm_case(dtype, 136, 200, 96, True, True, B.EPI_ACC32 | B.EPI_BSUM | flags)
+        gemm_case(dtype, 72, 64, 128, False, True, B.EPI_BIAS | flags)
