@@ -151,16 +151,22 @@ static hipError_t launch(const GemmArgs& g, hipStream_t st) {
   return hipGetLastError();
 }
 
-// Where they take less than the smallest tiles of the MFMA kernel, whose workgroups have more columns and one wave each.  us, tiles / these:
-//   k-contiguous weights, 16 rows: 4096 columns of depth 1024 6.0 / 4.4, 1024 of 8192 20.2 / 16.8, 8192 of 2048 10.1 / 11.6; 32 rows
-//     5.8 / 5.5, 19.8 / 23.3; a depth that is no multiple of 64 (there the tiles are of 64x64): 32 rows, 1032 of 8208 37.2 / 17.8
-//   k-strided, 16 rows: 1024 of 4096 11.9 / 12.8, 1032 of 4104 21.0 / 11.8 (32 rows 21.3 / 14.4)
+// Where they take less than the smallest tiles of the MFMA kernel, whose workgroups have more columns and one wave each: while each of
+// the 256 units has one of these workgroups, 4096 columns; beyond that the tiles have enough workgroups and read larger pieces.
+// us, tiles / these, weights out of memory:
+//   k-contiguous weights, 16 rows, depth 1024, 1024 columns 5.7 / 4.5, 4096 7.2 / 5.4, 8192 7.5 / 8.6, 16384 9.4 / 14.4; depth 4096, 4096 columns
+//     16.6 / 10.8, 8192 16.8 / 19.1; 1024 of depth 8192 27.5 / 17.5 (one row 6.6 / 4.5, 7.0 / 7.1 and 15.7 / 8.2, 15.6 / 13.9 for 4096, 8192 of 1024, 4096);
+//     32 rows, 4096 of depth 1024 5.8 / 5.5, 1024 of 8192 19.8 / 23.3
+//   the same, a depth that is no multiple of 64 (there the tiles are of 64x64): 32 rows, depth 1032, 4096 columns 10.5 / 5.9, 8192 11.0 / 9.2, 16384
+//     12.9 / 15.9; depth 4104, 4096 columns 25.1 / 13.5, 8192 25.6 / 24.2
+//   k-strided, 16 rows: 1024 of 4096 11.9 / 12.8, 1032 of 4104 21.0 / 11.8 (32 rows 21.3 / 14.4); with the gate and value product, depth
+//     4104, 32 rows, 4096 columns 49.5 / 43.9, 8192 91 / 102
 //   gate and value, 16 rows: 256 of 2048 10.2 / 8.0, 2048 of 768 7.1 / 6.5, 4096 of 1024 8.2 / 8.4, 8192 of 2048 19 / 26; 32 rows, 256 of 2048
 //     10.4 / 12.1
 bool gemm_rows_takes(const GemmArgs& g, bool gate) {
   const bool ragged = g.K % 64 != 0;
-  if (!g.b_kstrided) return g.M <= (ragged ? 32 : 16);
-  return gate ? g.M <= 16 && g.N <= 2048 : g.M <= 32 && ragged;
+  if (!g.b_kstrided) return ragged ? g.M <= 32 && g.N <= 8192 : g.M <= 16 && g.N <= 4096;
+  return gate ? g.M <= 16 && g.N <= 2048 : g.M <= 32 && g.N <= 4096 && ragged;
 }
 hipError_t launch_rows_gate_fwd(const GemmArgs& g, hipStream_t st) { return launch<RowsOut::H, true>(g, st); }
 hipError_t launch_rows_gate_bwd(const GemmArgs& g, hipStream_t st) { return launch<RowsOut::G, false>(g, st); }

@@ -272,3 +272,13 @@ def test_same_bits_on_another_stream_and_in_a_graph(dtype, accumulate):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(outs, eager)), k
+
+
+@pytest.mark.parametrize("shape", [(16, 64, 4096), (16, 64, 4104), (9, 128, 9000), (32, 72, 8192), (32, 72, 8200), (1, 72, 8200), (20, 4096, 72),
+                                   (20, 4104, 72), (16, 4096, 64), (16, 4104, 64)], ids=lambda s: "-".join(map(str, s)))
+def test_few_rows_of_many_columns(shape):
+    # on either side of the columns from which on few rows are the tiles' again, each product
+    for kw in (dict(), dict(act=B.ACT_GELU, pad=8, accumulate=1)):
+        c = Case(BF, *shape, **kw)
+        c.run()
+        c.check()
