@@ -255,3 +255,16 @@ def test_many_sinks(case):
     c = Case(*case)
     c.run()
     c.check()
+
+
+@pytest.mark.parametrize("case", [  # fp32 in groups of four waves: from 512 tiles of 64 rows on, a wide head's forward from 192 on
+    (F, 4, 260, 32, 8, 32, 50, 4, True, [260, 0, 77, 259]), (F, 4, 260, 32, 32, 16, 0, 0, False, None), (F, 3, 450, 24, 8, 64, 100, 7, False, [450, 64, 333]),
+    (F, 2, 330, 48, 16, 128, 70, 3, True, None), (F, 3, 333, 12, 4, 128, 40, 2, True, [333, 1, 200]), (F, 3, 333, 12, 12, 72, 0, 0, False, None),
+    # and with walks of few key heads in parts: fp32, and bf16 in workgroups of four waves
+    (F, 1, 600, 64, 2, 36, 0, 0, True, None), (F, 1, 600, 64, 2, 128, 200, 70, False, [577]), (F, 2, 300, 64, 2, 64, 60, 1, True, [300, 131]),
+    (H, 1, 600, 64, 2, 64, 0, 0, True, None), (H, 1, 600, 64, 2, 64, 200, 130, False, [577]), (H, 2, 300, 64, 2, 32, 60, 1, True, [300, 131])],
+    ids=lambda c: "-".join("x" if v is None else str(v).replace(", ", "_") for v in c))
+def test_many_tiles(case):
+    c = Case(*case)
+    c.run()
+    c.check()

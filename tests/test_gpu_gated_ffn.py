@@ -282,3 +282,17 @@ def test_few_rows_of_many_columns(shape):
         c = Case(BF, *shape, **kw)
         c.run()
         c.check()
+
+
+@pytest.mark.parametrize("shape,kw", [
+    ((4090, 36, 1020), dict(act=B.ACT_GELU)),                      # gate and value
+    ((4090, 2044, 36), dict(pad=4)),                               # the output product
+    ((4090, 36, 2044), dict(bias=False, accumulate=1)),            # dh with the gate's gradient
+    ((2040, 2044, 2044), dict()), ((2040, 2044, 2044), dict(accumulate=1, act=B.ACT_GELU)),      # the last gradients, dx with them
+    ((100, 2044, 2804), dict(dx=False)), ((100, 2044, 2804), dict(dx=False, bias=False, accumulate=1)),
+    ((4090, 36, 1020), dict(keep=False, bias=False))], ids=str)
+def test_fp32_wide_tiles(shape, kw):
+    # two 128-wide tiles for each unit, with rests in every direction
+    c = Case(F32, *shape, **kw)
+    c.run()
+    c.check()
