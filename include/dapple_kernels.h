@@ -126,7 +126,7 @@ int dapple_colsum_static(int dtype, const void* X, int rows, int cols, int ld, f
  * stage_last_error() says why.  Nothing is allocated and nothing waited for; results are the same bits from call to call;
  * every call can be captured into a HIP graph (after one eager call of the same kind).  The calling thread's current device is the
  * stream's.  `workspace` is device memory of
- * the size that the operator's *_workspace function returns (host only; a negative code for a call that would be refused),
+ * the size that the operator's *_workspace function returns (host only; a negative code for sizes that would be refused),
  * 16-byte aligned, whose contents do not matter before or after: calls that may overlap need one each. */
 
 /* Attention with a window, first tokens that stay visible, shared key heads and sequences of their own lengths.
@@ -219,7 +219,7 @@ int dapple_rope_table(float* table, int max_pos, int rot, double base, double fa
  * dw_in, dw_out (both or neither) with db_in, db_out (NULL = not wanted).  accumulate = 0: these four are of dtype and set;
  * accumulate != 0: fp32, and added to, as a stage sums its micro-batches.
  * Outputs overlap no input.  bf16: H, F and strides multiples of 8; fp32: of 4; all 16-byte aligned; T * 2F, T * stride and H * 2F
- * below 2^30 - 4096.  bf16 calls round g, u, h, dg and du once each (products are summed in fp32). */
+ * below 2^30 - 4096; bf16: 2F, ldx and lddy below 2^24.  bf16 calls round g, u, h, dg and du once each (products are summed in fp32). */
 enum { DAPPLE_ACT_SILU = 0, DAPPLE_ACT_GELU = 1 };
 typedef struct {
   const void* x;

@@ -189,6 +189,9 @@ static int ffn_args(int dtype, const dapple_gated_ffn_desc* d, bool bwd, bool si
     *l.to = l.given ? l.given : d->H;
     if (*l.to < d->H || *l.to % v || (long)d->T * *l.to >= most) return set_error(STAGE_E_CONFIG, "a row stride of %d", l.given);
   }
+  // (64 rows of an operand are counted in 31 bits of bytes: see gemm_uses_mfma)
+  if (dtype == STAGE_DTYPE_BF16 && (2L * d->F >= 1 << 24 || a.ldx >= 1 << 24 || (bwd && a.lddy >= 1 << 24)))
+    return set_error(STAGE_E_CONFIG, "2F or a stride of x or dy of 2^24 and more");
   if (sizes_only) return STAGE_OK;
   if (!d->x || !d->w_in || !d->w_out || !d->h) return set_error(STAGE_E_NULL, "x, w_in, w_out and h must not be NULL");
   if (!bwd && !d->y) return set_error(STAGE_E_NULL, "y must not be NULL");

@@ -182,3 +182,17 @@ def test_the_last_sizes_of_a_launch():
     for sizes in ([most], [1 << 31] * 127 + [(1 << 31) - (1 << 22)]):
         assert B.dapple_grad_norm_workspace(sizes) > 0
         refused(B.STAGE_E_CONFIG, B.dapple_grad_norm_workspace, sizes + [1])
+
+
+def test_gated_ffn_rows_of_2_to_the_24():
+    ok = dict(x=P, w_in=P, w_out=P, h=P, y=P, gu=P, dy=P, dgu=P, workspace=P, T=1, H=8, F=8)
+    for change in (dict(F=1 << 23), dict(ldx=1 << 24), dict(H=1 << 24)):
+        desc = B.gated_ffn_desc(**dict(ok, **change))
+        for f in (B.dapple_gated_ffn_fwd, B.dapple_gated_ffn_bwd, B.dapple_gated_ffn_workspace):
+            with pytest.raises(B.StageError) as e:
+                f(B.DTYPE_BF16, desc)
+            assert e.value.code == B.STAGE_E_CONFIG and "2^24" in str(e.value)
+        assert B.dapple_gated_ffn_workspace(B.DTYPE_F32, desc) > 0
+    for change in (dict(F=(1 << 23) - 8), dict(ldx=(1 << 24) - 8, lddy=(1 << 24) - 8), dict(ldy=1 << 24)):
+        assert B.dapple_gated_ffn_workspace(B.DTYPE_BF16, B.gated_ffn_desc(**dict(ok, **change))) > 0
+    refused(B.STAGE_E_CONFIG, B.dapple_gated_ffn_bwd, B.DTYPE_BF16, B.gated_ffn_desc(**dict(ok, lddy=1 << 24)))
