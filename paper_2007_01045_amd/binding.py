@@ -609,7 +609,7 @@ class StageRunner:
                                  self.step + 1, lr, norm.data_ptr(), beta1, beta2, eps, grad_scale, zero_grads)
         self.step += 1
         if cur is not None and given:      # (one norm for the stages of a pipeline: their updates do not wait for each other)
-            self.held = (norm, self.stream.record_event())
+            self.held = (norm, self.stream.record_event(), cur)
         elif cur is not None:
             cur.wait_stream(self.stream)
         return norm
@@ -623,11 +623,10 @@ class StageRunner:
         return cur
 
     def _release_norm(self):
-        """Drops the last given norm, whose memory is used again on the current stream behind the update that read it."""
+        """Drops the last given norm, whose memory is used again, on the stream it was given on, behind the update that read it."""
         if self.held is not None:
-            cur = self.torch.cuda.current_stream(self.device)
-            if cur.cuda_stream != self.stream.cuda_stream:
-                cur.wait_event(self.held[1])
+            _, event, cur = self.held
+            cur.wait_event(event)
             self.held = None
 
     def to_dev(self, a, dtype=None):
