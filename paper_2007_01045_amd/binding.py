@@ -686,8 +686,11 @@ class PipelineRunner:
                                  self.act_bytes, max_M)
 
     def run(self, M, K, order, xs, dys=None, auxs=None, ys=None, dxs=None):
-        """Enqueue one iteration (device tensors in, device tensors written) and wait for it."""
+        """Enqueue one iteration (device tensors in, device tensors written), behind what torch's current stream holds, and wait
+        for it."""
         ptr = lambda ts: None if ts is None else [t.data_ptr() for t in ts]
+        for r in self.runners:
+            r._after_current()      # (inputs, and whoever had the outputs' memory before)
         pipeline_run(self.p, M, K, order, ptr(xs), ptr(dys), ptr(auxs), ptr(ys), ptr(dxs))
         pipeline_sync(self.p)
 

@@ -240,3 +240,34 @@ def test_recomputing_stages_in_a_pipeline_give_the_same_bits():
         assert o["peak"] == K and np.array_equal(o["grads"], out[0]["grads"])
         for m in range(M):
             assert np.array_equal(o["dxs"][m], out[0]["dxs"][m]) and np.array_equal(o["ys"][m], out[0]["ys"][m])
+
+
+def test_an_iteration_waits_for_inputs_made_late_on_the_current_stream():
+    import torch
+    cfg = I.StageConfig(2, 64, 4, 128, 16, 2, 3, 2, "f32")
+    theta, mbs = make_inputs(cfg, SEED, 3)
+    part = I.StageConfig(1, 64, 4, 128, 16, 2, 3, 2, "f32")
+    n = I.n_params(part)
+    results = []
+    for late in (False, True):
+        pr = B.PipelineRunner([c_config(part, 2)] * 2, [theta[:n], theta[n:]], 3, parts=0)
+        try:
+            x, dy = (torch.from_numpy(np.stack([mb[k].reshape(cfg.tokens, cfg.hidden) for mb in mbs]).astype(np.float32)).cuda() for k in ("x", "dy"))
+            xs, dys = ([torch.full((cfg.tokens, cfg.hidden), float("nan"), device="cuda") for _ in mbs] for _ in "ab")
+            ys, dxs = ([torch.empty(cfg.tokens, cfg.hidden, device="cuda") for _ in mbs] for _ in "ab")
+            torch.cuda.synchronize()
+            if late:
+                w = torch.ones(4096, 4096, device="cuda")
+                for _ in range(80):
+                    w = w @ w * 2.0 ** -12
+            for i in range(3):
+                xs[i].copy_(x[i])
+                dys[i].copy_(dy[i])
+            if not late:
+                torch.cuda.synchronize()
+            pr.run(3, [2, 1], B.ORDER_EARLY_BACKWARD, xs, dys, None, ys, dxs)
+            torch.cuda.synchronize()
+            results.append([t.clone() for t in ys + dxs + [r.grads for r in pr.runners]])
+        finally:
+            pr.close()
+    assert all(bool(t.isfinite().all()) for t in results[0]) and all(torch.equal(a, b) for a, b in zip(*results))
