@@ -245,6 +245,73 @@ int dapple_gated_ffn_fwd(int dtype, const dapple_gated_ffn_desc* d, void* stream
 int64_t dapple_gated_ffn_workspace(int dtype, const dapple_gated_ffn_desc* d);
 int dapple_gated_ffn_bwd(int dtype, const dapple_gated_ffn_desc* d, void* stream);
 
+/* The end of a block: dropout, the residual sum and a norm in one pass, and their gradients.
+ *   z = residual + m (x + bias),   y = norm(z) gamma + beta,   m = 1 / (1 - p) where an element is kept, else 0
+ *   norm: layer (z - mean) / sqrt(var + eps), RMS z / sqrt(mean(z^2) + eps) (no beta), or none (y, dy, stats are not looked at)
+ * rows of H columns, row r of a tensor at r times its stride.  bias, residual, gamma, beta [H]: NULL = 0, 0, 1, 0.  z may be NULL where it
+ * is not wanted (the backward of a norm reads it, and stats [rows][2], mean and 1 / sqrt(...), NULL = not wanted).  What is normed is z
+ * as it is stored (z NULL too).
+ * The mask is made again where it is needed and never stored: element (r, c) belongs to group r * ceil(H / 8) + c / 8, whose four words
+ * are Philox4x32-10 of the counter (group, low and high word of rng[1], site) under the key (low and high word of rng[0]); half word
+ * c % 8, low halves first, decides: it is kept where that is not below 65536 p, rounded (p is that / 65536 then in 1 / (1 - p), too;
+ * p = 1 drops everything).  rng: DEVICE memory, a seed and the number of the step, read when the kernel runs: a captured graph
+ * draws another mask where its owner changes them between replays, but not between forward and backward.  site: tells the calls of a step
+ * apart.  p = 0: rng is not looked at.
+ * bwd: from dy, z and stats, and dz (what comes in through z otherwise; NULL = 0; without a norm it must be given):
+ *   g = dz + norm's gradient at dy gamma;   dresidual = g,  dx = m g;   dbias = sum of dx over the rows, dgamma of dy norm(z), dbeta of dy
+ * each NULL = not wanted; the sums are fp32 [H], of unrounded values, set, or with accumulate != 0 added to; workspace only where one is
+ * wanted.
+ * Types: dtype; residual, z, dz and dresidual fp32 with stream32 != 0; statistics and arithmetic fp32.  An output may be an input of the
+ * same type and stride (z = residual, dresidual = dz, dx = dy, ...), else they do not overlap.  H <= 16384, rows <= 2^26, rows *
+ * ceil(H / 8) < 2^32; any strides and addresses of whole elements. */
+enum { DAPPLE_NORM_NONE = 0, DAPPLE_NORM_LAYER = 1, DAPPLE_NORM_RMS = 2 };
+typedef struct {
+  const void* x;
+  const void* bias;
+  const void* residual;
+  const void* gamma;
+  const void* beta;
+  const uint64_t* rng;
+  void* z;
+  void* y;
+  float* stats;
+  const void* dy;
+  const void* dz;
+  void* dx;
+  void* dresidual;
+  float* dbias;
+  float* dgamma;
+  float* dbeta;
+  void* workspace;
+  int32_t rows, H, norm, stream32, accumulate, site;
+  int32_t ldx, ldr, ldz, ldy, lddy, lddz, lddx, lddr; /* in elements, 0 = H */
+  float p, eps;
+} dapple_dropout_norm_desc;
+int dapple_dropout_norm_fwd(int dtype, const dapple_dropout_norm_desc* d, void* stream);
+int64_t dapple_dropout_norm_workspace(int dtype, const dapple_dropout_norm_desc* d);
+int dapple_dropout_norm_bwd(int dtype, const dapple_dropout_norm_desc* d, void* stream);
+
+/* Rows of a table:  y[r] = scale * table[ids[r]], and the table's gradient  dtable[v] = scale * sum of dy[r] over the rows with ids[r] = v.
+ * table [V, H], ids int32 [rows].  An id outside [0, V) (padding) reads nothing, gives a row of zeros and has no gradient.
+ * bwd: accumulate = 0: dtable is of dtype and set, rows of absent ids to zero; accumulate != 0: fp32, and added to, rows of absent ids
+ * are not touched.  Sums in fp32, each id's rows in an order that sizes and ids alone decide.
+ * Outputs overlap no input.  rows, V <= 2^28, H <= 2^16; any strides and addresses of whole elements; workspace: 16 bytes a row, and at most
+ * 64 KiB a column. */
+typedef struct {
+  const void* table;
+  const int32_t* ids;
+  void* y;
+  const void* dy;
+  void* dtable;
+  void* workspace; /* bwd */
+  int32_t rows, V, H, accumulate;
+  int32_t ldt, ldy, lddy, lddt; /* in elements, 0 = H */
+  float scale;
+} dapple_embedding_desc;
+int dapple_embedding_fwd(int dtype, const dapple_embedding_desc* d, void* stream);
+int64_t dapple_embedding_workspace(int dtype, const dapple_embedding_desc* d);
+int dapple_embedding_bwd(int dtype, const dapple_embedding_desc* d, void* stream);
+
 /* The global norm of n gradient tensors, all of one dtype: grads and sizes are HOST arrays of n device pointers (aligned to
  * their elements) and element counts (0 is allowed, its pointer is not looked at).
  *   norm_dev[0] = |grad_scale| * sqrt(sum of all squares)      (squares and sums in 64 bits)

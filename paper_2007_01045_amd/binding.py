@@ -26,6 +26,7 @@ FLAG_ONE_STREAM = 4
 EPI_BIAS, EPI_ADD, EPI_MUL, EPI_GELU, EPI_ACC32, EPI_BSUM = 1, 2, 4, 8, 16, 128
 EPI_OUT32, EPI_AUX32, EPI_ROWDOT = 32, 64, 256
 ACT_SILU, ACT_GELU = 0, 1
+NORM_NONE, NORM_LAYER, NORM_RMS = 0, 1, 2
 
 
 class stage_config(C.Structure):
@@ -79,6 +80,20 @@ class gated_ffn_desc(C.Structure):      # dapple_gated_ffn_desc
                 ("x", "w_in", "b_in", "w_out", "b_out", "gu", "h", "y", "dy", "dgu", "dx", "dw_in", "db_in", "dw_out", "db_out",
                  "workspace")] + \
                [(n, C.c_int32) for n in ("T", "H", "F", "act", "accumulate", "ldx", "ldy", "lddy", "lddx")]
+
+
+class dropout_norm_desc(C.Structure):      # dapple_dropout_norm_desc
+    _fields_ = [(n, C.c_void_p) for n in
+                ("x", "bias", "residual", "gamma", "beta", "rng", "z", "y", "stats", "dy", "dz", "dx", "dresidual", "dbias", "dgamma", "dbeta",
+                 "workspace")] + \
+               [(n, C.c_int32) for n in ("rows", "H", "norm", "stream32", "accumulate", "site",
+                                         "ldx", "ldr", "ldz", "ldy", "lddy", "lddz", "lddx", "lddr")] + \
+               [("p", C.c_float), ("eps", C.c_float)]
+
+
+class embedding_desc(C.Structure):      # dapple_embedding_desc
+    _fields_ = [(n, C.c_void_p) for n in ("table", "ids", "y", "dy", "dtable", "workspace")] + \
+               [(n, C.c_int32) for n in ("rows", "V", "H", "accumulate", "ldt", "ldy", "lddy", "lddt")] + [("scale", C.c_float)]
 
 
 # every symbol the two headers declare: name -> (restype, argtypes)
@@ -138,6 +153,12 @@ SYMBOLS = {
     "dapple_gated_ffn_fwd": (_i, [_i, C.POINTER(gated_ffn_desc), _vp]),
     "dapple_gated_ffn_workspace": (C.c_int64, [_i, C.POINTER(gated_ffn_desc)]),
     "dapple_gated_ffn_bwd": (_i, [_i, C.POINTER(gated_ffn_desc), _vp]),
+    "dapple_dropout_norm_fwd": (_i, [_i, C.POINTER(dropout_norm_desc), _vp]),
+    "dapple_dropout_norm_workspace": (C.c_int64, [_i, C.POINTER(dropout_norm_desc)]),
+    "dapple_dropout_norm_bwd": (_i, [_i, C.POINTER(dropout_norm_desc), _vp]),
+    "dapple_embedding_fwd": (_i, [_i, C.POINTER(embedding_desc), _vp]),
+    "dapple_embedding_workspace": (C.c_int64, [_i, C.POINTER(embedding_desc)]),
+    "dapple_embedding_bwd": (_i, [_i, C.POINTER(embedding_desc), _vp]),
     "dapple_grad_norm_workspace": (C.c_int64, [C.POINTER(C.c_int64), _i]),
     "dapple_grad_norm": (_i, [_i, _pp, C.POINTER(C.c_int64), _i, _f, _f, _vp, _vp, _vp]),
     "dapple_grad_clip": (_i, [_i, _pp, _pp, C.POINTER(C.c_int64), _i, _vp, _vp]),
@@ -512,6 +533,30 @@ def dapple_gated_ffn_workspace(dtype, desc: gated_ffn_desc) -> int:
 
 def dapple_gated_ffn_bwd(dtype, desc: gated_ffn_desc, stream_ptr=None):
     _check(load().dapple_gated_ffn_bwd(dtype, C.byref(desc), stream_ptr))
+
+
+def dapple_dropout_norm_fwd(dtype, desc: dropout_norm_desc, stream_ptr=None):
+    _check(load().dapple_dropout_norm_fwd(dtype, C.byref(desc), stream_ptr))
+
+
+def dapple_dropout_norm_workspace(dtype, desc: dropout_norm_desc) -> int:
+    return _check(load().dapple_dropout_norm_workspace(dtype, C.byref(desc)))
+
+
+def dapple_dropout_norm_bwd(dtype, desc: dropout_norm_desc, stream_ptr=None):
+    _check(load().dapple_dropout_norm_bwd(dtype, C.byref(desc), stream_ptr))
+
+
+def dapple_embedding_fwd(dtype, desc: embedding_desc, stream_ptr=None):
+    _check(load().dapple_embedding_fwd(dtype, C.byref(desc), stream_ptr))
+
+
+def dapple_embedding_workspace(dtype, desc: embedding_desc) -> int:
+    return _check(load().dapple_embedding_workspace(dtype, C.byref(desc)))
+
+
+def dapple_embedding_bwd(dtype, desc: embedding_desc, stream_ptr=None):
+    _check(load().dapple_embedding_bwd(dtype, C.byref(desc), stream_ptr))
 
 
 # lists of tensors: a stage of many layers has hundreds, and ctypes converts one by one in twice the time

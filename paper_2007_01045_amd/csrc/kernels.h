@@ -308,6 +308,48 @@ hipError_t launch_qk_rope_bwd(Dtype dt, const QkRopeArgs& a, float* partial, hip
 // freq: host, up to 128 of them
 hipError_t launch_rope_table(float* table, int max_pos, int pairs, const double* freq, double magnitude, hipStream_t st);
 
+// ---------------------------------------------------------------- dropout, residual sum and norm (dropout_norm.hip)
+enum { NORM_NONE = 0, NORM_LAYER = 1, NORM_RMS = 2 };
+struct DropNormArgs {
+  const void *x, *bias, *residual, *gamma, *beta;   // x may alone be not NULL
+  const uint64_t* rng;                              // seed and step, on the device; NULL: level = 0
+  void *z, *y;                                      // z NULL: not wanted
+  float* stats;                                     // [rows][2] mean and rstd
+  const void *dy, *dz;                              // dz NULL: no gradient comes in through z
+  void *dx, *dr;                                    // NULL: not wanted, as the sums
+  float *dbias, *dgamma, *dbeta;
+  float* partial;                                   // dropout_norm_blocks() times 3 H
+  int rows, H, norm, stream32, accumulate;
+  int ldx, ldr, ldz, ldy, lddy, lddz, lddx, lddr;
+  uint32_t site, level;                             // an element is kept where its 16 bits are not below level (0 .. 65536)
+  float up, eps;                                    // 65536 / (65536 - level)
+};
+int dropout_norm_blocks(int rows, int H);
+hipError_t launch_dropout_norm_fwd(Dtype dt, const DropNormArgs& a, hipStream_t st);
+hipError_t launch_dropout_norm_bwd(Dtype dt, const DropNormArgs& a, hipStream_t st);
+
+// ---------------------------------------------------------------- embedding by itself (embedding.hip)
+struct EmbeddingArgs {
+  const void* table;
+  const int32_t* ids;
+  void* y;
+  const void* dy;
+  void* dtable;                                     // accumulate: fp32, added to; else of dtype, set
+  int rows, V, H, accumulate;
+  int ldt, ldy, lddy, lddt;
+  float scale;
+};
+// the gradient's sort and sums: `wgs` workgroups of `per` rows each, `passes` digits of `bits` bits; runs of `run` sorted rows
+struct EmbedPlan {
+  uint32_t *list[4], *counts;
+  float* parts;
+  int passes, bits, per, wgs, run, runs, slabs;
+  long bytes;
+};
+int64_t embedding_workspace(const EmbeddingArgs& a);
+hipError_t launch_embedding_fwd(Dtype dt, const EmbeddingArgs& a, hipStream_t st);
+hipError_t launch_embedding_bwd(Dtype dt, const EmbeddingArgs& a, void* ws, hipStream_t st);
+
 // ---------------------------------------------------------------- embedding / head
 // e[r] = E_w[ids[r]] + E_p[r % s]
 hipError_t launch_embed_gather(Dtype dt, const int32_t* ids, const void* Ew, const void* Ep, void* e, int rows, int s,

@@ -230,6 +230,127 @@ int dapple_gated_ffn_bwd(int dtype, const dapple_gated_ffn_desc* d, void* stream
 
 }  // extern "C"
 
+// ------------------------------------------------------------------ dropout, residual sum and norm
+static int norm_args(int dtype, const dapple_dropout_norm_desc* d, bool bwd, bool sizes_only, DropNormArgs& a) {
+  if (!d) return set_error(STAGE_E_NULL, "the descriptor is NULL");
+  if (bad_dtype(dtype)) return set_error(STAGE_E_CONFIG, "dtype %d", dtype);
+  if (d->rows < 1 || d->H < 1 || d->H > 16384) return set_error(STAGE_E_CONFIG, "%d rows of %d columns (at most 16384)", d->rows, d->H);
+  // (a group of eight elements is counted in 32 bits; so are a launch's work-items)
+  if (d->rows > 1 << 26 || (long)d->rows * ((d->H + 7) / 8) >= 1L << 32) return set_error(STAGE_E_CONFIG, "2^26 rows or 2^32 groups of eight columns and more");
+  if (sizes_only) return STAGE_OK;
+  if (d->norm != DAPPLE_NORM_NONE && d->norm != DAPPLE_NORM_LAYER && d->norm != DAPPLE_NORM_RMS) return set_error(STAGE_E_CONFIG, "norm %d", d->norm);
+  if (!(d->p >= 0.f && d->p <= 1.f)) return set_error(STAGE_E_CONFIG, "p must lie in [0, 1]");
+  const bool norm = d->norm != DAPPLE_NORM_NONE;
+  if (norm && !(d->eps >= 0.f)) return set_error(STAGE_E_CONFIG, "eps must not be negative");
+  if (!norm && (d->gamma || d->beta || (bwd && (d->dgamma || d->dbeta)))) return set_error(STAGE_E_CONFIG, "gamma or beta without a norm");
+  if (d->norm == DAPPLE_NORM_RMS && (d->beta || (bwd && d->dbeta))) return set_error(STAGE_E_CONFIG, "an RMS norm has no beta");
+  a.rows = d->rows; a.H = d->H; a.norm = d->norm; a.stream32 = d->stream32 != 0; a.accumulate = d->accumulate != 0;
+  a.site = (uint32_t)d->site; a.level = (uint32_t)std::nearbyint(65536.0 * d->p); a.eps = d->eps;
+  a.up = a.level < 65536 ? (float)(65536.0 / (65536.0 - a.level)) : 0.f;
+  if (a.level && !d->rng) return set_error(STAGE_E_NULL, "rng must not be NULL");
+  a.rng = a.level ? d->rng : nullptr;
+  const struct { int given; int* to; } lds[] = {{d->ldx, &a.ldx}, {d->ldr, &a.ldr}, {d->ldz, &a.ldz}, {d->ldy, &a.ldy},
+      {d->lddy, &a.lddy}, {d->lddz, &a.lddz}, {d->lddx, &a.lddx}, {d->lddr, &a.lddr}};
+  for (const auto& l : lds) {
+    if (l.given && l.given < d->H) return set_error(STAGE_E_CONFIG, "a row stride of %d for %d columns", l.given, d->H);
+    *l.to = l.given ? l.given : d->H;
+  }
+  if (!bwd && (!d->x || (norm ? !d->y : !d->z))) return set_error(STAGE_E_NULL, "x, and y (without a norm: z), must not be NULL");
+  if (bwd && (norm ? !d->dy || !d->z || !d->stats : !d->dz)) return set_error(STAGE_E_NULL, "dy, z and stats (without a norm: dz) must not be NULL");
+  if (bwd && !d->dx && !d->dresidual && !d->dbias && !d->dgamma && !d->dbeta) return set_error(STAGE_E_NULL, "no gradient is wanted");
+  const size_t es = dtype == STAGE_DTYPE_BF16 ? 2 : 4, zs = a.stream32 ? 4 : es;
+  a.gamma = d->gamma;
+  a.z = d->z; a.stats = d->stats;
+  if (!bwd) {
+    a.x = d->x; a.bias = d->bias; a.residual = d->residual; a.beta = d->beta; a.y = norm ? d->y : nullptr;
+  } else {
+    a.dy = norm ? d->dy : nullptr; a.dz = d->dz; a.dx = d->dx; a.dr = d->dresidual; a.dbias = d->dbias; a.dgamma = d->dgamma; a.dbeta = d->dbeta;
+    if (a.dbias || a.dgamma || a.dbeta) {
+      if (!d->workspace) return set_error(STAGE_E_NULL, "workspace is NULL");
+      if (!aligned_to(d->workspace, 16)) return set_error(STAGE_E_CONFIG, "workspace not aligned to 16 bytes");
+      a.partial = (float*)d->workspace;
+    }
+  }
+  for (const void* p : {a.x, a.bias, a.gamma, a.beta, (const void*)a.y, a.dy, (const void*)a.dx})
+    if (!aligned_to(p, es)) return set_error(STAGE_E_CONFIG, "a tensor is not aligned to its elements");
+  for (const void* p : {a.residual, (const void*)a.z, a.dz, (const void*)a.dr})
+    if (!aligned_to(p, zs)) return set_error(STAGE_E_CONFIG, "a tensor of the stream is not aligned to its elements");
+  for (const void* p : {a.stats, a.dbias, a.dgamma, a.dbeta})
+    if (!aligned_to(p, 4)) return set_error(STAGE_E_CONFIG, "stats or a sum is not aligned to its elements");
+  if (!aligned_to(a.rng, 8)) return set_error(STAGE_E_CONFIG, "rng not aligned to 8 bytes");
+  return STAGE_OK;
+}
+
+extern "C" {
+
+int dapple_dropout_norm_fwd(int dtype, const dapple_dropout_norm_desc* d, void* stream) {
+  DropNormArgs a{};
+  const int rc = norm_args(dtype, d, false, false, a);
+  return rc != STAGE_OK ? rc : rc_of(launch_dropout_norm_fwd(type_of(dtype), a, (hipStream_t)stream));
+}
+
+int64_t dapple_dropout_norm_workspace(int dtype, const dapple_dropout_norm_desc* d) {
+  DropNormArgs a{};
+  const int rc = norm_args(dtype, d, true, true, a);
+  return rc != STAGE_OK ? rc : (int64_t)dropout_norm_blocks(d->rows, d->H) * 3 * d->H * 4;
+}
+
+int dapple_dropout_norm_bwd(int dtype, const dapple_dropout_norm_desc* d, void* stream) {
+  DropNormArgs a{};
+  const int rc = norm_args(dtype, d, true, false, a);
+  return rc != STAGE_OK ? rc : rc_of(launch_dropout_norm_bwd(type_of(dtype), a, (hipStream_t)stream));
+}
+
+}  // extern "C"
+
+// ------------------------------------------------------------------ embedding
+static int embedding_args(int dtype, const dapple_embedding_desc* d, bool bwd, bool sizes_only, EmbeddingArgs& a) {
+  if (!d) return set_error(STAGE_E_NULL, "the descriptor is NULL");
+  if (bad_dtype(dtype)) return set_error(STAGE_E_CONFIG, "dtype %d", dtype);
+  if (d->rows < 1 || d->V < 1 || d->H < 1 || d->rows > 1 << 28 || d->V > 1 << 28 || d->H > 1 << 16)
+    return set_error(STAGE_E_CONFIG, "%d rows (at most 2^28) of a table of %d (at most 2^28) by %d (at most 2^16)", d->rows, d->V, d->H);
+  a.rows = d->rows; a.V = d->V; a.H = d->H;
+  if (sizes_only) return STAGE_OK;
+  if (!std::isfinite(d->scale)) return set_error(STAGE_E_CONFIG, "scale must be finite");
+  a.accumulate = d->accumulate != 0; a.scale = d->scale;
+  const struct { int given; int* to; } lds[] = {{d->ldt, &a.ldt}, {d->ldy, &a.ldy}, {d->lddy, &a.lddy}, {d->lddt, &a.lddt}};
+  for (const auto& l : lds) {
+    if (l.given && l.given < d->H) return set_error(STAGE_E_CONFIG, "a row stride of %d for %d columns", l.given, d->H);
+    *l.to = l.given ? l.given : d->H;
+  }
+  if (!d->ids || (bwd ? !d->dy || !d->dtable || !d->workspace : !d->table || !d->y))
+    return set_error(STAGE_E_NULL, bwd ? "ids, dy, dtable and workspace must not be NULL" : "table, ids and y must not be NULL");
+  const size_t es = dtype == STAGE_DTYPE_BF16 ? 2 : 4;
+  a.ids = d->ids;
+  if (bwd) { a.dy = d->dy; a.dtable = d->dtable; } else { a.table = d->table; a.y = d->y; }
+  if (!aligned_to(a.table, es) || !aligned_to(a.y, es) || !aligned_to(a.dy, es) || !aligned_to(a.dtable, a.accumulate ? 4 : es) || !aligned_to(a.ids, 4))
+    return set_error(STAGE_E_CONFIG, "a tensor is not aligned to its elements");
+  if (bwd && !aligned_to(d->workspace, 16)) return set_error(STAGE_E_CONFIG, "workspace not aligned to 16 bytes");
+  return STAGE_OK;
+}
+
+extern "C" {
+
+int dapple_embedding_fwd(int dtype, const dapple_embedding_desc* d, void* stream) {
+  EmbeddingArgs a{};
+  const int rc = embedding_args(dtype, d, false, false, a);
+  return rc != STAGE_OK ? rc : rc_of(launch_embedding_fwd(type_of(dtype), a, (hipStream_t)stream));
+}
+
+int64_t dapple_embedding_workspace(int dtype, const dapple_embedding_desc* d) {
+  EmbeddingArgs a{};
+  const int rc = embedding_args(dtype, d, true, true, a);
+  return rc != STAGE_OK ? rc : embedding_workspace(a);
+}
+
+int dapple_embedding_bwd(int dtype, const dapple_embedding_desc* d, void* stream) {
+  EmbeddingArgs a{};
+  const int rc = embedding_args(dtype, d, true, false, a);
+  return rc != STAGE_OK ? rc : rc_of(launch_embedding_bwd(type_of(dtype), a, d->workspace, (hipStream_t)stream));
+}
+
+}  // extern "C"
+
 // ------------------------------------------------------------------ gradient norm
 static int check_sizes(const int64_t* sizes, int n) {
   if (n < 0) return set_error(STAGE_E_CONFIG, "%d tensors", n);

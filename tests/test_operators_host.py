@@ -196,3 +196,62 @@ def test_gated_ffn_rows_of_2_to_the_24():
     for change in (dict(F=(1 << 23) - 8), dict(ldx=(1 << 24) - 8, lddy=(1 << 24) - 8), dict(ldy=1 << 24)):
         assert B.dapple_gated_ffn_workspace(B.DTYPE_BF16, B.gated_ffn_desc(**dict(ok, **change))) > 0
     refused(B.STAGE_E_CONFIG, B.dapple_gated_ffn_bwd, B.DTYPE_BF16, B.gated_ffn_desc(**dict(ok, lddy=1 << 24)))
+
+
+def test_philox_reference():
+    # the vectors that the generator's authors publish for ten rounds of four words
+    from tests.dropout_util import philox
+    full = 0xffffffff
+    for ctr, key, want in (([0] * 4, [0] * 2, [0x6627e8d5, 0xe169c58d, 0xbc57ac4c, 0x9b00dbd8]),
+                           ([full] * 4, [full] * 2, [0x408f276d, 0x41c83b0e, 0xa20bc7c6, 0x6d5451fd]),
+                           ([0x243f6a88, 0x85a308d3, 0x13198a2e, 0x03707344], [0xa4093822, 0x299f31d0], [0xd16cfe09, 0x94fdcceb, 0x5001e420, 0x24126ea1])):
+        assert [int(x) for x in philox(ctr, key)] == want
+
+
+def test_dropout_norm_refusals():
+    ok = dict(x=P, bias=P, residual=P, gamma=P, beta=P, rng=P, z=P, y=P, stats=P, dy=P, dz=P, dx=P, dresidual=P, dbias=P, dgamma=P, dbeta=P, workspace=P,
+              rows=10, H=64, norm=B.NORM_LAYER, p=0.1, eps=1e-5)
+    null, conf = B.STAGE_E_NULL, B.STAGE_E_CONFIG
+    both = [(null, dict(rng=None)), (conf, dict(rows=0)), (conf, dict(H=0)), (conf, dict(H=16385)), (conf, dict(norm=3)), (conf, dict(norm=-1)), (conf, dict(p=-0.1)),
+            (conf, dict(p=1.1)), (conf, dict(p=math.nan)), (conf, dict(eps=-1.0)), (conf, dict(eps=math.nan)), (conf, dict(ldx=63)), (conf, dict(lddr=-1)),
+            (conf, dict(rows=(1 << 26) + 1)), (conf, dict(rows=1 << 26, H=512)), (conf, dict(rng=P + 4)), (conf, dict(stats=P + 2)), (conf, dict(z=P + 1)),
+            (conf, dict(stream32=1, z=P + 2)), (conf, dict(gamma=P + 1)), (conf, dict(norm=B.NORM_NONE)), (conf, dict(norm=B.NORM_NONE, beta=None, gamma=P)),
+            (conf, dict(norm=B.NORM_RMS))]
+    for code, change in both:
+        for f in (B.dapple_dropout_norm_fwd, B.dapple_dropout_norm_bwd):
+            refused(code, f, B.DTYPE_BF16, B.dropout_norm_desc(**dict(ok, **change)))
+    none = dict(norm=B.NORM_NONE, gamma=None, beta=None, dgamma=None, dbeta=None)
+    for change in (dict(x=None), dict(y=None), dict(none, z=None)):
+        refused(null, B.dapple_dropout_norm_fwd, B.DTYPE_F32, B.dropout_norm_desc(**dict(ok, **change)))
+    for change in (dict(dy=None), dict(z=None), dict(stats=None), dict(workspace=None), dict(none, dz=None),
+                   dict(dx=None, dresidual=None, dbias=None, dgamma=None, dbeta=None)):
+        refused(null, B.dapple_dropout_norm_bwd, B.DTYPE_F32, B.dropout_norm_desc(**dict(ok, **change)))
+    for change in (dict(workspace=P + 8), dict(dx=P + 2), dict(dbias=P + 2), dict(dz=P + 2), dict(norm=B.NORM_RMS, beta=None)):
+        refused(conf, B.dapple_dropout_norm_bwd, B.DTYPE_F32, B.dropout_norm_desc(**dict(ok, **change)))
+    refused(conf, B.dapple_dropout_norm_fwd, 2, B.dropout_norm_desc(**ok))
+    size = lambda rows, H: B.dapple_dropout_norm_workspace(B.DTYPE_BF16, B.dropout_norm_desc(rows=rows, H=H))  # noqa: E731
+    assert size(1, 1) >= 12 and size(1 << 26, 504) > 0 and size((1 << 21) - 1, 16384) > 0
+    for sizes in ((1 << 26, 512), (1 << 21, 16384), (0, 8), (8, 16385)):
+        refused(conf, size, *sizes)
+
+
+def test_embedding_refusals():
+    ok = dict(table=P, ids=P, y=P, dy=P, dtable=P, workspace=P, rows=10, V=100, H=64, scale=1.0)
+    null, conf = B.STAGE_E_NULL, B.STAGE_E_CONFIG
+    both = [(null, dict(ids=None)), (conf, dict(rows=0)), (conf, dict(V=0)), (conf, dict(H=0)), (conf, dict(rows=(1 << 28) + 1)), (conf, dict(V=(1 << 28) + 1)),
+            (conf, dict(H=(1 << 16) + 1)), (conf, dict(scale=math.inf)), (conf, dict(scale=math.nan)), (conf, dict(ldt=63)), (conf, dict(lddt=-64)), (conf, dict(ids=P + 2))]
+    for code, change in both:
+        for f in (B.dapple_embedding_fwd, B.dapple_embedding_bwd):
+            refused(code, f, B.DTYPE_BF16, B.embedding_desc(**dict(ok, **change)))
+    for change in (dict(table=None), dict(y=None)):
+        refused(null, B.dapple_embedding_fwd, B.DTYPE_F32, B.embedding_desc(**dict(ok, **change)))
+    for change in (dict(dy=None), dict(dtable=None), dict(workspace=None)):
+        refused(null, B.dapple_embedding_bwd, B.DTYPE_F32, B.embedding_desc(**dict(ok, **change)))
+    for change in (dict(workspace=P + 8), dict(dy=P + 1), dict(accumulate=1, dtable=P + 2)):
+        refused(conf, B.dapple_embedding_bwd, B.DTYPE_BF16, B.embedding_desc(**dict(ok, **change)))
+    refused(conf, B.dapple_embedding_fwd, B.DTYPE_BF16, B.embedding_desc(**dict(ok, y=P + 1)))
+    refused(conf, B.dapple_embedding_fwd, -1, B.embedding_desc(**ok))
+    size = lambda rows, V, H: B.dapple_embedding_workspace(B.DTYPE_BF16, B.embedding_desc(rows=rows, V=V, H=H))  # noqa: E731
+    for rows, V, H in ((1, 1, 1), (65536, 30522, 1024), (1 << 28, 1 << 28, 1 << 16)):
+        assert 16 * rows <= size(rows, V, H) <= 16 * rows + (1 << 16) * H + (1 << 18)
+    refused(conf, size, 0, 1, 1)
