@@ -165,6 +165,43 @@ int dapple_attention_window_fwd(int dtype, const dapple_attention_window_desc* d
 int64_t dapple_attention_window_workspace(int dtype, const dapple_attention_window_desc* d);
 int dapple_attention_window_bwd(int dtype, const dapple_attention_window_desc* d, void* stream);
 
+/* Attention of packed documents: rows of one long row of tokens that see their own document only, with capped logits and a bias that
+ * falls with the distance.  q [rows, A heads of d], k and v [rows, Ak heads] and shared key heads as above.
+ * Document t holds the rows from ends[t - 1] (0) to ends[t]; what row i sees of its document, from begin to end:
+ *   (causal = 0 or j <= i or j < begin + prefix[t])  and  (window = 0 or |i - j| < window)
+ * dapple_doc_spans writes that down as runs of rows, spans int32 [4 * rows + 1], once for all calls on the same rows (all layers, both
+ * directions, any head counts and types).  ends: device int32 [n], ascending (equal ones: an empty document), clamped to [0, rows]; prefix:
+ * device int32 [n], clamped to the document, NULL = 0, only with causal.  Rows from ends[n - 1] on see nothing and are seen by nobody;
+ * what q, k, v and dctx hold there is not used, their ctx, dq, dk, dv are set to 0, their lse to -infinity.  Before them, inputs are finite.
+ *   logit = t - slopes[h] |i - j|,   t = cap tanh(scale q k / cap), or scale q k with cap = 0
+ * slopes: device fp32 [A], NULL = 0; constants (they have no gradient).  cap: 0 or 2^-20 to 2^10.  scale > 0; 0 = 1/sqrt(d).
+ * fwd: ctx, lse [A, rows] fp32 = log2 of the sum of 2^(log2(e) logit), ctx32 (may be NULL) as above.  bwd: dq, dk, dv from dctx and the ctx, ctx32
+ * (or NULL) and lse of fwd.  spans holds what dapple_doc_spans left, of the same rows (other contents: wrong results, nothing worse).
+ * Strides, alignment, limits (with b = 1, s = rows), rounding and overlaps as for dapple_attention_window; workspace: below 4 A rows bytes +
+ * 256 MiB. */
+typedef struct {
+  const void* q;
+  const void* k;
+  const void* v;
+  void* ctx;
+  float* ctx32;
+  float* lse;
+  const int32_t* spans;
+  const float* slopes;
+  const void* dctx;
+  void* dq;
+  void* dk;
+  void* dv;
+  void* workspace; /* bwd */
+  int32_t rows, A, Ak, d;
+  int32_t ldq, ldk, ldv, ldc, lddc, lddq, lddk, lddv; /* ldc: of ctx and ctx32 */
+  float scale, cap;
+} dapple_attention_docs_desc;
+int dapple_doc_spans(const int32_t* ends, const int32_t* prefix, int n, int rows, int causal, int window, int32_t* spans, void* stream);
+int dapple_attention_docs_fwd(int dtype, const dapple_attention_docs_desc* d, void* stream);
+int64_t dapple_attention_docs_workspace(int dtype, const dapple_attention_docs_desc* d);
+int dapple_attention_docs_bwd(int dtype, const dapple_attention_docs_desc* d, void* stream);
+
 /* RMS norm of every query and key head and the rotation by position, in one pass (forward), and its gradient.
  * Row r of q holds A heads of d columns, head h in columns [h d, (h+1) d) of q + r*ldq; k holds Ak heads likewise (Ak = 0: no
  * keys, its pointers are not looked at).  Per head:

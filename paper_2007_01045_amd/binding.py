@@ -75,6 +75,13 @@ class attention_window_desc(C.Structure):      # dapple_attention_window_desc
                  "ldq", "ldk", "ldv", "ldc", "lddc", "lddq", "lddk", "lddv")] + [("scale", C.c_float)]
 
 
+class attention_docs_desc(C.Structure):      # dapple_attention_docs_desc
+    _fields_ = [(n, C.c_void_p) for n in
+                ("q", "k", "v", "ctx", "ctx32", "lse", "spans", "slopes", "dctx", "dq", "dk", "dv", "workspace")] + \
+               [(n, C.c_int32) for n in
+                ("rows", "A", "Ak", "d", "ldq", "ldk", "ldv", "ldc", "lddc", "lddq", "lddk", "lddv")] + [("scale", C.c_float), ("cap", C.c_float)]
+
+
 class gated_ffn_desc(C.Structure):      # dapple_gated_ffn_desc
     _fields_ = [(n, C.c_void_p) for n in
                 ("x", "w_in", "b_in", "w_out", "b_out", "gu", "h", "y", "dy", "dgu", "dx", "dw_in", "db_in", "dw_out", "db_out",
@@ -146,6 +153,10 @@ SYMBOLS = {
     "dapple_attention_window_fwd": (_i, [_i, C.POINTER(attention_window_desc), _vp]),
     "dapple_attention_window_workspace": (C.c_int64, [_i, C.POINTER(attention_window_desc)]),
     "dapple_attention_window_bwd": (_i, [_i, C.POINTER(attention_window_desc), _vp]),
+    "dapple_doc_spans": (_i, [_vp, _vp, _i, _i, _i, _i, _vp, _vp]),
+    "dapple_attention_docs_fwd": (_i, [_i, C.POINTER(attention_docs_desc), _vp]),
+    "dapple_attention_docs_workspace": (C.c_int64, [_i, C.POINTER(attention_docs_desc)]),
+    "dapple_attention_docs_bwd": (_i, [_i, C.POINTER(attention_docs_desc), _vp]),
     "dapple_qk_rope_fwd": (_i, [_i, C.POINTER(qk_rope_desc), _vp]),
     "dapple_qk_rope_workspace": (C.c_int64, [_i, C.POINTER(qk_rope_desc)]),
     "dapple_qk_rope_bwd": (_i, [_i, C.POINTER(qk_rope_desc), _vp]),
@@ -503,6 +514,23 @@ def dapple_attention_window_workspace(dtype, desc: attention_window_desc) -> int
 
 def dapple_attention_window_bwd(dtype, desc: attention_window_desc, stream_ptr=None):
     _check(load().dapple_attention_window_bwd(dtype, C.byref(desc), stream_ptr))
+
+
+def dapple_doc_spans(ends_ptr, n, rows, spans_ptr, causal=1, window=0, prefix_ptr=None, stream_ptr=None):
+    """spans_ptr (device int32 [4 * rows + 1]): what each row of n packed documents that end at ends sees, for dapple_attention_docs."""
+    _check(load().dapple_doc_spans(ends_ptr, prefix_ptr, n, rows, causal, window, spans_ptr, stream_ptr))
+
+
+def dapple_attention_docs_fwd(dtype, desc: attention_docs_desc, stream_ptr=None):
+    _check(load().dapple_attention_docs_fwd(dtype, C.byref(desc), stream_ptr))
+
+
+def dapple_attention_docs_workspace(dtype, desc: attention_docs_desc) -> int:
+    return _check(load().dapple_attention_docs_workspace(dtype, C.byref(desc)))
+
+
+def dapple_attention_docs_bwd(dtype, desc: attention_docs_desc, stream_ptr=None):
+    _check(load().dapple_attention_docs_bwd(dtype, C.byref(desc), stream_ptr))
 
 
 def dapple_qk_rope_fwd(dtype, desc: qk_rope_desc, stream_ptr=None):

@@ -251,11 +251,25 @@ struct AttnWinArgs {
   int ldq, ldk, ldv, ldc, lddc, lddq, lddk, lddv;
   float scale;
   WinPlan plan;
+  // attention_docs.hip: b = 1 and s packed rows, W = S = 0; what a row sees (launch_doc_spans); slopes [A] or NULL;
+  // cap2 = cap log2(e) (0: none), bend = what tanh's argument is made with (bf16: 2 log2(e) scale / cap; fp32: scale / cap)
+  const int32_t* spans;
+  const float* slopes;
+  float cap2, bend;
 };
+enum { MASK_WINDOW = 0, MASK_SPANS = 1 };
+enum { SCORE_PLAIN = 0, SCORE_SLOPE = 1, SCORE_CAP = 2 };   // SCORE_CAP: with slopes or without; fp32: any
 bool attn_win_takes(Dtype dt, const AttnWinArgs& a);
 int64_t attn_win_workspace(Dtype dt, AttnWinArgs a);   // bytes of the backward's
 hipError_t launch_attn_win_fwd(Dtype dt, const AttnWinArgs& a, hipStream_t st);
-hipError_t launch_attn_win_bwd(Dtype dt, AttnWinArgs a, void* workspace, hipStream_t st);
+hipError_t launch_attn_win_bwd(Dtype dt, const AttnWinArgs& a, void* workspace, hipStream_t st);
+// spans [4 rows + 1] of n documents that end at ends[t]; prefix [n] (may be NULL) rows of each that all of it sees
+hipError_t launch_doc_spans(const int32_t* ends, const int32_t* prefix, int n, int rows, int causal, int window, int32_t* spans, hipStream_t st);
+hipError_t launch_attn_docs_fwd(Dtype dt, const AttnWinArgs& a, hipStream_t st);
+hipError_t launch_attn_docs_fwd_f32(const AttnWinArgs& a, hipStream_t st);
+hipError_t launch_attn_docs_bwd(Dtype dt, const AttnWinArgs& a, void* workspace, hipStream_t st);
+hipError_t launch_attn_docs_bwd_f32(const AttnWinArgs& a, void* workspace, hipStream_t st);
+hipError_t launch_attn_docs_bwd_cap(const AttnWinArgs& a, void* workspace, hipStream_t st);
 
 // ---------------------------------------------------------------- row kernels
 // y = LN(z) over the last dim (H), stats[2*r] = mean, stats[2*r+1] = rstd.  z_f32: z is fp32

@@ -82,6 +82,60 @@ int dapple_attention_window_bwd(int dtype, const dapple_attention_window_desc* d
 
 }  // extern "C"
 
+// ------------------------------------------------------------------ attention of packed documents
+static int docs_args(int dtype, const dapple_attention_docs_desc* d, bool bwd, bool sizes_only, AttnWinArgs& a) {
+  if (!d) return set_error(STAGE_E_NULL, "the descriptor is NULL");
+  // (one sequence, whose gradient's walks are unequal like those of a causal one)
+  dapple_attention_window_desc w{};
+  w.q = d->q; w.k = d->k; w.v = d->v; w.ctx = d->ctx; w.ctx32 = d->ctx32; w.lse = d->lse; w.dctx = d->dctx; w.dq = d->dq; w.dk = d->dk; w.dv = d->dv;
+  w.workspace = d->workspace; w.b = 1; w.s = d->rows; w.A = d->A; w.Ak = d->Ak; w.d = d->d; w.causal = 1;
+  w.ldq = d->ldq; w.ldk = d->ldk; w.ldv = d->ldv; w.ldc = d->ldc; w.lddc = d->lddc; w.lddq = d->lddq; w.lddk = d->lddk; w.lddv = d->lddv;
+  w.scale = d->scale;
+  const int rc = win_args(dtype, &w, bwd, sizes_only, a);
+  if (rc != STAGE_OK || sizes_only) return rc;
+  if (!(d->cap == 0.f || (d->cap >= 0x1p-20f && d->cap <= 0x1p10f))) return set_error(STAGE_E_CONFIG, "cap must be 0 or lie in [2^-20, 2^10]");
+  if (!d->spans) return set_error(STAGE_E_NULL, "spans must not be NULL");
+  if (!aligned_to(d->spans, 4) || !aligned_to(d->slopes, 4)) return set_error(STAGE_E_CONFIG, "spans or slopes not aligned");
+  a.spans = d->spans; a.slopes = d->slopes;
+  if (d->cap > 0.f) {
+    const double log2e = 1.4426950408889634;
+    a.cap2 = (float)(d->cap * log2e);
+    a.bend = (float)((dtype == STAGE_DTYPE_BF16 ? 2.0 * log2e : 1.0) * a.scale / d->cap);
+  }
+  return STAGE_OK;
+}
+
+extern "C" {
+
+int dapple_doc_spans(const int32_t* ends, const int32_t* prefix, int n, int rows, int causal, int window, int32_t* spans, void* stream) {
+  if (!spans || (n > 0 && !ends)) return set_error(STAGE_E_NULL, "spans, and ends of a document, must not be NULL");
+  if (n < 0 || rows < 1 || rows > (1 << 26) - 4) return set_error(STAGE_E_CONFIG, "%d documents, %d rows (1 to 2^26 - 4)", n, rows);
+  if (window < 0) return set_error(STAGE_E_CONFIG, "window %d", window);
+  if (prefix && !causal) return set_error(STAGE_E_CONFIG, "a prefix without causal");
+  if (!aligned_to(ends, 4) || !aligned_to(prefix, 4) || !aligned_to(spans, 4)) return set_error(STAGE_E_CONFIG, "ends, prefix or spans not aligned");
+  return rc_of(launch_doc_spans(ends, prefix, n, rows, causal != 0, window < rows ? window : 0, spans, (hipStream_t)stream));
+}
+
+int dapple_attention_docs_fwd(int dtype, const dapple_attention_docs_desc* d, void* stream) {
+  AttnWinArgs a{};
+  const int rc = docs_args(dtype, d, false, false, a);
+  return rc != STAGE_OK ? rc : rc_of(launch_attn_docs_fwd(type_of(dtype), a, (hipStream_t)stream));
+}
+
+int64_t dapple_attention_docs_workspace(int dtype, const dapple_attention_docs_desc* d) {
+  AttnWinArgs a{};
+  const int rc = docs_args(dtype, d, true, true, a);
+  return rc != STAGE_OK ? rc : attn_win_workspace(type_of(dtype), a);
+}
+
+int dapple_attention_docs_bwd(int dtype, const dapple_attention_docs_desc* d, void* stream) {
+  AttnWinArgs a{};
+  const int rc = docs_args(dtype, d, true, false, a);
+  return rc != STAGE_OK ? rc : rc_of(launch_attn_docs_bwd(type_of(dtype), a, d->workspace, (hipStream_t)stream));
+}
+
+}  // extern "C"
+
 // ------------------------------------------------------------------ head norms and rotation
 // the launcher's arguments; workspace_only: what the size of the workspace depends on
 static int rope_args(int dtype, const dapple_qk_rope_desc* d, bool bwd, bool workspace_only, QkRopeArgs& a) {

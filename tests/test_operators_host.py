@@ -255,3 +255,35 @@ def test_embedding_refusals():
     for rows, V, H in ((1, 1, 1), (65536, 30522, 1024), (1 << 28, 1 << 28, 1 << 16)):
         assert 16 * rows <= size(rows, V, H) <= 16 * rows + (1 << 16) * H + (1 << 18)
     refused(conf, size, 0, 1, 1)
+
+
+def test_attention_docs_refusals():
+    ok = dict(q=P, k=P, v=P, ctx=P, lse=P, spans=P, slopes=P, dctx=P, dq=P, dk=P, dv=P, workspace=P, rows=100, A=4, Ak=2, d=64)
+    null, conf = B.STAGE_E_NULL, B.STAGE_E_CONFIG
+    both = [(null, dict(q=None)), (null, dict(k=None)), (null, dict(v=None)), (null, dict(ctx=None)), (null, dict(lse=None)), (null, dict(spans=None)),
+            (conf, dict(rows=0)), (conf, dict(A=0)), (conf, dict(Ak=3)), (conf, dict(d=60)), (conf, dict(d=136)), (conf, dict(scale=-1.0)),
+            (conf, dict(scale=math.nan)), (conf, dict(cap=-1.0)), (conf, dict(cap=1e-7)), (conf, dict(cap=1025.0)), (conf, dict(cap=math.inf)),
+            (conf, dict(cap=math.nan)), (conf, dict(ldq=255)), (conf, dict(ldk=-8)), (conf, dict(ldv=1 << 23)), (conf, dict(rows=1 << 22, ldq=264)),
+            (conf, dict(q=P + 8)), (conf, dict(ctx32=P + 4)), (conf, dict(lse=P + 2)), (conf, dict(spans=P + 2)), (conf, dict(slopes=P + 1)),
+            (conf, dict(rows=(1 << 26) - 3))]
+    for code, change in both:
+        for f in (B.dapple_attention_docs_fwd, B.dapple_attention_docs_bwd):
+            refused(code, f, B.DTYPE_BF16, B.attention_docs_desc(**dict(ok, **change)))
+    for change in (dict(dctx=None), dict(dq=None), dict(dk=None), dict(dv=None), dict(workspace=None)):
+        refused(null, B.dapple_attention_docs_bwd, B.DTYPE_F32, B.attention_docs_desc(**dict(ok, **change)))
+    for change in (dict(dctx=P + 8), dict(dv=P + 4), dict(lddq=258), dict(workspace=P + 8)):
+        refused(conf, B.dapple_attention_docs_bwd, B.DTYPE_F32, B.attention_docs_desc(**dict(ok, **change)))
+    refused(conf, B.dapple_attention_docs_fwd, 2, B.attention_docs_desc(**ok))
+    refused(conf, B.dapple_attention_docs_workspace, B.DTYPE_BF16, B.attention_docs_desc(**dict(ok, d=4)))
+    for dt in (B.DTYPE_F32, B.DTYPE_BF16):
+        for rows, A, Ak, d in ((100, 4, 2, 64), (1, 1, 1, 8), (65536, 32, 8, 128), (8192, 16, 4, 128), (1 << 22, 1, 1, 64), (3000, 64, 1, 32)):
+            assert 4 * A * rows <= B.dapple_attention_docs_workspace(dt, B.attention_docs_desc(rows=rows, A=A, Ak=Ak, d=d)) < 4 * A * rows + (1 << 28)
+
+
+def test_doc_spans_refusals():
+    null, conf = B.STAGE_E_NULL, B.STAGE_E_CONFIG
+    ok = dict(ends_ptr=P, n=3, rows=10, spans_ptr=P)
+    for code, change in ((null, dict(ends_ptr=None)), (null, dict(spans_ptr=None)), (conf, dict(n=-1)), (conf, dict(rows=0)), (conf, dict(rows=(1 << 26) - 3)),
+                         (conf, dict(window=-1)), (conf, dict(causal=0, prefix_ptr=P)), (conf, dict(ends_ptr=P + 2)), (conf, dict(prefix_ptr=P + 1)),
+                         (conf, dict(spans_ptr=P + 2))):
+        refused(code, B.dapple_doc_spans, **dict(ok, **change))
