@@ -177,8 +177,8 @@ int dapple_attention_window_bwd(int dtype, const dapple_attention_window_desc* d
  * slopes: device fp32 [A], NULL = 0; constants (they have no gradient).  cap: 0 or 2^-20 to 2^10.  scale > 0; 0 = 1/sqrt(d).
  * fwd: ctx, lse [A, rows] fp32 = log2 of the sum of 2^(log2(e) logit), ctx32 (may be NULL) as above.  bwd: dq, dk, dv from dctx and the ctx, ctx32
  * (or NULL) and lse of fwd.  spans holds what dapple_doc_spans left, of the same rows (other contents: wrong results, nothing worse).
- * Strides, alignment, limits (with b = 1, s = rows), rounding and overlaps as for dapple_attention_window; workspace: below 4 A rows bytes +
- * 256 MiB. */
+ * Strides, alignment, limits (with b = 1, s = rows; up to 2^26 - 8), rounding and overlaps as for dapple_attention_window; workspace: below
+ * 4 A rows bytes + 256 MiB. */
 typedef struct {
   const void* q;
   const void* k;

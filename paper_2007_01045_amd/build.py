@@ -12,7 +12,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libdapple_stage.so")
 SOURCES = ["gemm_nn.hip", "gemm_nt.hip", "gemm_nn_pack.hip", "gemm_nt_pack.hip", "gemm_tn.hip", "gemm_tn_pack.hip", "gemm_tt.hip",
            "gemm_tt_pack.hip", "gemm_wgrad.hip", "gemm_gate.hip", "gemm.hip", "gemm_f32.hip", "attention.hip", "attention_f32.hip",
-           "attention_window.hip", "attention_docs.hip", "attention_docs_cap.hip", "attention_docs_f32.hip", "rowops.hip", "embed_head.hip", "optimizer.hip", "grad_norm.hip", "qk_rope.hip", "gated_ffn.hip", "gated_ffn_f32.hip", "gemm_rows.hip",
+           "attention_window.hip", "attention_docs.hip", "attention_docs_cap.hip", "attention_docs_both.hip", "attention_docs_f32.hip", "rowops.hip", "embed_head.hip", "optimizer.hip", "grad_norm.hip", "qk_rope.hip", "gated_ffn.hip", "gated_ffn_f32.hip", "gemm_rows.hip",
            "dropout_norm.hip", "embedding.hip",
            "stage.hip", "pipeline.hip", "kernel_api.hip", "operators_api.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-result", "-Wno-inline-asm",

@@ -49,15 +49,21 @@ hipError_t launch_doc_spans(const int32_t* ends, const int32_t* prefix, int n, i
 }
 
 // ------------------------------------------------------------------ launchers
+int64_t attn_docs_workspace(Dtype dt, AttnWinArgs a) {
+  make_docs_plan(dt, a);
+  const int width = pick_width(dt, a.d, [](auto D) { return (int)decltype(D)::value; });
+  return (int64_t)(delta_bytes(a) + table_bytes(a)) + (int64_t)a.Ak * a.plan.slots * 2 * a.plan.kt * width * 4;
+}
+
 hipError_t launch_attn_docs_fwd(Dtype dt, const AttnWinArgs& a, hipStream_t st) {
   if (dt != DT_BF16) return launch_attn_docs_fwd_f32(a, st);
-  if (a.cap2 > 0.f) return attn_win_fwd_launch_bf16<MASK_SPANS, SCORE_CAP>(a, st);
+  if (a.cap2 > 0.f) return launch_attn_docs_fwd_cap(a, st);
   return a.slopes ? attn_win_fwd_launch_bf16<MASK_SPANS, SCORE_SLOPE>(a, st) : attn_win_fwd_launch_bf16<MASK_SPANS, SCORE_PLAIN>(a, st);
 }
 
 hipError_t launch_attn_docs_bwd(Dtype dt, const AttnWinArgs& a, void* workspace, hipStream_t st) {
   if (dt != DT_BF16) return launch_attn_docs_bwd_f32(a, workspace, st);
-  if (a.cap2 > 0.f) return launch_attn_docs_bwd_cap(a, workspace, st);
+  if (a.cap2 > 0.f) return a.slopes ? launch_attn_docs_bwd_both(a, workspace, st) : launch_attn_docs_bwd_cap(a, workspace, st);
   return a.slopes ? attn_win_bwd_launch_bf16<MASK_SPANS, SCORE_SLOPE>(a, workspace, st) : attn_win_bwd_launch_bf16<MASK_SPANS, SCORE_PLAIN>(a, workspace, st);
 }
 

@@ -78,26 +78,82 @@ __device__ __forceinline__ int query_hi(const AttnWinArgs& a, int j, int len) {
 template <int M>
 __device__ __forceinline__ bool is_sink(const AttnWinArgs& a, int j) { return M == MASK_WINDOW && a.W && j < a.S; }
 
-// The logit, in log2 units, of a product `raw`: what it is scaled, capped and lowered with
+// The logit, in log2 units, of a product `raw`: what it is scaled, capped and lowered with.
+// The cap, t = cap2 tanh(x), x = raw scale / cap, is bound by its instructions (an exponential or a reciprocal takes four times one of
+// the others).  Where |x| <= 0.6 for all that a wave looks at, tanh(x) = x (1 + c1 x^2 + c2 x^4 + c3 x^6), c fitted for the least relative error, 2.5e-6, which
+// is below 2^-13 of a probability for any logit up to 30.  Else tanh(x) = 1 - 2 r, r = 1 / (1 + e^2x), off by 2^-23 of 1, times cap2.
+// XXX measured
 struct Score {
   float scale2, bend, cap2, slope2;   // cap2: cap log2(e), bend: 2 scale log2(e) / cap;  slope2: -slope log2(e)
-  __device__ __forceinline__ Score(const AttnWinArgs& a, float scale2) : scale2(scale2), bend(a.bend), cap2(a.cap2), slope2(0.f) {}
+  float p0, p1, p2, small, down;
+  __device__ __forceinline__ Score(const AttnWinArgs& a, float scale2) : scale2(scale2), bend(a.bend), cap2(a.cap2), slope2(0.f),
+    p0(a.poly[0]), p1(a.poly[1]), p2(a.poly[2]), small(a.small), down(a.down) {}
   template <int S>
   __device__ __forceinline__ void head(const AttnWinArgs& a, int h) {
-    if (S != SCORE_PLAIN) slope2 = a.slopes ? a.slopes[h] * -LOG2E : 0.f;
+    if (S == SCORE_SLOPE || S == SCORE_BOTH) slope2 = a.slopes ? a.slopes[h] * -LOG2E : 0.f;
   }
-  // far: the rows' distance, of either sign.  d: d logit / d raw over scale2.
-  // The cap's tanh(x) = 1 - 2 r, r = 1 / (1 + e^2x), and its slope 4 r (1 - r): of errors of 2^-23 of 1, times cap2, which is
-  // nothing beside the rounding of a probability to bf16
+  // whether the wave's products are all small
+  template <int S, typename V>
+  __device__ __forceinline__ bool is_small(const V& raw) const {
+    if (S != SCORE_CAP && S != SCORE_BOTH) return true;
+    float m = 0.f;
+    bool fit = true;
+#pragma unroll
+    for (int v = 0; v < 16; v += 2) m = fmaxf(m, fmaxf(fabsf(raw[v]), fabsf(raw[v + 1])));
+    fit = m <= small;
+    return __builtin_amdgcn_ballot_w64(fit) == ~0ull;
+  }
+  // what raw is multiplied with
   template <int S>
+  __device__ __forceinline__ float factor(float raw) const {
+    if (S != SCORE_CAP && S != SCORE_BOTH) return scale2;
+    const float r = raw * raw;
+    return fmaf(fmaf(fmaf(p2, r, p1), r, p0), r, scale2);
+  }
+  // far: the rows' distance, of either sign.  d: d logit / d raw over scale2
+  template <int S, bool SMALL>
   __device__ __forceinline__ float at(float raw, float far, float& d) const {
-    if (S == SCORE_SLOPE) {
-      d = 1.f;
-      return fmaf(slope2, fabsf(far), raw * scale2);
-    }
+    float t;
+    d = 1.f;
+    if (S == SCORE_SLOPE) return fmaf(slope2, fabsf(far), raw * scale2);
+    const float f = factor<S>(raw);
+    t = raw * f;
+    d = fmaf(t * t, down, 1.f);
+    if (SMALL) return S == SCORE_BOTH ? fmaf(slope2, fabsf(far), raw * f) : t;
     const float r = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(raw * bend));
-    d = fmaf(-4.f * r, r, 4.f * r);
-    return fmaf(slope2, fabsf(far), fmaf(-2.f * cap2, r, cap2));
+    const bool in = fabsf(raw) <= small;   // (each logit by its own size, whatever stands beside it)
+    d = in ? d : fmaf(-4.f * r, r, 4.f * r);
+    t = in ? t : fmaf(-2.f * cap2, r, cap2);
+    return S == SCORE_BOTH ? fmaf(slope2, fabsf(far), t) : t;
+  }
+  // The logits of a block of the other side's rows r0 + 8 (v >> 2) + (v & 3) (4 h is in r0) against the lane's row, less what is
+  // returned, which is the same for all of them: on one side of the rows the bias is linear, and a constant for each v.  row0: the wave's
+  // first row, b0: the block's (both the same for the wave)
+  template <int S, bool SMALL, typename V>
+  __device__ __forceinline__ float block(const V& raw, float (&t)[16], int row, int r0, int row0, int b0) const {
+    if constexpr (S == SCORE_SLOPE || S == SCORE_BOTH) {
+      auto plus = [&](float q, float c) {
+        const float s = fmaf(q, factor<S>(q), c);
+        if (SMALL || S == SCORE_SLOPE || fabsf(q) <= small) return s;
+        return c + fmaf(-2.f * cap2, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(q * bend)), cap2);
+      };
+      const float x = (float)(row - r0) * slope2;
+      if (b0 + 31 <= row0) {
+#pragma unroll
+        for (int v = 0; v < 16; ++v) t[v] = plus(raw[v], -(float)(8 * (v >> 2) + (v & 3)) * slope2);
+        return x;
+      }
+      if (b0 >= row0 + 31) {
+#pragma unroll
+        for (int v = 0; v < 16; ++v) t[v] = plus(raw[v], (float)(8 * (v >> 2) + (v & 3)) * slope2);
+        return -x;
+      }
+    }
+    const float x = (float)(row - r0);
+    float d;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) t[v] = at<S, SMALL>(raw[v], x - (8 * (v >> 2) + (v & 3)), d);
+    return 0.f;
   }
   // fp32: tanh of full precision, and no cap at all at run time
   __device__ __forceinline__ float at32(float raw, float far, float& d) const {
@@ -152,11 +208,57 @@ __device__ __forceinline__ void hide(float (&x)[16], float hidden, int r0, int h
   }
 }
 
+// Workgroup id's head and its place among that head's, where the heads take turns: a head's workgroups (eight heads and more) or those of few
+// heads on one XCD each
+__device__ __forceinline__ void by_heads(unsigned id, int heads, int& head, int& rank) {
+  const unsigned per = (unsigned)heads / 8, turn = id >> 3;
+  const bool eight = heads % 8 == 0;
+  head = eight ? (id & 7) * per + turn % per : id % heads;
+  rank = eight ? turn / per : id / heads;
+}
+
+// The query tile of workgroup id of n.  MASK_WINDOW: the last tiles first (causal: they have the longest walks).
+// MASK_SPANS: where they do not all run at once, the tiles with the longest walks first, all heads by turns: a long one that begins last would
+// be what the launch ends with.  Each wave ranks the tiles itself, up to 64 groups of neighbours, one to a lane, by the walk of a
+// group's last row.  Us forward, ranked / as they lie: XXX
+template <int M>
+struct QueryTask {
+  int tile, bi, hh;
+  __device__ __forceinline__ QueryTask(const AttnWinArgs& a, unsigned id, unsigned n, int q_tiles, int rows, int lane) {
+    if constexpr (M == MASK_WINDOW) {
+      id = spread(id, n);
+      tile = q_tiles - 1 - id % q_tiles;
+      unit_of(a, id / q_tiles, a.A, bi, hh);
+      return;
+    }
+    int rank;
+    by_heads(id, a.A, hh, rank);
+    bi = 0;
+    tile = q_tiles - 1 - rank;
+    if (n <= 256) return;
+    const int group = (q_tiles + 63) / 64, groups = (q_tiles + group - 1) / group, first = lane * group, last = min(first + group, q_tiles) - 1;
+    int walk = -1;
+    if (lane < groups) {
+      const int row = min((last + 1) * rows, a.s) - 1;
+      walk = max(span_of(a, 1, row) - span_of(a, 0, last * rows), 0);
+    }
+    int before = 0;   // tiles of the groups that come before the lane's
+    for (int g = 0; g < groups; ++g) {
+      const int other = __builtin_amdgcn_readlane(walk, g);
+      if (other > walk || (other == walk && g > lane)) before += g == groups - 1 ? q_tiles - g * group : group;
+    }
+    const unsigned long long mine = __ballot(lane < groups && rank >= before && rank < before + last - first + 1);
+    const int at = __builtin_ctzll(mine);
+    tile = __builtin_amdgcn_readlane(last, at) - (rank - __builtin_amdgcn_readlane(before, at));
+  }
+};
+
 // A workgroup of the dk, dv launch: KT keys of a key head, and a part of their walk over the sharing heads' query blocks
 template <int M>
 struct KeyTask {
   int bi, kv, k0, len, qlo, nq, n0, n1, slot;   // blocks of the walk [n0, n1): head n / nq, block qlo + n % nq; slot < 0: no parts
   bool run;
+  __device__ __forceinline__ KeyTask() {}
   __device__ __forceinline__ void span(const AttnWinArgs& a, int kt, int blk) {
     const int k1 = min(k0 + kt, len) - 1;
     qlo = nq = 0;
@@ -167,7 +269,29 @@ struct KeyTask {
     nq = ((sink ? len : query_hi<M>(a, k1, len)) + blk - 1) / blk - qlo;
     if (M == MASK_SPANS) nq = max(nq, 0);
   }
-  __device__ __forceinline__ KeyTask(const AttnWinArgs& a, unsigned t, int kt, int blk) {
+  // t: the workgroup of n
+  __device__ __forceinline__ KeyTask(const AttnWinArgs& a, unsigned t, unsigned n, int kt, int blk) {
+    const WinPlan& p = a.plan;
+    if constexpr (M == MASK_SPANS) {
+      int rank;
+      by_heads(t, a.Ak, kv, rank);
+      bi = 0;
+      slot = -1;
+      n0 = n1 = 0;
+      run = rank < a.table[0];
+      if (!run) return;
+      const int32_t* const e = a.table + 4 + 4L * rank;   // tile, the part's blocks, slot
+      k0 = e[0] * kt;
+      len = len_of<M>(a, bi);
+      span(a, kt, blk);
+      n0 = e[1];
+      n1 = e[2];
+      if (e[3] >= 0) slot = kv * p.slots + e[3];
+      return;
+    }
+    init(a, spread(t, n), kt, blk);
+  }
+  __device__ __forceinline__ void init(const AttnWinArgs& a, unsigned t, int kt, int blk) {
     const WinPlan& p = a.plan;
     const int sinks = p.sink_tiles * p.sink_parts, per = sinks + (p.key_tiles - p.sink_tiles) * p.parts;
     const int head = t / per, r = t % per;
@@ -209,10 +333,8 @@ __global__ __launch_bounds__(64 * NW, D <= 64 ? 3 : 2) void attn_win_fwd(AttnWin
   const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int q_tiles = (a.s + 32 * NW - 1) / (32 * NW);
-  const unsigned id = spread(blockIdx.x, gridDim.x);
-  const int tile = q_tiles - 1 - id % q_tiles;   // (causal: the longest walks first)
-  int bi, hh;
-  unit_of(a, id / q_tiles, a.A, bi, hh);
+  const QueryTask<M> task(a, blockIdx.x, gridDim.x, q_tiles, 32 * NW, lane);
+  const int tile = task.tile, bi = task.bi, hh = task.hh;
   const int kv = hh / (a.A / a.Ak);
   const int len = len_of<M>(a, bi), d = a.d;
   const long r0 = (long)bi * a.s;
@@ -255,7 +377,7 @@ __global__ __launch_bounds__(64 * NW, D <= 64 ? 3 : 2) void attn_win_fwd(AttnWin
     const int k0 = walk.block(t) * 64;
     if (row0 >= len) continue;
     if (!any_seen<M>(a, k0, k0 + 63, lo_min, hi_max)) continue;
-    float p[2][16];
+    float p[2][16], shift[2] = {0.f, 0.f};   // (logits less their shift)
     float mx = -INFINITY;
     // (all LDS reads of a phase before its first MFMA: see attn_fwd_mfma)
     bf16x8 kf[2][NKK], vf[4][NDB];
@@ -280,18 +402,26 @@ __global__ __launch_bounds__(64 * NW, D <= 64 ? 3 : 2) void attn_win_fwd(AttnWin
 #pragma unroll
       for (int v = 0; v < 16; ++v) p[kb2][v] = sa[v];
       if constexpr (S != SCORE_PLAIN) {
-        const float x = (float)(qrow - k0 - 32 * kb2 - 4 * h);
-        float unused;
-#pragma unroll
-        for (int v = 0; v < 16; ++v) p[kb2][v] = sc.at<S>(sa[v], x - (8 * (v >> 2) + (v & 3)), unused);
+        const int b0 = k0 + 32 * kb2;
+        if (sc.is_small<S>(sa)) shift[kb2] = sc.block<S, true>(sa, p[kb2], qrow, b0 + 4 * h, row0, b0);
+        else shift[kb2] = sc.block<S, false>(sa, p[kb2], qrow, b0 + 4 * h, row0, b0);
       }
     }
 #pragma unroll
     for (int kb2 = 0; kb2 < 2; ++kb2) hide<M == MASK_WINDOW>(p[kb2], -INFINITY, k0 + kb2 * 32, h, lo, hi, a.S, lo_max > k0 + kb2 * 32, hi_min < k0 + kb2 * 32 + 32);
+    if constexpr (S == SCORE_PLAIN) {
 #pragma unroll
-    for (int kb2 = 0; kb2 < 2; ++kb2)
+      for (int kb2 = 0; kb2 < 2; ++kb2)
 #pragma unroll
-      for (int v = 0; v < 16; ++v) mx = fmaxf(mx, p[kb2][v]);
+        for (int v = 0; v < 16; ++v) mx = fmaxf(mx, p[kb2][v]);
+    } else {
+      float m1 = -INFINITY;
+#pragma unroll
+      for (int v = 0; v < 16; ++v) mx = fmaxf(mx, p[0][v]);
+#pragma unroll
+      for (int v = 0; v < 16; ++v) m1 = fmaxf(m1, p[1][v]);
+      mx = fmaxf(mx + shift[0], m1 + shift[1]);
+    }
     if (WHOLE) {
 #pragma unroll
       for (int ks = 0; ks < 4; ++ks)
@@ -310,7 +440,7 @@ __global__ __launch_bounds__(64 * NW, D <= 64 ? 3 : 2) void attn_win_fwd(AttnWin
 #pragma unroll
       for (int v = 0; v < 16; ++v) {
         // (the bare v_exp_f32: a probability below 2^-126 may be zero, it is rounded to bf16)
-        p[kb2][v] = __builtin_amdgcn_exp2f(S == SCORE_PLAIN ? fmaf(p[kb2][v], scale2, -mn) : p[kb2][v] - mn);
+        p[kb2][v] = __builtin_amdgcn_exp2f(S == SCORE_PLAIN ? fmaf(p[kb2][v], scale2, -mn) : p[kb2][v] + (shift[kb2] - mn));
         rs += p[kb2][v];
       }
     l = l * alpha + halves_sum(rs);
@@ -360,9 +490,9 @@ __device__ __forceinline__ void store_part(const AttnWinArgs& a, int slot, int w
 
 // dk, dv of 32 keys a wave; query blocks of 64 stream through LDS with their lse and delta
 template <int M, int S, int D, int NW, typename R>
-__device__ __forceinline__ void win_dkdv(const AttnWinArgs& a, unsigned task, float scale2, float scale, unsigned char* sm) {
+__device__ __forceinline__ void win_dkdv(const AttnWinArgs& a, unsigned task, unsigned tasks, float scale2, float scale, unsigned char* sm) {
   constexpr int NKK = D / 16, NDB = D / 32;
-  const KeyTask<M> w(a, task, 32 * NW, 64);
+  const KeyTask<M> w(a, task, tasks, 32 * NW, 64);
   if (!w.run) return;
   const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -460,19 +590,25 @@ __device__ __forceinline__ void win_dkdv(const AttnWinArgs& a, unsigned task, fl
         }
       __builtin_amdgcn_sched_barrier(0);
       float p[16], ds[16];
+      auto probabilities = [&](auto SMALL) __attribute__((always_inline)) {
 #pragma unroll
-      for (int blk = 0; blk < 4; ++blk)
+        for (int blk = 0; blk < 4; ++blk)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          if constexpr (S == SCORE_PLAIN) {
-            p[4 * blk + e] = __builtin_amdgcn_exp2f(fmaf(sa[4 * blk + e], scale2, -L4[blk][e]));
-            ds[4 * blk + e] = dp[4 * blk + e] * p[4 * blk + e];
-          } else {
-            float d;
-            p[4 * blk + e] = __builtin_amdgcn_exp2f(sc.at<S>(sa[4 * blk + e], (float)(krow - j0 - 4 * h) - (8 * blk + e), d) - L4[blk][e]);
-            ds[4 * blk + e] = dp[4 * blk + e] * p[4 * blk + e] * d;
+          for (int e = 0; e < 4; ++e) {
+            const int v = 4 * blk + e;
+            if constexpr (S == SCORE_PLAIN) {
+              p[v] = __builtin_amdgcn_exp2f(fmaf(sa[v], scale2, -L4[blk][e]));
+              ds[v] = dp[v] * p[v];
+            } else {
+              float d;
+              p[v] = __builtin_amdgcn_exp2f(sc.at<S, decltype(SMALL)::value>(sa[v], (float)(krow - j0 - 4 * h) - (8 * blk + e), d) - L4[blk][e]);
+              ds[v] = dp[v] * p[v];
+              if (S != SCORE_SLOPE) ds[v] *= d;
+            }
           }
-        }
+      };
+      if (S == SCORE_PLAIN || sc.is_small<S>(sa)) probabilities(std::true_type{});
+      else probabilities(std::false_type{});
       hide<false>(p, 0.f, j0, h, lo, hi, 0, lo_max > j0, hi_min < j0 + 32);
       hide<false>(ds, 0.f, j0, h, lo, hi, 0, lo_max > j0, hi_min < j0 + 32);
 #pragma unroll
@@ -498,14 +634,13 @@ __device__ __forceinline__ void win_dkdv(const AttnWinArgs& a, unsigned task, fl
 
 // dq of 32 queries a wave; key blocks of 64 stream through LDS
 template <int M, int S, int D, int NW, typename R>
-__device__ __forceinline__ void win_dq(const AttnWinArgs& a, unsigned id, float scale2, float scale, unsigned char* sm) {
+__device__ __forceinline__ void win_dq(const AttnWinArgs& a, unsigned id, unsigned ids, float scale2, float scale, unsigned char* sm) {
   constexpr int NKK = D / 16, NDB = D / 32;
   const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int q_tiles = (a.s + 32 * NW - 1) / (32 * NW);
-  const int tile = q_tiles - 1 - id % q_tiles;
-  int bi, hh;
-  unit_of(a, id / q_tiles, a.A, bi, hh);
+  const QueryTask<M> task(a, id, ids, q_tiles, 32 * NW, lane);
+  const int tile = task.tile, bi = task.bi, hh = task.hh;
   const int kv = hh / (a.A / a.Ak);
   const int len = len_of<M>(a, bi), d = a.d;
   const long r0 = (long)bi * a.s;
@@ -584,15 +719,24 @@ __device__ __forceinline__ void win_dq(const AttnWinArgs& a, unsigned id, float 
         for (int db = 0; db < NDB; ++db) kc[ks][db] = frag_cols<D>(Ks, db * 32, kb2 * 32 + ks * 16, lane);
       __builtin_amdgcn_sched_barrier(0);
       float ds[16];
+      if constexpr (S == SCORE_PLAIN) {
 #pragma unroll
-      for (int v = 0; v < 16; ++v) {
-        if constexpr (S == SCORE_PLAIN) {
-          ds[v] = __builtin_amdgcn_exp2f(fmaf(sa[v], scale2, -Lq)) * (ADDS ? dp[v] : dp[v] + Dq);
-        } else {
-          float d;
-          ds[v] = __builtin_amdgcn_exp2f(sc.at<S>(sa[v], (float)(qrow - j0 - 4 * h) - (8 * (v >> 2) + (v & 3)), d) - Lq);
-          ds[v] *= (ADDS ? dp[v] : dp[v] + Dq) * d;
-        }
+        for (int v = 0; v < 16; ++v) ds[v] = __builtin_amdgcn_exp2f(fmaf(sa[v], scale2, -Lq)) * (ADDS ? dp[v] : dp[v] + Dq);
+      } else if constexpr (S == SCORE_SLOPE) {
+        const float c = sc.block<S, true>(sa, ds, qrow, j0 + 4 * h, row0, j0) - Lq;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) ds[v] = __builtin_amdgcn_exp2f(ds[v] + c) * (ADDS ? dp[v] : dp[v] + Dq);
+      } else {
+        auto gradients = [&](auto SMALL) __attribute__((always_inline)) {
+#pragma unroll
+          for (int v = 0; v < 16; ++v) {
+            float d;
+            ds[v] = __builtin_amdgcn_exp2f(sc.at<S, decltype(SMALL)::value>(sa[v], (float)(qrow - j0 - 4 * h) - (8 * (v >> 2) + (v & 3)), d) - Lq);
+            ds[v] *= (ADDS ? dp[v] : dp[v] + Dq) * d;
+          }
+        };
+        if (sc.is_small<S>(sa)) gradients(std::true_type{});
+        else gradients(std::false_type{});
       }
       hide<M == MASK_WINDOW>(ds, 0.f, j0, h, lo, hi, a.S, lo_max > j0, hi_min < j0 + 32);
 #pragma unroll
@@ -623,8 +767,8 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_win_bwd(AttnWinArgs a, float 
   extern __shared__ __attribute__((aligned(1024))) unsigned char asm_[];
   typedef WinRing<D, NW, true> R;
   const unsigned nk = a.plan.key_tasks;
-  if (blockIdx.x < nk) win_dkdv<M, S, D, NW, R>(a, spread(blockIdx.x, nk), scale2, scale, asm_);
-  else win_dq<M, S, D, NW, R>(a, spread(blockIdx.x - nk, gridDim.x - nk), scale2, scale, asm_);
+  if (blockIdx.x < nk) win_dkdv<M, S, D, NW, R>(a, blockIdx.x, nk, scale2, scale, asm_);
+  else win_dq<M, S, D, NW, R>(a, blockIdx.x - nk, gridDim.x - nk, scale2, scale, asm_);
 }
 
 // dk and dv of 128 keys at D = 128.  A wave that does all four products holds 128 registers of sums, 64 of keys and values and 32 of
@@ -675,10 +819,10 @@ static_assert(PAIR_BYTES <= 160 * 1024 && PairDqRing::BYTES <= PAIR_BYTES && 8 *
               "LDS of a compute unit; the output's staging lies where the ring was");
 
 template <int M, int S>
-__device__ __forceinline__ void win_dkdv_pair(const AttnWinArgs& a, unsigned task, float scale2, float scale, unsigned char* sm) {
+__device__ __forceinline__ void win_dkdv_pair(const AttnWinArgs& a, unsigned task, unsigned tasks, float scale2, float scale, unsigned char* sm) {
   constexpr int D = 128, NKK = 8, NDB = 4;
   typedef PairRing R;
-  const KeyTask<M> w(a, task, 128, 32);
+  const KeyTask<M> w(a, task, tasks, 128, 32);
   if (!w.run) return;
   const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), own = wave & 3;   // which 32 of the keys
@@ -740,7 +884,7 @@ __device__ __forceinline__ void win_dkdv_pair(const AttnWinArgs& a, unsigned tas
     // sa, dp: S and dP of the current step (rows: query 8 blk + 4 h + e of its block, column: key); sn, dn: of the next one, made
     // meanwhile: two MFMAs and two elements' exponentials by turns
     enum { HIDDEN, WHOLE, PART };
-    auto step = [&](auto MODE, const f32x16& sa, const f32x16& dp, f32x16& sn, f32x16& dn, unsigned cur, unsigned at, unsigned next, unsigned char* x,
+    auto step = [&](auto MODE, auto SMALL, const f32x16& sa, const f32x16& dp, f32x16& sn, f32x16& dn, unsigned cur, unsigned at, unsigned next, unsigned char* x,
                     int j0) __attribute__((always_inline)) {
       constexpr int mode = decltype(MODE)::value;
       const float *Ls = (const float*)(sm + cur + R::S_OFF) + 4 * h, *Ds = Ls + 64;
@@ -768,8 +912,9 @@ __device__ __forceinline__ void win_dkdv_pair(const AttnWinArgs& a, unsigned tas
               ds[v] = (dp[v] + D4[v >> 2][v & 3]) * p[v];
             } else {
               float d;
-              p[v] = __builtin_amdgcn_exp2f(sc.at<S>(sa[v], (float)(krow - j0 - 4 * h) - (8 * (v >> 2) + (v & 3)), d) - L4[v >> 2][v & 3]);
-              ds[v] = (dp[v] + D4[v >> 2][v & 3]) * p[v] * d;
+              p[v] = __builtin_amdgcn_exp2f(sc.at<S, decltype(SMALL)::value>(sa[v], (float)(krow - j0 - 4 * h) - (8 * (v >> 2) + (v & 3)), d) - L4[v >> 2][v & 3]);
+              ds[v] = (dp[v] + D4[v >> 2][v & 3]) * p[v];
+              if (S != SCORE_SLOPE) ds[v] *= d;
             }
             if constexpr (mode == PART) {
               const bool in = 8 * (v >> 2) + (v & 3) >= l && 8 * (v >> 2) + (v & 3) < u;
@@ -816,9 +961,13 @@ __device__ __forceinline__ void win_dkdv_pair(const AttnWinArgs& a, unsigned tas
       barrier();
       ask();
       const unsigned c = cur * R::STAGE, f = at * R::STAGE, g = after * R::STAGE;
-      if (j0 >= hi_max || j0 + 31 < lo_min) step(Hidden{}, sa, dp, sn, dn, c, f, g, x, j0);   // none of the wave's keys is seen
-      else if (lo_max > j0 || hi_min < j0 + 32) step(Part{}, sa, dp, sn, dn, c, f, g, x, j0);
-      else step(Whole{}, sa, dp, sn, dn, c, f, g, x, j0);
+      if (j0 >= hi_max || j0 + 31 < lo_min) step(Hidden{}, std::true_type{}, sa, dp, sn, dn, c, f, g, x, j0);   // none of the wave's keys is seen
+      else if (S == SCORE_PLAIN || S == SCORE_SLOPE || sc.is_small<S>(sa)) {
+        if (lo_max > j0 || hi_min < j0 + 32) step(Part{}, std::true_type{}, sa, dp, sn, dn, c, f, g, x, j0);
+        else step(Whole{}, std::true_type{}, sa, dp, sn, dn, c, f, g, x, j0);
+      } else {
+        step(Part{}, std::integral_constant<bool, S == SCORE_PLAIN || S == SCORE_SLOPE>{}, sa, dp, sn, dn, c, f, g, x, j0);
+      }
       cur = at;
       at = after;
       return ++n < w.n1;
@@ -885,13 +1034,13 @@ template <int M, int S>
 __global__ __launch_bounds__(512, 2) void attn_win_bwd_pair(AttnWinArgs a, float scale2, float scale) {
   extern __shared__ __attribute__((aligned(1024))) unsigned char asm_[];
   const unsigned nk = a.plan.key_tasks;
-  if (blockIdx.x < nk) win_dkdv_pair<M, S>(a, spread(blockIdx.x, nk), scale2, scale, asm_);
-  else win_dq<M, S, 128, 8, PairDqRing>(a, spread(blockIdx.x - nk, gridDim.x - nk), scale2, scale, asm_);
+  if (blockIdx.x < nk) win_dkdv_pair<M, S>(a, blockIdx.x, nk, scale2, scale, asm_);
+  else win_dq<M, S, 128, 8, PairDqRing>(a, blockIdx.x - nk, gridDim.x - nk, scale2, scale, asm_);
 }
 template <int M, int S, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void attn_win_dq(AttnWinArgs a, float scale2, float scale) {
   extern __shared__ __attribute__((aligned(1024))) unsigned char asm_[];
-  win_dq<M, S, 128, NW, WinRing<128, NW, true>>(a, spread(blockIdx.x, gridDim.x), scale2, scale, asm_);
+  win_dq<M, S, 128, NW, WinRing<128, NW, true>>(a, blockIdx.x, gridDim.x, scale2, scale, asm_);
 }
 
 // ------------------------------------------------------------------ fp32 (see attention_f32.hip)
@@ -925,10 +1074,8 @@ __global__ __launch_bounds__(64 * RG * NG) void attn_win_fwd_f32(AttnWinArgs a, 
   const int group = __builtin_amdgcn_readfirstlane(threadIdx.x / (64 * RG));
   float *const Ks = fsm + group * 2 * F32Lds<D, RG, NG>::BLK, *const Vs = Ks + F32Lds<D, RG, NG>::BLK;
   const int q_tiles = (a.s + 16 * RG - 1) / (16 * RG);
-  const unsigned id = spread(blockIdx.x, gridDim.x);
-  const int tile = q_tiles - 1 - id % q_tiles;
-  int bi, hh;
-  unit_of(a, id / q_tiles, a.A, bi, hh);
+  const QueryTask<M> task(a, blockIdx.x, gridDim.x, q_tiles, 16 * RG, lane);
+  const int tile = task.tile, bi = task.bi, hh = task.hh;
   const int kv = hh / (a.A / a.Ak), len = len_of<M>(a, bi), d = a.d;
   const long r0 = (long)bi * a.s;
   const float *Q = (const float*)a.q + r0 * a.ldq + hh * d, *K = (const float*)a.k + r0 * a.ldk + kv * d, *V = (const float*)a.v + r0 * a.ldv + kv * d;
@@ -1067,14 +1214,14 @@ __device__ __forceinline__ bool join_groups(f32x4 (&x)[N], float* fsm, int group
 }
 
 template <int M, int S, int D, int RG, int NG>
-__device__ __forceinline__ void win_dq_f32(const AttnWinArgs& a, unsigned id, float scale2, float scale, float* fsm) {
+__device__ __forceinline__ void win_dq_f32(const AttnWinArgs& a, unsigned id, unsigned ids, float scale2, float scale, float* fsm) {
   constexpr int NK = D / 16;
   const int tid = threadIdx.x & (64 * RG - 1), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g4 = lane >> 4;
   const int group = __builtin_amdgcn_readfirstlane(threadIdx.x / (64 * RG));
   float *const Ks = fsm + group * 2 * F32Lds<D, RG, NG>::BLK, *const Vs = Ks + F32Lds<D, RG, NG>::BLK;
-  const int q_tiles = (a.s + 16 * RG - 1) / (16 * RG), tile = q_tiles - 1 - id % q_tiles;
-  int bi, hh;
-  unit_of(a, id / q_tiles, a.A, bi, hh);
+  const int q_tiles = (a.s + 16 * RG - 1) / (16 * RG);
+  const QueryTask<M> task(a, id, ids, q_tiles, 16 * RG, lane);
+  const int tile = task.tile, bi = task.bi, hh = task.hh;
   const int kv = hh / (a.A / a.Ak), len = len_of<M>(a, bi), d = a.d;
   const long r0 = (long)bi * a.s;
   const float *K = (const float*)a.k + r0 * a.ldk + kv * d, *V = (const float*)a.v + r0 * a.ldv + kv * d;
@@ -1158,9 +1305,9 @@ __device__ __forceinline__ void win_dq_f32(const AttnWinArgs& a, unsigned id, fl
 }
 
 template <int M, int S, int D, int RG, int NG>
-__device__ __forceinline__ void win_dkdv_f32(const AttnWinArgs& a, unsigned task, float scale2, float scale, float* fsm) {
+__device__ __forceinline__ void win_dkdv_f32(const AttnWinArgs& a, unsigned task, unsigned tasks, float scale2, float scale, float* fsm) {
   constexpr int NK = D / 16;
-  const KeyTask<M> w(a, task, 16 * RG, BR);
+  const KeyTask<M> w(a, task, tasks, 16 * RG, BR);
   if (!w.run) return;
   const int tid = threadIdx.x & (64 * RG - 1), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g4 = lane >> 4;
   const int group = __builtin_amdgcn_readfirstlane(threadIdx.x / (64 * RG));
@@ -1280,17 +1427,86 @@ template <int M, int S, int D, int RG, int NG>
 __global__ __launch_bounds__(64 * RG * NG) void attn_win_bwd_f32(AttnWinArgs a, float scale2, float scale) {
   extern __shared__ __attribute__((aligned(16))) float fsm[];
   const unsigned nk = a.plan.key_tasks;
-  if (blockIdx.x < nk) win_dkdv_f32<M, S, D, RG, NG>(a, spread(blockIdx.x, nk), scale2, scale, fsm);
-  else win_dq_f32<M, S, D, RG, NG>(a, spread(blockIdx.x - nk, gridDim.x - nk), scale2, scale, fsm);
+  if (blockIdx.x < nk) win_dkdv_f32<M, S, D, RG, NG>(a, blockIdx.x, nk, scale2, scale, fsm);
+  else win_dq_f32<M, S, D, RG, NG>(a, blockIdx.x - nk, gridDim.x - nk, scale2, scale, fsm);
 }
 
 // ------------------------------------------------------------------ both types
+// MASK_SPANS: the walks' lengths are known on the device alone, and so is how they are cut: into parts no longer than a unit's share of all of
+// them.  table: {tasks, cut tiles, -, -}, then tasks of four words (tile, first and last block of the part, slot of its sums or
+// -1), the longest first, then cut tiles of four (tile, first slot, parts, -); per key head, for all have the same.  One workgroup writes it.  The
+// order among tasks of about one length and the slots' numbers may differ from call to call, but no sum goes by them.
+// A walk longer than the share has at most twice its length over the share parts: no more than 2 units of them in all.
+template <int M>
+__device__ __forceinline__ void docs_plan(const AttnWinArgs& a) {
+  constexpr int NB = 64;
+  __shared__ unsigned long long all;
+  __shared__ int count[NB], slots, cuts;
+  const WinPlan& p = a.plan;
+  const int tid = threadIdx.x, G = a.A / a.Ak;
+  KeyTask<M> w;
+  w.len = len_of<M>(a, 0);
+  auto walk = [&](int tile) {
+    w.k0 = tile * p.kt;
+    w.span(a, p.kt, p.blk);
+    return w.nq * G;   // (below 2^31: A times blocks of 32 rows is)
+  };
+  if (tid == 0) all = 0, slots = cuts = 0;
+  if (tid < NB) count[tid] = 0;
+  __syncthreads();
+  const int first = tid < p.key_tiles ? walk(tid) : 0;   // (of most calls, all)
+  auto length = [&](int t) { return t == tid ? first : walk(t); };
+  unsigned long long mine = 0;
+  for (int t = tid; t < p.key_tiles; t += 256) mine += length(t);
+  atomicAdd(&all, mine);
+  __syncthreads();
+  const int steps = (int)max((unsigned long long)p.min_steps, (all * a.Ak + p.units - 1) / p.units);
+  auto parts_of = [&](int n) { return n > steps ? (n + steps - 1) / steps : 1; };
+  auto bucket = [&](int n) { return NB - 1 - min(NB - 1, (int)((long)n * NB / (steps + 1))); };
+  for (int t = tid; t < p.key_tiles; t += 256) {
+    const int n = length(t), parts = parts_of(n);
+    atomicAdd(&count[bucket((n + parts - 1) / parts)], parts);
+  }
+  __syncthreads();
+  if (tid < NB) {   // (one wave)
+    int at = count[tid];
+    const int own = at;
+#pragma unroll
+    for (int o = 1; o < NB; o <<= 1) {
+      const int v = __shfl_up(at, o, 64);
+      if (tid >= o) at += v;
+    }
+    count[tid] = at - own;
+    if (tid == NB - 1) a.table[0] = at;
+  }
+  __syncthreads();
+  for (int t = tid; t < p.key_tiles; t += 256) {
+    const int n = length(t), parts = parts_of(n), per = (n + parts - 1) / parts, at = atomicAdd(&count[bucket(per)], parts);
+    int slot = -1;
+    if (parts > 1) {
+      slot = atomicAdd(&slots, parts);
+      int32_t* const e = a.table + 4 + 4L * p.max_tasks + 4L * atomicAdd(&cuts, 1);
+      e[0] = t, e[1] = slot, e[2] = parts, e[3] = 0;
+    }
+    for (int i = 0; i < parts; ++i) {
+      int32_t* const e = a.table + 4 + 4L * (at + i);
+      e[0] = t, e[1] = min(n, i * per), e[2] = min(n, (i + 1) * per), e[3] = slot < 0 ? -1 : slot + i;
+    }
+  }
+  __syncthreads();
+  if (tid == 0) a.table[1] = cuts;
+}
+
 // -delta [b, A, s]: 16 lanes per head, V columns each, four heads of a row per wave
 template <int M, typename T>
 __global__ __launch_bounds__(256) void attn_win_delta(AttnWinArgs a) {
   constexpr int V = 16 / sizeof(T);
   const int lane = threadIdx.x & 63;
-  const long row = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (M == MASK_SPANS && blockIdx.x == 0) {   // (a workgroup of its own)
+    docs_plan<M>(a);
+    return;
+  }
+  const long row = (long)(blockIdx.x - (M == MASK_SPANS)) * 4 + (threadIdx.x >> 6);
   if (row >= (long)a.b * a.s) return;
   const int bi = (int)(row / a.s), qi = (int)(row % a.s);
   if (qi >= len_of<M>(a, bi)) return;   // (nothing reads it)
@@ -1327,38 +1543,49 @@ template <int M, typename T, int D, int KT, int RW, int BLK>
 __global__ __launch_bounds__(256) void attn_win_join(AttnWinArgs a, float scale) {
   constexpr int JT = join_threads(KT * D), UNITS = KT * D / 4 / JT;   // workgroups per tile, four elements to a lane
   const WinPlan& p = a.plan;
-  const int head = blockIdx.y, nt = (p.sink_parts > 1 ? p.sink_tiles : 0);
-  int tile = blockIdx.x / UNITS;
-  if (nt == 0) tile += p.sink_tiles;   // (then the other tiles have parts)
-  const bool sink = tile < p.sink_tiles;
-  const int sinks = p.sink_tiles * p.sink_parts;
-  // the tile's first task (KeyTask counts the same)
-  KeyTask<M> w(a, head * (sinks + (p.key_tiles - p.sink_tiles) * p.parts) + (sink ? tile * p.sink_parts : sinks + (tile - p.sink_tiles) * p.parts), KT, BLK);
-  const int all = w.nq * (a.A / a.Ak), steps = sink ? p.sink_steps : p.steps, used = (all + steps - 1) / steps;
+  const int head = blockIdx.y;
   const int u = (blockIdx.x % UNITS) * JT + threadIdx.x, lane = u & 63, blk = u >> 6;
   constexpr int CB = 256 / RW;              // columns of an accumulator register block
   const int row = blk / (D / CB) * RW + (lane & (RW - 1)), col = blk % (D / CB) * CB + 4 * (lane / RW);
-  const float* src = a.partial + ((long)w.slot * 2 + blockIdx.z) * KT * D + (long)u * 4;
-  f32x4 t{0.f, 0.f, 0.f, 0.f};
-  int i = 0;
-  for (; i + 3 < used; i += 4) {
-    f32x4 x[4];
+  auto join = [&](int bi, int kv, int k0, int slot, int used) {
+    const float* src = a.partial + ((long)slot * 2 + blockIdx.z) * KT * D + (long)u * 4;
+    f32x4 t{0.f, 0.f, 0.f, 0.f};
+    int i = 0;
+    for (; i + 3 < used; i += 4) {
+      f32x4 x[4];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) x[q] = *(const f32x4*)(src + (long)(i + q) * 2 * KT * D);
+      for (int q = 0; q < 4; ++q) x[q] = *(const f32x4*)(src + (long)(i + q) * 2 * KT * D);
 #pragma unroll
-    for (int q = 0; q < 4; ++q) t += x[q];
-  }
-  for (; i < used; ++i) t += *(const f32x4*)(src + (long)i * 2 * KT * D);
-  if (w.k0 + row >= a.s || col >= a.d) return;
-  if (blockIdx.z == 0) t *= scale;
-  T* const out = (T*)(blockIdx.z ? a.dv : a.dk) + ((long)w.bi * a.s + w.k0 + row) * (blockIdx.z ? a.lddv : a.lddk) + w.kv * a.d + col;
-  if constexpr (sizeof(T) == 2) {
-    bf16x4 o;
+      for (int q = 0; q < 4; ++q) t += x[q];
+    }
+    for (; i < used; ++i) t += *(const f32x4*)(src + (long)i * 2 * KT * D);
+    if (k0 + row >= a.s || col >= a.d) return;
+    if (blockIdx.z == 0) t *= scale;
+    T* const out = (T*)(blockIdx.z ? a.dv : a.dk) + ((long)bi * a.s + k0 + row) * (blockIdx.z ? a.lddv : a.lddk) + kv * a.d + col;
+    if constexpr (sizeof(T) == 2) {
+      bf16x4 o;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) o[e] = (bf16)t[e];
-    *(bf16x4*)out = o;
+      for (int e = 0; e < 4; ++e) o[e] = (bf16)t[e];
+      *(bf16x4*)out = o;
+    } else {
+      *(f32x4*)out = t;
+    }
+  };
+  if constexpr (M == MASK_SPANS) {   // (how many there are is known on the device alone)
+    const int32_t* const cuts = a.table + 4 + 4L * p.max_tasks;
+    for (int c = blockIdx.x / UNITS; c < a.table[1]; c += gridDim.x / UNITS)
+      join(0, head, cuts[4 * c] * KT, head * p.slots + cuts[4 * c + 1], cuts[4 * c + 2]);
   } else {
-    *(f32x4*)out = t;
+    const int nt = (p.sink_parts > 1 ? p.sink_tiles : 0);
+    int tile = blockIdx.x / UNITS;
+    if (nt == 0) tile += p.sink_tiles;   // (then the other tiles have parts)
+    const bool sink = tile < p.sink_tiles;
+    const int sinks = p.sink_tiles * p.sink_parts;
+    // the tile's first task (KeyTask counts the same)
+    KeyTask<M> w;
+    w.init(a, head * (sinks + (p.key_tiles - p.sink_tiles) * p.parts) + (sink ? tile * p.sink_parts : sinks + (tile - p.sink_tiles) * p.parts), KT, BLK);
+    const int all = w.nq * (a.A / a.Ak), steps = sink ? p.sink_steps : p.steps;
+    join(w.bi, w.kv, w.k0, w.slot, (all + steps - 1) / steps);
   }
 }
 
@@ -1425,6 +1652,29 @@ auto pick_width(Dtype dt, int d, F&& f) {
 
 inline size_t delta_bytes(const AttnWinArgs& a) { return ((size_t)a.b * a.A * a.s * 4 + 255) / 256 * 256; }
 
+// D = 128: whether dq's workgroups of 256 queries (a unit holds one) are in the launch of dk and dv
+inline bool pair_has_dq(const AttnWinArgs& a) { return (long)((a.s + 255) / 256) * a.b * a.A >= 256; }
+
+// what docs_plan may cut the walks into (b = 1)
+inline void make_docs_plan(Dtype dt, AttnWinArgs& a) {
+  WinPlan& p = a.plan;
+  p.kt = key_tile(dt, a);
+  p.blk = walk_block(dt, a);
+  // Parts of up to a share of all walks of dk and dv for each workgroup that runs at once: a unit holds one of D = 128 in bf16, and two
+  // others.  Where dq's workgroups are in the same launch, behind them, one and a half times that: the longest begin first, and
+  // dq's fill what they leave.
+  p.units = dt == DT_BF16 && a.d > 64 ? (pair_has_dq(a) ? 170 : 256) : 340;
+  p.min_steps = 16;
+  p.key_tiles = (a.s + p.kt - 1) / p.kt;
+  const long parts = ((long)(a.s + p.blk - 1) / p.blk * (a.A / a.Ak) + p.min_steps - 1) / p.min_steps;   // of the longest walk there can be
+  const long share = p.units / a.Ak;   // walks longer than a unit's share, of a head
+  p.max_cuts = parts > 1 ? (int)std::min<long>(share, p.key_tiles) : 0;
+  p.slots = parts > 1 ? (int)std::min<long>(2L * p.units / a.Ak, p.key_tiles * parts) : 0;
+  p.max_tasks = p.key_tiles + (int)std::min<long>(share, p.key_tiles * parts);
+  p.key_tasks = (unsigned)(((long)p.max_tasks * a.Ak + 7) / 8 * 8);   // (what follows begins at XCD 0)
+}
+inline size_t table_bytes(const AttnWinArgs& a) { return (16 + 16 * ((size_t)a.plan.max_tasks + a.plan.max_cuts) + 255) / 256 * 256; }
+
 template <typename K>
 hipError_t allow_lds(K kern, int bytes) {
   return hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
@@ -1468,17 +1718,26 @@ hipError_t attn_win_fwd_launch_bf16(const AttnWinArgs& a, hipStream_t st) {
 // the plan, the workspace's parts, -delta
 template <int M, typename T>
 hipError_t attn_win_bwd_begin(Dtype dt, AttnWinArgs& a, void* workspace, hipStream_t st) {
-  make_plan(dt, a);
+  if (M == MASK_SPANS) make_docs_plan(dt, a);
+  else make_plan(dt, a);
   a.delta = (float*)workspace;
   a.partial = (float*)((char*)workspace + delta_bytes(a));
-  hipLaunchKernelGGL((attn_win_delta<M, T>), dim3((unsigned)(((long)a.b * a.s + 3) / 4)), dim3(256), 0, st, a);
+  if (M == MASK_SPANS) {
+    a.table = (int32_t*)a.partial;
+    a.partial = (float*)((char*)a.table + table_bytes(a));
+  }
+  hipLaunchKernelGGL((attn_win_delta<M, T>), dim3((unsigned)(((long)a.b * a.s + 3) / 4) + (M == MASK_SPANS)), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 template <typename K>
 hipError_t attn_win_bwd_join(K kern, const AttnWinArgs& a, int kt, int d, hipStream_t st) {
-  const int joined = a.plan.slots ? (a.plan.sink_parts > 1 ? a.plan.sink_tiles : 0) + (a.plan.parts > 1 ? a.plan.key_tiles - a.plan.sink_tiles : 0) : 0;
-  if (!joined) return hipSuccess;
+  int joined = a.plan.slots ? (a.plan.sink_parts > 1 ? a.plan.sink_tiles : 0) + (a.plan.parts > 1 ? a.plan.key_tiles - a.plan.sink_tiles : 0) : 0;
   const int threads = join_threads(kt * d);
+  if (a.spans) {   // (workgroups enough for the memory; what finds no cut tile costs time, too)
+    const long per = (long)(kt * d / 4 / threads) * a.Ak * 2;
+    joined = std::min<long>(a.plan.max_cuts, std::max<long>(1, 1024 / per));
+  }
+  if (!joined) return hipSuccess;
   hipLaunchKernelGGL(kern, dim3(joined * (kt * d / 4 / threads), a.b * a.Ak, 2), dim3(threads), 0, st, a, a.scale);
   return hipGetLastError();
 }
@@ -1514,7 +1773,7 @@ hipError_t attn_win_bwd_launch_bf16(AttnWinArgs a, void* workspace, hipStream_t 
       static const hipError_t rc = allow_lds(attn_win_bwd_pair<M, S>, PAIR_BYTES);
       if (rc != hipSuccess) return rc;
       const long q_tiles = (long)((a.s + 255) / 256) * a.b * a.A;
-      const bool both = q_tiles >= 256;   // (a unit holds one of these workgroups)
+      const bool both = pair_has_dq(a);
       hipLaunchKernelGGL((attn_win_bwd_pair<M, S>), dim3((unsigned)(a.plan.key_tasks + (both ? q_tiles : 0))), dim3(512), PAIR_BYTES, st, a, scale2, scale);
       e = hipGetLastError();
       if (e == hipSuccess) e = attn_win_bwd_join(attn_win_join<M, bf16, d, 128, 32, 32>, a, 128, d, st);

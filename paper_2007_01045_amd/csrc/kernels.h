@@ -236,6 +236,8 @@ struct WinPlan {
   int steps, sink_steps;         // blocks of a part of either
   int slots;                     // of fp32 sums, per sequence and key head
   unsigned key_tasks;
+  // attention of packed documents: what the device's plan (docs_plan) is made with, and the most that it may hold per key head
+  int kt, blk, units, min_steps, max_tasks, max_cuts;
 };
 // rows b*s at row strides in elements, 0 <= W < s (0: no window), 0 <= S <= s; lse, delta [b, A, s]; ctx32 (may be NULL) in ctx's
 // layout
@@ -256,11 +258,14 @@ struct AttnWinArgs {
   const int32_t* spans;
   const float* slopes;
   float cap2, bend;
+  float small, poly[3], down;   // bf16: where raw is at most `small` the cap is a polynomial (Score); down = -1 / cap2^2
+  int32_t* table;   // of docs_plan
 };
 enum { MASK_WINDOW = 0, MASK_SPANS = 1 };
-enum { SCORE_PLAIN = 0, SCORE_SLOPE = 1, SCORE_CAP = 2 };   // SCORE_CAP: with slopes or without; fp32: any
+enum { SCORE_PLAIN = 0, SCORE_SLOPE = 1, SCORE_CAP = 2, SCORE_BOTH = 3 };   // fp32: plain or both
 bool attn_win_takes(Dtype dt, const AttnWinArgs& a);
 int64_t attn_win_workspace(Dtype dt, AttnWinArgs a);   // bytes of the backward's
+int64_t attn_docs_workspace(Dtype dt, AttnWinArgs a);
 hipError_t launch_attn_win_fwd(Dtype dt, const AttnWinArgs& a, hipStream_t st);
 hipError_t launch_attn_win_bwd(Dtype dt, const AttnWinArgs& a, void* workspace, hipStream_t st);
 // spans [4 rows + 1] of n documents that end at ends[t]; prefix [n] (may be NULL) rows of each that all of it sees
@@ -269,7 +274,9 @@ hipError_t launch_attn_docs_fwd(Dtype dt, const AttnWinArgs& a, hipStream_t st);
 hipError_t launch_attn_docs_fwd_f32(const AttnWinArgs& a, hipStream_t st);
 hipError_t launch_attn_docs_bwd(Dtype dt, const AttnWinArgs& a, void* workspace, hipStream_t st);
 hipError_t launch_attn_docs_bwd_f32(const AttnWinArgs& a, void* workspace, hipStream_t st);
+hipError_t launch_attn_docs_fwd_cap(const AttnWinArgs& a, hipStream_t st);
 hipError_t launch_attn_docs_bwd_cap(const AttnWinArgs& a, void* workspace, hipStream_t st);
+hipError_t launch_attn_docs_bwd_both(const AttnWinArgs& a, void* workspace, hipStream_t st);
 
 // ---------------------------------------------------------------- row kernels
 // y = LN(z) over the last dim (H), stats[2*r] = mean, stats[2*r+1] = rstd.  z_f32: z is fp32

@@ -85,10 +85,11 @@ int dapple_attention_window_bwd(int dtype, const dapple_attention_window_desc* d
 // ------------------------------------------------------------------ attention of packed documents
 static int docs_args(int dtype, const dapple_attention_docs_desc* d, bool bwd, bool sizes_only, AttnWinArgs& a) {
   if (!d) return set_error(STAGE_E_NULL, "the descriptor is NULL");
-  // (one sequence, whose gradient's walks are unequal like those of a causal one)
+  // (one sequence; a workgroup of the gradient's first launch beside four rows each is the plan's)
+  if (d->rows > (1 << 26) - 8) return set_error(STAGE_E_CONFIG, "2^26 - 7 rows and more");
   dapple_attention_window_desc w{};
   w.q = d->q; w.k = d->k; w.v = d->v; w.ctx = d->ctx; w.ctx32 = d->ctx32; w.lse = d->lse; w.dctx = d->dctx; w.dq = d->dq; w.dk = d->dk; w.dv = d->dv;
-  w.workspace = d->workspace; w.b = 1; w.s = d->rows; w.A = d->A; w.Ak = d->Ak; w.d = d->d; w.causal = 1;
+  w.workspace = d->workspace; w.b = 1; w.s = d->rows; w.A = d->A; w.Ak = d->Ak; w.d = d->d;
   w.ldq = d->ldq; w.ldk = d->ldk; w.ldv = d->ldv; w.ldc = d->ldc; w.lddc = d->lddc; w.lddq = d->lddq; w.lddk = d->lddk; w.lddv = d->lddv;
   w.scale = d->scale;
   const int rc = win_args(dtype, &w, bwd, sizes_only, a);
@@ -101,6 +102,15 @@ static int docs_args(int dtype, const dapple_attention_docs_desc* d, bool bwd, b
     const double log2e = 1.4426950408889634;
     a.cap2 = (float)(d->cap * log2e);
     a.bend = (float)((dtype == STAGE_DTYPE_BF16 ? 2.0 * log2e : 1.0) * a.scale / d->cap);
+    const double k = (double)a.scale / d->cap, s2 = log2e * a.scale, c[3] = {-0.33319074494554746, 0.1308641832442356, -0.041387786259018865};
+    a.small = (float)(0.6 / k);
+    a.down = (float)(-1.0 / ((double)a.cap2 * a.cap2));
+    double f = s2;
+    for (int i = 0; i < 3; ++i) {
+      f *= k * k;
+      a.poly[i] = (float)(f * c[i]);
+      if (!std::isnormal(a.poly[i])) a.small = -1.f;   // (cap or scale of extreme sizes: never the polynomial)
+    }
   }
   return STAGE_OK;
 }
@@ -109,7 +119,7 @@ extern "C" {
 
 int dapple_doc_spans(const int32_t* ends, const int32_t* prefix, int n, int rows, int causal, int window, int32_t* spans, void* stream) {
   if (!spans || (n > 0 && !ends)) return set_error(STAGE_E_NULL, "spans, and ends of a document, must not be NULL");
-  if (n < 0 || rows < 1 || rows > (1 << 26) - 4) return set_error(STAGE_E_CONFIG, "%d documents, %d rows (1 to 2^26 - 4)", n, rows);
+  if (n < 0 || rows < 1 || rows > (1 << 26) - 8) return set_error(STAGE_E_CONFIG, "%d documents, %d rows (1 to 2^26 - 8)", n, rows);
   if (window < 0) return set_error(STAGE_E_CONFIG, "window %d", window);
   if (prefix && !causal) return set_error(STAGE_E_CONFIG, "a prefix without causal");
   if (!aligned_to(ends, 4) || !aligned_to(prefix, 4) || !aligned_to(spans, 4)) return set_error(STAGE_E_CONFIG, "ends, prefix or spans not aligned");
@@ -125,7 +135,7 @@ int dapple_attention_docs_fwd(int dtype, const dapple_attention_docs_desc* d, vo
 int64_t dapple_attention_docs_workspace(int dtype, const dapple_attention_docs_desc* d) {
   AttnWinArgs a{};
   const int rc = docs_args(dtype, d, true, true, a);
-  return rc != STAGE_OK ? rc : attn_win_workspace(type_of(dtype), a);
+  return rc != STAGE_OK ? rc : attn_docs_workspace(type_of(dtype), a);
 }
 
 int dapple_attention_docs_bwd(int dtype, const dapple_attention_docs_desc* d, void* stream) {

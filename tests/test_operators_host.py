@@ -265,7 +265,7 @@ def test_attention_docs_refusals():
             (conf, dict(scale=math.nan)), (conf, dict(cap=-1.0)), (conf, dict(cap=1e-7)), (conf, dict(cap=1025.0)), (conf, dict(cap=math.inf)),
             (conf, dict(cap=math.nan)), (conf, dict(ldq=255)), (conf, dict(ldk=-8)), (conf, dict(ldv=1 << 23)), (conf, dict(rows=1 << 22, ldq=264)),
             (conf, dict(q=P + 8)), (conf, dict(ctx32=P + 4)), (conf, dict(lse=P + 2)), (conf, dict(spans=P + 2)), (conf, dict(slopes=P + 1)),
-            (conf, dict(rows=(1 << 26) - 3))]
+            (conf, dict(rows=(1 << 26) - 7))]
     for code, change in both:
         for f in (B.dapple_attention_docs_fwd, B.dapple_attention_docs_bwd):
             refused(code, f, B.DTYPE_BF16, B.attention_docs_desc(**dict(ok, **change)))
@@ -283,7 +283,7 @@ def test_attention_docs_refusals():
 def test_doc_spans_refusals():
     null, conf = B.STAGE_E_NULL, B.STAGE_E_CONFIG
     ok = dict(ends_ptr=P, n=3, rows=10, spans_ptr=P)
-    for code, change in ((null, dict(ends_ptr=None)), (null, dict(spans_ptr=None)), (conf, dict(n=-1)), (conf, dict(rows=0)), (conf, dict(rows=(1 << 26) - 3)),
+    for code, change in ((null, dict(ends_ptr=None)), (null, dict(spans_ptr=None)), (conf, dict(n=-1)), (conf, dict(rows=0)), (conf, dict(rows=(1 << 26) - 7)),
                          (conf, dict(window=-1)), (conf, dict(causal=0, prefix_ptr=P)), (conf, dict(ends_ptr=P + 2)), (conf, dict(prefix_ptr=P + 1)),
                          (conf, dict(spans_ptr=P + 2))):
         refused(code, B.dapple_doc_spans, **dict(ok, **change))
