@@ -74,8 +74,8 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float* red, int& turn) {
   }
 }
 
-// NW waves to a row, NCH chunks of a row to a lane; a workgroup has max(4, NW) waves
-template <int NW> constexpr int row_waves() { return NW > 4 ? NW : 4; }
+// NW waves to a row, NCH chunks of a row to a lane; a workgroup has NW waves, or four with a row each
+template <int NW> constexpr int row_waves() { return NW > 1 ? NW : 4; }
 
 template <typename T, typename Z, int NORM, int NW, int NCH>
 __global__ __launch_bounds__(64 * row_waves<NW>()) void dropout_norm_fwd(DropNormArgs a) {
@@ -98,16 +98,26 @@ __global__ __launch_bounds__(64 * row_waves<NW>()) void dropout_norm_fwd(DropNor
     if (NORM && a.beta) load8((const T*)a.beta + col[c], a.H - col[c], bet[c]);
     if (a.bias) load8((const T*)a.bias + col[c], a.H - col[c], bia[c]);
   }
-  for (long row = (long)blockIdx.x * RPB + wave / NW; row < a.rows; row += (long)gridDim.x * RPB) {
-    float z[NCH][8], r[NCH][8];
+  Raw8<T> xn[NCH] = {};
+  Raw8<Z> rn[NCH] = {};
+  auto load = [&](long row) {
 #pragma unroll
     for (int c = 0; c < NCH; ++c) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) z[c][e] = r[c][e] = 0.f;
       if (col[c] >= a.H) continue;
-      load8((const T*)a.x + row * a.ldx + col[c], a.H - col[c], z[c]);
-      if (a.residual) load8((const Z*)a.residual + row * a.ldr + col[c], a.H - col[c], r[c]);
+      xn[c].load((const T*)a.x + row * a.ldx + col[c], a.H - col[c]);
+      if (a.residual) rn[c].load((const Z*)a.residual + row * a.ldr + col[c], a.H - col[c]);
     }
+  };
+  const long step = (long)gridDim.x * RPB;
+  long row = (long)blockIdx.x * RPB + wave / NW;
+  if (row < a.rows) load(row);
+  for (; row < a.rows; row += step) {
+    float z[NCH][8], r[NCH][8];
+#pragma unroll
+    for (int c = 0; c < NCH; ++c)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) z[c][e] = xn[c].get(e), r[c][e] = rn[c].get(e);
+    if (row + step < a.rows) load(row + step);   // (beside this row's sums)
     float s[1] = {0.f};
 #pragma unroll
     for (int c = 0; c < NCH; ++c) {
@@ -176,19 +186,32 @@ __global__ __launch_bounds__(64 * row_waves<NW>()) void dropout_norm_bwd(DropNor
     for (int e = 0; e < 8; ++e) gam[c][e] = 1.f, sum[0][c][e] = sum[1][c][e] = sum[2][c][e] = 0.f;
     if (NORM && a.gamma && col[c] < a.H) load8((const T*)a.gamma + col[c], a.H - col[c], gam[c]);
   }
-  for (long row = (long)blockIdx.x * RPB + wave / NW; row < a.rows; row += (long)gridDim.x * RPB) {
-    float g[NCH][8], h[NCH][8], t[NCH][8];
+  Raw8<Z> gn[NCH] = {}, hn[NCH] = {};
+  Raw8<T> tn[NCH] = {};
+  float mean_n = 0.f, rstd_n = 0.f;
+  auto load = [&](long row) {
 #pragma unroll
     for (int c = 0; c < NCH; ++c) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) g[c][e] = h[c][e] = t[c][e] = 0.f;
       if (col[c] >= a.H) continue;
-      if (a.dz) load8((const Z*)a.dz + row * a.lddz + col[c], a.H - col[c], g[c]);
-      if (NORM) load8((const Z*)a.z + row * a.ldz + col[c], a.H - col[c], h[c]);
-      if (NORM) load8((const T*)a.dy + row * a.lddy + col[c], a.H - col[c], t[c]);
+      if (a.dz) gn[c].load((const Z*)a.dz + row * a.lddz + col[c], a.H - col[c]);
+      if (NORM) hn[c].load((const Z*)a.z + row * a.ldz + col[c], a.H - col[c]);
+      if (NORM) tn[c].load((const T*)a.dy + row * a.lddy + col[c], a.H - col[c]);
     }
+    if (NORM == NORM_LAYER) mean_n = a.stats[2 * row];
+    if (NORM) rstd_n = a.stats[2 * row + 1];
+  };
+  const long step = (long)gridDim.x * RPB;
+  long row = (long)blockIdx.x * RPB + wave / NW;
+  if (row < a.rows) load(row);
+  for (; row < a.rows; row += step) {
+    float g[NCH][8], h[NCH][8], t[NCH][8];
+#pragma unroll
+    for (int c = 0; c < NCH; ++c)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) g[c][e] = gn[c].get(e), h[c][e] = hn[c].get(e), t[c][e] = tn[c].get(e);
+    const float mean = mean_n, rstd = rstd_n;
+    if (row + step < a.rows) load(row + step);   // (beside this row's sums)
     if constexpr (NORM != NORM_NONE) {
-      const float mean = NORM == NORM_LAYER ? a.stats[2 * row] : 0.f, rstd = a.stats[2 * row + 1];
       float s[2] = {0.f, 0.f};
 #pragma unroll
       for (int c = 0; c < NCH; ++c)
@@ -276,10 +299,13 @@ __global__ __launch_bounds__(1024) void dropout_norm_sums(DropNormArgs a, int bl
 // ------------------------------------------------------------------ launchers
 // f(waves to a row, chunks of a lane)
 template <typename F>
-static hipError_t for_width(int H, F&& f) {
+static hipError_t for_width(int H, bool bwd, F&& f) {
   using std::integral_constant;
   if (H <= 512) return f(integral_constant<int, 1>{}, integral_constant<int, 1>{});
-  if (H <= 1024) return f(integral_constant<int, 1>{}, integral_constant<int, 2>{});
+  // (us forward, a wave / two waves to a row of 1024 in bf16, fp32 stream: 256 rows 5.1 / 3.8, 2048 7.4 / 6.6, 8192 20.1 / 17.4, 32768
+  // 78.0 / 77.5; 3001 rows of 1001 in fp32 11.7 / 9.8.  The gradient: 2048 12.7 / 14.8, 8192 23.4 / 24.7, 32768 79 / 84, but 256 rows 9.0 / 8.1)
+  if (H <= 1024 && bwd) return f(integral_constant<int, 1>{}, integral_constant<int, 2>{});
+  if (H <= 1024) return f(integral_constant<int, 2>{}, integral_constant<int, 1>{});
   if (H <= 2048) return f(integral_constant<int, 4>{}, integral_constant<int, 1>{});
   if (H <= 4096) return f(integral_constant<int, 4>{}, integral_constant<int, 2>{});
   if (H <= 8192) return f(integral_constant<int, 8>{}, integral_constant<int, 2>{});
@@ -298,18 +324,21 @@ static hipError_t for_types(Dtype dt, const DropNormArgs& a, F&& f) {
   return a.stream32 ? norm((bf16)0.f, 0.f) : norm((bf16)0.f, (bf16)0.f);
 }
 
-static int rows_at_once(int H) { return H <= 1024 ? 4 : 1; }
-// Workgroups of the backward: each leaves 12 bytes a column behind, which are written and read once more
+// Workgroups of the backward: each leaves 12 bytes a column behind, which are written and read once more, and its rows' loads run
+// ahead of their sums, so that few waves keep the memory busy.  Us with 256 / 512 of them: rows of 256, 16384 rows 21.0 / 18.5, 2048 8.5 / 8.8;
+// of 1024, 8192 rows 23.6 / 23.4, 32768 79 / 82; of 2048, 1024 rows 14.0 / 16.1, 8192 43.1 / 38.0; of 4096, 32768 rows 241 / 264; of
+// 8192, 16384 rows 306 / 313 (1024 of them were the slowest of all).
 int dropout_norm_blocks(int rows, int H) {
-  const int per = rows_at_once(H);
-  return std::min((rows + 2 * per - 1) / (2 * per), 1024);
+  const int per = H <= 1024 ? 4 : 1;
+  return std::min((rows + per - 1) / per, H <= 512 || (H > 1024 && H <= 2048 && rows >= 4096) ? 512 : 256);
 }
 
 hipError_t launch_dropout_norm_fwd(Dtype dt, const DropNormArgs& a, hipStream_t st) {
   return for_types(dt, a, [&](auto t, auto z, auto N) {
-    return for_width(a.H, [&](auto NW, auto NCH) {
+    return for_width(a.H, false, [&](auto NW, auto NCH) {
       constexpr int nw = decltype(NW)::value, per = row_waves<nw>() / nw;
-      const unsigned grid = (unsigned)std::min<long>(((long)a.rows + per - 1) / per, 2048);
+      // (us with 2048 / 4096 workgroups: rows of 1024, 8192 of them 17.4 / 18.1; of 4096, 32768 204 / 199)
+      const unsigned grid = (unsigned)std::min<long>(((long)a.rows + per - 1) / per, a.H > 1024 ? 4096 : 2048);
       hipLaunchKernelGGL((dropout_norm_fwd<decltype(t), decltype(z), decltype(N)::value, nw, decltype(NCH)::value>), dim3(grid),
                          dim3(64 * row_waves<nw>()), 0, st, a);
       return hipGetLastError();
@@ -320,7 +349,7 @@ hipError_t launch_dropout_norm_fwd(Dtype dt, const DropNormArgs& a, hipStream_t 
 hipError_t launch_dropout_norm_bwd(Dtype dt, const DropNormArgs& a, hipStream_t st) {
   const int blocks = dropout_norm_blocks(a.rows, a.H);
   hipError_t e = for_types(dt, a, [&](auto t, auto z, auto N) {
-    return for_width(a.H, [&](auto NW, auto NCH) {
+    return for_width(a.H, true, [&](auto NW, auto NCH) {
       constexpr int nw = decltype(NW)::value;
       hipLaunchKernelGGL((dropout_norm_bwd<decltype(t), decltype(z), decltype(N)::value, nw, decltype(NCH)::value>), dim3(blocks),
                          dim3(64 * row_waves<nw>()), 0, st, a);

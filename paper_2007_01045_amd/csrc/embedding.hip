@@ -3,7 +3,7 @@
 //
 // Forward: a copy, bound by memory.  Backward: the rows are sorted by id (stable: a row's place among those of its id is its order),
 // so that an id's rows lie one behind the other, and every row of dy is read once and every row of dtable written once, without atomics
-// on values.  The sort is one of least significant digits first, of at most nine bits: per digit a count and a placing, each
+// on values.  The sort is one of least significant digits first, of at most ten bits: per digit a count and a placing, each
 // workgroup a run of the rows.  Sums: a wave takes a run of the sorted rows and 512 columns; an id whose rows lie in one run is stored,
 // of one that goes on in the next runs each leaves its part, and a second kernel adds the parts in ascending order.
 #include <algorithm>
@@ -18,7 +18,7 @@ template <typename T>
 __global__ __launch_bounds__(256) void embed_fwd(EmbeddingArgs a, int chunks) {
   const long all = (long)a.rows * chunks, stride = (long)gridDim.x * 256;
   for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < all; i += stride) {
-    const long row = all < (1L << 31) ? (long)((uint32_t)i / (uint32_t)chunks) : i / chunks;
+    const long row = all < (1L << 32) ? (long)((uint32_t)i / (uint32_t)chunks) : i / chunks;
     const int col = (int)(i - row * chunks) * 8, id = a.ids[row];
     float v[8];
     if (id >= 0 && id < a.V) {
@@ -34,88 +34,122 @@ __global__ __launch_bounds__(256) void embed_fwd(EmbeddingArgs a, int chunks) {
 }
 
 // ------------------------------------------------------------------ sort
-constexpr int DIGITS = 512, SORT_T = 1024, SUM_ROWS = 16;
+constexpr int DIGITS = 1024, SORT_T = 1024, SORT_W = SORT_T / 64;
 
-// key of sorted place i, V (no token's) behind the last; ids outside the table come last
+// ids outside the table come last
 __device__ __forceinline__ uint32_t key_of(int id, int V) { return id < 0 || id > V ? (uint32_t)V : (uint32_t)id; }
 
-// counts[workgroup][digit] of the workgroups' rows.  T: the workgroups behind them clear dtable, of that type
+// the lanes of the wave that hold the same digit (of those that hold one)
+__device__ __forceinline__ unsigned long long same_digit(uint32_t d, bool in, int bits) {
+  unsigned long long same = __ballot(in);
+  for (int b = 0; b < bits; ++b) {
+    const unsigned long long m = __ballot((d >> b) & 1);
+    same &= (d >> b) & 1 ? m : ~m;
+  }
+  return same;
+}
+
+// dtable, of type T, cleared by workgroups `wg` of `wgs`
+template <typename T>
+__device__ __forceinline__ void clear_table(const EmbeddingArgs& a, int wg, int wgs) {
+  const bool dense = a.lddt == a.H;   // one row
+  const long cols = dense ? (long)a.V * a.H : a.H, chunks = (cols + 7) / 8, all = dense ? chunks : a.V * chunks;
+  const float zero[8] = {};
+  for (long i = (long)wg * SORT_T + threadIdx.x; i < all; i += (long)wgs * SORT_T) {
+    const long row = dense ? 0 : i / chunks, col = (i - row * chunks) * 8;
+    store8((T*)a.dtable + row * a.lddt + col, (int)min(8L, cols - col), zero);
+  }
+}
+
+// The digits of rows first .. end - 1 counted into hist: once a wave and digit (frequent tokens, and the upper digits of most, are the
+// same in many lanes)
+template <bool FIRST, typename F>
+__device__ __forceinline__ void count_digits(const EmbeddingArgs& a, const EmbedPlan& p, const uint32_t* keys, int shift, int first, int end, F&& add) {
+  const int lane = threadIdx.x & 63;
+  for (int i0 = first; i0 < end; i0 += 8 * SORT_T) {
+    uint32_t k[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const int i = min(i0 + u * SORT_T + (int)threadIdx.x, end - 1);
+      k[u] = FIRST ? key_of(a.ids[i], a.V) : keys[i];
+    }
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      if (i0 + u * SORT_T >= end) break;
+      const bool in = i0 + u * SORT_T + (int)threadIdx.x < end;
+      const uint32_t d = (k[u] >> shift) & ((1u << p.bits) - 1);
+      const unsigned long long same = same_digit(d, in, p.bits);
+      if (in && (same & ((1ull << lane) - 1)) == 0) add(d, (uint32_t)__builtin_popcountll(same), i0 + u * SORT_T);
+    }
+  }
+}
+
+// counts[workgroup][digit] of the workgroups' rows (where they are many: see embed_place)
 template <typename T, bool FIRST>
 __global__ __launch_bounds__(SORT_T) void embed_count(EmbeddingArgs a, EmbedPlan p, const uint32_t* keys, int shift) {
   __shared__ uint32_t hist[DIGITS];
   const int tid = threadIdx.x;
-  if ((int)blockIdx.x >= p.wgs) {
-    const bool dense = a.lddt == a.H;   // one row
-    const long cols = dense ? (long)a.V * a.H : a.H, chunks = (cols + 7) / 8, all = dense ? chunks : a.V * chunks;
-    const float zero[8] = {};
-    for (long i = (long)(blockIdx.x - p.wgs) * SORT_T + tid; i < all; i += (long)(gridDim.x - p.wgs) * SORT_T) {
-      const long row = dense ? 0 : i / chunks, col = (i - row * chunks) * 8;
-      store8((T*)a.dtable + row * a.lddt + col, (int)min(8L, cols - col), zero);
-    }
-    return;
-  }
-  if (tid < DIGITS) hist[tid] = 0;
+  if ((int)blockIdx.x >= p.wgs) return clear_table<T>(a, blockIdx.x - p.wgs, gridDim.x - p.wgs);
+  hist[tid] = 0;
   __syncthreads();
-  const int first = blockIdx.x * p.per, end = min(a.rows, first + p.per);
-  for (int i = first + tid; i < end; i += SORT_T) {
-    const uint32_t k = FIRST ? key_of(a.ids[i], a.V) : keys[i];
-    atomicAdd(&hist[(k >> shift) & (DIGITS - 1) & ((1u << p.bits) - 1)], 1u);
-  }
+  const int first = blockIdx.x * p.per;
+  count_digits<FIRST>(a, p, keys, shift, first, min(a.rows, first + p.per), [&](uint32_t d, uint32_t n, int) { atomicAdd(&hist[d], n); });
   __syncthreads();
-  if (tid < DIGITS) p.counts[(long)blockIdx.x * DIGITS + tid] = hist[tid];
+  if (tid < 1 << p.bits) p.counts[(long)blockIdx.x * DIGITS + tid] = hist[tid];
 }
 
-template <bool FIRST>
+// The workgroup's rows to their places by one digit.  Few rows: each workgroup counts them all itself, without a launch for it, and the
+// workgroups behind those of the first digit clear dtable
+template <typename T, bool FIRST, bool COUNTS>
 __global__ __launch_bounds__(SORT_T) void embed_place(EmbeddingArgs a, EmbedPlan p, const uint32_t* keys, const uint32_t* rows, uint32_t* keys_out,
                                                       uint32_t* rows_out, int shift) {
-  constexpr int NWV = SORT_T / 64;
-  __shared__ uint32_t base[DIGITS], part[2][2][DIGITS], run[DIGITS / 64];
-  __shared__ uint16_t of_wave[NWV][DIGITS];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, digit = tid & (DIGITS - 1), half = tid >> 9;
-  {   // rows of a digit in the workgroups before this one, and in all: half of the workgroups to a thread
-    uint32_t before = 0, total = 0;
-    const int w0 = half * ((p.wgs + 1) / 2), w1 = half ? p.wgs : (p.wgs + 1) / 2;
-#pragma unroll 8
-    for (int w = w0; w < w1; ++w) {
-      const uint32_t c = p.counts[(long)w * DIGITS + digit];
+  __shared__ uint32_t base[DIGITS], part[2][DIGITS], run[SORT_W];
+  __shared__ uint16_t of_wave[SORT_W][DIGITS];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int first = blockIdx.x * p.per, end = min(a.rows, first + p.per);
+  if (FIRST && blockIdx.x == 0 && tid < 2) p.joins[tid] = 0;
+  // a thread's digit's rows in the workgroups before this one, and in all
+  uint32_t before = 0, total = 0;
+  if constexpr (COUNTS) {
+    const int wgs = tid < 1 << p.bits ? p.wgs : 0;
+#pragma unroll 16
+    for (int w = 0; w < wgs; ++w) {
+      const uint32_t c = p.counts[(long)w * DIGITS + tid];
       before += w < (int)blockIdx.x ? c : 0;
       total += c;
     }
-    part[half][0][digit] = before;
-    part[half][1][digit] = total;
+  } else {
+    if ((int)blockIdx.x >= p.wgs) return clear_table<T>(a, blockIdx.x - p.wgs, gridDim.x - p.wgs);
+    part[0][tid] = part[1][tid] = 0;
+    __syncthreads();
+    count_digits<FIRST>(a, p, keys, shift, 0, a.rows, [&](uint32_t d, uint32_t n, int i0) {
+      atomicAdd(&part[1][d], n);
+      if (i0 < first) atomicAdd(&part[0][d], n);
+    });
+    __syncthreads();
+    before = part[0][tid], total = part[1][tid];
   }
-  __syncthreads();
-  uint32_t total = 0, upto = 0;
-  if (tid < DIGITS) {   // the digits' first places: sums of the totals before them
-    total = part[0][1][tid] + part[1][1][tid];
-    upto = total;
+  // the digits' first places: sums of the totals before them
+  uint32_t upto = total;
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const uint32_t v = __shfl_up(upto, o, 64);
-      if (lane >= o) upto += v;
-    }
-    if (lane == 63) run[wave] = upto;
+  for (int o = 1; o < 64; o <<= 1) {
+    const uint32_t v = __shfl_up(upto, o, 64);
+    if (lane >= o) upto += v;
   }
-  for (int i = tid; i < NWV * DIGITS; i += SORT_T) (&of_wave[0][0])[i] = 0;
+  if (lane == 63) run[wave] = upto;
+  for (int i = tid; i < SORT_W * DIGITS / 2; i += SORT_T) ((uint32_t*)&of_wave[0][0])[i] = 0;
   __syncthreads();
-  if (tid < DIGITS) {
-    uint32_t b = upto - total + part[0][0][tid] + part[1][0][tid];
-    for (int w = 0; w < wave; ++w) b += run[w];
-    base[tid] = b;
-  }
+  uint32_t b0 = upto - total + before;
+  for (int w = 0; w < wave; ++w) b0 += run[w];
+  base[tid] = b0;
   __syncthreads();
-  const int first = blockIdx.x * p.per, end = min(a.rows, first + p.per);
   for (int i0 = first; i0 < end; i0 += SORT_T) {
     const int i = i0 + tid;
     const bool in = i < end;
     const uint32_t k = in ? (FIRST ? key_of(a.ids[i], a.V) : keys[i]) : 0;
     const uint32_t r = FIRST ? (uint32_t)i : (in ? rows[i] : 0);
     const uint32_t d = (k >> shift) & ((1u << p.bits) - 1);
-    unsigned long long same = __ballot(in);   // the wave's rows of this lane's digit
-    for (int b = 0; b < p.bits; ++b) {
-      const unsigned long long m = __ballot((d >> b) & 1);
-      same &= (d >> b) & 1 ? m : ~m;
-    }
+    const unsigned long long same = same_digit(d, in, p.bits);
     const int mine = __builtin_popcountll(same & ((1ull << lane) - 1));
     if (in && mine == 0) of_wave[wave][d] = (uint16_t)__builtin_popcountll(same);
     __syncthreads();
@@ -126,75 +160,106 @@ __global__ __launch_bounds__(SORT_T) void embed_place(EmbeddingArgs a, EmbedPlan
       rows_out[at] = r;
     }
     __syncthreads();
-    if (tid < DIGITS) {
+    if (i0 + SORT_T < end) {
       uint32_t n = 0;
 #pragma unroll
-      for (int w = 0; w < NWV; ++w) {
+      for (int w = 0; w < SORT_W; ++w) {
         n += of_wave[w][tid];
         of_wave[w][tid] = 0;
       }
       base[tid] += n;
+      __syncthreads();
     }
-    __syncthreads();
   }
 }
 
 // ------------------------------------------------------------------ sums
-template <typename T>
-__device__ __forceinline__ void store_sum(const EmbeddingArgs& a, uint32_t id, int col, const float (&s)[8]) {
+// SUM_ROWS sorted rows at once; LONG: an id of so many runs or more is joined by a workgroup, another by a wave
+constexpr int SUM_ROWS = 16, LONG = 33;
+
+// The eight columns of a lane in a slab of 512: neighbours where H is a multiple of eight (WHOLE), else 64 apart, so that a row's end
+// needs no path of its own (copied for every row that is loaded, it made the code larger than the instruction cache).  Lanes behind the row's
+// end load its last columns and store nothing.
+template <bool WHOLE>
+struct Cols {
+  int col;
+  __device__ __forceinline__ Cols(int slab, int lane) : col(slab * 512 + (WHOLE ? 8 * lane : lane)) {}
+  template <typename T>
+  __device__ __forceinline__ void load(const T* row, int H, Raw8<T>& x) const {
+    if constexpr (WHOLE) {
+      x.load(row + min(col, H - 8), 8);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x.set(e, row[min(col + 64 * e, H - 1)]);
+    }
+  }
+  template <typename T>
+  __device__ __forceinline__ void store(T* row, int H, const float (&v)[8]) const {
+    if constexpr (WHOLE) {
+      if (col < H) store8(row + col, 8, v);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (col + 64 * e < H) row[col + 64 * e] = from_f32<T>(v[e]);
+    }
+  }
+};
+
+template <typename T, bool ADD, bool WHOLE>
+__device__ __forceinline__ void store_sum(const EmbeddingArgs& a, uint32_t id, const Cols<WHOLE>& cols, const float (&s)[8], const Raw8<float>& old) {
   float o[8];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) o[e] = s[e] * a.scale;
-  if (a.accumulate) {
-    float* const D = (float*)a.dtable + (long)id * a.lddt + col;
-    float v[8];
-    load8(D, a.H - col, v);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] += o[e];
-    store8(D, a.H - col, v);
-  } else {
-    store8((T*)a.dtable + (long)id * a.lddt + col, a.H - col, o);
-  }
+  for (int e = 0; e < 8; ++e) o[e] = ADD ? s[e] * a.scale + old.get(e) : s[e] * a.scale;
+  if (ADD) cols.store((float*)a.dtable + (long)id * a.lddt, a.H, o);
+  else cols.store((T*)a.dtable + (long)id * a.lddt, a.H, o);
 }
 
-// One wave: sorted rows [run p.run, ...) and 512 columns from 512 slab on.  parts[run][0]: of an id that began before the run, [1]: of one
-// that begins in it and goes on behind it
-template <typename T>
-__global__ __launch_bounds__(64) void embed_sum(EmbeddingArgs a, EmbedPlan p, const uint32_t* keys, const uint32_t* rows) {
-  const int lane = threadIdx.x;
-  for (long u = blockIdx.x; u < (long)p.runs * p.slabs; u += gridDim.x) {
-    const int run = (int)(u / p.slabs), col = ((int)(u % p.slabs) * 64 + lane) * 8;
+// A wave: sorted rows [run p.run, ...) and 512 columns from 512 slab on.  parts[run][0]: of an id that began before the run, [1]: of one
+// that begins in it and goes on behind it.  ADD (accumulate): the rows of dtable come in with those of dy, eight at once, for registers
+template <typename T, bool ADD, bool WHOLE>
+__global__ __launch_bounds__(256) void embed_sum(EmbeddingArgs a, EmbedPlan p, const uint32_t* keys, const uint32_t* rows) {
+  constexpr int N = ADD ? SUM_ROWS / 2 : SUM_ROWS;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  for (long u = (long)blockIdx.x * 4 + wave; u < (long)p.runs * p.slabs; u += (long)gridDim.x * 4) {
+    const int run = (int)(u / p.slabs), slab = (int)(u % p.slabs);
+    const Cols<WHOLE> cols(slab, lane);
     const int first = run * p.run, end = min(a.rows, first + p.run);
-    if (keys[first] >= (uint32_t)a.V) continue;
-    const uint32_t ahead = first ? keys[first - 1] : 0xffffffffu, behind = end < a.rows ? keys[end] : 0xffffffffu;
-    bool begun = ahead == keys[first];   // the current id began before the run
+    bool begun = false;   // the current id began before the run
     float acc[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) acc[e] = 0.f;
-    auto part = [&](int which) {
-      if (col < a.H) store8(p.parts + ((long)run * 2 + which) * a.H + col, a.H - col, acc);
-    };
-    for (int i0 = first; i0 < end; i0 += SUM_ROWS) {
-      const int i = i0 + (lane & (SUM_ROWS - 1));
-      const uint32_t k = i < end ? keys[i] : behind, r = i < end ? rows[i] : 0;
-      const uint32_t after = i0 + SUM_ROWS < end ? keys[i0 + SUM_ROWS] : behind;
-      float x[SUM_ROWS][8];
+    for (int i0 = first; i0 < end; i0 += N) {
+      // lanes 0 .. N: the keys from i0 on; lane N + 1: the one before
+      const int i = lane <= N ? i0 + lane : i0 - 1, at = min(max(i, 0), a.rows - 1);
+      const uint32_t found = keys[at], r = rows[at], k = i == at ? found : 0xffffffffu;
+      const uint32_t k0 = __builtin_amdgcn_readlane(k, 0);
+      if (k0 >= (uint32_t)a.V) break;
+      if (i0 == first) begun = (uint32_t)__builtin_amdgcn_readlane(k, N + 1) == k0;
+      Raw8<T> x[N];   // (rows that are not summed up are loaded, too: no branch stands between the loads)
+      Raw8<float> old[ADD ? N : 1];
 #pragma unroll
-      for (int q = 0; q < SUM_ROWS; ++q) {
-        const uint32_t kq = __builtin_amdgcn_readlane(k, q), rq = __builtin_amdgcn_readlane(r, q);
-        if (i0 + q < end && kq < (uint32_t)a.V && col < a.H) load8((const T*)a.dy + (long)rq * a.lddy + col, a.H - col, x[q]);
+      for (int q = 0; q < N; ++q) {
+        cols.load((const T*)a.dy + (long)__builtin_amdgcn_readlane(r, q) * a.lddy, a.H, x[q]);
+        if (ADD) cols.load((const float*)a.dtable + (long)min((uint32_t)__builtin_amdgcn_readlane(k, q), (uint32_t)a.V - 1) * a.lddt, a.H, old[q]);
       }
 #pragma unroll
-      for (int q = 0; q < SUM_ROWS; ++q) {
-        const uint32_t kq = __builtin_amdgcn_readlane(k, q);
-        if (i0 + q >= end || kq >= (uint32_t)a.V) break;
+      for (int q = 0; q < N; ++q) {
+        const uint32_t kq = __builtin_amdgcn_readlane(k, q), next = __builtin_amdgcn_readlane(k, q + 1);
+        if (kq >= (uint32_t)a.V) break;   // (behind the last row, too)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) acc[e] += x[q][e];
-        const uint32_t next = i0 + q + 1 >= end ? behind : q + 1 < SUM_ROWS ? (uint32_t)__builtin_amdgcn_readlane(k, (q + 1) & (SUM_ROWS - 1)) : after;
-        if (next == kq && i0 + q + 1 < end) continue;
-        if (begun) part(0);
-        else if (next == kq) part(1);
-        else if (col < a.H) store_sum<T>(a, kq, col, acc);
+        for (int e = 0; e < 8; ++e) acc[e] += x[q].get(e);
+        const bool on = next == kq;
+        if (on && i0 + q + 1 < end) continue;
+        if (begun || on) {
+          cols.store(p.parts + ((long)run * 2 + (begun ? 0 : 1)) * a.H, a.H, acc);
+          if (!begun && slab == 0) {   // (listed in any order: each is by itself)
+            const long far = first + (long)LONG * p.run;
+            const bool many = far < a.rows && keys[far] == kq;
+            if (lane == 0) p.join_list[many ? p.runs - 1 - atomicAdd(p.joins + 1, 1) : atomicAdd(p.joins, 1)] = run;
+          }
+        } else {
+          store_sum<T, ADD>(a, kq, cols, acc, old[ADD ? q : 0]);
+        }
         begun = false;
 #pragma unroll
         for (int e = 0; e < 8; ++e) acc[e] = 0.f;
@@ -203,52 +268,66 @@ __global__ __launch_bounds__(64) void embed_sum(EmbeddingArgs a, EmbedPlan p, co
   }
 }
 
-// The parts of the id that begins in a run and goes on behind it, in ascending order: four waves, an equal share of the runs each
-template <typename T>
+// The parts of the ids that begin in a listed run and go on behind it, in ascending order.  A wave each; ids of many runs, which stand at the
+// list's end, a workgroup each, an equal share of the runs to each of its waves
+template <typename T, bool ADD, bool WHOLE>
 __global__ __launch_bounds__(256) void embed_join(EmbeddingArgs a, EmbedPlan p, const uint32_t* keys) {
   __shared__ float red[4][64][8];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  for (long u = blockIdx.x; u < (long)p.runs * p.slabs; u += gridDim.x) {
-    const int run = (int)(u / p.slabs), col = ((int)(u % p.slabs) * 64 + lane) * 8;
-    const long first = (long)run * p.run, end = first + p.run;
-    if (end >= a.rows) continue;
-    const uint32_t k = keys[end - 1];
-    if (k >= (uint32_t)a.V || keys[end] != k) continue;
-    if (keys[first] == k && first && keys[first - 1] == k) continue;   // it began in an earlier run
-    int n = 1;   // runs behind this one that hold rows of it: those that begin with one
-    for (;; n += 64) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int few = p.joins[0], many = p.joins[1];
+  // runs behind `run` that hold rows of its last id: those that begin with one
+  auto runs_of = [&](int run, uint32_t k) {
+    for (int n = 1;; n += 64) {
       const long at = (long)(run + n + lane) * p.run;
       const unsigned long long m = __ballot(at < a.rows && keys[at < a.rows ? at : 0] == k);
-      if (~m) {
-        n += __builtin_ctzll(~m);
-        break;
-      }
+      if (~m) return n + (int)__builtin_ctzll(~m);
     }
-    // parts 0 .. n - 1: the run's own, then the n - 1 behind it
-    const int per = (n + 3) / 4, q1 = min(n, (wave + 1) * per);
-    float t[8];
+  };
+  auto add = [&](int run, int q0, int q1, const Cols<WHOLE>& cols, float (&t)[8]) {
+    for (int q = q0; q < q1; q += 8) {
+      Raw8<float> x[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) t[e] = 0.f;
-    if (col < a.H) {
-#pragma unroll 8
-      for (int q = wave * per; q < q1; ++q) {
-        float x[8];
-        load8(p.parts + ((long)(run + q) * 2 + (q == 0)) * a.H + col, a.H - col, x);
+      for (int i = 0; i < 8; ++i) cols.load((const float*)p.parts + ((long)(run + min(q + i, q1 - 1)) * 2 + (q + i == 0)) * a.H, a.H, x[i]);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) t[e] += x[e];
-      }
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) t[e] += q + i < q1 ? x[i].get(e) : 0.f;
     }
+  };
+  auto old_of = [&](uint32_t k, const Cols<WHOLE>& cols) {
+    Raw8<float> old;
+    if (ADD) cols.load((const float*)a.dtable + (long)k * a.lddt, a.H, old);
+    return old;
+  };
+  for (long u = (long)blockIdx.x; u < (long)many * p.slabs; u += gridDim.x) {
+    const int run = p.join_list[p.runs - 1 - u / p.slabs];
+    const Cols<WHOLE> cols((int)(u % p.slabs), lane);
+    const uint32_t k = keys[(long)run * p.run + p.run - 1];
+    const Raw8<float> old = old_of(k, cols);
+    const int n = runs_of(run, k), per = (n + 3) / 4;
+    float t[8] = {};
+    add(run, wave * per, min(n, (wave + 1) * per), cols, t);
     __syncthreads();
 #pragma unroll
     for (int e = 0; e < 8; ++e) red[wave][lane][e] = t[e];
     __syncthreads();
-    if (wave == 0 && col < a.H) {
+    if (wave == 0) {
 #pragma unroll
       for (int w = 1; w < 4; ++w)
 #pragma unroll
         for (int e = 0; e < 8; ++e) t[e] += red[w][lane][e];
-      store_sum<T>(a, k, col, t);
+      store_sum<T, ADD>(a, k, cols, t, old);
     }
+  }
+  for (long u = (long)blockIdx.x * 4 + wave; u < (long)few * p.slabs; u += (long)gridDim.x * 4) {
+    const int run = p.join_list[u / p.slabs];
+    const Cols<WHOLE> cols((int)(u % p.slabs), lane);
+    const uint32_t k = keys[(long)run * p.run + p.run - 1];
+    const Raw8<float> old = old_of(k, cols);
+    const int n = runs_of(run, k);
+    float t[8] = {};
+    add(run, 0, n, cols, t);
+    store_sum<T, ADD>(a, k, cols, t, old);
   }
 }
 
@@ -257,7 +336,7 @@ static EmbedPlan plan_of(const EmbeddingArgs& a, void* ws) {
   EmbedPlan p{};
   int bits = 1;
   while (bits < 31 && a.V >> bits) ++bits;   // keys are 0 .. V
-  p.passes = (bits + 8) / 9;
+  p.passes = (bits + 9) / 10;
   p.bits = (bits + p.passes - 1) / p.passes;
   // at most 64 workgroups: each adds up the counts of all
   p.per = std::max(1, (int)((a.rows + 64L * SORT_T - 1) / (64L * SORT_T))) * SORT_T;
@@ -274,6 +353,8 @@ static EmbedPlan plan_of(const EmbeddingArgs& a, void* ws) {
   };
   for (int i = 0; i < 4; ++i) p.list[i] = (uint32_t*)take(4L * a.rows);
   p.counts = (uint32_t*)take(4L * p.wgs * DIGITS);
+  p.joins = (int32_t*)take(8);
+  p.join_list = (int32_t*)take(4L * p.runs);
   p.parts = (float*)take(8L * p.runs * a.H);
   p.bytes = at - (char*)ws;
   return p;
@@ -290,24 +371,36 @@ hipError_t launch_embedding_fwd(Dtype dt, const EmbeddingArgs& a, hipStream_t st
 
 template <typename T>
 static hipError_t bwd(const EmbeddingArgs& a, const EmbedPlan& p, hipStream_t st) {
+  // (16 KiB of dtable to a workgroup's turn; two to a unit keep the memory busy)
+  const unsigned clear = a.accumulate ? 0 : (unsigned)std::min<long>(512, ((long)a.V * a.H * (long)sizeof(T) + 16383) / 16384);
+  // XXX both sides measured
+  const bool few = a.rows <= 16384;
   const uint32_t *keys = nullptr, *rows = nullptr;
   for (int i = 0; i < p.passes; ++i) {
+    const int shift = i * p.bits;
     uint32_t *const ko = p.list[i & 1], *const ro = p.list[2 + (i & 1)];
-    if (i == 0) {
-      // (16 KiB of dtable to a workgroup's turn; two to a unit keep the memory busy)
-      const long clear = a.accumulate ? 0 : std::min<long>(512, ((long)a.V * a.H * (long)sizeof(T) + 16383) / 16384);
-      hipLaunchKernelGGL((embed_count<T, true>), dim3(p.wgs + (unsigned)clear), dim3(SORT_T), 0, st, a, p, keys, 0);
-      hipLaunchKernelGGL(embed_place<true>, dim3(p.wgs), dim3(SORT_T), 0, st, a, p, keys, rows, ko, ro, 0);
+    auto place = [&](auto kern, unsigned more) { hipLaunchKernelGGL(kern, dim3(p.wgs + more), dim3(SORT_T), 0, st, a, p, keys, rows, ko, ro, shift); };
+    auto count = [&](auto kern, unsigned more) { hipLaunchKernelGGL(kern, dim3(p.wgs + more), dim3(SORT_T), 0, st, a, p, keys, shift); };
+    if (few) {
+      if (i == 0) place(embed_place<T, true, false>, clear);
+      else place(embed_place<T, false, false>, 0);
+    } else if (i == 0) {
+      count(embed_count<T, true>, clear);
+      place(embed_place<T, true, true>, 0);
     } else {
-      hipLaunchKernelGGL((embed_count<T, false>), dim3(p.wgs), dim3(SORT_T), 0, st, a, p, keys, i * p.bits);
-      hipLaunchKernelGGL(embed_place<false>, dim3(p.wgs), dim3(SORT_T), 0, st, a, p, keys, rows, ko, ro, i * p.bits);
+      count(embed_count<T, false>, 0);
+      place(embed_place<T, false, true>, 0);
     }
     keys = ko;
     rows = ro;
   }
-  const unsigned units = (unsigned)std::min<long>((long)p.runs * p.slabs, 1 << 20);
-  hipLaunchKernelGGL(embed_sum<T>, dim3(units), dim3(64), 0, st, a, p, keys, rows);
-  hipLaunchKernelGGL(embed_join<T>, dim3(units), dim3(256), 0, st, a, p, keys);
+  const unsigned units = (unsigned)std::min<long>(((long)p.runs * p.slabs + 3) / 4, 1 << 20);   // four to a workgroup
+  auto sums = [&](auto ADD, auto WHOLE) {
+    hipLaunchKernelGGL((embed_sum<T, decltype(ADD)::value, decltype(WHOLE)::value>), dim3(units), dim3(256), 0, st, a, p, keys, rows);
+    hipLaunchKernelGGL((embed_join<T, decltype(ADD)::value, decltype(WHOLE)::value>), dim3(std::min(units, 2048u)), dim3(256), 0, st, a, p, keys);
+  };
+  auto whole = [&](auto ADD) { a.H % 8 ? sums(ADD, std::false_type{}) : sums(ADD, std::true_type{}); };
+  a.accumulate ? whole(std::true_type{}) : whole(std::false_type{});
   return hipGetLastError();
 }
 hipError_t launch_embedding_bwd(Dtype dt, const EmbeddingArgs& a, void* ws, hipStream_t st) {

@@ -363,6 +363,7 @@ struct EmbeddingArgs {
 // the gradient's sort and sums: `wgs` workgroups of `per` rows each, `passes` digits of `bits` bits; runs of `run` sorted rows
 struct EmbedPlan {
   uint32_t *list[4], *counts;
+  int32_t *joins, *join_list;   // runs in which an id begins that goes on behind them: joins[0] of them from the front, joins[1] from the end
   float* parts;
   int passes, bits, per, wgs, run, runs, slabs;
   long bytes;

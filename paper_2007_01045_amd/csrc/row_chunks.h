@@ -6,32 +6,48 @@
 
 namespace dapple {
 
+// A chunk as it is loaded: converted where it is used, so that a row of loads waits for none of them.
 // n: columns from p to the row's end, at least 1; what lies behind them reads as zero
-__device__ __forceinline__ void load8(const float* p, int n, float (&o)[8]) {
-  if (n >= 8) {
-    f32x4 a, b;
-    __builtin_memcpy(&a, p, 16);
-    __builtin_memcpy(&b, p + 4, 16);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      o[e] = a[e];
-      o[4 + e] = b[e];
-    }
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) o[e] = e < n ? p[e] : 0.f;
-  }
-}
-__device__ __forceinline__ void load8(const bf16* p, int n, float (&o)[8]) {
+template <typename T> struct Raw8;
+template <> struct Raw8<bf16> {
   bf16x8 a;
-  if (n >= 8) {
-    __builtin_memcpy(&a, p, 16);
-  } else {
+  __device__ __forceinline__ void load(const bf16* p, int n) {
+    if (n >= 8) {
+      __builtin_memcpy(&a, p, 16);
+    } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) a[e] = e < n ? p[e] : (bf16)0.f;
+      for (int e = 0; e < 8; ++e) a[e] = e < n ? p[e] : (bf16)0.f;
+    }
   }
+  __device__ __forceinline__ float get(int e) const { return (float)a[e]; }
+  __device__ __forceinline__ void set(int e, bf16 v) { a[e] = v; }
+};
+template <> struct Raw8<float> {
+  f32x4 a, b;
+  __device__ __forceinline__ void load(const float* p, int n) {
+    if (n >= 8) {
+      __builtin_memcpy(&a, p, 16);
+      __builtin_memcpy(&b, p + 4, 16);
+    } else {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) o[e] = (float)a[e];
+      for (int e = 0; e < 4; ++e) {
+        a[e] = e < n ? p[e] : 0.f;
+        b[e] = 4 + e < n ? p[4 + e] : 0.f;
+      }
+    }
+  }
+  __device__ __forceinline__ float get(int e) const { return e < 4 ? a[e & 3] : b[e & 3]; }
+  __device__ __forceinline__ void set(int e, float v) {
+    if (e < 4) a[e & 3] = v;
+    else b[e & 3] = v;
+  }
+};
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, int n, float (&o)[8]) {
+  Raw8<T> r;
+  r.load(p, n);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) o[e] = r.get(e);
 }
 __device__ __forceinline__ void store8(float* p, int n, const float (&o)[8]) {
   if (n >= 8) {

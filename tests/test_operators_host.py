@@ -253,7 +253,7 @@ def test_embedding_refusals():
     refused(conf, B.dapple_embedding_fwd, -1, B.embedding_desc(**ok))
     size = lambda rows, V, H: B.dapple_embedding_workspace(B.DTYPE_BF16, B.embedding_desc(rows=rows, V=V, H=H))  # noqa: E731
     for rows, V, H in ((1, 1, 1), (65536, 30522, 1024), (1 << 28, 1 << 28, 1 << 16)):
-        assert 16 * rows <= size(rows, V, H) <= 16 * rows + (1 << 16) * H + (1 << 18)
+        assert 16 * rows <= size(rows, V, H) <= 16 * rows + (1 << 16) * H + (1 << 19)
     refused(conf, size, 0, 1, 1)
 
 
