@@ -61,8 +61,8 @@ __device__ __forceinline__ void clear_table(const EmbeddingArgs& a, int wg, int 
   }
 }
 
-// The digits of rows first .. end - 1 counted into hist: once a wave and digit (frequent tokens, and the upper digits of most, are the
-// same in many lanes)
+// The digits of rows first .. end - 1: add(digit, how often, row).  Once a wave and digit, for the upper digits of frequent tokens are the same in
+// most lanes; the lowest ones seldom
 template <bool FIRST, typename F>
 __device__ __forceinline__ void count_digits(const EmbeddingArgs& a, const EmbedPlan& p, const uint32_t* keys, int shift, int first, int end, F&& add) {
   const int lane = threadIdx.x & 63;
@@ -78,8 +78,12 @@ __device__ __forceinline__ void count_digits(const EmbeddingArgs& a, const Embed
       if (i0 + u * SORT_T >= end) break;
       const bool in = i0 + u * SORT_T + (int)threadIdx.x < end;
       const uint32_t d = (k[u] >> shift) & ((1u << p.bits) - 1);
-      const unsigned long long same = same_digit(d, in, p.bits);
-      if (in && (same & ((1ull << lane) - 1)) == 0) add(d, (uint32_t)__builtin_popcountll(same), i0 + u * SORT_T);
+      if constexpr (FIRST) {
+        if (in) add(d, 1u, i0 + u * SORT_T);
+      } else {
+        const unsigned long long same = same_digit(d, in, p.bits);
+        if (in && (same & ((1ull << lane) - 1)) == 0) add(d, (uint32_t)__builtin_popcountll(same), i0 + u * SORT_T);
+      }
     }
   }
 }
@@ -184,13 +188,16 @@ template <bool WHOLE>
 struct Cols {
   int col;
   __device__ __forceinline__ Cols(int slab, int lane) : col(slab * 512 + (WHOLE ? 8 * lane : lane)) {}
-  template <typename T>
+  template <bool FAR = false, typename T>
   __device__ __forceinline__ void load(const T* row, int H, Raw8<T>& x) const {
     if constexpr (WHOLE) {
-      x.load(row + min(col, H - 8), 8);
+      x.template load<FAR>(row + min(col, H - 8), 8);
     } else {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x.set(e, row[min(col + 64 * e, H - 1)]);
+      for (int e = 0; e < 8; ++e) {
+        const T* const p = row + min(col + 64 * e, H - 1);
+        x.set(e, FAR ? __builtin_nontemporal_load(p) : *p);
+      }
     }
   }
   template <typename T>
@@ -216,7 +223,7 @@ __device__ __forceinline__ void store_sum(const EmbeddingArgs& a, uint32_t id, c
 
 // A wave: sorted rows [run p.run, ...) and 512 columns from 512 slab on.  parts[run][0]: of an id that began before the run, [1]: of one
 // that begins in it and goes on behind it.  ADD (accumulate): the rows of dtable come in with those of dy, eight at once, for registers
-template <typename T, bool ADD, bool WHOLE>
+template <typename T, bool ADD, bool WHOLE, bool FAR>
 __global__ __launch_bounds__(256) void embed_sum(EmbeddingArgs a, EmbedPlan p, const uint32_t* keys, const uint32_t* rows) {
   constexpr int N = ADD ? SUM_ROWS / 2 : SUM_ROWS;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -232,6 +239,7 @@ __global__ __launch_bounds__(256) void embed_sum(EmbeddingArgs a, EmbedPlan p, c
       // lanes 0 .. N: the keys from i0 on; lane N + 1: the one before
       const int i = lane <= N ? i0 + lane : i0 - 1, at = min(max(i, 0), a.rows - 1);
       const uint32_t found = keys[at], r = rows[at], k = i == at ? found : 0xffffffffu;
+      __builtin_amdgcn_sched_barrier(0);   // (both loads before either is waited for)
       const uint32_t k0 = __builtin_amdgcn_readlane(k, 0);
       if (k0 >= (uint32_t)a.V) break;
       if (i0 == first) begun = (uint32_t)__builtin_amdgcn_readlane(k, N + 1) == k0;
@@ -239,7 +247,7 @@ __global__ __launch_bounds__(256) void embed_sum(EmbeddingArgs a, EmbedPlan p, c
       Raw8<float> old[ADD ? N : 1];
 #pragma unroll
       for (int q = 0; q < N; ++q) {
-        cols.load((const T*)a.dy + (long)__builtin_amdgcn_readlane(r, q) * a.lddy, a.H, x[q]);
+        cols.template load<FAR>((const T*)a.dy + (long)__builtin_amdgcn_readlane(r, q) * a.lddy, a.H, x[q]);
         if (ADD) cols.load((const float*)a.dtable + (long)min((uint32_t)__builtin_amdgcn_readlane(k, q), (uint32_t)a.V - 1) * a.lddt, a.H, old[q]);
       }
 #pragma unroll
@@ -373,8 +381,7 @@ template <typename T>
 static hipError_t bwd(const EmbeddingArgs& a, const EmbedPlan& p, hipStream_t st) {
   // (16 KiB of dtable to a workgroup's turn; two to a unit keep the memory busy)
   const unsigned clear = a.accumulate ? 0 : (unsigned)std::min<long>(512, ((long)a.V * a.H * (long)sizeof(T) + 16383) / 16384);
-  // XXX both sides measured
-  const bool few = a.rows <= 16384;
+  const bool few = a.rows <= 16384;   // XXX
   const uint32_t *keys = nullptr, *rows = nullptr;
   for (int i = 0; i < p.passes; ++i) {
     const int shift = i * p.bits;
@@ -395,12 +402,17 @@ static hipError_t bwd(const EmbeddingArgs& a, const EmbedPlan& p, hipStream_t st
     rows = ro;
   }
   const unsigned units = (unsigned)std::min<long>(((long)p.runs * p.slabs + 3) / 4, 1 << 20);   // four to a workgroup
-  auto sums = [&](auto ADD, auto WHOLE) {
-    hipLaunchKernelGGL((embed_sum<T, decltype(ADD)::value, decltype(WHOLE)::value>), dim3(units), dim3(256), 0, st, a, p, keys, rows);
+  using std::false_type;
+  using std::true_type;
+  auto sums = [&](auto ADD, auto WHOLE, auto FAR) {
+    hipLaunchKernelGGL((embed_sum<T, decltype(ADD)::value, decltype(WHOLE)::value, decltype(FAR)::value>), dim3(units), dim3(256), 0, st, a, p, keys, rows);
     hipLaunchKernelGGL((embed_join<T, decltype(ADD)::value, decltype(WHOLE)::value>), dim3(std::min(units, 2048u)), dim3(256), 0, st, a, p, keys);
   };
-  auto whole = [&](auto ADD) { a.H % 8 ? sums(ADD, std::false_type{}) : sums(ADD, std::true_type{}); };
-  a.accumulate ? whole(std::true_type{}) : whole(std::false_type{});
+  // (dy past the cache, us: 268 MB 130 / 76 without / with; 17 MB, which are still in it, 12.4 / 14.9)
+  const bool far = (long)a.rows * a.H * (long)sizeof(T) >= 128L << 20;
+  auto pick = [&](auto ADD, auto WHOLE) { far ? sums(ADD, WHOLE, true_type{}) : sums(ADD, WHOLE, false_type{}); };
+  auto whole = [&](auto ADD) { a.H % 8 ? pick(ADD, false_type{}) : pick(ADD, true_type{}); };
+  a.accumulate ? whole(true_type{}) : whole(false_type{});
   return hipGetLastError();
 }
 hipError_t launch_embedding_bwd(Dtype dt, const EmbeddingArgs& a, void* ws, hipStream_t st) {
