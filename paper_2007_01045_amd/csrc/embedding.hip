@@ -13,8 +13,11 @@
 
 namespace dapple {
 
+// what is of this size and more is not kept in the memory-side cache (256 MB), to which a part of it would be no use
+constexpr long FAR_BYTES = 128L << 20;
+
 // ------------------------------------------------------------------ forward
-template <typename T>
+template <typename T, bool FAR>
 __global__ __launch_bounds__(256) void embed_fwd(EmbeddingArgs a, int chunks) {
   const long all = (long)a.rows * chunks, stride = (long)gridDim.x * 256;
   for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < all; i += stride) {
@@ -29,7 +32,7 @@ __global__ __launch_bounds__(256) void embed_fwd(EmbeddingArgs a, int chunks) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = 0.f;
     }
-    store8((T*)a.y + row * a.ldy + col, a.H - col, v);
+    store8<FAR>((T*)a.y + row * a.ldy + col, a.H - col, v);
   }
 }
 
@@ -55,9 +58,12 @@ __device__ __forceinline__ void clear_table(const EmbeddingArgs& a, int wg, int 
   const bool dense = a.lddt == a.H;   // one row
   const long cols = dense ? (long)a.V * a.H : a.H, chunks = (cols + 7) / 8, all = dense ? chunks : a.V * chunks;
   const float zero[8] = {};
+  const bool far = (long)a.V * a.H * (long)sizeof(T) >= FAR_BYTES;
   for (long i = (long)wg * SORT_T + threadIdx.x; i < all; i += (long)wgs * SORT_T) {
     const long row = dense ? 0 : i / chunks, col = (i - row * chunks) * 8;
-    store8((T*)a.dtable + row * a.lddt + col, (int)min(8L, cols - col), zero);
+    T* const to = (T*)a.dtable + row * a.lddt + col;
+    if (far) store8<true>(to, (int)min(8L, cols - col), zero);
+    else store8(to, (int)min(8L, cols - col), zero);
   }
 }
 
@@ -369,13 +375,15 @@ static EmbedPlan plan_of(const EmbeddingArgs& a, void* ws) {
 }
 int64_t embedding_workspace(const EmbeddingArgs& a) { return plan_of(a, nullptr).bytes; }
 
-hipError_t launch_embedding_fwd(Dtype dt, const EmbeddingArgs& a, hipStream_t st) {
+template <typename T>
+static hipError_t fwd(const EmbeddingArgs& a, hipStream_t st) {
   const int chunks = (a.H + 7) / 8;
-  const unsigned grid = (unsigned)std::min<long>(((long)a.rows * chunks + 255) / 256, 1 << 20);
-  if (dt == DT_BF16) hipLaunchKernelGGL(embed_fwd<bf16>, dim3(grid), dim3(256), 0, st, a, chunks);
-  else hipLaunchKernelGGL(embed_fwd<float>, dim3(grid), dim3(256), 0, st, a, chunks);
+  const dim3 grid((unsigned)std::min<long>(((long)a.rows * chunks + 255) / 256, 1 << 20));
+  if ((long)a.rows * a.H * (long)sizeof(T) >= FAR_BYTES) hipLaunchKernelGGL((embed_fwd<T, true>), grid, dim3(256), 0, st, a, chunks);
+  else hipLaunchKernelGGL((embed_fwd<T, false>), grid, dim3(256), 0, st, a, chunks);
   return hipGetLastError();
 }
+hipError_t launch_embedding_fwd(Dtype dt, const EmbeddingArgs& a, hipStream_t st) { return dt == DT_BF16 ? fwd<bf16>(a, st) : fwd<float>(a, st); }
 
 template <typename T>
 static hipError_t bwd(const EmbeddingArgs& a, const EmbedPlan& p, hipStream_t st) {
@@ -409,7 +417,7 @@ static hipError_t bwd(const EmbeddingArgs& a, const EmbedPlan& p, hipStream_t st
     hipLaunchKernelGGL((embed_join<T, decltype(ADD)::value, decltype(WHOLE)::value>), dim3(std::min(units, 2048u)), dim3(256), 0, st, a, p, keys);
   };
   // (dy past the cache, us: 268 MB 130 / 76 without / with; 17 MB, which are still in it, 12.4 / 14.9)
-  const bool far = (long)a.rows * a.H * (long)sizeof(T) >= 128L << 20;
+  const bool far = (long)a.rows * a.H * (long)sizeof(T) >= FAR_BYTES;
   auto pick = [&](auto ADD, auto WHOLE) { far ? sums(ADD, WHOLE, true_type{}) : sums(ADD, WHOLE, false_type{}); };
   auto whole = [&](auto ADD) { a.H % 8 ? pick(ADD, false_type{}) : pick(ADD, true_type{}); };
   a.accumulate ? whole(true_type{}) : whole(false_type{});

@@ -55,23 +55,31 @@ __device__ __forceinline__ void load8(const T* p, int n, float (&o)[8]) {
 #pragma unroll
   for (int e = 0; e < 8; ++e) o[e] = r.get(e);
 }
+template <bool FAR = false>
 __device__ __forceinline__ void store8(float* p, int n, const float (&o)[8]) {
   if (n >= 8) {
-    const f32x4 a{o[0], o[1], o[2], o[3]}, b{o[4], o[5], o[6], o[7]};
-    __builtin_memcpy(p, &a, 16);
-    __builtin_memcpy(p + 4, &b, 16);
+    const f32x4_any a{o[0], o[1], o[2], o[3]}, b{o[4], o[5], o[6], o[7]};
+    if (FAR) {
+      __builtin_nontemporal_store(a, (f32x4_any*)p);
+      __builtin_nontemporal_store(b, (f32x4_any*)(p + 4));
+    } else {
+      *(f32x4_any*)p = a;
+      *(f32x4_any*)(p + 4) = b;
+    }
   } else {
 #pragma unroll
     for (int e = 0; e < 7; ++e)
       if (e < n) p[e] = o[e];
   }
 }
+template <bool FAR = false>
 __device__ __forceinline__ void store8(bf16* p, int n, const float (&o)[8]) {
-  bf16x8 a;
+  bf16x8_any a;
 #pragma unroll
   for (int e = 0; e < 8; ++e) a[e] = (bf16)o[e];
   if (n >= 8) {
-    __builtin_memcpy(p, &a, 16);
+    if (FAR) __builtin_nontemporal_store(a, (bf16x8_any*)p);
+    else *(bf16x8_any*)p = a;
   } else {
 #pragma unroll
     for (int e = 0; e < 7; ++e)
