@@ -78,93 +78,89 @@ __device__ __forceinline__ int query_hi(const AttnWinArgs& a, int j, int len) {
 template <int M>
 __device__ __forceinline__ bool is_sink(const AttnWinArgs& a, int j) { return M == MASK_WINDOW && a.W && j < a.S; }
 
-// The logit, in log2 units, of a product `raw`: what it is scaled, capped and lowered with.
-// The cap, t = cap2 tanh(x), x = raw scale / cap, is bound by its instructions (an exponential or a reciprocal takes four times one of
-// the others).  Where |x| <= 0.6 for all that a wave looks at, tanh(x) = x (1 + c1 x^2 + c2 x^4 + c3 x^6), c fitted for the least relative error, 2.5e-6, which
-// is below 2^-13 of a probability for any logit up to 30.  Else tanh(x) = 1 - 2 r, r = 1 / (1 + e^2x), off by 2^-23 of 1, times cap2.
-// XXX measured
+// The logit, in log2 units, of a product `raw`: unit t - slope2 |distance|, where t is raw, or its cap:
+//   t = tanh(x), x = raw scale / cap, unit = cap log2(e);   d logit / d raw = (1 - t^2) scale log2(e).
+// The cap is bound by its instructions (an exponential or a reciprocal takes four times one of the others).  Where |x| <= 0.6 for all that
+// a wave looks at, tanh(x) = x (1 + c1 x^2 + c2 x^4 + c3 x^6), c fitted for the least relative error, 2.5e-6, which is below 2^-13 of a probability for any
+// logit up to 30; else each logit has that or, by its own size alone (what stands beside it must not show), tanh(x) = 1 - 2 r, r = 1 / (1 +
+// e^2x), off by 2^-23 of 1.  XXX measured
+constexpr bool capped(int S) { return S == SCORE_CAP || S == SCORE_BOTH; }
+constexpr bool sloped(int S) { return S == SCORE_SLOPE || S == SCORE_BOTH; }
+template <int S>
 struct Score {
-  float scale2, bend, cap2, slope2;   // cap2: cap log2(e), bend: 2 scale log2(e) / cap;  slope2: -slope log2(e)
-  float p0, p1, p2, small, down;
-  __device__ __forceinline__ Score(const AttnWinArgs& a, float scale2) : scale2(scale2), bend(a.bend), cap2(a.cap2), slope2(0.f),
-    p0(a.poly[0]), p1(a.poly[1]), p2(a.poly[2]), small(a.small), down(a.down) {}
-  template <int S>
+  float unit, slope2, bend, small, c1, c2, c3;   // slope2: -slope log2(e); bend: scale / cap; small: 0.6 / bend; c: with powers of bend
+  __device__ __forceinline__ Score(const AttnWinArgs& a, float scale2) : unit(capped(S) ? a.cap2 : scale2), slope2(0.f), bend(a.bend), small(a.small),
+    c1(a.poly[0]), c2(a.poly[1]), c3(a.poly[2]) {}
   __device__ __forceinline__ void head(const AttnWinArgs& a, int h) {
-    if (S == SCORE_SLOPE || S == SCORE_BOTH) slope2 = a.slopes ? a.slopes[h] * -LOG2E : 0.f;
+    if (sloped(S)) slope2 = a.slopes ? a.slopes[h] * -LOG2E : 0.f;
+  }
+  __device__ __forceinline__ float polynomial(float raw) const {
+    const float y = raw * raw;
+    return raw * fmaf(fmaf(fmaf(c3, y, c2), y, c1), y, bend);
   }
   // whether the wave's products are all small
-  template <int S, typename V>
+  template <typename V>
   __device__ __forceinline__ bool is_small(const V& raw) const {
-    if (S != SCORE_CAP && S != SCORE_BOTH) return true;
     float m = 0.f;
-    bool fit = true;
 #pragma unroll
     for (int v = 0; v < 16; v += 2) m = fmaxf(m, fmaxf(fabsf(raw[v]), fabsf(raw[v + 1])));
-    fit = m <= small;
-    return __builtin_amdgcn_ballot_w64(fit) == ~0ull;
+    return __builtin_amdgcn_ballot_w64(m <= small) == ~0ull;
   }
-  // what raw is multiplied with
-  template <int S>
-  __device__ __forceinline__ float factor(float raw) const {
-    if (S != SCORE_CAP && S != SCORE_BOTH) return scale2;
-    const float r = raw * raw;
-    return fmaf(fmaf(fmaf(p2, r, p1), r, p0), r, scale2);
+  template <typename V>
+  __device__ __forceinline__ void cap_all(V& raw) const {
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+      const float t = polynomial(raw[v]), r = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(raw[v] * bend * (2.f * LOG2E)));
+      raw[v] = fabsf(raw[v]) <= small ? t : fmaf(-2.f, r, 1.f);
+    }
   }
-  // far: the rows' distance, of either sign.  d: d logit / d raw over scale2
-  template <int S, bool SMALL>
-  __device__ __forceinline__ float at(float raw, float far, float& d) const {
-    float t;
-    d = 1.f;
-    if (S == SCORE_SLOPE) return fmaf(slope2, fabsf(far), raw * scale2);
-    const float f = factor<S>(raw);
-    t = raw * f;
-    d = fmaf(t * t, down, 1.f);
-    if (SMALL) return S == SCORE_BOTH ? fmaf(slope2, fabsf(far), raw * f) : t;
-    const float r = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(raw * bend));
-    const bool in = fabsf(raw) <= small;   // (each logit by its own size, whatever stands beside it)
-    d = in ? d : fmaf(-4.f * r, r, 4.f * r);
-    t = in ? t : fmaf(-2.f * cap2, r, cap2);
-    return S == SCORE_BOTH ? fmaf(slope2, fabsf(far), t) : t;
+  // raw = t
+  template <typename V>
+  __device__ __forceinline__ void cap(V& raw) const {
+    if constexpr (capped(S)) {
+      if (is_small(raw)) {
+#pragma unroll
+        for (int v = 0; v < 16; ++v) raw[v] = polynomial(raw[v]);
+      } else {
+        cap_all(raw);
+      }
+    }
   }
-  // The logits of a block of the other side's rows r0 + 8 (v >> 2) + (v & 3) (4 h is in r0) against the lane's row, less what is
+  // the logit less l; far: the rows' distance, of either sign
+  __device__ __forceinline__ float less(float t, float far, float l) const {
+    const float s = fmaf(t, unit, -l);
+    return sloped(S) ? fmaf(slope2, fabsf(far), s) : s;
+  }
+  __device__ __forceinline__ float derivative(float t) const { return capped(S) ? fmaf(-t, t, 1.f) : 1.f; }
+  // With slopes: the logits of a block of the other side's rows r0 + 8 (v >> 2) + (v & 3) (4 h is in r0) against the lane's row, less what is
   // returned, which is the same for all of them: on one side of the rows the bias is linear, and a constant for each v.  row0: the wave's
   // first row, b0: the block's (both the same for the wave)
-  template <int S, bool SMALL, typename V>
-  __device__ __forceinline__ float block(const V& raw, float (&t)[16], int row, int r0, int row0, int b0) const {
-    if constexpr (S == SCORE_SLOPE || S == SCORE_BOTH) {
-      auto plus = [&](float q, float c) {
-        const float s = fmaf(q, factor<S>(q), c);
-        if (SMALL || S == SCORE_SLOPE || fabsf(q) <= small) return s;
-        return c + fmaf(-2.f * cap2, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(q * bend)), cap2);
-      };
-      const float x = (float)(row - r0) * slope2;
-      if (b0 + 31 <= row0) {
+  template <typename V>
+  __device__ __forceinline__ float block(const V& t, float (&o)[16], int row, int r0, int row0, int b0) const {
+    if (b0 + 31 <= row0) {
 #pragma unroll
-        for (int v = 0; v < 16; ++v) t[v] = plus(raw[v], -(float)(8 * (v >> 2) + (v & 3)) * slope2);
-        return x;
-      }
-      if (b0 >= row0 + 31) {
+      for (int v = 0; v < 16; ++v) o[v] = fmaf(t[v], unit, -(float)(8 * (v >> 2) + (v & 3)) * slope2);
+      return (float)(row - r0) * slope2;
+    }
+    if (b0 >= row0 + 31) {
 #pragma unroll
-        for (int v = 0; v < 16; ++v) t[v] = plus(raw[v], (float)(8 * (v >> 2) + (v & 3)) * slope2);
-        return -x;
-      }
+      for (int v = 0; v < 16; ++v) o[v] = fmaf(t[v], unit, (float)(8 * (v >> 2) + (v & 3)) * slope2);
+      return (float)(r0 - row) * slope2;
     }
     const float x = (float)(row - r0);
-    float d;
 #pragma unroll
-    for (int v = 0; v < 16; ++v) t[v] = at<S, SMALL>(raw[v], x - (8 * (v >> 2) + (v & 3)), d);
+    for (int v = 0; v < 16; ++v) o[v] = less(t[v], x - (8 * (v >> 2) + (v & 3)), 0.f);
     return 0.f;
   }
-  // fp32: tanh of full precision, and no cap at all at run time
-  __device__ __forceinline__ float at32(float raw, float far, float& d) const {
-    float t = raw * scale2;
-    d = 1.f;
-    if (cap2 > 0.f) {
-      const float b = tanhf(raw * bend);
-      t = cap2 * b;
-      d = fmaf(-b, b, 1.f);
+  // fp32: tanh of full precision, and no cap at all at run time (bend 0).  t: for derivative()
+  __device__ __forceinline__ float less32(float raw, float scale2, float far, float l, float& t) const {
+    t = 0.f;
+    float s = raw * scale2;
+    if (bend > 0.f) {
+      t = tanhf(raw * bend);
+      s = unit * t;
     }
-    return fmaf(slope2, fabsf(far), t);
+    return fmaf(slope2, fabsf(far), s) - l;
   }
 };
 
@@ -208,13 +204,17 @@ __device__ __forceinline__ void hide(float (&x)[16], float hidden, int r0, int h
   }
 }
 
-// Workgroup id's head and its place among that head's, where the heads take turns: a head's workgroups (eight heads and more) or those of few
-// heads on one XCD each
-__device__ __forceinline__ void by_heads(unsigned id, int heads, int& head, int& rank) {
-  const unsigned per = (unsigned)heads / 8, turn = id >> 3;
-  const bool eight = heads % 8 == 0;
-  head = eight ? (id & 7) * per + turn % per : id % heads;
-  rank = eight ? turn / per : id / heads;
+// Workgroup id's head and its place among that head's.  Of g heads' greatest common divisor with the eight XCDs: 8 / g XCDs share heads / g heads,
+// which take turns.  A launch has heads_grid() workgroups, some of them with a place past the last.
+__host__ __device__ inline int heads_gcd(int heads) { return heads % 8 == 0 ? 8 : heads % 4 == 0 ? 4 : heads % 2 == 0 ? 2 : 1; }
+__host__ __device__ inline unsigned heads_grid(int heads, long places) {
+  const int g = heads_gcd(heads), xcds = 8 / g;
+  return (unsigned)((places * (heads / g) + xcds - 1) / xcds * 8);
+}
+__device__ __forceinline__ void by_heads(unsigned id, int heads, int& head, int& place) {
+  const unsigned g = heads_gcd(heads), each = (unsigned)heads / g, x = id & 7, turn = (id >> 3) * (8 / g) + x / g;
+  head = (x % g) * each + turn % each;
+  place = turn / each;
 }
 
 // The query tile of workgroup id of n.  MASK_WINDOW: the last tiles first (causal: they have the longest walks).
@@ -224,6 +224,7 @@ __device__ __forceinline__ void by_heads(unsigned id, int heads, int& head, int&
 template <int M>
 struct QueryTask {
   int tile, bi, hh;
+  bool run = true;
   __device__ __forceinline__ QueryTask(const AttnWinArgs& a, unsigned id, unsigned n, int q_tiles, int rows, int lane) {
     if constexpr (M == MASK_WINDOW) {
       id = spread(id, n);
@@ -235,7 +236,8 @@ struct QueryTask {
     by_heads(id, a.A, hh, rank);
     bi = 0;
     tile = q_tiles - 1 - rank;
-    if (n <= 256) return;
+    run = rank < q_tiles;
+    if (n <= 256 || !run) return;
     const int group = (q_tiles + 63) / 64, groups = (q_tiles + group - 1) / group, first = lane * group, last = min(first + group, q_tiles) - 1;
     int walk = -1;
     if (lane < groups) {
@@ -334,6 +336,7 @@ __global__ __launch_bounds__(64 * NW, D <= 64 ? 3 : 2) void attn_win_fwd(AttnWin
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int q_tiles = (a.s + 32 * NW - 1) / (32 * NW);
   const QueryTask<M> task(a, blockIdx.x, gridDim.x, q_tiles, 32 * NW, lane);
+  if (!task.run) return;
   const int tile = task.tile, bi = task.bi, hh = task.hh;
   const int kv = hh / (a.A / a.Ak);
   const int len = len_of<M>(a, bi), d = a.d;
@@ -361,8 +364,8 @@ __global__ __launch_bounds__(64 * NW, D <= 64 ? 3 : 2) void attn_win_fwd(AttnWin
   for (int t = 0; t < R::NS - 1; ++t) ask(t);
   __builtin_amdgcn_s_waitcnt(0x0F70);   // (once, with the ring's first blocks: below, the counts are the ring's alone)
 
-  Score sc(a, scale2);
-  sc.head<S>(a, hh);
+  Score<S> sc(a, scale2);
+  sc.head(a, hh);
   float m = -3e38f, l = 0.f;   // (finite: a row that has seen nothing yet keeps m - m = 0)
   f32x16 o[NDB];  // rows d = 32 dblk + 8 blk + 4 h + e, column = the lane's query
 #pragma unroll
@@ -377,7 +380,7 @@ __global__ __launch_bounds__(64 * NW, D <= 64 ? 3 : 2) void attn_win_fwd(AttnWin
     const int k0 = walk.block(t) * 64;
     if (row0 >= len) continue;
     if (!any_seen<M>(a, k0, k0 + 63, lo_min, hi_max)) continue;
-    float p[2][16], shift[2] = {0.f, 0.f};   // (logits less their shift)
+    float p[2][16], shift[2] = {0.f, 0.f};   // (with slopes: logits less their shift)
     float mx = -INFINITY;
     // (all LDS reads of a phase before its first MFMA: see attn_fwd_mfma)
     bf16x8 kf[2][NKK], vf[4][NDB];
@@ -399,17 +402,18 @@ __global__ __launch_bounds__(64 * NW, D <= 64 ? 3 : 2) void attn_win_fwd(AttnWin
       f32x16 sa = zero16();  // rows: key 32 kb2 + 8 blk + 4 h + e, column: query
 #pragma unroll
       for (int kk = 0; kk < NKK; ++kk) sa = MFMA(kf[kb2][kk], qf[kk], sa);
-#pragma unroll
-      for (int v = 0; v < 16; ++v) p[kb2][v] = sa[v];
-      if constexpr (S != SCORE_PLAIN) {
+      sc.cap(sa);
+      if constexpr (sloped(S)) {
         const int b0 = k0 + 32 * kb2;
-        if (sc.is_small<S>(sa)) shift[kb2] = sc.block<S, true>(sa, p[kb2], qrow, b0 + 4 * h, row0, b0);
-        else shift[kb2] = sc.block<S, false>(sa, p[kb2], qrow, b0 + 4 * h, row0, b0);
+        shift[kb2] = sc.block(sa, p[kb2], qrow, b0 + 4 * h, row0, b0);
+      } else {
+#pragma unroll
+        for (int v = 0; v < 16; ++v) p[kb2][v] = sa[v];
       }
     }
 #pragma unroll
     for (int kb2 = 0; kb2 < 2; ++kb2) hide<M == MASK_WINDOW>(p[kb2], -INFINITY, k0 + kb2 * 32, h, lo, hi, a.S, lo_max > k0 + kb2 * 32, hi_min < k0 + kb2 * 32 + 32);
-    if constexpr (S == SCORE_PLAIN) {
+    if constexpr (!sloped(S)) {
 #pragma unroll
       for (int kb2 = 0; kb2 < 2; ++kb2)
 #pragma unroll
@@ -432,7 +436,7 @@ __global__ __launch_bounds__(64 * NW, D <= 64 ? 3 : 2) void attn_win_fwd(AttnWin
     // (what the row's sums are relative to follows its maximum only when that is 2^8 above: seldom after a walk's first block.  The
     // probabilities keep their relative precision and the fp32 sums have room for it.  16 heads of 64, 4 x 1987 rows 42.2 -> 39.5 us,
     // 16 of 128, 8192 rows 114 -> 107)
-    const float top = S == SCORE_PLAIN ? halves_max(mx) * scale2 : halves_max(mx), mn = top > m + 8.f ? top : m;
+    const float top = sloped(S) ? halves_max(mx) : halves_max(mx) * sc.unit, mn = top > m + 8.f ? top : m;
     const float alpha = __builtin_amdgcn_exp2f(m - mn);
     float rs = 0.f;
 #pragma unroll
@@ -440,7 +444,7 @@ __global__ __launch_bounds__(64 * NW, D <= 64 ? 3 : 2) void attn_win_fwd(AttnWin
 #pragma unroll
       for (int v = 0; v < 16; ++v) {
         // (the bare v_exp_f32: a probability below 2^-126 may be zero, it is rounded to bf16)
-        p[kb2][v] = __builtin_amdgcn_exp2f(S == SCORE_PLAIN ? fmaf(p[kb2][v], scale2, -mn) : p[kb2][v] + (shift[kb2] - mn));
+        p[kb2][v] = __builtin_amdgcn_exp2f(sloped(S) ? p[kb2][v] + (shift[kb2] - mn) : fmaf(p[kb2][v], sc.unit, -mn));
         rs += p[kb2][v];
       }
     l = l * alpha + halves_sum(rs);
@@ -541,9 +545,9 @@ __device__ __forceinline__ void win_dkdv(const AttnWinArgs& a, unsigned task, un
   for (int t = 0; t < R::NS - 1; ++t) ask(t);
   __builtin_amdgcn_s_waitcnt(0x0F70);   // (as in attn_win_fwd)
 
-  Score sc(a, scale2);
+  Score<S> sc(a, scale2);
   int stage = 0, qblk = w.nq ? w.n0 % w.nq : 0, qhead = h0 + (w.nq ? w.n0 / w.nq : 0);
-  sc.head<S>(a, min(qhead, a.A - 1));
+  sc.head(a, min(qhead, a.A - 1));
   for (int n = w.n0; n < w.n1; ++n) {
     R::wait();
     ask(stage == 0 ? R::NS - 1 : stage - 1);
@@ -551,7 +555,7 @@ __device__ __forceinline__ void win_dkdv(const AttnWinArgs& a, unsigned task, un
     const float *Ls = (const float*)((const unsigned char*)Qs + R::S_OFF), *Ds = Ls + 64;
     stage = stage + 1 == R::NS ? 0 : stage + 1;
     const int i0 = (w.qlo + qblk) * 64;
-    if (S != SCORE_PLAIN && qblk == 0) sc.head<S>(a, min(qhead, a.A - 1));
+    if (sloped(S) && qblk == 0) sc.head(a, min(qhead, a.A - 1));
     qblk = qblk + 1 == w.nq ? 0 : qblk + 1;
     qhead += qblk == 0;
     if (row0 >= len) continue;
@@ -590,25 +594,13 @@ __device__ __forceinline__ void win_dkdv(const AttnWinArgs& a, unsigned task, un
         }
       __builtin_amdgcn_sched_barrier(0);
       float p[16], ds[16];
-      auto probabilities = [&](auto SMALL) __attribute__((always_inline)) {
+      sc.cap(sa);
 #pragma unroll
-        for (int blk = 0; blk < 4; ++blk)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int v = 4 * blk + e;
-            if constexpr (S == SCORE_PLAIN) {
-              p[v] = __builtin_amdgcn_exp2f(fmaf(sa[v], scale2, -L4[blk][e]));
-              ds[v] = dp[v] * p[v];
-            } else {
-              float d;
-              p[v] = __builtin_amdgcn_exp2f(sc.at<S, decltype(SMALL)::value>(sa[v], (float)(krow - j0 - 4 * h) - (8 * blk + e), d) - L4[blk][e]);
-              ds[v] = dp[v] * p[v];
-              if (S != SCORE_SLOPE) ds[v] *= d;
-            }
-          }
-      };
-      if (S == SCORE_PLAIN || sc.is_small<S>(sa)) probabilities(std::true_type{});
-      else probabilities(std::false_type{});
+      for (int v = 0; v < 16; ++v) {
+        p[v] = __builtin_amdgcn_exp2f(sc.less(sa[v], (float)(krow - j0 - 4 * h) - (8 * (v >> 2) + (v & 3)), L4[v >> 2][v & 3]));
+        ds[v] = dp[v] * p[v];
+        if (capped(S)) ds[v] *= sc.derivative(sa[v]);
+      }
       hide<false>(p, 0.f, j0, h, lo, hi, 0, lo_max > j0, hi_min < j0 + 32);
       hide<false>(ds, 0.f, j0, h, lo, hi, 0, lo_max > j0, hi_min < j0 + 32);
 #pragma unroll
@@ -640,6 +632,7 @@ __device__ __forceinline__ void win_dq(const AttnWinArgs& a, unsigned id, unsign
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int q_tiles = (a.s + 32 * NW - 1) / (32 * NW);
   const QueryTask<M> task(a, id, ids, q_tiles, 32 * NW, lane);
+  if (!task.run) return;
   const int tile = task.tile, bi = task.bi, hh = task.hh;
   const int kv = hh / (a.A / a.Ak);
   const int len = len_of<M>(a, bi), d = a.d;
@@ -660,8 +653,8 @@ __device__ __forceinline__ void win_dq(const AttnWinArgs& a, unsigned id, unsign
     qf[kk] = frag_global<true>(Q, qrow, qok, a.ldq, kk, lane, d);
     gf[kk] = frag_global<true>(G, qrow, qok, a.lddc, kk, lane, d);
   }
-  Score sc(a, scale2);
-  sc.head<S>(a, hh);
+  Score<S> sc(a, scale2);
+  sc.head(a, hh);
   constexpr bool ADDS = D <= 64;   // the product dctx v adds to -delta (D = 128: no registers for it)
   f32x16 dp0;
 #pragma unroll
@@ -719,24 +712,17 @@ __device__ __forceinline__ void win_dq(const AttnWinArgs& a, unsigned id, unsign
         for (int db = 0; db < NDB; ++db) kc[ks][db] = frag_cols<D>(Ks, db * 32, kb2 * 32 + ks * 16, lane);
       __builtin_amdgcn_sched_barrier(0);
       float ds[16];
-      if constexpr (S == SCORE_PLAIN) {
-#pragma unroll
-        for (int v = 0; v < 16; ++v) ds[v] = __builtin_amdgcn_exp2f(fmaf(sa[v], scale2, -Lq)) * (ADDS ? dp[v] : dp[v] + Dq);
-      } else if constexpr (S == SCORE_SLOPE) {
-        const float c = sc.block<S, true>(sa, ds, qrow, j0 + 4 * h, row0, j0) - Lq;
+      sc.cap(sa);
+      if constexpr (S == SCORE_SLOPE) {
+        const float c = sc.block(sa, ds, qrow, j0 + 4 * h, row0, j0) - Lq;
 #pragma unroll
         for (int v = 0; v < 16; ++v) ds[v] = __builtin_amdgcn_exp2f(ds[v] + c) * (ADDS ? dp[v] : dp[v] + Dq);
       } else {
-        auto gradients = [&](auto SMALL) __attribute__((always_inline)) {
 #pragma unroll
-          for (int v = 0; v < 16; ++v) {
-            float d;
-            ds[v] = __builtin_amdgcn_exp2f(sc.at<S, decltype(SMALL)::value>(sa[v], (float)(qrow - j0 - 4 * h) - (8 * (v >> 2) + (v & 3)), d) - Lq);
-            ds[v] *= (ADDS ? dp[v] : dp[v] + Dq) * d;
-          }
-        };
-        if (sc.is_small<S>(sa)) gradients(std::true_type{});
-        else gradients(std::false_type{});
+        for (int v = 0; v < 16; ++v) {
+          ds[v] = __builtin_amdgcn_exp2f(sc.less(sa[v], (float)(qrow - j0 - 4 * h) - (8 * (v >> 2) + (v & 3)), Lq)) * (ADDS ? dp[v] : dp[v] + Dq);
+          if (capped(S)) ds[v] *= sc.derivative(sa[v]);
+        }
       }
       hide<M == MASK_WINDOW>(ds, 0.f, j0, h, lo, hi, a.S, lo_max > j0, hi_min < j0 + 32);
 #pragma unroll
@@ -859,12 +845,13 @@ __device__ __forceinline__ void win_dkdv_pair(const AttnWinArgs& a, unsigned tas
   auto barrier = []() __attribute__((always_inline)) { R::wait<-3 * R::LOADS>(); };   // all but the two newest blocks have landed
   int stage = 0;
   if (first) {
-    Score sc(a, scale2);
+    Score<S> sc(a, scale2);
     int qblk = w.nq ? w.n0 % w.nq : 0, qhead = h0 + (w.nq ? w.n0 / w.nq : 0);
-    sc.head<S>(a, min(qhead, a.A - 1));
+    sc.head(a, min(qhead, a.A - 1));
     const bf16 *K = (const bf16*)a.k + r0 * a.ldk + w.kv * d, *V = (const bf16*)a.v + r0 * a.ldv + w.kv * d;
     const int lo = query_lo<M>(a, krow), hi = kok ? query_hi<M>(a, krow, len) : 0;
-    bf16x8 kf[NKK], vf[NKK], qf[4], gf[4];   // (qf, gf: four k-steps' fragments, read four ahead of their use)
+    constexpr int FD = capped(S) ? 2 : 4;
+    bf16x8 kf[NKK], vf[NKK], qf[FD], gf[FD];   // (qf, gf: FD k-steps' fragments, read so many ahead of their use)
 #pragma unroll
     for (int kk = 0; kk < NKK; ++kk) {
       kf[kk] = frag_global<true>(K, krow, kok, a.ldk, kk, lane, d);
@@ -877,14 +864,14 @@ __device__ __forceinline__ void win_dkdv_pair(const AttnWinArgs& a, unsigned tas
     const RowsAt fr(lane);
     // k-step kk of the fragments' block at `at` (kk < 8), or kk - 8 of the one at `next`
     auto fetch = [&](int kk, unsigned at, unsigned next) __attribute__((always_inline)) {
-      qf[kk & 3] = fr.get<0>(sm, kk < 8 ? at : next, kk & 7);
-      gf[kk & 3] = fr.get<R::Y_OFF>(sm, kk < 8 ? at : next, kk & 7);
+      qf[kk & (FD - 1)] = fr.get<0>(sm, kk < 8 ? at : next, kk & 7);
+      gf[kk & (FD - 1)] = fr.get<R::Y_OFF>(sm, kk < 8 ? at : next, kk & 7);
     };
     auto slot_after = [](int t) { return t == R::NS - 1 ? 0 : t + 1; };
     // sa, dp: S and dP of the current step (rows: query 8 blk + 4 h + e of its block, column: key); sn, dn: of the next one, made
     // meanwhile: two MFMAs and two elements' exponentials by turns
     enum { HIDDEN, WHOLE, PART };
-    auto step = [&](auto MODE, auto SMALL, const f32x16& sa, const f32x16& dp, f32x16& sn, f32x16& dn, unsigned cur, unsigned at, unsigned next, unsigned char* x,
+    auto step = [&](auto MODE, auto CAPPED, const f32x16& sa, const f32x16& dp, f32x16& sn, f32x16& dn, unsigned cur, unsigned at, unsigned next, unsigned char* x,
                     int j0) __attribute__((always_inline)) {
       constexpr int mode = decltype(MODE)::value;
       const float *Ls = (const float*)(sm + cur + R::S_OFF) + 4 * h, *Ds = Ls + 64;
@@ -901,21 +888,16 @@ __device__ __forceinline__ void win_dkdv_pair(const AttnWinArgs& a, unsigned tas
       float p[16], ds[16];
 #pragma unroll
       for (int kk = 0; kk < NKK; ++kk) {
-        sn = MFMA(qf[kk & 3], kf[kk], sn);
-        dn = MFMA(gf[kk & 3], vf[kk], dn);
-        fetch(kk + 4, at, next);
+        sn = MFMA(qf[kk & (FD - 1)], kf[kk], sn);
+        dn = MFMA(gf[kk & (FD - 1)], vf[kk], dn);
+        fetch(kk + FD, at, next);
         if constexpr (mode != HIDDEN) {
 #pragma unroll
           for (int v = 2 * kk; v < 2 * kk + 2; ++v) {
-            if constexpr (S == SCORE_PLAIN) {
-              p[v] = __builtin_amdgcn_exp2f(fmaf(sa[v], scale2, -L4[v >> 2][v & 3]));
-              ds[v] = (dp[v] + D4[v >> 2][v & 3]) * p[v];
-            } else {
-              float d;
-              p[v] = __builtin_amdgcn_exp2f(sc.at<S, decltype(SMALL)::value>(sa[v], (float)(krow - j0 - 4 * h) - (8 * (v >> 2) + (v & 3)), d) - L4[v >> 2][v & 3]);
-              ds[v] = (dp[v] + D4[v >> 2][v & 3]) * p[v];
-              if (S != SCORE_SLOPE) ds[v] *= d;
-            }
+            const float t = capped(S) && !decltype(CAPPED)::value ? sc.polynomial(sa[v]) : sa[v];
+            p[v] = __builtin_amdgcn_exp2f(sc.less(t, (float)(krow - j0 - 4 * h) - (8 * (v >> 2) + (v & 3)), L4[v >> 2][v & 3]));
+            ds[v] = (dp[v] + D4[v >> 2][v & 3]) * p[v];
+            if (capped(S)) ds[v] *= sc.derivative(t);
             if constexpr (mode == PART) {
               const bool in = 8 * (v >> 2) + (v & 3) >= l && 8 * (v >> 2) + (v & 3) < u;
               p[v] = in ? p[v] : 0.f;
@@ -942,31 +924,32 @@ __device__ __forceinline__ void win_dkdv_pair(const AttnWinArgs& a, unsigned tas
     int cur = 0, at = 1;   // places of the current step's block and the next one's
     {
 #pragma unroll
-      for (int kk = 0; kk < 4; ++kk) fetch(kk, 0, 0);
+      for (int kk = 0; kk < FD; ++kk) fetch(kk, 0, 0);
       s0 = d0 = zero16();
 #pragma unroll
       for (int kk = 0; kk < NKK; ++kk) {
-        s0 = MFMA(qf[kk & 3], kf[kk], s0);
-        d0 = MFMA(gf[kk & 3], vf[kk], d0);
-        fetch(kk + 4, 0, R::STAGE);
+        s0 = MFMA(qf[kk & (FD - 1)], kf[kk], s0);
+        d0 = MFMA(gf[kk & (FD - 1)], vf[kk], d0);
+        fetch(kk + FD, 0, R::STAGE);
       }
     }
     int n = w.n0;
-    auto one = [&](const f32x16& sa, const f32x16& dp, f32x16& sn, f32x16& dn) __attribute__((always_inline)) {
+    auto one = [&](f32x16& sa, const f32x16& dp, f32x16& sn, f32x16& dn) __attribute__((always_inline)) {
       const int after = slot_after(at), j0 = (w.qlo + qblk) * 32;
-      if (S != SCORE_PLAIN && qblk == 0) sc.head<S>(a, min(qhead, a.A - 1));
+      if (sloped(S) && qblk == 0) sc.head(a, min(qhead, a.A - 1));
       qblk = qblk + 1 == w.nq ? 0 : qblk + 1;
       qhead += qblk == 0;
       unsigned char* const x = X + (n & 1) * PAIR_X;
       barrier();
       ask();
       const unsigned c = cur * R::STAGE, f = at * R::STAGE, g = after * R::STAGE;
-      if (j0 >= hi_max || j0 + 31 < lo_min) step(Hidden{}, std::true_type{}, sa, dp, sn, dn, c, f, g, x, j0);   // none of the wave's keys is seen
-      else if (S == SCORE_PLAIN || S == SCORE_SLOPE || sc.is_small<S>(sa)) {
-        if (lo_max > j0 || hi_min < j0 + 32) step(Part{}, std::true_type{}, sa, dp, sn, dn, c, f, g, x, j0);
-        else step(Whole{}, std::true_type{}, sa, dp, sn, dn, c, f, g, x, j0);
+      if (j0 >= hi_max || j0 + 31 < lo_min) step(Hidden{}, std::false_type{}, sa, dp, sn, dn, c, f, g, x, j0);   // none of the wave's keys is seen
+      else if (!capped(S) || sc.is_small(sa)) {
+        if (lo_max > j0 || hi_min < j0 + 32) step(Part{}, std::false_type{}, sa, dp, sn, dn, c, f, g, x, j0);
+        else step(Whole{}, std::false_type{}, sa, dp, sn, dn, c, f, g, x, j0);
       } else {
-        step(Part{}, std::integral_constant<bool, S == SCORE_PLAIN || S == SCORE_SLOPE>{}, sa, dp, sn, dn, c, f, g, x, j0);
+        sc.cap_all(sa);
+        step(Part{}, std::integral_constant<bool, capped(S)>{}, sa, dp, sn, dn, c, f, g, x, j0);
       }
       cur = at;
       at = after;
@@ -1075,6 +1058,7 @@ __global__ __launch_bounds__(64 * RG * NG) void attn_win_fwd_f32(AttnWinArgs a, 
   float *const Ks = fsm + group * 2 * F32Lds<D, RG, NG>::BLK, *const Vs = Ks + F32Lds<D, RG, NG>::BLK;
   const int q_tiles = (a.s + 16 * RG - 1) / (16 * RG);
   const QueryTask<M> task(a, blockIdx.x, gridDim.x, q_tiles, 16 * RG, lane);
+  if (!task.run) return;
   const int tile = task.tile, bi = task.bi, hh = task.hh;
   const int kv = hh / (a.A / a.Ak), len = len_of<M>(a, bi), d = a.d;
   const long r0 = (long)bi * a.s;
@@ -1094,8 +1078,8 @@ __global__ __launch_bounds__(64 * RG * NG) void attn_win_fwd_f32(AttnWinArgs a, 
   };
   __builtin_amdgcn_s_waitcnt(0x0F70);   // (the wave's own rows: waited for in the loop, the next block would be too)
   if (group < walk.n) load(group);
-  Score sc(a, scale2);
-  sc.head<S>(a, hh);
+  Score<S> sc(a, scale2);
+  sc.head(a, hh);
   float m = -3e38f, l = 0.f;
   f32x4 o[NK];   // rows d = 16 i + 4 g4 + e, column = the lane's query
 #pragma unroll
@@ -1136,8 +1120,8 @@ __global__ __launch_bounds__(64 * RG * NG) void attn_win_fwd_f32(AttnWinArgs a, 
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        float d;
-        const float x = S == SCORE_PLAIN ? p[t][e] * scale2 : sc.at32(p[t][e], (float)(qrow - k0 - 16 * t - 4 * g4 - e), d);
+        float bent;
+        const float x = S == SCORE_PLAIN ? p[t][e] * scale2 : sc.less32(p[t][e], scale2, (float)(qrow - k0 - 16 * t - 4 * g4 - e), 0.f, bent);
         p[t][e] = sees<M>(a, k0 + 16 * t + 4 * g4 + e, lo, hi) ? x : -INFINITY;
         mx = fmaxf(mx, p[t][e]);
       }
@@ -1221,6 +1205,7 @@ __device__ __forceinline__ void win_dq_f32(const AttnWinArgs& a, unsigned id, un
   float *const Ks = fsm + group * 2 * F32Lds<D, RG, NG>::BLK, *const Vs = Ks + F32Lds<D, RG, NG>::BLK;
   const int q_tiles = (a.s + 16 * RG - 1) / (16 * RG);
   const QueryTask<M> task(a, id, ids, q_tiles, 16 * RG, lane);
+  if (!task.run) return;
   const int tile = task.tile, bi = task.bi, hh = task.hh;
   const int kv = hh / (a.A / a.Ak), len = len_of<M>(a, bi), d = a.d;
   const long r0 = (long)bi * a.s;
@@ -1235,8 +1220,8 @@ __device__ __forceinline__ void win_dq_f32(const AttnWinArgs& a, unsigned id, un
   own_row<D>((const float*)a.dctx + (r0 + qrow) * a.lddc + hh * d, qok, d, lane, gf);
   const long st = ((long)bi * a.A + hh) * a.s + qrow;
   const float Lq = qok ? a.lse[st] : 0.f, Dq = qok ? a.delta[st] : 0.f;
-  Score sc(a, scale2);
-  sc.head<S>(a, hh);
+  Score<S> sc(a, scale2);
+  sc.head(a, hh);
   f32x4 dq[NK];
 #pragma unroll
   for (int i = 0; i < NK; ++i) dq[i] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -1282,10 +1267,10 @@ __device__ __forceinline__ void win_dq_f32(const AttnWinArgs& a, unsigned id, un
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        float d = 1.f;
-        const float x = S == SCORE_PLAIN ? s[e] * scale2 : sc.at32(s[e], (float)(qrow - k0 - 16 * t - 4 * g4 - e), d);
-        ds[e] = __builtin_amdgcn_exp2f(x - Lq) * (dp[e] + Dq);
-        if (S != SCORE_PLAIN) ds[e] *= d;
+        float bent = 0.f;
+        const float x = S == SCORE_PLAIN ? s[e] * scale2 - Lq : sc.less32(s[e], scale2, (float)(qrow - k0 - 16 * t - 4 * g4 - e), Lq, bent);
+        ds[e] = __builtin_amdgcn_exp2f(x) * (dp[e] + Dq);
+        if (capped(S)) ds[e] *= sc.derivative(bent);
         if (!sees<M>(a, k0 + 16 * t + 4 * g4 + e, lo, hi)) ds[e] = 0.f;
       }
 #pragma unroll
@@ -1329,7 +1314,7 @@ __device__ __forceinline__ void win_dkdv_f32(const AttnWinArgs& a, unsigned task
   own_row<D>((const float*)a.v + (r0 + krow) * a.ldv + w.kv * d, kok, d, lane, vf);
 #pragma unroll
   for (int i = 0; i < NK; ++i) dk[i] = dv[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-  Score sc(a, scale2);
+  Score<S> sc(a, scale2);
   F32Block<D, 64 * RG> qb, gb;
   float L = 0.f, De = 0.f;
   auto load = [&](int n) {
@@ -1354,7 +1339,7 @@ __device__ __forceinline__ void win_dkdv_f32(const AttnWinArgs& a, unsigned task
     if (n + NG < w.n1) load(n + NG);
     if (row0 >= len || n >= w.n1) continue;
     const int i0 = (w.qlo + n % w.nq) * BR;
-    sc.head<S>(a, h0 + n / w.nq);
+    sc.head(a, h0 + n / w.nq);
 #pragma unroll
     for (int t = 0; t < 2; ++t) {   // rows: query i0 + 16 t + 4 g4 + e, column: key
       if (i0 + 16 * t >= hi_max || i0 + 16 * t + 15 < lo_min) continue;
@@ -1386,11 +1371,11 @@ __device__ __forceinline__ void win_dkdv_f32(const AttnWinArgs& a, unsigned task
       for (int e = 0; e < 4; ++e) {
         const int i = i0 + 16 * t + 4 * g4 + e;
         const bool ok = i >= lo && i < hi;
-        float d = 1.f;
-        const float x = S == SCORE_PLAIN ? s[e] * scale2 : sc.at32(s[e], (float)(krow - i), d);
-        p[e] = ok ? __builtin_amdgcn_exp2f(x - L4[e]) : 0.f;
+        float bent = 0.f;
+        const float x = S == SCORE_PLAIN ? s[e] * scale2 - L4[e] : sc.less32(s[e], scale2, (float)(krow - i), L4[e], bent);
+        p[e] = ok ? __builtin_amdgcn_exp2f(x) : 0.f;
         ds[e] = ok ? p[e] * (dp[e] + D4[e]) : 0.f;
-        if (S != SCORE_PLAIN) ds[e] *= d;
+        if (capped(S)) ds[e] *= sc.derivative(bent);
       }
 #pragma unroll
       for (int e = 0; e < 4; ++e)
@@ -1671,13 +1656,20 @@ inline void make_docs_plan(Dtype dt, AttnWinArgs& a) {
   p.max_cuts = parts > 1 ? (int)std::min<long>(share, p.key_tiles) : 0;
   p.slots = parts > 1 ? (int)std::min<long>(2L * p.units / a.Ak, p.key_tiles * parts) : 0;
   p.max_tasks = p.key_tiles + (int)std::min<long>(share, p.key_tiles * parts);
-  p.key_tasks = (unsigned)(((long)p.max_tasks * a.Ak + 7) / 8 * 8);   // (what follows begins at XCD 0)
+  p.key_tasks = heads_grid(a.Ak, p.max_tasks);
 }
 inline size_t table_bytes(const AttnWinArgs& a) { return (16 + 16 * ((size_t)a.plan.max_tasks + a.plan.max_cuts) + 255) / 256 * 256; }
 
 template <typename K>
 hipError_t allow_lds(K kern, int bytes) {
   return hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+}
+
+// workgroups of the query tiles of so many rows
+template <int M>
+unsigned query_grid(const AttnWinArgs& a, int rows) {
+  const long tiles = (a.s + rows - 1) / rows;
+  return M == MASK_SPANS ? heads_grid(a.A, tiles) : (unsigned)(tiles * a.b * a.A);
 }
 
 template <int M, int S>
@@ -1689,7 +1681,7 @@ hipError_t attn_win_fwd_launch_f32(const AttnWinArgs& a, hipStream_t st) {
       constexpr int rg = decltype(RG)::value, lds = F32Lds<d, rg, 2>::FLOATS * 4;
       static const hipError_t rc = allow_lds(attn_win_fwd_f32<M, S, d, rg, 2>, lds);
       if (rc != hipSuccess) return rc;
-      hipLaunchKernelGGL((attn_win_fwd_f32<M, S, d, rg, 2>), dim3((unsigned)((long)((a.s + 16 * rg - 1) / (16 * rg)) * a.b * a.A)), dim3(128 * rg), lds, st, a, scale2);
+      hipLaunchKernelGGL((attn_win_fwd_f32<M, S, d, rg, 2>), dim3(query_grid<M>(a, 16 * rg)), dim3(128 * rg), lds, st, a, scale2);
       return hipGetLastError();
     };
     return f32_fwd_rows(a) == 4 ? go(std::integral_constant<int, 4>{}) : go(std::integral_constant<int, 2>{});
@@ -1706,7 +1698,7 @@ hipError_t attn_win_fwd_launch_bf16(const AttnWinArgs& a, hipStream_t st) {
         constexpr int nw = decltype(NW)::value, lds = WinRing<d, nw, false>::BYTES;
         static const hipError_t rc = allow_lds(attn_win_fwd<M, S, d, nw>, lds);
         if (rc != hipSuccess) return rc;
-        hipLaunchKernelGGL((attn_win_fwd<M, S, d, nw>), dim3((unsigned)((long)((a.s + 32 * nw - 1) / (32 * nw)) * a.b * a.A)), dim3(64 * nw), lds, st, a, scale2);
+        hipLaunchKernelGGL((attn_win_fwd<M, S, d, nw>), dim3(query_grid<M>(a, 32 * nw)), dim3(64 * nw), lds, st, a, scale2);
         return hipGetLastError();
       };
       return fwd_waves(a) == 4 ? go(std::integral_constant<int, 4>{}) : go(std::integral_constant<int, 2>{});
@@ -1735,7 +1727,7 @@ hipError_t attn_win_bwd_join(K kern, const AttnWinArgs& a, int kt, int d, hipStr
   const int threads = join_threads(kt * d);
   if (a.spans) {   // (workgroups enough for the memory; what finds no cut tile costs time, too)
     const long per = (long)(kt * d / 4 / threads) * a.Ak * 2;
-    joined = std::min<long>(a.plan.max_cuts, std::max<long>(1, 1024 / per));
+    joined = std::min<long>(a.plan.max_cuts, std::max<long>(1, 512 / per));
   }
   if (!joined) return hipSuccess;
   hipLaunchKernelGGL(kern, dim3(joined * (kt * d / 4 / threads), a.b * a.Ak, 2), dim3(threads), 0, st, a, a.scale);
@@ -1753,8 +1745,8 @@ hipError_t attn_win_bwd_launch_f32(AttnWinArgs a, void* workspace, hipStream_t s
       constexpr int rg = decltype(RG)::value, lds = F32Lds<d, rg, 2>::FLOATS * 4;
       static const hipError_t rc = allow_lds(attn_win_bwd_f32<M, S, d, rg, 2>, lds);
       if (rc != hipSuccess) return rc;
-      const long grid = a.plan.key_tasks + (long)((a.s + 16 * rg - 1) / (16 * rg)) * a.b * a.A;
-      hipLaunchKernelGGL((attn_win_bwd_f32<M, S, d, rg, 2>), dim3((unsigned)grid), dim3(128 * rg), lds, st, a, scale2, scale);
+      const unsigned grid = a.plan.key_tasks + query_grid<M>(a, 16 * rg);
+      hipLaunchKernelGGL((attn_win_bwd_f32<M, S, d, rg, 2>), dim3(grid), dim3(128 * rg), lds, st, a, scale2, scale);
       e = hipGetLastError();
       return e != hipSuccess ? e : attn_win_bwd_join(attn_win_join<M, float, d, 16 * rg, 16, BR>, a, 16 * rg, d, st);
     };
@@ -1772,9 +1764,8 @@ hipError_t attn_win_bwd_launch_bf16(AttnWinArgs a, void* workspace, hipStream_t 
     if constexpr (d == 128) {
       static const hipError_t rc = allow_lds(attn_win_bwd_pair<M, S>, PAIR_BYTES);
       if (rc != hipSuccess) return rc;
-      const long q_tiles = (long)((a.s + 255) / 256) * a.b * a.A;
       const bool both = pair_has_dq(a);
-      hipLaunchKernelGGL((attn_win_bwd_pair<M, S>), dim3((unsigned)(a.plan.key_tasks + (both ? q_tiles : 0))), dim3(512), PAIR_BYTES, st, a, scale2, scale);
+      hipLaunchKernelGGL((attn_win_bwd_pair<M, S>), dim3(a.plan.key_tasks + (both ? query_grid<M>(a, 256) : 0)), dim3(512), PAIR_BYTES, st, a, scale2, scale);
       e = hipGetLastError();
       if (e == hipSuccess) e = attn_win_bwd_join(attn_win_join<M, bf16, d, 128, 32, 32>, a, 128, d, st);
       if (e != hipSuccess || both) return e;
@@ -1782,7 +1773,7 @@ hipError_t attn_win_bwd_launch_bf16(AttnWinArgs a, void* workspace, hipStream_t 
         constexpr int nw = decltype(NW)::value, lds = WinRing<d, nw, true>::BYTES;
         static const hipError_t rc = allow_lds(attn_win_dq<M, S, nw>, lds);
         if (rc != hipSuccess) return rc;
-        hipLaunchKernelGGL((attn_win_dq<M, S, nw>), dim3((unsigned)((long)((a.s + 32 * nw - 1) / (32 * nw)) * a.b * a.A)), dim3(64 * nw), lds, st, a, scale2, scale);
+        hipLaunchKernelGGL((attn_win_dq<M, S, nw>), dim3(query_grid<M>(a, 32 * nw)), dim3(64 * nw), lds, st, a, scale2, scale);
         return hipGetLastError();
       };
       return fwd_waves(a) == 4 ? dq(std::integral_constant<int, 4>{}) : dq(std::integral_constant<int, 2>{});
@@ -1791,8 +1782,8 @@ hipError_t attn_win_bwd_launch_bf16(AttnWinArgs a, void* workspace, hipStream_t 
         constexpr int nw = decltype(NW)::value, lds = WinRing<d, nw, true>::BYTES;
         static const hipError_t rc = allow_lds(attn_win_bwd<M, S, d, nw>, lds);
         if (rc != hipSuccess) return rc;
-        const long grid = a.plan.key_tasks + (long)((a.s + 32 * nw - 1) / (32 * nw)) * a.b * a.A;
-        hipLaunchKernelGGL((attn_win_bwd<M, S, d, nw>), dim3((unsigned)grid), dim3(64 * nw), lds, st, a, scale2, scale);
+        const unsigned grid = a.plan.key_tasks + query_grid<M>(a, 32 * nw);
+        hipLaunchKernelGGL((attn_win_bwd<M, S, d, nw>), dim3(grid), dim3(64 * nw), lds, st, a, scale2, scale);
         e = hipGetLastError();
         return e != hipSuccess ? e : attn_win_bwd_join(attn_win_join<M, bf16, d, 32 * nw, 32, 64>, a, 32 * nw, d, st);
       };

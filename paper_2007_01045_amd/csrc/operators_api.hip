@@ -99,17 +99,16 @@ static int docs_args(int dtype, const dapple_attention_docs_desc* d, bool bwd, b
   if (!aligned_to(d->spans, 4) || !aligned_to(d->slopes, 4)) return set_error(STAGE_E_CONFIG, "spans or slopes not aligned");
   a.spans = d->spans; a.slopes = d->slopes;
   if (d->cap > 0.f) {
-    const double log2e = 1.4426950408889634;
-    a.cap2 = (float)(d->cap * log2e);
-    a.bend = (float)((dtype == STAGE_DTYPE_BF16 ? 2.0 * log2e : 1.0) * a.scale / d->cap);
-    const double k = (double)a.scale / d->cap, s2 = log2e * a.scale, c[3] = {-0.33319074494554746, 0.1308641832442356, -0.041387786259018865};
-    a.small = (float)(0.6 / k);
-    a.down = (float)(-1.0 / ((double)a.cap2 * a.cap2));
-    double f = s2;
+    a.cap2 = (float)(d->cap * 1.4426950408889634);
+    a.bend = a.scale / d->cap;
+    a.small = 0.6f / a.bend;
+    if (!std::isnormal(a.bend) || !std::isnormal(a.small)) return set_error(STAGE_E_CONFIG, "scale %g over cap %g", a.scale, d->cap);
+    const double c[3] = {-0.33319074494554746, 0.1308641832442356, -0.041387786259018865};   // (see Score)
+    double power = a.bend;
     for (int i = 0; i < 3; ++i) {
-      f *= k * k;
-      a.poly[i] = (float)(f * c[i]);
-      if (!std::isnormal(a.poly[i])) a.small = -1.f;   // (cap or scale of extreme sizes: never the polynomial)
+      power *= (double)a.bend * a.bend;
+      a.poly[i] = (float)(c[i] * power);
+      if (!std::isnormal(a.poly[i])) a.small = -1.f;
     }
   }
   return STAGE_OK;
