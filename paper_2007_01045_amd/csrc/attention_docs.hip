@@ -11,22 +11,29 @@ namespace dapple {
 // ------------------------------------------------------------------ spans
 // spans[0 .. 3][rows]: key_lo, key_hi, query_lo, query_hi; behind them the number of rows that documents hold.  Document t holds the rows
 // from ends[t - 1] (0) to ends[t].  Rows behind the last see nothing.
+constexpr int NEAR_ENDS = 2048;   // as many are searched in LDS
 __global__ __launch_bounds__(256) void doc_spans_kernel(const int32_t* __restrict__ ends, const int32_t* __restrict__ prefix, int n, int rows, int causal, int window,
                                                         int32_t* __restrict__ spans) {
+  __shared__ int32_t near[NEAR_ENDS];
   const int i = blockIdx.x * 256 + threadIdx.x;
   const int len = n > 0 ? min(max(ends[n - 1], 0), rows) : 0;
+  if (n <= NEAR_ENDS) {
+    for (int t = threadIdx.x; t < n; t += 256) near[t] = ends[t];
+    __syncthreads();
+  }
   if (i == 0) spans[4L * rows] = len;
   if (i >= rows) return;
   int v[4] = {len, len, len, len};
   if (i < len) {
+    auto end_of = [&](int t) { return n <= NEAR_ENDS ? near[t] : ends[t]; };
     int lo = 0, hi = n - 1;   // the first document that ends behind row i
     while (lo < hi) {
       const int mid = (lo + hi) >> 1;
-      if (ends[mid] > i) hi = mid;
+      if (end_of(mid) > i) hi = mid;
       else lo = mid + 1;
     }
     // (ends that are not ascending: some document, within the rows)
-    const int begin = lo ? min(max(ends[lo - 1], 0), i) : 0, end = min(max(ends[lo], i + 1), len);
+    const int begin = lo ? min(max(end_of(lo - 1), 0), i) : 0, end = min(max(end_of(lo), i + 1), len);
     const int free = causal && prefix ? min(max(prefix[lo], 0), end - begin) + begin : begin;   // first row behind the prefix
     v[0] = begin;
     v[1] = causal ? max(i + 1, free) : end;

@@ -48,10 +48,14 @@ __device__ __forceinline__ int len_of(const AttnWinArgs& a, int bi) {
   return a.lens ? min(max(a.lens[bi], 0), a.s) : a.s;
 }
 
-// MASK_SPANS: the runs come from arrays (doc_spans), of key_lo, key_hi, query_lo and query_hi, none of which ever falls from row to row
+// MASK_SPANS: the runs come from arrays (doc_spans), of key_lo, key_hi, query_lo and query_hi, none of which ever falls from row to row (behind
+// the last document all are its end: a row there may stand for the last one, and no index waits for the length)
 __device__ __forceinline__ int span_of(const AttnWinArgs& a, int which, int i) {
   return min(max(a.spans[(long)which * a.s + min(i, a.s - 1)], 0), a.s);
 }
+// the last of n rows from row i on that may be asked for
+template <int M>
+__device__ __forceinline__ int last_row(const AttnWinArgs& a, int i, int n, int len) { return min(i + n, M == MASK_SPANS ? a.s : len) - 1; }
 // keys that query i sees: [lo, hi) and [0, min(S, hi))
 template <int M>
 __device__ __forceinline__ int key_lo(const AttnWinArgs& a, int i) {
@@ -262,7 +266,7 @@ struct KeyTask {
   bool run;
   __device__ __forceinline__ KeyTask() {}
   __device__ __forceinline__ void span(const AttnWinArgs& a, int kt, int blk) {
-    const int k1 = min(k0 + kt, len) - 1;
+    const int k1 = last_row<M>(a, k0, kt, len);
     qlo = nq = 0;
     if (k0 >= len) return;
     const bool sink = is_sink<M>(a, k0);   // the walk of the tile's first key has the lower end of all, its last key's the upper,
@@ -344,10 +348,10 @@ __global__ __launch_bounds__(64 * NW, D <= 64 ? 3 : 2) void attn_win_fwd(AttnWin
   const bf16 *Q = (const bf16*)a.q + r0 * a.ldq + hh * d, *K = (const bf16*)a.k + r0 * a.ldk + kv * d, *V = (const bf16*)a.v + r0 * a.ldv + kv * d;
   const int q0 = tile * 32 * NW, row0 = q0 + wave * 32, qrow = row0 + (lane & 31);
   const bool qok = qrow < len;
-  const KeyWalk<M> walk(a, q0, min(q0 + 32 * NW, len) - 1, len, 64);
+  const KeyWalk<M> walk(a, q0, last_row<M>(a, q0, 32 * NW, len), len, 64);
   const int lo = key_lo<M>(a, qrow), hi = qok ? key_hi<M>(a, qrow, len) : 0;
-  const int qb = min(row0 + 32, len) - 1;   // the wave's last row; the ends of its rows' runs
-  const int lo_min = key_lo<M>(a, row0), lo_max = key_lo<M>(a, qb), hi_min = row0 + 31 < len ? key_hi<M>(a, row0, len) : 0, hi_max = key_hi<M>(a, qb, len);
+  const int qb = last_row<M>(a, row0, 32, len);   // the wave's last row; the ends of its rows' runs
+  const int lo_min = key_lo<M>(a, row0), lo_max = key_lo<M>(a, qb), hi_min = row0 + 31 < len || M == MASK_SPANS ? key_hi<M>(a, row0, len) : 0, hi_max = key_hi<M>(a, qb, len);
   bf16x8 qf[NKK];
 #pragma unroll
   for (int kk = 0; kk < NKK; ++kk) qf[kk] = frag_global<true>(Q, qrow, qok, a.ldq, kk, lane, d);
@@ -509,7 +513,7 @@ __device__ __forceinline__ void win_dkdv(const AttnWinArgs& a, unsigned task, un
   const bool kok = krow < len;
   const int lo = query_lo<M>(a, krow), hi = kok ? query_hi<M>(a, krow, len) : 0;
   // of the wave's keys: the least and the greatest end of what sees them
-  const int kb = min(row0 + 32, len) - 1;
+  const int kb = last_row<M>(a, row0, 32, len);
   const bool sink = is_sink<M>(a, row0);
   const int lo_min = sink && !a.causal ? 0 : query_lo<M>(a, row0), lo_max = query_lo<M>(a, kb);
   const int hi_max = sink ? len : query_hi<M>(a, kb, len);
@@ -641,10 +645,10 @@ __device__ __forceinline__ void win_dq(const AttnWinArgs& a, unsigned id, unsign
   const bf16 *K = (const bf16*)a.k + r0 * a.ldk + kv * d, *V = (const bf16*)a.v + r0 * a.ldv + kv * d;
   const int q0 = tile * 32 * NW, row0 = q0 + wave * 32, qrow = row0 + (lane & 31);
   const bool qok = qrow < len;
-  const KeyWalk<M> walk(a, q0, min(q0 + 32 * NW, len) - 1, len, 64);
+  const KeyWalk<M> walk(a, q0, last_row<M>(a, q0, 32 * NW, len), len, 64);
   const int lo = key_lo<M>(a, qrow), hi = qok ? key_hi<M>(a, qrow, len) : 0;
-  const int qb = min(row0 + 32, len) - 1;   // the wave's last row; the ends of its rows' runs
-  const int lo_min = key_lo<M>(a, row0), lo_max = key_lo<M>(a, qb), hi_min = row0 + 31 < len ? key_hi<M>(a, row0, len) : 0, hi_max = key_hi<M>(a, qb, len);
+  const int qb = last_row<M>(a, row0, 32, len);   // the wave's last row; the ends of its rows' runs
+  const int lo_min = key_lo<M>(a, row0), lo_max = key_lo<M>(a, qb), hi_min = row0 + 31 < len || M == MASK_SPANS ? key_hi<M>(a, row0, len) : 0, hi_max = key_hi<M>(a, qb, len);
   const long st = ((long)bi * a.A + hh) * a.s + qrow;
   const float Lq = qok ? a.lse[st] : 0.f, Dq = qok ? a.delta[st] : 0.f;
   bf16x8 qf[NKK], gf[NKK];
@@ -818,7 +822,7 @@ __device__ __forceinline__ void win_dkdv_pair(const AttnWinArgs& a, unsigned tas
   const float *lse = a.lse + ((long)w.bi * a.A + h0) * a.s, *delta = a.delta + ((long)w.bi * a.A + h0) * a.s;
   const int row0 = w.k0 + own * 32, krow = row0 + (lane & 31);
   const bool kok = krow < len;
-  const int kb = min(row0 + 32, len) - 1;   // (as in win_dkdv)
+  const int kb = last_row<M>(a, row0, 32, len);   // (as in win_dkdv)
   const bool sink = is_sink<M>(a, row0);
   const int lo_min = sink && !a.causal ? 0 : query_lo<M>(a, row0), lo_max = query_lo<M>(a, kb);
   const int hi_max = row0 < len ? (sink ? len : query_hi<M>(a, kb, len)) : 0;
@@ -1063,10 +1067,10 @@ __global__ __launch_bounds__(64 * RG * NG) void attn_win_fwd_f32(AttnWinArgs a, 
   const int kv = hh / (a.A / a.Ak), len = len_of<M>(a, bi), d = a.d;
   const long r0 = (long)bi * a.s;
   const float *Q = (const float*)a.q + r0 * a.ldq + hh * d, *K = (const float*)a.k + r0 * a.ldk + kv * d, *V = (const float*)a.v + r0 * a.ldv + kv * d;
-  const int q0 = tile * 16 * RG, row0 = q0 + wave * 16, qrow = row0 + (lane & 15), qb = min(row0 + 16, len) - 1;
+  const int q0 = tile * 16 * RG, row0 = q0 + wave * 16, qrow = row0 + (lane & 15), qb = last_row<M>(a, row0, 16, len);
   const int lo_min = key_lo<M>(a, row0), hi_max = key_hi<M>(a, qb, len);
   const bool qok = qrow < len;
-  const KeyWalk<M> walk(a, q0, min(q0 + 16 * RG, len) - 1, len, BR);
+  const KeyWalk<M> walk(a, q0, last_row<M>(a, q0, 16 * RG, len), len, BR);
   const int lo = key_lo<M>(a, qrow), hi = qok ? key_hi<M>(a, qrow, len) : 0;
   f32x4 qf[NK];
   own_row<D>(Q + (long)qrow * a.ldq, qok, d, lane, qf);
@@ -1210,10 +1214,10 @@ __device__ __forceinline__ void win_dq_f32(const AttnWinArgs& a, unsigned id, un
   const int kv = hh / (a.A / a.Ak), len = len_of<M>(a, bi), d = a.d;
   const long r0 = (long)bi * a.s;
   const float *K = (const float*)a.k + r0 * a.ldk + kv * d, *V = (const float*)a.v + r0 * a.ldv + kv * d;
-  const int q0 = tile * 16 * RG, row0 = q0 + wave * 16, qrow = row0 + (lane & 15), qb = min(row0 + 16, len) - 1;
+  const int q0 = tile * 16 * RG, row0 = q0 + wave * 16, qrow = row0 + (lane & 15), qb = last_row<M>(a, row0, 16, len);
   const int lo_min = key_lo<M>(a, row0), hi_max = key_hi<M>(a, qb, len);
   const bool qok = qrow < len;
-  const KeyWalk<M> walk(a, q0, min(q0 + 16 * RG, len) - 1, len, BR);
+  const KeyWalk<M> walk(a, q0, last_row<M>(a, q0, 16 * RG, len), len, BR);
   const int lo = key_lo<M>(a, qrow), hi = qok ? key_hi<M>(a, qrow, len) : 0;
   f32x4 qf[NK], gf[NK];
   own_row<D>((const float*)a.q + (r0 + qrow) * a.ldq + hh * d, qok, d, lane, qf);
@@ -1305,7 +1309,7 @@ __device__ __forceinline__ void win_dkdv_f32(const AttnWinArgs& a, unsigned task
   const int row0 = w.k0 + wave * 16, krow = row0 + (lane & 15);
   const bool kok = krow < len;
   const int lo = query_lo<M>(a, krow), hi = kok ? query_hi<M>(a, krow, len) : 0;
-  const int kb = min(row0 + 16, len) - 1;
+  const int kb = last_row<M>(a, row0, 16, len);
   const bool sink = is_sink<M>(a, row0);
   const int lo_min = sink && !a.causal ? 0 : query_lo<M>(a, row0), hi_max = sink ? len : query_hi<M>(a, kb, len);
   f32x4 kf[NK], vf[NK], sum[2 * NK];   // sums: dk, dv
@@ -1645,10 +1649,12 @@ inline void make_docs_plan(Dtype dt, AttnWinArgs& a) {
   WinPlan& p = a.plan;
   p.kt = key_tile(dt, a);
   p.blk = walk_block(dt, a);
-  // Parts of up to a share of all walks of dk and dv for each workgroup that runs at once: a unit holds one of D = 128 in bf16, and two
-  // others.  Where dq's workgroups are in the same launch, behind them, one and a half times that: the longest begin first, and
-  // dq's fill what they leave.
-  p.units = dt == DT_BF16 && a.d > 64 ? (pair_has_dq(a) ? 170 : 256) : 340;
+  // Parts of up to one of `units` shares of all walks of dk and dv: the longest begin first, and dq's workgroups, in the same launch behind them,
+  // fill what they leave; where those are alone, a share for each unit.  Us forward and gradient with 170 / 340 / 512 shares, of 3, 6 and 12 documents:
+  // 8192 rows of 16 heads of 128 on 4 1003 / 1010 / 1026, 544 / 560 / 571, 345 / 360 / 378; 6001 rows of 16 heads of 64, of 6, 8 and 14
+  // documents 265 / 281 / 278, 177 / 184 / 184, 145 / 146 / 151; fp32, 1554 rows, 3, 6 and 7 documents 152 / 163 / 167, 134 / 142 / 145, 125 /
+  // 127 / 126.
+  p.units = dt == DT_BF16 && a.d > 64 && !pair_has_dq(a) ? 256 : 170;
   p.min_steps = 16;
   p.key_tiles = (a.s + p.kt - 1) / p.kt;
   const long parts = ((long)(a.s + p.blk - 1) / p.blk * (a.A / a.Ak) + p.min_steps - 1) / p.min_steps;   // of the longest walk there can be
