@@ -87,7 +87,9 @@ __device__ __forceinline__ bool is_sink(const AttnWinArgs& a, int j) { return M 
 // The cap is bound by its instructions (an exponential or a reciprocal takes four times one of the others).  Where |x| <= 0.6 for all that
 // a wave looks at, tanh(x) = x (1 + c1 x^2 + c2 x^4 + c3 x^6), c fitted for the least relative error, 2.5e-6, which is below 2^-13 of a probability for any
 // logit up to 30; else each logit has that or, by its own size alone (what stands beside it must not show), tanh(x) = 1 - 2 r, r = 1 / (1 +
-// e^2x), off by 2^-23 of 1.  XXX measured
+// e^2x), off by 2^-23 of 1.
+// Us forward and gradient with the polynomial / with that always, 4 documents of 2048 rows, both directions, cap 50, normal q and k: 16 heads of 128 on 4
+// 223 + 563 / 246 + 689, 16 of 64 135 + 364 / 191 + 466.
 constexpr bool capped(int S) { return S == SCORE_CAP || S == SCORE_BOTH; }
 constexpr bool sloped(int S) { return S == SCORE_SLOPE || S == SCORE_BOTH; }
 template <int S>
@@ -222,10 +224,13 @@ __device__ __forceinline__ void by_heads(unsigned id, int heads, int& head, int&
 }
 
 // The query tile of workgroup id of n.  MASK_WINDOW: the last tiles first (causal: they have the longest walks).
-// MASK_SPANS: where they do not all run at once, the tiles with the longest walks first, all heads by turns: a long one that begins last would
-// be what the launch ends with.  Each wave ranks the tiles itself, up to 64 groups of neighbours, one to a lane, by the walk of a
-// group's last row.  Us forward, ranked / as they lie: XXX
-template <int M>
+// MASK_SPANS: likewise, all heads by turns.  RANKED: where the workgroups do not all run at once, the longest walks first: a long one that
+// begins last would be what the launch ends with.  Each wave ranks the tiles itself, up to 64 groups of neighbours, one to a lane, by the walk
+// of a group's last row.  That is for dq, whose workgroups follow those of dk and dv; a forward whose long walks share the units from the start
+// is slower.  Us ranked / as they lie, packed documents of 3, 6 and 12 (6, 8, 14; 3, 6, 7), gradient: 8192 rows of 16 heads of 128 749 / 778, 409 / 412,
+// 253 / 287; 6001 rows of 16 heads of 64 180 / 178, 114 / 115, 89 / 100; fp32, 1554 rows of 12 heads 101 / 98, 88 / 93, 85 / 85.  Forward: 291 / 258, 149 /
+// 145, 95 / 97; 104 / 95, 65 / 61, 56 / 54; 49 / 44, 44 / 43, 40 / 34.
+template <int M, bool RANKED>
 struct QueryTask {
   int tile, bi, hh;
   bool run = true;
@@ -241,7 +246,7 @@ struct QueryTask {
     bi = 0;
     tile = q_tiles - 1 - rank;
     run = rank < q_tiles;
-    if (n <= 256 || !run) return;
+    if (!RANKED || n <= 256 || !run) return;
     const int group = (q_tiles + 63) / 64, groups = (q_tiles + group - 1) / group, first = lane * group, last = min(first + group, q_tiles) - 1;
     int walk = -1;
     if (lane < groups) {
@@ -339,7 +344,7 @@ __global__ __launch_bounds__(64 * NW, D <= 64 ? 3 : 2) void attn_win_fwd(AttnWin
   const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int q_tiles = (a.s + 32 * NW - 1) / (32 * NW);
-  const QueryTask<M> task(a, blockIdx.x, gridDim.x, q_tiles, 32 * NW, lane);
+  const QueryTask<M, false> task(a, blockIdx.x, gridDim.x, q_tiles, 32 * NW, lane);
   if (!task.run) return;
   const int tile = task.tile, bi = task.bi, hh = task.hh;
   const int kv = hh / (a.A / a.Ak);
@@ -635,7 +640,7 @@ __device__ __forceinline__ void win_dq(const AttnWinArgs& a, unsigned id, unsign
   const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int q_tiles = (a.s + 32 * NW - 1) / (32 * NW);
-  const QueryTask<M> task(a, id, ids, q_tiles, 32 * NW, lane);
+  const QueryTask<M, true> task(a, id, ids, q_tiles, 32 * NW, lane);
   if (!task.run) return;
   const int tile = task.tile, bi = task.bi, hh = task.hh;
   const int kv = hh / (a.A / a.Ak);
@@ -1061,7 +1066,7 @@ __global__ __launch_bounds__(64 * RG * NG) void attn_win_fwd_f32(AttnWinArgs a, 
   const int group = __builtin_amdgcn_readfirstlane(threadIdx.x / (64 * RG));
   float *const Ks = fsm + group * 2 * F32Lds<D, RG, NG>::BLK, *const Vs = Ks + F32Lds<D, RG, NG>::BLK;
   const int q_tiles = (a.s + 16 * RG - 1) / (16 * RG);
-  const QueryTask<M> task(a, blockIdx.x, gridDim.x, q_tiles, 16 * RG, lane);
+  const QueryTask<M, false> task(a, blockIdx.x, gridDim.x, q_tiles, 16 * RG, lane);
   if (!task.run) return;
   const int tile = task.tile, bi = task.bi, hh = task.hh;
   const int kv = hh / (a.A / a.Ak), len = len_of<M>(a, bi), d = a.d;
@@ -1208,7 +1213,7 @@ __device__ __forceinline__ void win_dq_f32(const AttnWinArgs& a, unsigned id, un
   const int group = __builtin_amdgcn_readfirstlane(threadIdx.x / (64 * RG));
   float *const Ks = fsm + group * 2 * F32Lds<D, RG, NG>::BLK, *const Vs = Ks + F32Lds<D, RG, NG>::BLK;
   const int q_tiles = (a.s + 16 * RG - 1) / (16 * RG);
-  const QueryTask<M> task(a, id, ids, q_tiles, 16 * RG, lane);
+  const QueryTask<M, true> task(a, id, ids, q_tiles, 16 * RG, lane);
   if (!task.run) return;
   const int tile = task.tile, bi = task.bi, hh = task.hh;
   const int kv = hh / (a.A / a.Ak), len = len_of<M>(a, bi), d = a.d;
