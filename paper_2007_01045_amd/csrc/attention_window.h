@@ -174,12 +174,54 @@ struct Score {
 template <int M>
 struct KeyWalk {
   int first, lo, n;
-  __device__ __forceinline__ KeyWalk(const AttnWinArgs& a, int q0, int q1, int len, int blk) {
-    lo = key_lo<M>(a, q0) / blk;
+  // the queries' runs begin at key `begin` and end before `end`; any: whether there are queries at all
+  __device__ __forceinline__ KeyWalk(const AttnWinArgs& a, int begin, int end, bool any, int blk) {
+    lo = begin / blk;
     first = M == MASK_WINDOW && a.W ? min((a.S + blk - 1) / blk, lo) : 0;
-    n = q0 < len ? first + (key_hi<M>(a, q1, len) + blk - 1) / blk - lo : 0;
+    n = any ? first + (end + blk - 1) / blk - lo : 0;
   }
   __device__ __forceinline__ int block(int t) const { return t < first ? t : lo + t - first; }
+};
+// What the R queries of a wave from row0 on see, what the n of its workgroup from t0 on do, and the documents' length.  Of MASK_SPANS in two
+// loads, a row's ends and the rest to a lane each, that wait for nothing and are waited for once: one by one, each had to wait for the last
+// (8192 rows of 16 heads, forward: 2 % less at widths 64 and 128).  For what sees a wave's keys (KeyRows) it gave nothing and took 1 to 3 % at width 64.
+template <int M, int R>
+struct WaveRows {
+  int len, lo, hi;                        // the lane's row's run; hi = 0 behind the last
+  int lo_min, lo_max, hi_min, hi_max;     // of the wave's rows: the least and the greatest beginning and end of a run
+  int walk_lo, walk_hi;                   // of the workgroup's rows: where the first run begins, the last ends
+  __device__ __forceinline__ WaveRows(const AttnWinArgs& a, int bi, int row0, int t0, int n, int lane) {
+    const int row = row0 + (lane & (R - 1));
+    if constexpr (M == MASK_SPANS) {
+      const int end = a.s - 1, x = lane & 3;
+      const long at = (lane / R & 1) * (long)a.s + min(row, end);
+      const long of = x == 2 ? 4L * a.s : x % 2 * (long)a.s + min(x ? t0 + n - 1 : t0, end);
+      const int own = min(max(a.spans[at], 0), a.s), rest = min(max(a.spans[of], 0), a.s);
+      len = __builtin_amdgcn_readlane(rest, 2);
+      walk_lo = __builtin_amdgcn_readlane(rest, 0);
+      walk_hi = min(len, __builtin_amdgcn_readlane(rest, 1));
+      lo_min = __builtin_amdgcn_readlane(own, 0);
+      lo_max = __builtin_amdgcn_readlane(own, R - 1);
+      hi_min = min(len, __builtin_amdgcn_readlane(own, R));
+      hi_max = min(len, __builtin_amdgcn_readlane(own, 2 * R - 1));
+      if constexpr (R == 32) {
+        const auto r = __builtin_amdgcn_permlane32_swap((unsigned)own, (unsigned)own, false, false);
+        lo = (int)r[0];
+        hi = (int)r[1];
+      } else {
+        lo = __shfl(own, lane & (R - 1), 64);
+        hi = __shfl(own, R + (lane & (R - 1)), 64);
+      }
+      hi = row < len ? min(len, hi) : 0;
+    } else {
+      len = len_of<M>(a, bi);
+      const int qb = min(row0 + R, len) - 1;   // the wave's last row
+      lo = key_lo<M>(a, row), hi = row < len ? key_hi<M>(a, row, len) : 0;
+      lo_min = key_lo<M>(a, row0), lo_max = key_lo<M>(a, qb);
+      hi_min = row0 + R - 1 < len ? key_hi<M>(a, row0, len) : 0, hi_max = key_hi<M>(a, qb, len);
+      walk_lo = key_lo<M>(a, t0), walk_hi = key_hi<M>(a, min(t0 + n, len) - 1, len);
+    }
+  }
 };
 // whether a wave's rows, whose runs begin at lo_min and end at hi_max, see any of keys k0 .. k1
 template <int M>
@@ -321,6 +363,20 @@ struct KeyTask {
   }
 };
 
+// What sees the R keys of a wave from row0 on: of the lane's key, and the least and the greatest beginning and end of the wave's
+template <int M, int R>
+struct KeyRows {
+  int lo, hi, lo_min, lo_max, hi_min, hi_max;
+  __device__ __forceinline__ KeyRows(const AttnWinArgs& a, int row0, int len, int lane) {
+    const int krow = row0 + (lane & (R - 1)), kb = last_row<M>(a, row0, R, len);
+    lo = query_lo<M>(a, krow), hi = krow < len ? query_hi<M>(a, krow, len) : 0;
+    const bool sink = is_sink<M>(a, row0);
+    lo_min = sink && !a.causal ? 0 : query_lo<M>(a, row0), lo_max = query_lo<M>(a, kb);
+    hi_max = sink ? len : query_hi<M>(a, kb, len);
+    hi_min = row0 + R - 1 < len ? query_hi<M>(a, sink ? min(kb, a.S) : row0, len) : 0;
+  }
+};
+
 // ------------------------------------------------------------------ bf16
 template <int D, int NW, bool STATS>
 using WinRing = Ring<D, NW, D == 128 ? 2 : 3, STATS>;
@@ -347,16 +403,16 @@ __global__ __launch_bounds__(64 * NW, D <= 64 ? 3 : 2) void attn_win_fwd(AttnWin
   const QueryTask<M, false> task(a, blockIdx.x, gridDim.x, q_tiles, 32 * NW, lane);
   if (!task.run) return;
   const int tile = task.tile, bi = task.bi, hh = task.hh;
+  Score<S> sc(a, scale2);
+  sc.head(a, hh);
   const int kv = hh / (a.A / a.Ak);
-  const int len = len_of<M>(a, bi), d = a.d;
+  const int q0 = tile * 32 * NW, row0 = q0 + wave * 32, qrow = row0 + (lane & 31);
+  const WaveRows<M, 32> seen(a, bi, row0, q0, 32 * NW, lane);
+  const int len = seen.len, d = a.d, lo = seen.lo, hi = seen.hi, lo_min = seen.lo_min, lo_max = seen.lo_max, hi_min = seen.hi_min, hi_max = seen.hi_max;
   const long r0 = (long)bi * a.s;
   const bf16 *Q = (const bf16*)a.q + r0 * a.ldq + hh * d, *K = (const bf16*)a.k + r0 * a.ldk + kv * d, *V = (const bf16*)a.v + r0 * a.ldv + kv * d;
-  const int q0 = tile * 32 * NW, row0 = q0 + wave * 32, qrow = row0 + (lane & 31);
   const bool qok = qrow < len;
-  const KeyWalk<M> walk(a, q0, last_row<M>(a, q0, 32 * NW, len), len, 64);
-  const int lo = key_lo<M>(a, qrow), hi = qok ? key_hi<M>(a, qrow, len) : 0;
-  const int qb = last_row<M>(a, row0, 32, len);   // the wave's last row; the ends of its rows' runs
-  const int lo_min = key_lo<M>(a, row0), lo_max = key_lo<M>(a, qb), hi_min = row0 + 31 < len || M == MASK_SPANS ? key_hi<M>(a, row0, len) : 0, hi_max = key_hi<M>(a, qb, len);
+  const KeyWalk<M> walk(a, seen.walk_lo, seen.walk_hi, q0 < len, 64);
   bf16x8 qf[NKK];
 #pragma unroll
   for (int kk = 0; kk < NKK; ++kk) qf[kk] = frag_global<true>(Q, qrow, qok, a.ldq, kk, lane, d);
@@ -373,8 +429,6 @@ __global__ __launch_bounds__(64 * NW, D <= 64 ? 3 : 2) void attn_win_fwd(AttnWin
   for (int t = 0; t < R::NS - 1; ++t) ask(t);
   __builtin_amdgcn_s_waitcnt(0x0F70);   // (once, with the ring's first blocks: below, the counts are the ring's alone)
 
-  Score<S> sc(a, scale2);
-  sc.head(a, hh);
   float m = -3e38f, l = 0.f;   // (finite: a row that has seen nothing yet keeps m - m = 0)
   f32x16 o[NDB];  // rows d = 32 dblk + 8 blk + 4 h + e, column = the lane's query
 #pragma unroll
@@ -516,13 +570,8 @@ __device__ __forceinline__ void win_dkdv(const AttnWinArgs& a, unsigned task, un
   const float *lse = a.lse + ((long)w.bi * a.A + h0) * a.s, *delta = a.delta + ((long)w.bi * a.A + h0) * a.s;
   const int row0 = w.k0 + wave * 32, krow = row0 + (lane & 31);
   const bool kok = krow < len;
-  const int lo = query_lo<M>(a, krow), hi = kok ? query_hi<M>(a, krow, len) : 0;
-  // of the wave's keys: the least and the greatest end of what sees them
-  const int kb = last_row<M>(a, row0, 32, len);
-  const bool sink = is_sink<M>(a, row0);
-  const int lo_min = sink && !a.causal ? 0 : query_lo<M>(a, row0), lo_max = query_lo<M>(a, kb);
-  const int hi_max = sink ? len : query_hi<M>(a, kb, len);
-  const int hi_min = row0 + 31 < len ? query_hi<M>(a, sink ? min(kb, a.S) : row0, len) : 0;
+  const KeyRows<M, 32> seen(a, row0, len, lane);
+  const int lo = seen.lo, hi = seen.hi, lo_min = seen.lo_min, lo_max = seen.lo_max, hi_min = seen.hi_min, hi_max = seen.hi_max;
 
   bf16x8 kf[NKK], vf[NKK];
 #pragma unroll
@@ -643,17 +692,17 @@ __device__ __forceinline__ void win_dq(const AttnWinArgs& a, unsigned id, unsign
   const QueryTask<M, true> task(a, id, ids, q_tiles, 32 * NW, lane);
   if (!task.run) return;
   const int tile = task.tile, bi = task.bi, hh = task.hh;
+  Score<S> sc(a, scale2);
+  sc.head(a, hh);
   const int kv = hh / (a.A / a.Ak);
-  const int len = len_of<M>(a, bi), d = a.d;
+  const int q0 = tile * 32 * NW, row0 = q0 + wave * 32, qrow = row0 + (lane & 31);
+  const WaveRows<M, 32> seen(a, bi, row0, q0, 32 * NW, lane);
+  const int len = seen.len, d = a.d, lo = seen.lo, hi = seen.hi, lo_min = seen.lo_min, lo_max = seen.lo_max, hi_min = seen.hi_min, hi_max = seen.hi_max;
   const long r0 = (long)bi * a.s;
   const bf16 *Q = (const bf16*)a.q + r0 * a.ldq + hh * d, *G = (const bf16*)a.dctx + r0 * a.lddc + hh * d;
   const bf16 *K = (const bf16*)a.k + r0 * a.ldk + kv * d, *V = (const bf16*)a.v + r0 * a.ldv + kv * d;
-  const int q0 = tile * 32 * NW, row0 = q0 + wave * 32, qrow = row0 + (lane & 31);
   const bool qok = qrow < len;
-  const KeyWalk<M> walk(a, q0, last_row<M>(a, q0, 32 * NW, len), len, 64);
-  const int lo = key_lo<M>(a, qrow), hi = qok ? key_hi<M>(a, qrow, len) : 0;
-  const int qb = last_row<M>(a, row0, 32, len);   // the wave's last row; the ends of its rows' runs
-  const int lo_min = key_lo<M>(a, row0), lo_max = key_lo<M>(a, qb), hi_min = row0 + 31 < len || M == MASK_SPANS ? key_hi<M>(a, row0, len) : 0, hi_max = key_hi<M>(a, qb, len);
+  const KeyWalk<M> walk(a, seen.walk_lo, seen.walk_hi, q0 < len, 64);
   const long st = ((long)bi * a.A + hh) * a.s + qrow;
   const float Lq = qok ? a.lse[st] : 0.f, Dq = qok ? a.delta[st] : 0.f;
   bf16x8 qf[NKK], gf[NKK];
@@ -662,8 +711,6 @@ __device__ __forceinline__ void win_dq(const AttnWinArgs& a, unsigned id, unsign
     qf[kk] = frag_global<true>(Q, qrow, qok, a.ldq, kk, lane, d);
     gf[kk] = frag_global<true>(G, qrow, qok, a.lddc, kk, lane, d);
   }
-  Score<S> sc(a, scale2);
-  sc.head(a, hh);
   constexpr bool ADDS = D <= 64;   // the product dctx v adds to -delta (D = 128: no registers for it)
   f32x16 dp0;
 #pragma unroll
@@ -827,11 +874,8 @@ __device__ __forceinline__ void win_dkdv_pair(const AttnWinArgs& a, unsigned tas
   const float *lse = a.lse + ((long)w.bi * a.A + h0) * a.s, *delta = a.delta + ((long)w.bi * a.A + h0) * a.s;
   const int row0 = w.k0 + own * 32, krow = row0 + (lane & 31);
   const bool kok = krow < len;
-  const int kb = last_row<M>(a, row0, 32, len);   // (as in win_dkdv)
-  const bool sink = is_sink<M>(a, row0);
-  const int lo_min = sink && !a.causal ? 0 : query_lo<M>(a, row0), lo_max = query_lo<M>(a, kb);
-  const int hi_max = row0 < len ? (sink ? len : query_hi<M>(a, kb, len)) : 0;
-  const int hi_min = row0 + 31 < len ? query_hi<M>(a, sink ? min(kb, a.S) : row0, len) : 0;
+  const KeyRows<M, 32> seen(a, row0, len, lane);
+  const int lo_min = seen.lo_min, lo_max = seen.lo_max, hi_min = seen.hi_min, hi_max = row0 < len ? seen.hi_max : 0;
   unsigned char* const X = sm + R::BYTES + own * 4096 + lane * 16;
 
   R ring;
@@ -858,7 +902,7 @@ __device__ __forceinline__ void win_dkdv_pair(const AttnWinArgs& a, unsigned tas
     int qblk = w.nq ? w.n0 % w.nq : 0, qhead = h0 + (w.nq ? w.n0 / w.nq : 0);
     sc.head(a, min(qhead, a.A - 1));
     const bf16 *K = (const bf16*)a.k + r0 * a.ldk + w.kv * d, *V = (const bf16*)a.v + r0 * a.ldv + w.kv * d;
-    const int lo = query_lo<M>(a, krow), hi = kok ? query_hi<M>(a, krow, len) : 0;
+    const int lo = seen.lo, hi = seen.hi;
     constexpr int FD = capped(S) ? 2 : 4;
     bf16x8 kf[NKK], vf[NKK], qf[FD], gf[FD];   // (qf, gf: FD k-steps' fragments, read so many ahead of their use)
 #pragma unroll
@@ -1069,14 +1113,15 @@ __global__ __launch_bounds__(64 * RG * NG) void attn_win_fwd_f32(AttnWinArgs a, 
   const QueryTask<M, false> task(a, blockIdx.x, gridDim.x, q_tiles, 16 * RG, lane);
   if (!task.run) return;
   const int tile = task.tile, bi = task.bi, hh = task.hh;
-  const int kv = hh / (a.A / a.Ak), len = len_of<M>(a, bi), d = a.d;
+  Score<S> sc(a, scale2);
+  sc.head(a, hh);
+  const int kv = hh / (a.A / a.Ak), q0 = tile * 16 * RG, row0 = q0 + wave * 16, qrow = row0 + (lane & 15);
+  const WaveRows<M, 16> seen(a, bi, row0, q0, 16 * RG, lane);
+  const int len = seen.len, d = a.d, lo = seen.lo, hi = seen.hi, lo_min = seen.lo_min, hi_max = seen.hi_max;
   const long r0 = (long)bi * a.s;
   const float *Q = (const float*)a.q + r0 * a.ldq + hh * d, *K = (const float*)a.k + r0 * a.ldk + kv * d, *V = (const float*)a.v + r0 * a.ldv + kv * d;
-  const int q0 = tile * 16 * RG, row0 = q0 + wave * 16, qrow = row0 + (lane & 15), qb = last_row<M>(a, row0, 16, len);
-  const int lo_min = key_lo<M>(a, row0), hi_max = key_hi<M>(a, qb, len);
   const bool qok = qrow < len;
-  const KeyWalk<M> walk(a, q0, last_row<M>(a, q0, 16 * RG, len), len, BR);
-  const int lo = key_lo<M>(a, qrow), hi = qok ? key_hi<M>(a, qrow, len) : 0;
+  const KeyWalk<M> walk(a, seen.walk_lo, seen.walk_hi, q0 < len, BR);
   f32x4 qf[NK];
   own_row<D>(Q + (long)qrow * a.ldq, qok, d, lane, qf);
   F32Block<D, 64 * RG> kb, vb;
@@ -1087,8 +1132,6 @@ __global__ __launch_bounds__(64 * RG * NG) void attn_win_fwd_f32(AttnWinArgs a, 
   };
   __builtin_amdgcn_s_waitcnt(0x0F70);   // (the wave's own rows: waited for in the loop, the next block would be too)
   if (group < walk.n) load(group);
-  Score<S> sc(a, scale2);
-  sc.head(a, hh);
   float m = -3e38f, l = 0.f;
   f32x4 o[NK];   // rows d = 16 i + 4 g4 + e, column = the lane's query
 #pragma unroll
@@ -1216,21 +1259,20 @@ __device__ __forceinline__ void win_dq_f32(const AttnWinArgs& a, unsigned id, un
   const QueryTask<M, true> task(a, id, ids, q_tiles, 16 * RG, lane);
   if (!task.run) return;
   const int tile = task.tile, bi = task.bi, hh = task.hh;
-  const int kv = hh / (a.A / a.Ak), len = len_of<M>(a, bi), d = a.d;
+  Score<S> sc(a, scale2);
+  sc.head(a, hh);
+  const int kv = hh / (a.A / a.Ak), q0 = tile * 16 * RG, row0 = q0 + wave * 16, qrow = row0 + (lane & 15);
+  const WaveRows<M, 16> seen(a, bi, row0, q0, 16 * RG, lane);
+  const int len = seen.len, d = a.d, lo = seen.lo, hi = seen.hi, lo_min = seen.lo_min, hi_max = seen.hi_max;
   const long r0 = (long)bi * a.s;
   const float *K = (const float*)a.k + r0 * a.ldk + kv * d, *V = (const float*)a.v + r0 * a.ldv + kv * d;
-  const int q0 = tile * 16 * RG, row0 = q0 + wave * 16, qrow = row0 + (lane & 15), qb = last_row<M>(a, row0, 16, len);
-  const int lo_min = key_lo<M>(a, row0), hi_max = key_hi<M>(a, qb, len);
   const bool qok = qrow < len;
-  const KeyWalk<M> walk(a, q0, last_row<M>(a, q0, 16 * RG, len), len, BR);
-  const int lo = key_lo<M>(a, qrow), hi = qok ? key_hi<M>(a, qrow, len) : 0;
+  const KeyWalk<M> walk(a, seen.walk_lo, seen.walk_hi, q0 < len, BR);
   f32x4 qf[NK], gf[NK];
   own_row<D>((const float*)a.q + (r0 + qrow) * a.ldq + hh * d, qok, d, lane, qf);
   own_row<D>((const float*)a.dctx + (r0 + qrow) * a.lddc + hh * d, qok, d, lane, gf);
   const long st = ((long)bi * a.A + hh) * a.s + qrow;
   const float Lq = qok ? a.lse[st] : 0.f, Dq = qok ? a.delta[st] : 0.f;
-  Score<S> sc(a, scale2);
-  sc.head(a, hh);
   f32x4 dq[NK];
 #pragma unroll
   for (int i = 0; i < NK; ++i) dq[i] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -1313,10 +1355,8 @@ __device__ __forceinline__ void win_dkdv_f32(const AttnWinArgs& a, unsigned task
   const float *lse = a.lse + ((long)w.bi * a.A + h0) * a.s, *delta = a.delta + ((long)w.bi * a.A + h0) * a.s;
   const int row0 = w.k0 + wave * 16, krow = row0 + (lane & 15);
   const bool kok = krow < len;
-  const int lo = query_lo<M>(a, krow), hi = kok ? query_hi<M>(a, krow, len) : 0;
-  const int kb = last_row<M>(a, row0, 16, len);
-  const bool sink = is_sink<M>(a, row0);
-  const int lo_min = sink && !a.causal ? 0 : query_lo<M>(a, row0), hi_max = sink ? len : query_hi<M>(a, kb, len);
+  const KeyRows<M, 16> seen(a, row0, len, lane);
+  const int lo = seen.lo, hi = seen.hi, lo_min = seen.lo_min, hi_max = seen.hi_max;
   f32x4 kf[NK], vf[NK], sum[2 * NK];   // sums: dk, dv
   f32x4 *const dk = sum, *const dv = sum + NK;
   own_row<D>((const float*)a.k + (r0 + krow) * a.ldk + w.kv * d, kok, d, lane, kf);
