@@ -174,7 +174,8 @@ int dapple_attention_window_bwd(int dtype, const dapple_attention_window_desc* d
  * device int32 [n], clamped to the document, NULL = 0, only with causal.  Rows from ends[n - 1] on see nothing and are seen by nobody;
  * what q, k, v and dctx hold there is not used, their ctx, dq, dk, dv are set to 0, their lse to -infinity.  Before them, inputs are finite.
  *   logit = t - slopes[h] |i - j|,   t = cap tanh(scale q k / cap), or scale q k with cap = 0
- * slopes: device fp32 [A], NULL = 0; constants (they have no gradient).  cap: 0 or 2^-20 to 2^10.  scale > 0; 0 = 1/sqrt(d).
+ * slopes: device fp32 [A], NULL = 0; finite, and constants (they have no gradient).  cap: 0 or 2^-20 to 2^10.  scale > 0; 0 = 1/sqrt(d);
+ * scale / cap and cap / scale that fp32 does not hold as normal numbers are refused.
  * fwd: ctx, lse [A, rows] fp32 = log2 of the sum of 2^(log2(e) logit), ctx32 (may be NULL) as above.  bwd: dq, dk, dv from dctx and the ctx, ctx32
  * (or NULL) and lse of fwd.  spans holds what dapple_doc_spans left, of the same rows (other contents: wrong results, nothing worse).
  * Strides, alignment, limits (with b = 1, s = rows; up to 2^26 - 8), rounding and overlaps as for dapple_attention_window; workspace: below
@@ -333,7 +334,7 @@ int dapple_dropout_norm_bwd(int dtype, const dapple_dropout_norm_desc* d, void* 
  * bwd: accumulate = 0: dtable is of dtype and set, rows of absent ids to zero; accumulate != 0: fp32, and added to, rows of absent ids
  * are not touched.  Sums in fp32, each id's rows in an order that sizes and ids alone decide.
  * Outputs overlap no input.  rows, V <= 2^28, H <= 2^16; any strides and addresses of whole elements; workspace: 16 bytes a row, and at most
- * 64 KiB a column. */
+ * 64 KiB a column and 512 KiB. */
 typedef struct {
   const void* table;
   const int32_t* ids;

@@ -265,7 +265,7 @@ def test_attention_docs_refusals():
             (conf, dict(scale=math.nan)), (conf, dict(cap=-1.0)), (conf, dict(cap=1e-7)), (conf, dict(cap=1025.0)), (conf, dict(cap=math.inf)),
             (conf, dict(cap=math.nan)), (conf, dict(ldq=255)), (conf, dict(ldk=-8)), (conf, dict(ldv=1 << 23)), (conf, dict(rows=1 << 22, ldq=264)),
             (conf, dict(q=P + 8)), (conf, dict(ctx32=P + 4)), (conf, dict(lse=P + 2)), (conf, dict(spans=P + 2)), (conf, dict(slopes=P + 1)),
-            (conf, dict(rows=(1 << 26) - 7))]
+            (conf, dict(rows=(1 << 26) - 7)), (conf, dict(scale=1e38, cap=2.0 ** -20)), (conf, dict(scale=1e-38, cap=1024.0))]
     for code, change in both:
         for f in (B.dapple_attention_docs_fwd, B.dapple_attention_docs_bwd):
             refused(code, f, B.DTYPE_BF16, B.attention_docs_desc(**dict(ok, **change)))
