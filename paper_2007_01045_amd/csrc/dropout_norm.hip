@@ -177,6 +177,20 @@ __global__ __launch_bounds__(64 * row_waves<NW>()) void dropout_norm_bwd(DropNor
   const int at = wave % NW, groups = (a.H + 7) / 8;
   int turn = 0;
   const Philox gen(a.rng, a.site);
+  // Four chunks of a lane are more than its registers hold: dgamma's and dbeta's sums are in LDS (a lane's own), only z and dy of the next row
+  // come in ahead, and beside an fp32 stream gamma is loaded for every row.  Us, 4096 rows of 16384, all in registers and memory / so: layer,
+  // fp32 stream 627 / 257, RMS 479 / 222; 8192 rows of bf16, layer 759 / 266 (with gamma loaded 309; beside the fp32 stream, not loaded, 306).
+  constexpr bool WIDE = NORM && NCH == 4, GAMMA_AGAIN = WIDE && sizeof(Z) == 4;
+  __shared__ f32x4 kept[WIDE ? 2 * NCH * 2 * 64 * NW : 1];
+  auto in_lds = [&](int v, int c, int half) -> f32x4& { return kept[((v * NCH + c) * 2 + half) * 64 * NW + threadIdx.x]; };
+  auto fetch = [&](int v, int c, float (&x)[8]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = in_lds(v, c, e / 4)[e % 4];
+  };
+  auto keep = [&](int v, int c, const float (&x)[8]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int e = 0; e < 8; e += 4) in_lds(v, c, e / 4) = f32x4{x[e], x[e + 1], x[e + 2], x[e + 3]};
+  };
   float gam[NCH][8], sum[3][NCH][8];
   int col[NCH];
 #pragma unroll
@@ -184,7 +198,8 @@ __global__ __launch_bounds__(64 * row_waves<NW>()) void dropout_norm_bwd(DropNor
     col[c] = ((c * NW + at) * 64 + lane) * 8;
 #pragma unroll
     for (int e = 0; e < 8; ++e) gam[c][e] = 1.f, sum[0][c][e] = sum[1][c][e] = sum[2][c][e] = 0.f;
-    if (NORM && a.gamma && col[c] < a.H) load8((const T*)a.gamma + col[c], a.H - col[c], gam[c]);
+    if (NORM && !GAMMA_AGAIN && a.gamma && col[c] < a.H) load8((const T*)a.gamma + col[c], a.H - col[c], gam[c]);
+    if (WIDE) keep(0, c, sum[0][c]), keep(1, c, sum[0][c]);
   }
   Raw8<Z> gn[NCH] = {}, hn[NCH] = {};
   Raw8<T> tn[NCH] = {};
@@ -193,7 +208,7 @@ __global__ __launch_bounds__(64 * row_waves<NW>()) void dropout_norm_bwd(DropNor
 #pragma unroll
     for (int c = 0; c < NCH; ++c) {
       if (col[c] >= a.H) continue;
-      if (a.dz) gn[c].load((const Z*)a.dz + row * a.lddz + col[c], a.H - col[c]);
+      if (!WIDE && a.dz) gn[c].load((const Z*)a.dz + row * a.lddz + col[c], a.H - col[c]);
       if (NORM) hn[c].load((const Z*)a.z + row * a.ldz + col[c], a.H - col[c]);
       if (NORM) tn[c].load((const T*)a.dy + row * a.lddy + col[c], a.H - col[c]);
     }
@@ -206,30 +221,53 @@ __global__ __launch_bounds__(64 * row_waves<NW>()) void dropout_norm_bwd(DropNor
   for (; row < a.rows; row += step) {
     float g[NCH][8], h[NCH][8], t[NCH][8];
 #pragma unroll
-    for (int c = 0; c < NCH; ++c)
+    for (int c = 0; c < NCH; ++c) {
+      if (WIDE && a.dz && col[c] < a.H) gn[c].load((const Z*)a.dz + row * a.lddz + col[c], a.H - col[c]);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) g[c][e] = gn[c].get(e), h[c][e] = hn[c].get(e), t[c][e] = tn[c].get(e);
+      for (int e = 0; e < 8; ++e) {
+        h[c][e] = hn[c].get(e), t[c][e] = tn[c].get(e);
+        if (!WIDE) g[c][e] = gn[c].get(e);
+      }
+    }
     const float mean = mean_n, rstd = rstd_n;
     if (row + step < a.rows) load(row + step);   // (beside this row's sums)
     if constexpr (NORM != NORM_NONE) {
       float s[2] = {0.f, 0.f};
 #pragma unroll
-      for (int c = 0; c < NCH; ++c)
+      for (int c = 0; c < NCH; ++c) {
+        float again[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
+        if (GAMMA_AGAIN && a.gamma && col[c] < a.H) load8((const T*)a.gamma + col[c], a.H - col[c], again);
+        auto add = [&](float (&dgam)[8], float (&dbet)[8]) __attribute__((always_inline)) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            h[c][e] = (h[c][e] - mean) * rstd;     // (behind the row's end t is 0)
+            dgam[e] = fmaf(t[c][e], h[c][e], dgam[e]);
+            if (NORM == NORM_LAYER) dbet[e] += t[c][e];
+          }
+        };
+        if constexpr (WIDE) {
+          float x[8], y[8];
+          fetch(0, c, x);
+          if (NORM == NORM_LAYER) fetch(1, c, y);
+          add(x, y);
+          keep(0, c, x);
+          if (NORM == NORM_LAYER) keep(1, c, y);
+        } else {
+          add(sum[1][c], sum[2][c]);
+        }
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          h[c][e] = (h[c][e] - mean) * rstd;     // (behind the row's end t is 0)
-          sum[1][c][e] = fmaf(t[c][e], h[c][e], sum[1][c][e]);
-          if (NORM == NORM_LAYER) sum[2][c][e] += t[c][e];
-          t[c][e] *= gam[c][e];
+          t[c][e] *= GAMMA_AGAIN ? again[e] : gam[c][e];
           s[0] += t[c][e];
           s[1] = fmaf(t[c][e], h[c][e], s[1]);
         }
+      }
       row_sums<NW>(s, red, turn);
       const float m0 = NORM == NORM_LAYER ? s[0] / (float)a.H : 0.f, m1 = s[1] / (float)a.H;
 #pragma unroll
       for (int c = 0; c < NCH; ++c)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) g[c][e] = fmaf(rstd, fmaf(-h[c][e], m1, t[c][e] - m0), g[c][e]);
+        for (int e = 0; e < 8; ++e) g[c][e] = fmaf(rstd, fmaf(-h[c][e], m1, t[c][e] - m0), WIDE ? gn[c].get(e) : g[c][e]);
     }
 #pragma unroll
     for (int c = 0; c < NCH; ++c) {
@@ -246,6 +284,10 @@ __global__ __launch_bounds__(64 * row_waves<NW>()) void dropout_norm_bwd(DropNor
   for (int v = 0; v < (NORM == NORM_LAYER ? 3 : NORM == NORM_RMS ? 2 : 1); ++v) {
     if (!(v == 0 ? a.dbias : v == 1 ? a.dgamma : a.dbeta)) continue;
     float* const P = a.partial + ((long)blockIdx.x * 3 + v) * a.H;
+    if (WIDE && v) {
+#pragma unroll
+      for (int c = 0; c < NCH; ++c) fetch(v - 1, c, sum[v][c]);
+    }
     if constexpr (NW == 1) {   // the four waves' sums of the same columns, in their order
       __syncthreads();
 #pragma unroll

@@ -136,6 +136,7 @@ CASES = [  # dtype, rows, H, norm, p, stream32
     (H16, 2500, 24, LAYER, 0.1, False), (H16, 9000, 40, RMS, 0.1, False), (H16, 3001, 1100, LAYER, 0.1, False), (H16, 12, 256, LAYER, 1.0, False),
     (F, 1, 1, LAYER, 0.1, False), (F, 2, 3, RMS, 0.5, False), (F, 19, 250, LAYER, 0.1, False), (F, 30, 1024, LAYER, 0.1, True), (F, 31, 1001, RMS, 0.2, False),
     (F, 11, 2047, LAYER, 0.1, False), (F, 9, 4096, NONE, 0.1, False), (F, 5, 8191, LAYER, 0.1, False), (F, 3, 16384, LAYER, 0.1, False), (F, 1200, 520, LAYER, 0.1, False),
+    (H16, 600, 8200, LAYER, 0.1, True), (H16, 520, 16384, LAYER, 0.1, False), (F, 530, 12288, LAYER, 0.1, False), (F, 520, 8208, RMS, 0.1, False),
 ]
 ids = lambda c: "-".join(str(v) for v in c)  # noqa: E731
 
