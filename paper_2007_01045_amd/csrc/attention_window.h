@@ -84,53 +84,26 @@ __device__ __forceinline__ bool is_sink(const AttnWinArgs& a, int j) { return M 
 
 // The logit, in log2 units, of a product `raw`: unit t - slope2 |distance|, where t is raw, or its cap:
 //   t = tanh(x), x = raw scale / cap, unit = cap log2(e);   d logit / d raw = (1 - t^2) scale log2(e).
-// The cap is bound by its instructions (an exponential or a reciprocal takes four times one of the others).  Where |x| <= 0.6 for all that
-// a wave looks at, tanh(x) = x (1 + c1 x^2 + c2 x^4 + c3 x^6), c fitted for the least relative error, 2.5e-6, which is below 2^-13 of a probability for any
-// logit up to 30; else each logit has that or, by its own size alone (what stands beside it must not show), tanh(x) = 1 - 2 r, r = 1 / (1 +
-// e^2x), off by 2^-23 of 1.
-// Us forward and gradient with the polynomial / with that always, 4 documents of 2048 rows, both directions, cap 50, normal q and k: 16 heads of 128 on 4
-// 223 + 563 / 246 + 689, 16 of 64 135 + 364 / 191 + 466.
+// tanh(x) = 1 - 2 / (1 + e^2x), off by an ulp or two of 1 whatever x: two instructions of four times
+// the others' time.  Us forward and gradient, 4 documents of 2048 rows, both directions, cap 50, products up to about 30 / four times that and more: 16
+// heads of 128 on 4 208 + 554 / 186 + 558, of 64 124 + 352 / 127 + 358.  A polynomial where all products of a wave's block are small, and there alone,
+// took 205 + 547 / 238 + 691 and 125 + 353 / 187 + 463.
 constexpr bool capped(int S) { return S == SCORE_CAP || S == SCORE_BOTH; }
 constexpr bool sloped(int S) { return S == SCORE_SLOPE || S == SCORE_BOTH; }
 template <int S>
 struct Score {
-  float unit, slope2, bend, small, c1, c2, c3;   // slope2: -slope log2(e); bend: scale / cap; small: 0.6 / bend; c: with powers of bend
-  __device__ __forceinline__ Score(const AttnWinArgs& a, float scale2) : unit(capped(S) ? a.cap2 : scale2), slope2(0.f), bend(a.bend), small(a.small),
-    c1(a.poly[0]), c2(a.poly[1]), c3(a.poly[2]) {}
+  float unit, slope2, bend, bend2;   // slope2: -slope log2(e); bend: scale / cap; bend2 = 2 bend log2(e)
+  __device__ __forceinline__ Score(const AttnWinArgs& a, float scale2) : unit(capped(S) ? a.cap2 : scale2), slope2(0.f), bend(a.bend), bend2(a.bend * (2.f * LOG2E)) {}
   __device__ __forceinline__ void head(const AttnWinArgs& a, int h) {
     if (sloped(S)) slope2 = a.slopes ? a.slopes[h] * -LOG2E : 0.f;
   }
-  __device__ __forceinline__ float polynomial(float raw) const {
-    const float y = raw * raw;
-    return raw * fmaf(fmaf(fmaf(c3, y, c2), y, c1), y, bend);
+  __device__ __forceinline__ float of(float raw) const {   // t
+    return capped(S) ? fmaf(-2.f, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(raw * bend2)), 1.f) : raw;
   }
-  // whether the wave's products are all small
-  template <typename V>
-  __device__ __forceinline__ bool is_small(const V& raw) const {
-    float m = 0.f;
-#pragma unroll
-    for (int v = 0; v < 16; v += 2) m = fmaxf(m, fmaxf(fabsf(raw[v]), fabsf(raw[v + 1])));
-    return __builtin_amdgcn_ballot_w64(m <= small) == ~0ull;
-  }
-  template <typename V>
-  __device__ __forceinline__ void cap_all(V& raw) const {
-#pragma unroll
-    for (int v = 0; v < 16; ++v) {
-      const float t = polynomial(raw[v]), r = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(raw[v] * bend * (2.f * LOG2E)));
-      raw[v] = fabsf(raw[v]) <= small ? t : fmaf(-2.f, r, 1.f);
-    }
-  }
-  // raw = t
   template <typename V>
   __device__ __forceinline__ void cap(V& raw) const {
-    if constexpr (capped(S)) {
-      if (is_small(raw)) {
 #pragma unroll
-        for (int v = 0; v < 16; ++v) raw[v] = polynomial(raw[v]);
-      } else {
-        cap_all(raw);
-      }
-    }
+    for (int v = 0; v < 16; ++v) raw[v] = of(raw[v]);
   }
   // the logit less l; far: the rows' distance, of either sign
   __device__ __forceinline__ float less(float t, float far, float l) const {
@@ -903,7 +876,7 @@ __device__ __forceinline__ void win_dkdv_pair(const AttnWinArgs& a, unsigned tas
     sc.head(a, min(qhead, a.A - 1));
     const bf16 *K = (const bf16*)a.k + r0 * a.ldk + w.kv * d, *V = (const bf16*)a.v + r0 * a.ldv + w.kv * d;
     const int lo = seen.lo, hi = seen.hi;
-    constexpr int FD = capped(S) ? 2 : 4;
+    constexpr int FD = 4;
     bf16x8 kf[NKK], vf[NKK], qf[FD], gf[FD];   // (qf, gf: FD k-steps' fragments, read so many ahead of their use)
 #pragma unroll
     for (int kk = 0; kk < NKK; ++kk) {
@@ -924,7 +897,7 @@ __device__ __forceinline__ void win_dkdv_pair(const AttnWinArgs& a, unsigned tas
     // sa, dp: S and dP of the current step (rows: query 8 blk + 4 h + e of its block, column: key); sn, dn: of the next one, made
     // meanwhile: two MFMAs and two elements' exponentials by turns
     enum { HIDDEN, WHOLE, PART };
-    auto step = [&](auto MODE, auto CAPPED, const f32x16& sa, const f32x16& dp, f32x16& sn, f32x16& dn, unsigned cur, unsigned at, unsigned next, unsigned char* x,
+    auto step = [&](auto MODE, const f32x16& sa, const f32x16& dp, f32x16& sn, f32x16& dn, unsigned cur, unsigned at, unsigned next, unsigned char* x,
                     int j0) __attribute__((always_inline)) {
       constexpr int mode = decltype(MODE)::value;
       const float *Ls = (const float*)(sm + cur + R::S_OFF) + 4 * h, *Ds = Ls + 64;
@@ -947,7 +920,7 @@ __device__ __forceinline__ void win_dkdv_pair(const AttnWinArgs& a, unsigned tas
         if constexpr (mode != HIDDEN) {
 #pragma unroll
           for (int v = 2 * kk; v < 2 * kk + 2; ++v) {
-            const float t = capped(S) && !decltype(CAPPED)::value ? sc.polynomial(sa[v]) : sa[v];
+            const float t = sc.of(sa[v]);
             p[v] = __builtin_amdgcn_exp2f(sc.less(t, (float)(krow - j0 - 4 * h) - (8 * (v >> 2) + (v & 3)), L4[v >> 2][v & 3]));
             ds[v] = (dp[v] + D4[v >> 2][v & 3]) * p[v];
             if (capped(S)) ds[v] *= sc.derivative(t);
@@ -987,7 +960,7 @@ __device__ __forceinline__ void win_dkdv_pair(const AttnWinArgs& a, unsigned tas
       }
     }
     int n = w.n0;
-    auto one = [&](f32x16& sa, const f32x16& dp, f32x16& sn, f32x16& dn) __attribute__((always_inline)) {
+    auto one = [&](const f32x16& sa, const f32x16& dp, f32x16& sn, f32x16& dn) __attribute__((always_inline)) {
       const int after = slot_after(at), j0 = (w.qlo + qblk) * 32;
       if (sloped(S) && qblk == 0) sc.head(a, min(qhead, a.A - 1));
       qblk = qblk + 1 == w.nq ? 0 : qblk + 1;
@@ -996,14 +969,9 @@ __device__ __forceinline__ void win_dkdv_pair(const AttnWinArgs& a, unsigned tas
       barrier();
       ask();
       const unsigned c = cur * R::STAGE, f = at * R::STAGE, g = after * R::STAGE;
-      if (j0 >= hi_max || j0 + 31 < lo_min) step(Hidden{}, std::false_type{}, sa, dp, sn, dn, c, f, g, x, j0);   // none of the wave's keys is seen
-      else if (!capped(S) || sc.is_small(sa)) {
-        if (lo_max > j0 || hi_min < j0 + 32) step(Part{}, std::false_type{}, sa, dp, sn, dn, c, f, g, x, j0);
-        else step(Whole{}, std::false_type{}, sa, dp, sn, dn, c, f, g, x, j0);
-      } else {
-        sc.cap_all(sa);
-        step(Part{}, std::integral_constant<bool, capped(S)>{}, sa, dp, sn, dn, c, f, g, x, j0);
-      }
+      if (j0 >= hi_max || j0 + 31 < lo_min) step(Hidden{}, sa, dp, sn, dn, c, f, g, x, j0);   // none of the wave's keys is seen
+      else if (lo_max > j0 || hi_min < j0 + 32) step(Part{}, sa, dp, sn, dn, c, f, g, x, j0);
+      else step(Whole{}, sa, dp, sn, dn, c, f, g, x, j0);
       cur = at;
       at = after;
       return ++n < w.n1;

@@ -254,10 +254,10 @@ struct AttnWinArgs {
   float scale;
   WinPlan plan;
   // attention_docs.hip: b = 1 and s packed rows, W = S = 0; what a row sees (launch_doc_spans); slopes [A] or NULL;
-  // cap2 = cap log2(e) (0: none), bend = scale / cap, small: up to where a product's cap is a polynomial (Score; negative: nowhere)
+  // cap2 = cap log2(e) (0: none), bend = scale / cap
   const int32_t* spans;
   const float* slopes;
-  float cap2, bend, small, poly[3];
+  float cap2, bend;
   int32_t* table;   // of docs_plan
 };
 enum { MASK_WINDOW = 0, MASK_SPANS = 1 };

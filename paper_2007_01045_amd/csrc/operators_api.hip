@@ -101,15 +101,7 @@ static int docs_args(int dtype, const dapple_attention_docs_desc* d, bool bwd, b
   if (d->cap > 0.f) {
     a.cap2 = (float)(d->cap * 1.4426950408889634);
     a.bend = a.scale / d->cap;
-    a.small = 0.6f / a.bend;
-    if (!std::isnormal(a.bend) || !std::isnormal(a.small)) return set_error(STAGE_E_CONFIG, "scale %g over cap %g", a.scale, d->cap);
-    const double c[3] = {-0.33319074494554746, 0.1308641832442356, -0.041387786259018865};   // (see Score)
-    double power = a.bend;
-    for (int i = 0; i < 3; ++i) {
-      power *= (double)a.bend * a.bend;
-      a.poly[i] = (float)(c[i] * power);
-      if (!std::isnormal(a.poly[i])) a.small = -1.f;
-    }
+    if (!std::isnormal(a.bend) || !std::isnormal(1.f / a.bend)) return set_error(STAGE_E_CONFIG, "scale %g over cap %g", a.scale, d->cap);
   }
   return STAGE_OK;
 }
