@@ -24,6 +24,7 @@
 #include <type_traits>
 
 #include "attention_tile.h"
+#include "walk_parts.h"
 
 namespace dapple {
 
@@ -1451,7 +1452,7 @@ __device__ __forceinline__ void docs_plan(const AttnWinArgs& a) {
   auto walk = [&](int tile) {
     w.k0 = tile * p.kt;
     w.span(a, p.kt, p.blk);
-    return w.nq * G;   // (below 2^31: A times blocks of 32 rows is)
+    return w.nq * G;   // (below 2^23: A times blocks of 32 rows is)
   };
   if (tid == 0) all = 0, slots = cuts = 0;
   if (tid < NB) count[tid] = 0;
@@ -1462,8 +1463,8 @@ __device__ __forceinline__ void docs_plan(const AttnWinArgs& a) {
   for (int t = tid; t < p.key_tiles; t += 256) mine += length(t);
   atomicAdd(&all, mine);
   __syncthreads();
-  const int steps = (int)max((unsigned long long)p.min_steps, (all * a.Ak + p.units - 1) / p.units);
-  auto parts_of = [&](int n) { return n > steps ? (n + steps - 1) / steps : 1; };
+  const int steps = walk_share(all, a.Ak, p.units, p.min_steps);
+  auto parts_of = [&](int n) { return walk_parts(n, steps); };
   auto bucket = [&](int n) { return NB - 1 - min(NB - 1, (int)((long)n * NB / (steps + 1))); };
   for (int t = tid; t < p.key_tiles; t += 256) {
     const int n = length(t), parts = parts_of(n);
