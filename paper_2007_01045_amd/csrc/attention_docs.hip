@@ -28,7 +28,7 @@ __global__ __launch_bounds__(256) void doc_spans_kernel(const int32_t* __restric
     auto end_of = [&](int t) { return n <= NEAR_ENDS ? near[t] : ends[t]; };
     int lo = 0, hi = n - 1;   // the first document that ends behind row i
     while (lo < hi) {
-      const int mid = (lo + hi) >> 1;
+      const int mid = lo + ((hi - lo) >> 1);   // (the sum of two may be beyond an int)
       if (end_of(mid) > i) hi = mid;
       else lo = mid + 1;
     }
