@@ -4,6 +4,7 @@ import pytest
 import torch
 
 from paper_2007_01045_amd import binding as B
+from tests.test_gpu_attention_docs import Case, F, H, name
 
 pytestmark = pytest.mark.gpu
 
@@ -20,3 +21,89 @@ def test_spans_of_more_than_2_to_the_30_documents():
     for i in range(rows):
         begin, end = (0, 40) if i < 40 else (40, 90)
         assert (lo[i], hi[i], qlo[i], qhi[i]) == ((begin, i + 1, i, end) if i < 90 else (90,) * 4), i
+
+
+def short(n, of=200):
+    """n documents of 30 to 30 + of rows"""
+    return [30 + (t * 53) % of for t in range(n)]
+
+
+# rows beyond 64 tiles of queries (ranked in groups of neighbours where a launch has more than 256 of them) and 256 of keys (more than the plan has
+# threads), walks of one document that are cut among many that are not
+LONG = [  # dtype, rows, docs, A, Ak, d, causal, prefix, W, cap, slope
+    (H, 9000, short(20) + [2400] + short(25) + [1], 8, 4, 64, True, None, 0, 0.0, 0.05), (H, 20011, short(60) + [2800, 1900] + short(40), 4, 1, 32, True, True, 0, 30.0, 0.0),
+    (H, 18000, [2300] + short(100), 1, 1, 64, False, None, 0, 0.0, 0.0), (H, 34000, short(130) + [2800] + short(80), 4, 2, 64, True, True, 0, 0.0, 0.0),
+    (H, 34000, short(130) + [2800] + short(90), 8, 2, 128, True, None, 0, 50.0, 0.0), (H, 33333, short(200) + [2000, 33], 4, 4, 80, False, None, 300, 50.0, 0.05),
+    (F, 8300, short(30) + [1700] + short(15), 2, 1, 64, True, None, 0, 0.0, 0.0), (F, 17000, short(50) + [1800] + short(40), 4, 2, 32, True, True, 0, 20.0, 0.05),
+]
+# heads wider than 64 whose dq is in the launch of dk and dv: every kind of logits
+WIDE = [(H, 2100, [900, 0, 700, 450], 32, 8, 128, causal, causal or None, W, cap, slope)
+        for causal, W, cap, slope in ((True, 0, 0.0, 0.0), (True, 0, 50.0, 0.0), (True, 0, 50.0, 0.1), (True, 0, 0.0, 0.1), (False, 150, 30.0, 0.1))]
+# more documents than are searched in LDS, a few of them empty
+MANY = [(dtype, 4500, [0, 1, 2, 3, 4] * 420 + [200], 4, 2, 64, True, True, 0, 20.0, 0.1) for dtype in (F, H)]
+
+
+@pytest.mark.parametrize("case", LONG + WIDE + MANY, ids=name)
+def test_forward_and_backward(case):
+    c = Case(*case)
+    c.run()
+    c.check()
+    first = c.dqkv.clone()      # (the plan lists its parts in an order that may change: no result goes by it)
+    c.dqkv.fill_(3)
+    c.run()
+    w = c.ld - c.pad
+    assert torch.equal(c.dqkv[:, :w], first[:, :w])
+
+
+@pytest.mark.parametrize("rows", [2090, 2091, 2092, 9000])
+def test_spans_of_many_documents(rows):
+    # one row each but for an empty one behind every seventh, and a long one: 2047, 2048, 2049 and 9944 of them
+    docs = [n for t in range(rows - 300) for n in ((1, 0) if t % 7 == 0 else (1,))] + [290]
+    ends = torch.tensor(docs).cumsum(0).int().cuda()
+    spans = torch.full((4 * rows + 1,), -9, dtype=torch.int32, device="cuda")
+    B.dapple_doc_spans(ends.data_ptr(), len(docs), rows, spans.data_ptr(), causal=0)
+    length = torch.tensor(docs, device="cuda")
+    end = ends.long().repeat_interleave(length)
+    begin = (ends - length).long().repeat_interleave(length)
+    behind = torch.full((10,), rows - 10, device="cuda")
+    lo, hi, qlo, qhi = spans[:-1].view(4, rows).long()
+    assert int(spans[-1]) == rows - 10
+    for got, want in ((lo, begin), (hi, end), (qlo, begin), (qhi, end)):
+        assert torch.equal(got, torch.cat([want, behind]))
+
+
+@pytest.mark.parametrize("s, A, Ak, d, W", [(300, 4, 2, 64, 90), (3000, 4, 1, 64, 0), (2500, 16, 4, 128, 0), (2500, 32, 8, 128, 700)])
+@pytest.mark.parametrize("dtype", [F, H])
+def test_gradients_equal_to_the_window_operator(dtype, s, A, Ak, d, W):
+    """One document, no cap, no slopes: dq is of the same products in the same order, dk and dv of the same products, whose walks may be cut
+    elsewhere.  A sum of m products in whatever order is off by m * 2^-24 of their sizes at most, and both are rounded once (r)."""
+    c = Case(dtype, s, [s], A, Ak, d, True, None, W, pad=0)
+    c.run()
+    got = c.dqkv.clone()
+    t = c.desc()
+    w = B.attention_window_desc(**{n: getattr(t, n) for n in ("q", "k", "v", "ctx", "ctx32", "lse", "dctx", "dq", "dk", "dv", "ldq", "ldk", "ldv", "ldc", "lddc", "lddq",
+                                                               "lddk", "lddv")}, b=1, s=s, A=A, Ak=Ak, d=d, window=W, causal=1)
+    ws = torch.empty(B.dapple_attention_window_workspace(dtype, w), dtype=torch.uint8, device="cuda")
+    w.workspace = ws.data_ptr()
+    c.dqkv.zero_()
+    B.dapple_attention_window_fwd(dtype, w)
+    B.dapple_attention_window_bwd(dtype, w)
+    assert torch.equal(got[:, :A * d], c.dqkv[:, :A * d])
+    heads = lambda t, at, n: t[:, at * d:(at + n) * d].double().view(s, n, d).transpose(0, 1)  # noqa: E731
+    q, k, v, g = heads(c.qkv, 0, A), heads(c.qkv, A, Ak), heads(c.qkv, A + Ak, Ak), heads(c.dctx, 0, A)
+    i = torch.arange(s, device="cuda")
+    gap = i[:, None] - i[None, :]
+    hidden = (gap < 0) | (gap >= (W or s))
+    r, m = (2.0 ** -8 if dtype == H else 2.0 ** -24), s * A // Ak
+    scale = d ** -0.5
+    for h in range(Ak):
+        sizes = [torch.zeros(s, d, dtype=torch.float64, device="cuda") for _ in range(2)]
+        for a in range(h * A // Ak, (h + 1) * A // Ak):
+            p = torch.softmax((q[a] @ k[h].T.contiguous() * scale).masked_fill_(hidden, float("-inf")), -1)
+            ds = p * (g[a] @ v[h].T.contiguous() - (g[a] * (p @ v[h])).sum(-1, keepdim=True))
+            sizes[0] += scale * (ds.abs().T.contiguous() @ q[a].abs())
+            sizes[1] += p.T.contiguous() @ g[a].abs()
+        for at, size in ((A + h, sizes[0]), (A + Ak + h, sizes[1])):
+            one, two = (x[:, at * d:(at + 1) * d].double() for x in (got, c.dqkv))
+            # (dS near 0 is itself off by 2^-13 of its terms at most, the probabilities by as much of themselves: the sizes' twice is enough)
+            assert bool(((one - two).abs() <= 2 * m * 2.0 ** -24 * 2 * size + r * (one.abs() + two.abs()) + 1e-12).all()), (at, "differs")
