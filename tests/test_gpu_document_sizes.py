@@ -107,3 +107,58 @@ def test_gradients_equal_to_the_window_operator(dtype, s, A, Ak, d, W):
             one, two = (x[:, at * d:(at + 1) * d].double() for x in (got, c.dqkv))
             # (dS near 0 is itself off by 2^-13 of its terms at most, the probabilities by as much of themselves: the sizes' twice is enough)
             assert bool(((one - two).abs() <= 2 * m * 2.0 ** -24 * 2 * size + r * (one.abs() + two.abs()) + 1e-12).all()), (at, "differs")
+
+
+# more key heads than a launch has shares, one, one and two of them; a bias that rises with the distance; prefixes beyond a tile of queries
+OTHERS = [(H, 1100, [1090], 200, 200, 64, True, None, 0, 0.0, 0.0), (H, 300, [100, 190], 256, 256, 32, False, None, 0, 20.0, 0.0), (F, 700, [690], 172, 172, 16, True, None, 0, 0.0, 0.0),
+          (H, 500, [170, 320], 8, 2, 64, True, None, 0, 0.0, -0.1), (H, 500, [320, 170], 8, 2, 128, False, None, 0, 30.0, -0.1), (F, 500, [320, 170], 4, 2, 64, True, True, 0, 0.0, -0.1),
+          (H, 900, [800, 77], 4, 2, 64, True, [500, 77], 0, 0.0, 0.1), (H, 900, [800, 77], 4, 2, 128, True, [500, 100], 300, 0.0, 0.0), (F, 900, [800, 77], 4, 2, 64, True, [500, 0], 0, 0.0, 0.0)]
+
+
+@pytest.mark.parametrize("case", OTHERS, ids=name)
+def test_other_heads_slopes_and_prefixes(case):
+    c = Case(*case)
+    c.run()
+    c.check()
+
+
+@pytest.mark.parametrize("dtype", [F, H])
+def test_tensors_of_their_own_strides(dtype):
+    # as they lie in one buffer, and each in a buffer of its own with another stride: the same bits
+    c = Case(dtype, 333, [100, 33, 180], 4, 2, 64, True, True, 0, 30.0, 0.1)
+    c.run()
+    A, Ak, d, rows = c.A, c.Ak, c.d, c.rows
+    td, t = c.qkv.dtype, c.desc()
+    room = lambda heads, more, kind=td: torch.full((rows, heads * d + more), 7.0, device="cuda").to(kind)  # noqa: E731
+    q, k, v, g = room(A, 16), room(Ak, 0), room(Ak, 40), room(A, 72)
+    for to, src, at, heads in ((q, c.qkv, 0, A), (k, c.qkv, A, Ak), (v, c.qkv, A + Ak, Ak), (g, c.dctx, 0, A)):
+        to[:, :heads * d] = src[:, at * d:(at + heads) * d]
+    ctx, c32, lse, dq, dk, dv = room(A, 24), room(A, 24, torch.float32), torch.empty_like(c.lse), room(A, 8), room(Ak, 56), room(Ak, 0)
+    for n, x in dict(q=q, k=k, v=v, ctx=ctx, ctx32=c32, lse=lse, dctx=g, dq=dq, dk=dk, dv=dv).items():
+        setattr(t, n, x.data_ptr())
+    for n, x in dict(ldq=q, ldk=k, ldv=v, ldc=ctx, lddc=g, lddq=dq, lddk=dk, lddv=dv).items():
+        setattr(t, n, x.shape[1])
+    t.ldk = t.lddv = 0      # (dense)
+    B.dapple_attention_docs_fwd(dtype, t)
+    B.dapple_attention_docs_bwd(dtype, t)
+    for got, want, at, heads in ((ctx, c.ctx, 0, A), (c32, c.c32, 0, A), (dq, c.dqkv, 0, A), (dk, c.dqkv, A, Ak), (dv, c.dqkv, A + Ak, Ak)):
+        assert torch.equal(got[:, :heads * d], want[:, at * d:(at + heads) * d]) and bool((got[:, heads * d:] == 7).all())
+    assert torch.equal(lse, c.lse)
+
+
+@pytest.mark.parametrize("dtype", [F, H])
+def test_offsets_beyond_32_bits(dtype):
+    # rows up to the last that the operator takes at this stride (below 2^30 - 4096 elements, 4 GiB in fp32); the documents at the end are checked
+    rows, docs = 1 << 20, [200, 1, 320, 55]
+    pad = 1016 - 4 * 64
+    n = sum(docs)
+    front = [1] * 63 + [1 << 10] * 1023
+    front += [rows - n - 7 - sum(front)]
+    c = Case(dtype, rows, front + docs, 2, 1, 64, True, None, 0, 0.0, 0.1, pad=pad)
+    assert c.ld == 1016 and rows * c.ld < (1 << 30) - 4096
+    c.run()
+    at = rows - n - 7
+    assert c.len == rows - 7
+    small = Case(dtype, n + 7, docs, 2, 1, 64, True, None, 0, 0.0, 0.1, pad=pad)
+    small.qkv, small.dctx, small.ctx, small.c32, small.dqkv, small.lse = c.qkv[at:], c.dctx[at:], c.ctx[at:], c.c32[at:], c.dqkv[at:], c.lse[:, at:]
+    small.check()
