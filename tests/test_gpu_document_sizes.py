@@ -162,3 +162,20 @@ def test_offsets_beyond_32_bits(dtype):
     small = Case(dtype, n + 7, docs, 2, 1, 64, True, None, 0, 0.0, 0.1, pad=pad)
     small.qkv, small.dctx, small.ctx, small.c32, small.dqkv, small.lse = c.qkv[at:], c.dctx[at:], c.ctx[at:], c.c32[at:], c.dqkv[at:], c.lse[:, at:]
     small.check()
+
+
+@pytest.mark.parametrize("cap", [2.0 ** -20, 1.0, 50.0, 1024.0])
+@pytest.mark.parametrize("dtype", [F, H])
+def test_how_far_capped_logits_are_off(dtype, cap):
+    """Documents of one row: lse is the logit.  bf16: tanh is off by 2^-21 whatever it is; fp32: by the roundings of its argument (three) and its own
+    (two); both: the constants and products around it and log2 of the sum, five roundings of the logit more."""
+    rows = 20000
+    x = torch.cat([torch.linspace(-12, 12, rows // 2, device="cuda"), 2.0 ** torch.linspace(-20, 4, rows // 2, device="cuda")]) * cap
+    c = Case(dtype, rows, [1] * rows, 1, 1, 8, cap=cap, scale=1.0, pad=0)
+    c.qkv.zero_()
+    c.qkv[:, 0], c.qkv[:, 8] = x.to(c.qkv.dtype), 1
+    c.make_spans()
+    B.dapple_attention_docs_fwd(dtype, c.desc())
+    logit = cap * torch.tanh(c.qkv[:, 0].double() / cap)
+    off = (c.lse[0].double() * 0.6931471805599453 - logit).abs() - 10 * 2.0 ** -24 * logit.abs()
+    assert float(off.max()) <= (cap * 2.0 ** -21 if dtype == H else 0.0), float(off.max()) / cap
