@@ -176,8 +176,8 @@ int dapple_attention_window_bwd(int dtype, const dapple_attention_window_desc* d
  *   logit = t - slopes[h] |i - j|,   t = cap tanh(scale q k / cap), or scale q k with cap = 0
  * slopes: device fp32 [A], NULL = 0; finite, and constants (they have no gradient).  cap: 0 or 2^-20 to 2^10.  scale > 0; 0 = 1/sqrt(d);
  * scale / cap and cap / scale that fp32 does not hold as normal numbers are refused.
- * bf16 calls make tanh of an exponential and a reciprocal, off by 2^-21 at most however small it is: a logit, and with it lse, by cap * 2^-21
- * beside the arithmetic's own error (2^-11 at the largest cap).  fp32 calls keep fp32's precision.
+ * bf16 calls make tanh of an exponential and a reciprocal: a logit, and with it lse, is off by 2^-24 cap + 2^-20 |logit| at most in fwd, the
+ * logits of bwd by 2^-21 cap.  fp32 calls keep fp32's precision.
  * fwd: ctx, lse [A, rows] fp32 = log2 of the sum of 2^(log2(e) logit), ctx32 (may be NULL) as above.  bwd: dq, dk, dv from dctx and the ctx, ctx32
  * (or NULL) and lse of fwd.  spans holds what dapple_doc_spans left, of the same rows (other contents: wrong results, nothing worse).
  * Strides, alignment, limits (with b = 1, s = rows; up to 2^26 - 8), rounding and overlaps as for dapple_attention_window; workspace: below

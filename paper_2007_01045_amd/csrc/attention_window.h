@@ -89,10 +89,14 @@ __device__ __forceinline__ bool is_sink(const AttnWinArgs& a, int j) { return M 
 
 // The logit, in log2 units, of a product `raw`: unit t - slope2 |distance|, where t is raw, or its cap:
 //   t = tanh(x), x = raw scale / cap, unit = cap log2(e);   d logit / d raw = (1 - t^2) scale log2(e).
-// tanh(x) = 1 - 2 / (1 + e^2x), off by an ulp or two of 1 whatever x: two instructions of four times
-// the others' time.  Us forward and gradient, 4 documents of 2048 rows, both directions, cap 50, products up to about 30 / four times that and more: 16
-// heads of 128 on 4 208 + 554 / 186 + 558, of 64 124 + 352 / 127 + 358.  A polynomial where all products of a wave's block are small, and there alone,
-// took 205 + 547 / 238 + 691 and 125 + 353 / 187 + 463.
+// Backward, whose results are rounded to bf16: tanh(x) = 1 - 2 / (1 + e^2x), off by an ulp or two of 1 whatever x: two instructions of four times
+// the others' time.  Us, 4 documents of 2048 rows, both directions, cap 50, products up to about 30 / four times that and more: 16
+// heads of 128 on 4 554 / 558, of 64 352 / 358; a polynomial where all products of a wave's block are small, and there alone, took 547 / 691 and
+// 353 / 463.  Forward, whose lse is fp32 and, where few keys are seen, hardly more than a logit: with e = e^-2|x|, tanh |x| = (1 - e) / (1 + e), where
+// only e's own rounding counts against 1 (by 2^-25) and the others against tanh x.  Documents of one row, random q and k of 64, cap 50: lse off by 4.6e-7 in the
+// 2-norm, 2.3e-6 by the backward's form.  It costs two instructions more, us: 191 where that took 181 (128 wide), 134 / 123 (64).  A polynomial
+// below |x| = 1/16 besides, for relative precision down to 0, took 211 and 154, and 185 and 123 for the rows that see fewer than 8 keys alone, but 33
+// where this takes 31 (30 before) on 200 documents of 40 rows.
 constexpr bool capped(int S) { return S == SCORE_CAP || S == SCORE_BOTH; }
 constexpr bool sloped(int S) { return S == SCORE_SLOPE || S == SCORE_BOTH; }
 template <int S>
@@ -105,10 +109,15 @@ struct Score {
   __device__ __forceinline__ float of(float raw) const {   // t
     return capped(S) ? fmaf(-2.f, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(raw * bend2)), 1.f) : raw;
   }
-  template <typename V>
+  __device__ __forceinline__ float of_fwd(float raw) const {
+    if (!capped(S)) return raw;
+    const float a = raw * bend2, e = __builtin_amdgcn_exp2f(-fabsf(a));
+    return copysignf((1.f - e) * __builtin_amdgcn_rcpf(1.f + e), a);
+  }
+  template <bool FWD = false, typename V>
   __device__ __forceinline__ void cap(V& raw) const {
 #pragma unroll
-    for (int v = 0; v < 16; ++v) raw[v] = of(raw[v]);
+    for (int v = 0; v < 16; ++v) raw[v] = FWD ? of_fwd(raw[v]) : of(raw[v]);
   }
   // the logit less l; far: the rows' distance, of either sign
   __device__ __forceinline__ float less(float t, float far, float l) const {
@@ -443,7 +452,7 @@ __global__ __launch_bounds__(64 * NW, D <= 64 ? 3 : 2) void attn_win_fwd(AttnWin
       f32x16 sa = zero16();  // rows: key 32 kb2 + 8 blk + 4 h + e, column: query
 #pragma unroll
       for (int kk = 0; kk < NKK; ++kk) sa = MFMA(kf[kb2][kk], qf[kk], sa);
-      sc.cap(sa);
+      sc.template cap<true>(sa);
       if constexpr (sloped(S)) {
         const int b0 = k0 + 32 * kb2;
         shift[kb2] = sc.block(sa, p[kb2], qrow, b0 + 4 * h, row0, b0);
